@@ -308,7 +308,7 @@ def _encode(x, bits16, positive):
     y = x.abs() / scale[:, None]
     small = y < 2.0 ** -6
     y = torch.where(small, y + 2.0 ** -6, y)
-    code = ((y.view(torch.int32) + ((bits16.int() << 4) + 8)) >> 20) - 960
+    code = ((y.view(torch.int32) + ((bits16.int() << 4) + 8)) >> 20) - 968
     code = torch.where(small, code, code + 8)
     code = code.clamp(max=126)
     if positive:
