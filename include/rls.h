@@ -14,6 +14,12 @@
  *   rls_replace_visited samples already in v_Theta give way to mode(s_Theta)
  *   rls_apply_actions   the search agent's configuration updater (producer of the trajectory)
  *
+ * and, for the search agent itself (Sec. 4.1) and other models trained or sampled beside it:
+ *
+ *   rls_sample          a draw per row of logits: temperature, top-k, top-p, min-p, from given uniform numbers
+ *   rls_linear_scan     the gated linear recurrence h_t = a_t h_{t-1} + b_t, and its backward pass
+ *   rls_adamw_step      one AdamW step over all tensors of a model, moments in 32 or in 8 bits
+ *
  * Conventions
  *   - Plain C. Every call returns an int32_t status: RLS_OK or a negative RLS_ERR_* code.
  *   - Pointers named *_dev are device (HBM) pointers owned by the caller; all others are host
@@ -279,6 +285,112 @@ int32_t rls_replace_visited(int32_t *cfg_dev, int32_t k, int32_t n_knobs, const 
  */
 int32_t rls_apply_actions(const int32_t *cfg_dev, const int8_t *action_dev, int64_t m, const rls_knob_domains *domains,
                           int32_t *cfg_out_dev, float *features_dev, int64_t ldf, void *stream);
+
+/* Element types of arrays that come in several. */
+#define RLS_F32 0
+#define RLS_BF16 1
+#define RLS_F16 2
+
+/*
+ * One draw per row of logits: the search agent's action in a knob (Sec. 4.1, "Action space"), a candidate out of a
+ * trajectory's scores, an entry of a vocabulary.  For a row x with largest logit x_max:
+ *   d_i = (x_i - x_max) * (1 / temperature) in fp32, e_i = exp(d_i) in fp32,
+ *   w_i = e_i rounded to a multiple of 2^-38, as a whole number of them; sums of w are exact, whatever their order
+ *   top-k:  the k first entries in the order of descending d, equal ones by ascending index
+ *   top-p:  of these the ones before which, in that order, the sum of w is less than p times the sum over all of them
+ *   min-p:  of these the ones with e_i >= min_p
+ *   token:  the first kept i (by index) up to which the kept w add up to more than uniform * (sum of the kept w)
+ *   logprob: d_token - log(sum of the kept w), the log-probability of the draw among what was kept, in fp32
+ * The first entry of the order is always kept.  Entries of -infinity (masked ones) and NaN are never drawn; a row without
+ * any other gets token -1 and logprob -infinity.  Entries of +infinity share a draw among themselves.
+ * Arguments
+ *   logits_dev       [rows][ld_logits] of logits_type (RLS_F32, RLS_BF16, RLS_F16), first n_choices columns used
+ *   uniform_dev      [rows] fp32 in [0, 1); NaN and less than 0 count as 0, 1 and more takes the last kept entry
+ *   temperature_dev  [rows] fp32 or null (1); 0, less or NaN: the first entry of the order at temperature 1 (logprob 0)
+ *   top_k_dev        [rows] int32 or null; less than 1: all
+ *   top_p_dev        [rows] fp32 or null; 1, more or NaN: all
+ *   min_p_dev        [rows] fp32 or null; 0, less or NaN: all
+ *   token_dev        [rows] int32 (written);  logprob_dev  [rows] fp32 (written) or null
+ *   workspace_dev    rls_sample_workspace_bytes(rows, n_choices) bytes, 256-byte aligned (may be 0 bytes, and null then)
+ * 1 <= rows <= RLS_MAX_N, 1 <= n_choices <= RLS_MAX_CHOICES.
+ */
+#define RLS_MAX_CHOICES (1LL << 24)
+int64_t rls_sample_workspace_bytes(int64_t rows, int64_t n_choices);
+int32_t rls_sample(const void *logits_dev, int32_t logits_type, int64_t rows, int64_t n_choices, int64_t ld_logits,
+                   const float *uniform_dev, const float *temperature_dev, const int32_t *top_k_dev, const float *top_p_dev,
+                   const float *min_p_dev, int32_t *token_dev, float *logprob_dev, void *workspace_dev,
+                   int64_t workspace_bytes, void *stream);
+
+/* A [batch][steps][channels] array: channels side by side, any strides (in elements) between steps and sequences.  Read-only
+ * ones may repeat themselves (stride 0); written ones must not overlap themselves or anything else. */
+typedef struct {
+    void *data_dev;
+    int64_t batch_stride, step_stride;
+} rls_sequence;
+
+typedef struct {
+    int64_t batch, steps, channels;
+    int32_t type;              /* of b, h and their gradients: RLS_F32, RLS_BF16 or RLS_F16 */
+    int32_t gate_type;         /* of a and its gradient: RLS_F32 or `type` */
+    int32_t reverse;           /* != 0: time runs from the last step to the first (returns and advantages) */
+} rls_scan_shape;
+
+/*
+ * The gated linear recurrence, sequence by sequence and channel by channel, in the direction of time:
+ *   h_t = a_t h_{t-1} + b_t, in fp32; at a step whose reset byte is not 0 nothing is carried over: h_t = b_t
+ * It is the search agent's discounted return or advantage (b the rewards or temporal differences, a the discount,
+ * resets where an episode begins in the direction of time), and a recurrent layer over long sequences.
+ *   h0_dev      [batch][channels] fp32, the state before the first step, or null (0)
+ *   reset_dev   [batch][steps] bytes or null
+ *   h           (written) every state, rounded to `type`;  h_last_dev [batch][channels] fp32 (written) or null, the state
+ *               after the last step in fp32; it may be h0_dev's memory: with steps = 1 the step of a single token
+ * steps = 0 leaves h alone and copies h0 (or 0) to h_last.
+ */
+int64_t rls_linear_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels);
+int32_t rls_linear_scan(const rls_scan_shape *shape, const rls_sequence *a, const rls_sequence *b, const float *h0_dev,
+                        const uint8_t *reset_dev, const rls_sequence *h, float *h_last_dev, void *workspace_dev,
+                        int64_t workspace_bytes, void *stream);
+/*
+ * Its backward pass, from the states h that the forward pass wrote and the gradients dh and dh_last (null: 0) by them:
+ *   g_t = dh_t + a_{t+1} g_{t+1} (nothing from a step that was reset), dh_last added at the last step;
+ *   db_t = g_t,  da_t = g_t h_{t-1} (0 at a reset),  dh0 = a_1 g_1 (0 where the first step is reset)
+ * For a broadcast input the caller adds up the gradients along the broadcast axis.
+ *   da, db      (written) of gate_type and type;  dh0_dev [batch][channels] fp32 (written) or null, may be dh_last_dev's memory
+ */
+int32_t rls_linear_scan_backward(const rls_scan_shape *shape, const rls_sequence *a, const rls_sequence *h, const rls_sequence *dh,
+                                 const float *h0_dev, const uint8_t *reset_dev, const float *dh_last_dev, const rls_sequence *da,
+                                 const rls_sequence *db, float *dh0_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/*
+ * One AdamW step (Table 2's optimizer, with decoupled weight decay) over any number of tensors.  Per element, in fp32:
+ *   g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g g
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * With a master array p is read from and written to it, and the parameter is its rounded copy.  NaN and infinite
+ * gradients go into the element's parameter and moments as the arithmetic has it.
+ * Moments in 8 bits (state_bits = 8): every 256 consecutive elements of a tensor share a scale, a power of two; m and sqrt(v)
+ * are held as 8-bit floats (1-4-3, the format whose largest value is 448) times it.  They are rounded up or down at random, in
+ * proportion: v moves by a thousandth a step, which rounding to nearest would lose every time.  The random bits come from
+ * (seed, step, tensor, element) alone.  A v that is not 0 is never rounded to 0.
+ */
+typedef struct {
+    int64_t n;                 /* elements, >= 0 */
+    int32_t param_type;        /* RLS_F32, RLS_BF16, RLS_F16 */
+    int32_t grad_type;         /* RLS_F32 or param_type */
+    void *param_dev;           /* [n] (updated) */
+    const void *grad_dev;      /* [n] */
+    float *master_dev;         /* [n] fp32 weights (updated), or null: param itself is read */
+    void *m_dev, *v_dev;       /* [n] fp32, or [n] 8-bit floats of m and sqrt(v) (updated) */
+    float *m_scale_dev, *v_scale_dev;   /* [(n + 255) / 256] fp32 (updated); not read with state_bits = 32 */
+} rls_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;              /* >= 1: the number of this step */
+    uint64_t seed;             /* of the rounding at random (state_bits = 8) */
+    int32_t state_bits;        /* 32 or 8 */
+    const float *grad_scale_dev;        /* one fp32 factor of all gradients (clipping, loss scaling), or null (1) */
+} rls_adamw_options;
+/* `tensors` is a host array, read before the call returns. */
+int32_t rls_adamw_step(const rls_adamw_tensor *tensors, int32_t n_tensors, const rls_adamw_options *options, void *stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,9 @@ RLS_OK = 0
 RLS_STATUS_NONFINITE = 1
 RLS_STATUS_RANGE = 2
 MAX_D, MAX_K, MAX_DEPTH = 32, 128, 12
+MAX_CHOICES = 1 << 24
+F32, BF16, F16 = 0, 1, 2
+_TYPE_OF = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
 
 class RlsError(RuntimeError):
@@ -35,6 +38,27 @@ class _Forest(ctypes.Structure):
 
 class _Domains(ctypes.Structure):
     _fields_ = [("n_knobs", ctypes.c_int32), ("offsets_dev", ctypes.c_void_p), ("values_dev", ctypes.c_void_p)]
+
+
+class _Sequence(ctypes.Structure):
+    _fields_ = [("data_dev", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("step_stride", ctypes.c_int64)]
+
+
+class _ScanShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("steps", ctypes.c_int64), ("channels", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("gate_type", ctypes.c_int32), ("reverse", ctypes.c_int32)]
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("param_dev", ctypes.c_void_p),
+                ("grad_dev", ctypes.c_void_p), ("master_dev", ctypes.c_void_p), ("m_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p),
+                ("m_scale_dev", ctypes.c_void_p), ("v_scale_dev", ctypes.c_void_p)]
+
+
+class _AdamwOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64), ("state_bits", ctypes.c_int32),
+                ("grad_scale_dev", ctypes.c_void_p)]
 
 
 _lib = None
@@ -87,6 +111,19 @@ def lib() -> ctypes.CDLL:
         L.rls_replace_visited.argtypes = [vp, i32, i32, vp, i64, vp, vp, vp]
         L.rls_apply_actions.restype = i32
         L.rls_apply_actions.argtypes = [vp, vp, i64, ctypes.POINTER(_Domains), vp, vp, i64, vp]
+        L.rls_sample_workspace_bytes.restype = i64
+        L.rls_sample_workspace_bytes.argtypes = [i64, i64]
+        L.rls_sample.restype = i32
+        L.rls_sample.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        seq = ctypes.POINTER(_Sequence)
+        L.rls_linear_scan_workspace_bytes.restype = i64
+        L.rls_linear_scan_workspace_bytes.argtypes = [i64, i64, i64]
+        L.rls_linear_scan.restype = i32
+        L.rls_linear_scan.argtypes = [ctypes.POINTER(_ScanShape), seq, seq, vp, vp, seq, vp, vp, i64, vp]
+        L.rls_linear_scan_backward.restype = i32
+        L.rls_linear_scan_backward.argtypes = [ctypes.POINTER(_ScanShape), seq, seq, seq, vp, vp, vp, seq, seq, vp, vp, i64, vp]
+        L.rls_adamw_step.restype = i32
+        L.rls_adamw_step.argtypes = [ctypes.POINTER(_AdamwTensor), i32, ctypes.POINTER(_AdamwOptions), vp]
         L.rls_profile_enable.restype = i32
         L.rls_profile_enable.argtypes = [i32]
         L.rls_profile_read.restype = i32
@@ -443,3 +480,190 @@ def snap_to_valid_batched(centroids: torch.Tensor, domains: Sequence[DeviceDomai
     _check(lib().rls_snap_to_valid_batched(B, _ptr(centroids), k, d, centroids.stride(1), centroids.stride(0), arr,
                                            _ptr(out), _stream()), "rls_snap_to_valid_batched")
     return out
+
+
+def sample_workspace_bytes(rows: int, n_choices: int) -> int:
+    n = int(lib().rls_sample_workspace_bytes(rows, n_choices))
+    if n < 0:
+        raise RlsError(n, "rls_sample_workspace_bytes")
+    return n
+
+
+def _space(workspace: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[torch.Tensor], ctypes.c_void_p, int]:
+    """Workspace of a call: the caller's, or one of its own where it needs any; with its 256-byte aligned start and what is left of it."""
+    ws = _workspace(need, device) if workspace is None and need > 0 else workspace
+    if ws is None:
+        return None, ctypes.c_void_p(None), 0
+    base = _aligned_ptr(ws)
+    return ws, ctypes.c_void_p(base), max(0, ws.numel() * ws.element_size() - (base - ws.data_ptr()))
+
+
+def _per_row(t: Optional[torch.Tensor], dtype: torch.dtype, rows: int, name: str) -> Optional[torch.Tensor]:
+    if t is not None:
+        _dev(t, dtype, name)
+        if t.numel() != rows:
+            raise ValueError(f"{name} needs an entry per row")
+    return t
+
+
+def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+           want_logprob: bool = True, out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """A draw per row of logits [rows, n_choices] (fp32, bf16 or fp16, rows contiguous) from uniform [rows]: (token int32, logprob fp32 or None).
+
+    temperature, top_p, min_p (fp32) and top_k (int32) have an entry per row; None leaves a rule out."""
+    if logits.dim() != 2 or not logits.is_cuda or logits.dtype not in _TYPE_OF or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be an fp32, bf16 or fp16 device matrix with unit stride along a row")
+    rows, n = logits.shape
+    _per_row(uniform, torch.float32, rows, "uniform")
+    _per_row(temperature, torch.float32, rows, "temperature")
+    _per_row(top_k, torch.int32, rows, "top_k")
+    _per_row(top_p, torch.float32, rows, "top_p")
+    _per_row(min_p, torch.float32, rows, "min_p")
+    token = torch.empty(rows, dtype=torch.int32, device=logits.device) if out is None else _per_row(out, torch.int32, rows, "out")
+    logprob = torch.empty(rows, dtype=torch.float32, device=logits.device) if want_logprob else None
+    ws, base, avail = _space(workspace, sample_workspace_bytes(rows, n), logits.device)
+    _check(lib().rls_sample(_ptr(logits), _TYPE_OF[logits.dtype], rows, n, logits.stride(0) if rows > 1 else n, _ptr(uniform), _ptr(temperature),
+                            _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(token), _ptr(logprob), base, avail, _stream()), "rls_sample")
+    return token, logprob
+
+
+def linear_scan_workspace_bytes(batch: int, steps: int, channels: int) -> int:
+    n = int(lib().rls_linear_scan_workspace_bytes(batch, steps, channels))
+    if n < 0:
+        raise RlsError(n, "rls_linear_scan_workspace_bytes")
+    return n
+
+
+def _sequence(t: torch.Tensor, shape, dtypes, name: str) -> _Sequence:
+    if not t.is_cuda or tuple(t.shape) != tuple(shape) or t.dtype not in dtypes or (shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be a device tensor of shape {tuple(shape)} with unit stride along the channels and of type {dtypes}")
+    return _Sequence(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _states(t: Optional[torch.Tensor], shape, name: str) -> Optional[torch.Tensor]:
+    if t is not None:
+        _dev(t, torch.float32, name)
+        if tuple(t.shape) != (shape[0], shape[2]):
+            raise ValueError(f"{name} must be [batch, channels]")
+    return t
+
+
+def _resets(t: Optional[torch.Tensor], shape) -> Optional[torch.Tensor]:
+    if t is not None:
+        if t.dtype == torch.bool:
+            t = t.view(torch.uint8)
+        _dev(t, torch.uint8, "reset")
+        if tuple(t.shape) != (shape[0], shape[1]):
+            raise ValueError("reset must be [batch, steps]")
+    return t
+
+
+def _scan_shape(a: torch.Tensor, x: torch.Tensor, reverse: bool) -> _ScanShape:
+    if x.dim() != 3 or x.dtype not in _TYPE_OF or a.dtype not in (torch.float32, x.dtype):
+        raise ValueError("a sequence is [batch, steps, channels] in fp32, bf16 or fp16, its gate of the same type or fp32")
+    return _ScanShape(*x.shape, _TYPE_OF[x.dtype], _TYPE_OF[a.dtype], 1 if reverse else 0)
+
+
+def linear_scan(a: torch.Tensor, b: torch.Tensor, h0: Optional[torch.Tensor] = None, reset: Optional[torch.Tensor] = None, reverse: bool = False,
+                workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                last: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """h_t = a_t h_{t-1} + b_t over [batch, steps, channels]: (every state in b's type, the last one in fp32 [batch, channels]).
+
+    a may be fp32 beside a b of fewer bits, and either may be an expanded view; reset [batch, steps] (bytes or bools) cuts the carry;
+    reverse runs from the last step to the first.  `last` may be h0 itself, for a state that is updated in place."""
+    shape = _scan_shape(a, b, reverse)
+    B, T, C = b.shape
+    h = torch.empty((B, T, C), dtype=b.dtype, device=b.device) if out is None else out
+    last = torch.empty((B, C), dtype=torch.float32, device=b.device) if last is None else _states(last, b.shape, "last")
+    ws, base, avail = _space(workspace, linear_scan_workspace_bytes(B, T, C), b.device)
+    args = [_sequence(a, b.shape, (a.dtype,), "a"), _sequence(b, b.shape, (b.dtype,), "b"), _sequence(h, b.shape, (b.dtype,), "out")]
+    _check(lib().rls_linear_scan(ctypes.byref(shape), ctypes.byref(args[0]), ctypes.byref(args[1]), _ptr(_states(h0, b.shape, "h0")),
+                                 _ptr(_resets(reset, b.shape)), ctypes.byref(args[2]), _ptr(last), base, avail, _stream()), "rls_linear_scan")
+    return h, last
+
+
+def linear_scan_backward(a: torch.Tensor, h: torch.Tensor, dh: torch.Tensor, h0: Optional[torch.Tensor] = None, reset: Optional[torch.Tensor] = None,
+                         dh_last: Optional[torch.Tensor] = None, reverse: bool = False,
+                         workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Gradients of linear_scan from its gates, the states it returned and the gradients by them: (da in a's type, db in h's, dh0 in fp32).
+
+    Where a or b was an expanded view, da or db is the gradient of every element: its sum along the expanded axes is the input's."""
+    shape = _scan_shape(a, h, reverse)
+    B, T, C = h.shape
+    da = torch.empty((B, T, C), dtype=a.dtype, device=h.device)
+    db = torch.empty((B, T, C), dtype=h.dtype, device=h.device)
+    dh0 = torch.empty((B, C), dtype=torch.float32, device=h.device)
+    ws, base, avail = _space(workspace, linear_scan_workspace_bytes(B, T, C), h.device)
+    args = [_sequence(a, h.shape, (a.dtype,), "a"), _sequence(h, h.shape, (h.dtype,), "h"), _sequence(dh, h.shape, (h.dtype,), "dh"),
+            _sequence(da, h.shape, (a.dtype,), "da"), _sequence(db, h.shape, (h.dtype,), "db")]
+    _check(lib().rls_linear_scan_backward(ctypes.byref(shape), ctypes.byref(args[0]), ctypes.byref(args[1]), ctypes.byref(args[2]),
+                                          _ptr(_states(h0, h.shape, "h0")), _ptr(_resets(reset, h.shape)), _ptr(_states(dh_last, h.shape, "dh_last")),
+                                          ctypes.byref(args[3]), ctypes.byref(args[4]), _ptr(dh0), base, avail, _stream()),
+           "rls_linear_scan_backward")
+    return da, db, dh0
+
+
+class AdamW:
+    """An AdamW optimizer over a list of tensors (fp32, bf16 or fp16): one call per step updates them all.
+
+    state_bits 32 keeps m and v in fp32; 8 keeps m and sqrt(v) as torch.float8_e4m3fn codes (stored as uint8) with a power-of-two scale per
+    256 elements, rounded at random from `seed`.  master=True keeps fp32 weights beside bf16 or fp16 parameters.  The moments start at zero;
+    exp_avg, exp_avg_sq, their scales and master, lists like params, take over existing ones (a resumed run: `step` steps already done)."""
+
+    def __init__(self, params: Sequence[torch.Tensor], state_bits: int = 32, master=None, seed: int = 0, step: int = 0, exp_avg=None,
+                 exp_avg_sq=None, exp_avg_scale=None, exp_avg_sq_scale=None):
+        self.params, self.state_bits, self.seed, self.step_count = list(params), int(state_bits), int(seed), int(step)
+        if self.state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        for p in self.params:
+            if not p.is_cuda or p.dtype not in _TYPE_OF or not p.is_contiguous():
+                raise ValueError("params must be contiguous device tensors of fp32, bf16 or fp16")
+        held = torch.float32 if self.state_bits == 32 else torch.uint8
+        blocks = [((p.numel() + 255) // 256,) for p in self.params]
+        shapes = [p.shape for p in self.params]
+        self.exp_avg = self._list(exp_avg, held, shapes, "exp_avg")
+        self.exp_avg_sq = self._list(exp_avg_sq, held, shapes, "exp_avg_sq")
+        self.exp_avg_scale = self.exp_avg_sq_scale = None
+        if self.state_bits == 8:
+            self.exp_avg_scale = self._list(exp_avg_scale, torch.float32, blocks, "exp_avg_scale")
+            self.exp_avg_sq_scale = self._list(exp_avg_sq_scale, torch.float32, blocks, "exp_avg_sq_scale")
+        if master is True:
+            master = [p.detach().float() for p in self.params]
+        self.master = self._list(master, torch.float32, shapes, "master") if master else None
+        self._tensors = (_AdamwTensor * max(1, len(self.params)))()
+        for i, p in enumerate(self.params):
+            t = self._tensors[i]
+            t.n, t.param_type, t.param_dev = p.numel(), _TYPE_OF[p.dtype], p.data_ptr()
+            t.m_dev, t.v_dev = self.exp_avg[i].data_ptr(), self.exp_avg_sq[i].data_ptr()
+            t.master_dev = self.master[i].data_ptr() if self.master and p.dtype != torch.float32 else None
+            if self.state_bits == 8:
+                t.m_scale_dev, t.v_scale_dev = self.exp_avg_scale[i].data_ptr(), self.exp_avg_sq_scale[i].data_ptr()
+
+    def _list(self, given, dtype, shapes, name):
+        if given is None:
+            return [torch.zeros(k, dtype=dtype, device=p.device) for p, k in zip(self.params, shapes)]
+        given = list(given)
+        if len(given) != len(self.params):
+            raise ValueError(f"{name} needs a tensor per parameter")
+        for t, k in zip(given, shapes):
+            _dev(t, dtype, name)
+            if t.numel() != torch.Size(k).numel():
+                raise ValueError(f"{name} has a tensor of another size than its parameter's")
+        return given
+
+    def step(self, grads: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
+             weight_decay: float = 0.01, grad_scale: Optional[torch.Tensor] = None) -> None:
+        """One step with these gradients (fp32 or the parameter's type), times grad_scale (one fp32 on the device) where given."""
+        if len(grads) != len(self.params):
+            raise ValueError("step needs a gradient per parameter")
+        for t, p, g in zip(self._tensors, self.params, grads):
+            if g.shape != p.shape or not g.is_cuda or g.dtype not in (torch.float32, p.dtype) or not g.is_contiguous():
+                raise ValueError("a gradient must be a contiguous device tensor of its parameter's shape, in fp32 or the parameter's type")
+            t.grad_dev, t.grad_type = g.data_ptr(), _TYPE_OF[g.dtype]
+        if grad_scale is not None and _dev(grad_scale, torch.float32, "grad_scale").numel() != 1:
+            raise ValueError("grad_scale must hold one number")
+        options = _AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, self.step_count + 1, ctypes.c_uint64(self.seed).value, self.state_bits,
+                                None if grad_scale is None else grad_scale.data_ptr())
+        _check(lib().rls_adamw_step(self._tensors, len(self.params), ctypes.byref(options), _stream()), "rls_adamw_step")
+        self.step_count += 1

@@ -12,7 +12,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librls.so")
 SOURCES = ["rls_api.hip", "gbt_score.hip", "kmeans_seed.hip", "kmeans_order.hip", "kmeans_lloyd.hip", "kmeans_small.hip", "snap.hip", "modes_visited.hip",
-           "sweep_static.hip", "matrix_step.hip"]
+           "sweep_static.hip", "matrix_step.hip", "sample.hip", "linear_scan.hip", "adamw.hip"]
 
 
 def sources():
@@ -23,7 +23,7 @@ def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = sources() + [os.path.join(CSRC, "rls_internal.h"), os.path.join(CSRC, "lloyd_device.h"), os.path.join(ROOT, "include", "rls.h"),
+    deps = sources() + [os.path.join(CSRC, "rls_internal.h"), os.path.join(CSRC, "lloyd_device.h"), os.path.join(CSRC, "element_types.h"), os.path.join(ROOT, "include", "rls.h"),
                         os.path.join(ROOT, "include", "rls_bench.h")]
     return any(os.path.getmtime(p) > t for p in deps)
 

@@ -1,0 +1,261 @@
+"""Draws from rows of logits (rls_sample) against the definition in 64 bits.
+
+The rules are cuts and a running sum, so a reference in fp64 and the kernel, whose exponentials are fp32, can only part at an
+edge: where the number drawn, p or min-p lies within rounding of one.  d = (x - max) / T takes two roundings of at most 2^-24 |d|
+each and its exponential one of about 2^-23, so a weight that counts (|d| < 27, 2^-38) is off by less than 27 * 2^-23 + 2^-23 < 2^-18
+of itself, and so is any sum of weights or its share.  A token is right if the reference draws it for some p and min-p within 2^-17 (relative)
+and some number within 2^-17 (absolute); its log-probability to 2^-17 + 2^-22 |logprob|.
+"""
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+EDGE = 2.0 ** -17
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def rls():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1905_12799_amd import binding
+    binding.lib()
+    return binding
+
+
+def prepare_row(x, temperature):
+    """fp32 row -> (d in fp64, order by descending d and ascending index, greedy?)."""
+    x = x.astype(np.float64)
+    x = np.where(np.isnan(x), -np.inf, x)
+    top = x.max()
+    greedy = not temperature > 0
+    with np.errstate(invalid="ignore"):
+        d = np.where(x == top, 0.0, (x - top) / (1.0 if greedy else temperature))
+    d = np.where(np.isnan(d) | (x == -np.inf), -np.inf, d)
+    return d, np.argsort(-d, kind="stable"), greedy
+
+
+def reference(d, order, u, k, p, min_p):
+    """(token, logprob) of one row in 64 bits."""
+    w = np.exp(d)
+    ws = w[order].copy()
+    ws[k:] = 0.0
+    if p < 1:
+        before = np.cumsum(ws) - ws
+        ws[1:][before[1:] >= p * ws.sum()] = 0.0
+    if min_p > 0:
+        ws[1:][np.exp(d[order][1:]) < min_p] = 0.0
+    kept = np.zeros_like(w)
+    kept[order] = ws
+    total = kept.sum()
+    run = np.cumsum(kept)
+    above = np.flatnonzero(run > max(u, 0.0) * total)
+    token = above[0] if len(above) else np.flatnonzero(kept)[-1]
+    while kept[token] == 0:                              # (a running sum that rounds up over entries that are not kept)
+        token += 1
+    return int(token), float(d[token] - np.log(total))
+
+
+def check(rls, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, device_logits=None):
+    dev = lambda t: None if t is None else t.cuda()      # noqa: E731
+    token, logprob = rls.sample(device_logits if device_logits is not None else logits.cuda(), dev(uniform), dev(temperature), dev(top_k), dev(top_p), dev(min_p))
+    token, logprob = token.cpu().numpy(), logprob.cpu().numpy()
+    x = logits.float().numpy()
+    for r in range(x.shape[0]):
+        t = 1.0 if temperature is None else float(temperature[r])
+        if not np.any(x[r] > -np.inf):
+            assert token[r] == -1 and logprob[r] == -np.inf
+            continue
+        d, order, greedy = prepare_row(x[r], t)
+        k = len(d) if top_k is None or top_k[r] < 1 else int(top_k[r])
+        k = 1 if greedy else k
+        p = 1.0 if top_p is None or not top_p[r] < 1 else float(top_p[r])
+        m = 0.0 if min_p is None or not min_p[r] > 0 else float(min_p[r])
+        u = float(uniform[r])
+        u = 0.0 if not u > 0 else u
+        right = {}
+        for du, dp, dm in itertools.product((0, -EDGE, EDGE), (0, -EDGE, EDGE) if p < 1 else (0,), (0, -EDGE, EDGE) if m > 0 else (0,)):
+            tok, lp = reference(d, order, u + du, k, p * (1 + dp), m * (1 + dm))
+            right.setdefault(tok, []).append(lp)
+        assert token[r] in right, (r, token[r], right)
+        assert min(abs(lp - logprob[r]) for lp in right[token[r]]) <= EDGE + 2.0 ** -22 * abs(logprob[r]), (r, logprob[r], right)
+    return token, logprob
+
+
+def settings(rows, n, which, gen):
+    return {"temperature": 0.4 + torch.rand(rows, generator=gen) if "t" in which else None,
+            "top_k": torch.randint(1, max(2, min(n, 300)), (rows,), generator=gen, dtype=torch.int32) if "k" in which else None,
+            "top_p": 0.02 + 0.97 * torch.rand(rows, generator=gen) if "p" in which else None,
+            "min_p": 0.2 * torch.rand(rows, generator=gen) if "m" in which else None}
+
+
+@pytest.mark.parametrize("which", ["", "t", "k", "p", "m", "tkpm"])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,n", [(1, 1), (300, 2), (1000, 3), (77, 8), (50, 9), (40, 63), (40, 64), (33, 65), (17, 1000), (5, 4097), (3, 50021)])
+def test_against_64_bits(rls, rows, n, dtype, which):
+    gen = torch.Generator().manual_seed(rows * n + len(which))
+    logits = (torch.randn(rows, n, generator=gen) * 2.5).to(TYPES[dtype])
+    check(rls, logits, torch.rand(rows, generator=gen), **settings(rows, n, which, gen))
+
+
+@pytest.mark.parametrize("which", ["t", "tk", "tp", "tkpm"])
+@pytest.mark.parametrize("rows,n,dtype", [(2, 131072, "bf16"), (1, 300007, "f32"), (3, 262144, "f32"), (1, 1000003, "bf16")])
+def test_long_rows(rls, rows, n, dtype, which):
+    gen = torch.Generator().manual_seed(n)
+    logits = (torch.randn(rows, n, generator=gen) * 2.0).to(TYPES[dtype])
+    check(rls, logits, torch.rand(rows, generator=gen), **settings(rows, n, which, gen))
+
+
+@pytest.mark.parametrize("n", [3, 8, 40, 700, 5000, 140000, 400001])
+def test_ties_go_to_the_lowest_index(rls, n):
+    """Logits of a few values: top-k cuts through entries that are equal, which keep the order of their indices."""
+    gen = torch.Generator().manual_seed(n)
+    rows = 6
+    logits = torch.randint(-2, 1, (rows, n), generator=gen).float()
+    logits[:, n // 2] = 0.0
+    x = logits.numpy()
+    for k in (1, 2, n // 3 + 1, n // 2 + 1, n):
+        uniform = torch.full((rows,), 1.0 - 2.0 ** -24)
+        token, _ = rls.sample(logits.cuda(), uniform.cuda(), top_k=torch.full((rows,), k, dtype=torch.int32).cuda())
+        for r in range(rows):
+            kept = np.sort(np.argsort(-x[r], kind="stable")[:k])
+            # the last kept entry, unless what lies behind the number drawn is less than its weight (n entries of weight 1/9 and more)
+            assert token[r].item() in kept[-(1 + n // 1000000):], (k, r)
+        token, _ = rls.sample(logits.cuda(), torch.zeros(rows).cuda(), top_k=torch.full((rows,), k, dtype=torch.int32).cuda())
+        assert [t.item() for t in token] == [int(np.argsort(-x[r], kind="stable")[:k].min()) for r in range(rows)]
+
+
+@pytest.mark.parametrize("n", [5, 100, 3000, 140000, 300001])
+def test_all_equal(rls, n):
+    """Equal logits: the nucleus of p holds the first ceil(p n) entries, and a number u of them draws the floor(u * kept)-th."""
+    for p, u in ((0.5, 0.25), (0.3, 0.999), (1.0, 0.5), (1e-9, 0.7)):
+        kept = max(1, int(np.ceil(np.float64(np.float32(p)) * n)))
+        token, logprob = rls.sample(torch.full((1, n), -3.25).cuda(), torch.tensor([u]).cuda(), top_p=torch.tensor([p]).cuda())
+        assert abs(token.item() - int(np.float64(np.float32(u)) * kept)) <= (1 if n > 100000 else 0)
+        assert abs(logprob.item() + np.log(kept)) < 1e-6 * (1 + np.log(kept))
+
+
+@pytest.mark.parametrize("n", [3, 8, 64, 1000, 70000, 280000])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_masks(rls, n, dtype):
+    gen = torch.Generator().manual_seed(n)
+    inf = float("inf")
+    logits = torch.randn(9, n, generator=gen).to(TYPES[dtype])
+    low = torch.finfo(TYPES[dtype]).min
+    logits[0] = -inf                                     # nothing left
+    logits[1] = -inf
+    logits[1, n - 1] = 0.5                               # one entry, the last
+    logits[2, : n // 2] = -inf
+    logits[3, n // 2:] = float("nan")
+    logits[4] = low                                      # all at the type's lowest value: equal ones
+    logits[5, 1:] = low
+    logits[6, n // 3] = inf                              # infinities share the draw
+    logits[6, n - 1] = inf
+    logits[7] = float("nan")
+    logits[8] = -inf
+    logits[8, 0] = low
+    for which in ("", "tkpm", "p"):
+        uniform = torch.rand(9, generator=gen)
+        token, logprob = check(rls, logits, uniform, **settings(9, n, which, gen))
+        assert token[0] == -1 and token[7] == -1 and token[1] == n - 1 and logprob[1] == 0.0 and token[5] == 0 and token[8] == 0
+        assert token[6] in (n // 3, n - 1) and not np.isnan(logits[3, token[3]].float().item())
+
+
+def test_settings_at_their_ends(rls):
+    """Temperatures of 0, below, infinite and NaN; k, p, min-p beyond their ranges; numbers drawn outside [0, 1)."""
+    for n in (5, 900, 30000):
+        gen = torch.Generator().manual_seed(n)
+        logits = torch.randn(1, n, generator=gen)
+        best = int(logits.argmax())
+        one = lambda v, t=torch.float32: torch.tensor([v], dtype=t).cuda()         # noqa: E731
+        u = one(0.73)
+        plain, plain_lp = rls.sample(logits.cuda(), u)
+        for t in (0.0, -1.0, float("nan")):
+            token, lp = rls.sample(logits.cuda(), u, temperature=one(t))
+            assert token.item() == best and lp.item() == 0.0
+        token, lp = rls.sample(logits.cuda(), u, temperature=one(float("inf")))
+        assert token.item() == int(np.float32(0.73) * np.float64(n)) and abs(lp.item() + np.log(n)) < 1e-5
+        token, _ = rls.sample(logits.cuda(), u, temperature=one(1e-42))
+        assert token.item() == best
+        for off in ({"top_k": one(0, torch.int32)}, {"top_k": one(-5, torch.int32)}, {"top_k": one(2 ** 31 - 1, torch.int32)}, {"top_p": one(1.0)},
+                    {"top_p": one(7.0)}, {"top_p": one(float("nan"))}, {"min_p": one(0.0)}, {"min_p": one(-1.0)}, {"min_p": one(float("nan"))}):
+            token, lp = rls.sample(logits.cuda(), u, **off)
+            assert token.item() == plain.item() and lp.item() == plain_lp.item(), off
+        for first in ({"top_k": one(1, torch.int32)}, {"top_p": one(0.0)}, {"top_p": one(-2.0)}, {"min_p": one(1.0)}, {"min_p": one(3.0)}):
+            token, lp = rls.sample(logits.cuda(), u, **first)
+            assert token.item() == best and lp.item() == 0.0, first
+        for v, want in ((0.0, 0), (-3.0, 0), (float("nan"), 0), (1.0, n - 1), (9.0, n - 1)):
+            token, _ = rls.sample(logits.cuda(), one(v))
+            assert token.item() == want, v
+
+
+def test_numbers_spread_over_a_row(rls):
+    """Evenly spread numbers draw every entry in proportion to its probability, to one draw."""
+    for n, rows in ((3, 9000), (40, 8000), (700, 7000)):
+        gen = torch.Generator().manual_seed(n)
+        row = torch.randn(n, generator=gen)
+        logits = row.cuda()[None].repeat(rows, 1)
+        u = ((torch.arange(rows) + 0.5) / rows).cuda()
+        token, _ = rls.sample(logits, u, temperature=torch.full((rows,), 0.7).cuda())
+        counts = torch.bincount(token.long(), minlength=n).double().cpu()
+        assert (counts - torch.softmax(row.double() / np.float32(0.7), 0) * rows).abs().max() <= 1.0 + rows * EDGE
+        assert (token[1:] >= token[:-1]).all()
+
+
+@pytest.mark.parametrize("n,pad,first", [(3, 5, 1), (8, 8, 0), (127, 3, 1), (1000, 24, 3), (70001, 8, 1), (270001, 2, 1)])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_inside_a_larger_matrix(rls, n, pad, first, dtype):
+    """Rows that start anywhere: any leading dimension and alignment; what lies around them is not read into the result."""
+    gen = torch.Generator().manual_seed(n)
+    whole = torch.full((7, n + pad), float("inf"), dtype=TYPES[dtype])
+    logits = (torch.randn(7, n, generator=gen) * 2).to(TYPES[dtype])
+    whole[:, first:first + n] = logits
+    view = whole.cuda()[:, first:first + n]
+    which = settings(7, n, "tkp", gen)
+    check(rls, logits, torch.rand(7, generator=gen), device_logits=view, **which)
+
+
+def test_without_logprob_and_on_another_stream(rls):
+    gen = torch.Generator().manual_seed(3)
+    logits, u = torch.randn(5, 4000, generator=gen).cuda(), torch.rand(5, generator=gen).cuda()
+    k = torch.full((5,), 50, dtype=torch.int32).cuda()
+    want, _ = rls.sample(logits, u, top_k=k)
+    token, logprob = rls.sample(logits, u, top_k=k, want_logprob=False)
+    assert logprob is None and torch.equal(token, want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        late, _ = rls.sample(logits * 1.0, u, top_k=k)
+    side.synchronize()
+    assert torch.equal(late, want)
+
+
+@pytest.mark.parametrize("rows,n", [(64, 3), (4, 5000), (2, 300000)])
+def test_in_a_graph(rls, rows, n):
+    """Recorded once and replayed on other inputs, with work and synchronisations in between."""
+    gen = torch.Generator().manual_seed(n)
+    logits, u = torch.empty(rows, n).cuda(), torch.empty(rows).cuda()
+    k, p = torch.full((rows,), 40, dtype=torch.int32).cuda(), torch.full((rows,), 0.9).cuda()
+    ws = torch.empty(rls.sample_workspace_bytes(rows, n) + 256, dtype=torch.uint8).cuda()
+    out = torch.empty(rows, dtype=torch.int32).cuda()
+    logits.copy_(torch.randn(rows, n, generator=gen))
+    u.copy_(torch.rand(rows, generator=gen))
+    call = lambda: rls.sample(logits, u, top_k=k, top_p=p, workspace=ws, want_logprob=False, out=out)      # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(4):
+        logits.copy_(torch.randn(rows, n, generator=gen))
+        u.copy_(torch.rand(rows, generator=gen))
+        want = rls.sample(logits, u, top_k=k, top_p=p, want_logprob=False)[0].clone()
+        out.fill_(-7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
