@@ -14,6 +14,7 @@
 
 #include "element_types.h"
 #include "rls_internal.h"
+#include "wave.h"
 
 namespace rls {
 
@@ -40,20 +41,18 @@ struct RowRules {
 };
 __device__ inline RowRules rules_of(const SampleArgs &a, int64_t row)
 {
-    RowRules r{1.0f, a.n, 1.0f, 0.0f, 0.0};
-    if (a.top_k) {
-        const int32_t k = a.top_k[row];
-        if (k >= 1 && k < a.n) r.k = k;
-    }
-    if (a.temperature) {
-        const float t = a.temperature[row];
-        if (t > 0.0f) r.inv = 1.0f / t;
-        else r.k = 1;
-    }
-    if (a.top_p && a.top_p[row] < 1.0f) r.p = a.top_p[row];
-    if (a.min_p && a.min_p[row] > 0.0f) r.least = a.min_p[row];
-    const float u = a.uniform[row];
-    if (u > 0.0f) r.u = (double)u;
+    // (every setting is read, from the numbers drawn where there is none, so that the reads are under way together)
+    const float *const none = a.uniform;
+    const float u = a.uniform[row], t = (a.temperature ? a.temperature : none)[row], p = (a.top_p ? a.top_p : none)[row],
+                m = (a.min_p ? a.min_p : none)[row];
+    const int32_t k = (a.top_k ? a.top_k : reinterpret_cast<const int32_t *>(none))[row];
+    RowRules r;
+    const bool greedy = a.temperature && !(t > 0.0f);
+    r.k = greedy ? 1 : (a.top_k && k >= 1 && k < a.n ? (int64_t)k : a.n);
+    r.inv = a.temperature && !greedy ? 1.0f / t : 1.0f;
+    r.p = a.top_p && p < 1.0f ? p : 1.0f;
+    r.least = a.min_p && m > 0.0f ? m : 0.0f;
+    r.u = u > 0.0f ? (double)u : 0.0;
     return r;
 }
 
@@ -80,9 +79,9 @@ __device__ inline uint64_t weight_of(float e)
 }
 __device__ inline uint64_t weight_of_key(uint32_t key) { return weight_of(expf(-distance_of(key))); }
 // whether an entry with so many entries, or so much weight, before it is inside top-k, or top-p (the first one always is)
-__device__ inline bool begins_below(bool by_mass, uint64_t count, uint64_t mass, uint64_t k, double limit)
+__device__ inline bool begins_below(bool by_mass, uint64_t before, uint64_t k, double limit)
 {
-    return by_mass ? mass == 0 || (double)mass < limit : count < k;
+    return by_mass ? (before == 0) | ((double)before < limit) : before < k;
 }
 // Bins of a histogram: equal parts of the distances up to the widest, or up to 40 (beyond, exp(d) counts for nothing and only top-k
 // can cut: with masks of the type's lowest value the bins keep their use); the last one takes the rest.
@@ -181,16 +180,19 @@ template <int NT>
 struct Group {
     static constexpr int kWaves = NT / 64;
     static constexpr int kBins = NT == 64 ? 256 : 1024;
-    static constexpr int kList = NT == 64 ? 256 : (NT < 1024 ? 512 : 1024);    // places that are counted against each other
+    static constexpr int kList = 128;                   // places that are counted against each other (1000 in 1000 threads take 12 us)
     static constexpr int kBinsOfThread = kBins / NT;
 
+    struct Waves {
+        uint64_t a[kWaves], b[kWaves];
+    };
     struct Shared {
         uint64_t mass[kBins];
         uint32_t count[kBins];
         uint64_t place[kList], weight[kList];
-        uint64_t wave_a[kWaves], wave_b[kWaves];
-        uint64_t found_mass;
-        uint32_t found_bin, found_n, found_count, listed;
+        Waves waves;
+        uint64_t found_before;
+        uint32_t found_bin, found_n, listed;
     };
 
     static __device__ inline void sync()
@@ -200,63 +202,59 @@ struct Group {
     }
     // reductions and scans over the workgroup; the results are the same in every thread
     template <typename F>
-    static __device__ inline uint64_t reduce(Shared &s, uint64_t x, F join)
+    static __device__ inline uint64_t reduce(Waves &waves, uint64_t x, F join)
     {
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) x = join(x, (uint64_t)__shfl_xor((unsigned long long)x, off, 64));
+        x = wave_reduce(x, (uint64_t)0, join);
         if constexpr (NT > 64) {
             __syncthreads();
-            if ((threadIdx.x & 63) == 0) s.wave_a[threadIdx.x >> 6] = x;
+            if ((threadIdx.x & 63) == 0) waves.a[threadIdx.x >> 6] = x;
             __syncthreads();
-            x = s.wave_a[0];
+            x = waves.a[0];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) x = join(x, s.wave_a[w]);
+            for (int w = 1; w < kWaves; ++w) x = join(x, waves.a[w]);
         }
         return x;
     }
     static __device__ inline uint64_t sum(Shared &s, uint64_t x)
     {
-        return reduce(s, x, [](uint64_t a, uint64_t b) { return a + b; });
+        return reduce(s.waves, x, [](uint64_t a, uint64_t b) { return a + b; });
     }
     static __device__ inline uint64_t most(Shared &s, uint64_t x)
     {
-        return reduce(s, x, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+        return reduce(s.waves, x, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
     }
-    static __device__ inline float most_float(Shared &s, float x)
+    // the largest of one value and the smallest of another
+    static __device__ inline void range(Shared &s, float &top, float &low)
     {
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
+        top = wave_max(top);
+        low = wave_min(low);
         if constexpr (NT > 64) {
             __syncthreads();
-            if ((threadIdx.x & 63) == 0) s.wave_a[threadIdx.x >> 6] = __float_as_uint(x);
+            if ((threadIdx.x & 63) == 0) s.waves.a[threadIdx.x >> 6] = (uint64_t)__float_as_uint(top) << 32 | __float_as_uint(low);
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) x = fmaxf(x, __uint_as_float((uint32_t)s.wave_a[w]));
+            for (int w = 0; w < kWaves; ++w) {
+                top = fmaxf(top, __uint_as_float((uint32_t)(s.waves.a[w] >> 32)));
+                low = fminf(low, __uint_as_float((uint32_t)s.waves.a[w]));
+            }
         }
-        return x;
     }
     // what the threads before this one have (and the sum of all)
-    static __device__ inline uint64_t scan(Shared &s, uint64_t x, uint64_t *total)
+    static __device__ inline uint64_t scan(Waves &waves, uint64_t x, uint64_t *total)
     {
-        const int lane = threadIdx.x & 63;
-        uint64_t run = x;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint64_t o = __shfl_up((unsigned long long)run, off, 64);
-            if (lane >= off) run += o;
-        }
+        const uint64_t run = wave_scan(x, (uint64_t)0, [](uint64_t a, uint64_t b) { return a + b; });
         if constexpr (NT == 64) {
-            *total = __shfl((unsigned long long)run, 63, 64);
+            *total = last_lane(run);
             return run - x;
         } else {
-            const int wave = threadIdx.x >> 6;
+            const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
             __syncthreads();
-            if (lane == 63) s.wave_b[wave] = run;
+            if (lane == 63) waves.b[wave] = run;
             __syncthreads();
             uint64_t before = 0, all = 0;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const uint64_t v = s.wave_b[w];
+                const uint64_t v = waves.b[w];
                 before += w < wave ? v : 0;
                 all += v;
             }
@@ -275,51 +273,42 @@ struct Group {
         }
         sync();
     }
-    // The last bin whose entries begin below: fewer than k entries before it, or less weight than `limit`, of which so many and so much come
-    // before all bins.  Leaves bin, its entries, and entries and weight before it in s.
-    static __device__ inline void find_bin(Shared &s, bool by_mass, uint64_t k, double limit, uint64_t base_count, uint64_t base_mass)
+    // The last bin whose entries begin below: fewer than k entries before it, or less weight than `limit`, of which `base` come before all
+    // bins.  Leaves the bin, its entries, and entries or weight before it in s.
+    static __device__ inline void find_bin(Shared &s, bool by_mass, uint64_t k, double limit, uint64_t base)
     {
-        sync();
-        uint64_t count = 0, mass = 0, all;
-#pragma unroll
-        for (int b = 0; b < kBinsOfThread; ++b) {
-            count += s.count[threadIdx.x * kBinsOfThread + b];
-            mass += s.mass[threadIdx.x * kBinsOfThread + b];
-        }
-        const uint64_t count_before = base_count + scan(s, count, &all), mass_before = base_mass + scan(s, mass, &all);
         if (threadIdx.x == 0) s.found_bin = 0;
         sync();
-        int mine = -1;
-        uint64_t c = count_before, m = mass_before;
+        uint64_t mine = 0, all;
 #pragma unroll
         for (int b = 0; b < kBinsOfThread; ++b) {
-            const uint32_t n = s.count[threadIdx.x * kBinsOfThread + b];
-            if (n > 0 && begins_below(by_mass, c, m, k, limit)) mine = threadIdx.x * kBinsOfThread + b;
-            c += n;
-            m += s.mass[threadIdx.x * kBinsOfThread + b];
+            const int i = threadIdx.x * kBinsOfThread + b;
+            mine += by_mass ? s.mass[i] : s.count[i];
         }
-        if (mine >= 0) atomicMax(&s.found_bin, (uint32_t)mine);
-        sync();
-        if ((int)(s.found_bin / kBinsOfThread) == (int)threadIdx.x) {
-            c = count_before;
-            m = mass_before;
+        const uint64_t before = base + scan(s.waves, mine, &all);
+        int last = -1;
+        uint64_t run = before, last_run = 0;
 #pragma unroll
-            for (int b = 0; b < kBinsOfThread; ++b) {
-                if (threadIdx.x * kBinsOfThread + b == s.found_bin) {
-                    s.found_n = s.count[s.found_bin];
-                    s.found_count = (uint32_t)c;
-                    s.found_mass = m;
-                }
-                c += s.count[threadIdx.x * kBinsOfThread + b];
-                m += s.mass[threadIdx.x * kBinsOfThread + b];
-            }
+        for (int b = 0; b < kBinsOfThread; ++b) {
+            const int i = threadIdx.x * kBinsOfThread + b;
+            const uint32_t n = s.count[i];
+            const bool below = (n > 0) & begins_below(by_mass, run, k, limit);
+            last = below ? i : last;
+            last_run = below ? run : last_run;
+            run += by_mass ? s.mass[i] : n;
+        }
+        if (last >= 0) atomicMax(&s.found_bin, (uint32_t)last);
+        sync();
+        if (last >= 0 && s.found_bin == (uint32_t)last) {
+            s.found_n = s.count[last];
+            s.found_before = last_run;
         }
         sync();
     }
     // Among the n entries that `visit` hands to a function of place and key, the last place that begins below (see find_bin).  Where they fit the
     // list they are counted against each other; more are cut into bins of places first, again and again.
     template <typename Visit>
-    static __device__ inline uint64_t last_below(Shared &s, Visit visit, uint64_t n, bool by_mass, uint64_t k, double limit, uint64_t count, uint64_t mass)
+    static __device__ inline uint64_t last_below(Shared &s, Visit visit, uint64_t n, bool by_mass, uint64_t k, double limit, uint64_t before)
     {
         uint64_t lo = 0, hi = ~0ull;
         if (n > kList) {
@@ -343,13 +332,12 @@ struct Group {
                 atomicAdd(&s.count[b], 1u);
                 if (by_mass) atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[b]), (unsigned long long)weight_of_key(key));
             });
-            find_bin(s, by_mass, k, limit, count, mass);
+            find_bin(s, by_mass, k, limit, before);
             lo += (uint64_t)s.found_bin << shift;
             const uint64_t end = lo + ((1ull << shift) - 1);
             hi = end < hi ? end : hi;
             n = s.found_n;
-            count = s.found_count;
-            mass = s.found_mass;
+            before = s.found_before;
             sync();
         }
         if (lo == hi) return lo;
@@ -366,13 +354,12 @@ struct Group {
         uint64_t cut = 0;
         for (uint32_t i = threadIdx.x; i < listed; i += NT) {
             const uint64_t at = s.place[i];
-            uint64_t c = count, m = mass;
+            uint64_t run = before;
             for (uint32_t o = 0; o < listed; ++o) {
-                const bool first = s.place[o] < at;
-                c += first;
-                m += first ? s.weight[o] : 0;
+                const uint64_t add = by_mass ? s.weight[o] : 1;
+                run += s.place[o] < at ? add : 0;
             }
-            if (begins_below(by_mass, c, m, k, limit)) cut = cut > at ? cut : at;
+            if (begins_below(by_mass, run, k, limit)) cut = cut > at ? cut : at;
         }
         return most(s, cut);
     }
@@ -419,7 +406,7 @@ struct Group {
         }
         uint64_t cut = ~0ull;
         // (the list's places overwrite no bin, and a second cut begins from the same bins unless the first one had to cut its bin up)
-        auto in_bin = [&](int bin, bool by_mass, double limit, uint64_t n, uint64_t c, uint64_t m) {
+        auto in_bin = [&](int bin, bool by_mass, double limit, uint64_t n, uint64_t before) {
             return last_below(s, [&](auto what) {
                 x.forget();
 #pragma unroll
@@ -427,16 +414,12 @@ struct Group {
                     if (x.there(j) && bin_of(x.key[j], scale, kBins) == bin && x.upto(j, cut)) what(x.place(j), x.key[j]);
                     pace(j);
                 }
-            }, n, by_mass, k, limit, c, m);
+            }, n, by_mass, k, limit, before);
         };
-        int p_bin = 0;
-        uint64_t n, c, m;
         if (use_k) {
-            find_bin(s, false, k, 0.0, 0, 0);
-            const int bin = (int)s.found_bin;
-            n = s.found_n, c = s.found_count;
-            const bool crowded = n > kList;
-            cut = in_bin(bin, false, 0.0, n, c, 0);
+            find_bin(s, false, k, 0.0, 0);
+            const bool crowded = s.found_n > kList;
+            cut = in_bin((int)s.found_bin, false, 0.0, s.found_n, s.found_before);
             if (use_p && crowded) {
                 clear(s);
                 x.forget();
@@ -461,10 +444,8 @@ struct Group {
             }
             const double limit = (double)p * (double)sum(s, kept);
             // (a bin that begins below the limit begins no later than the cut's)
-            find_bin(s, true, 0, limit, 0, 0);
-            p_bin = (int)s.found_bin;
-            n = s.found_n, m = s.found_mass;
-            cut = in_bin(p_bin, true, limit, n, 0, m);
+            find_bin(s, true, 0, limit, 0);
+            cut = in_bin((int)s.found_bin, true, limit, s.found_n, s.found_before);
         }
         return cut;
     }
@@ -495,27 +476,24 @@ __global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a)
                 for (int j = 0; j < N; ++j) l[q + j] = first + q + j < n ? logit_of(x[first + q + j]) : -INFINITY;
             }
         }
-        float top = -INFINITY;
+        const RowRules r = rules_of(a, row);
+        float top = -INFINITY, low = INFINITY;
 #pragma unroll
-        for (int j = 0; j < E; ++j) top = fmaxf(top, l[j]);
-        top = Grp::most_float(s, top);
+        for (int j = 0; j < E; ++j) {
+            top = fmaxf(top, l[j]);
+            low = fminf(low, l[j] > -INFINITY ? l[j] : INFINITY);
+        }
+        Grp::range(s, top, low);
         if (top == -INFINITY) {
             if (threadIdx.x == 0) no_draw(a, row);
             continue;
         }
-        const RowRules r = rules_of(a, row);
         typename Grp::template Entries<E> entry;
         entry.first = (uint32_t)first;
-        float widest = 0.0f;
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const float d = scaled_logit(l[j], top, r.inv);
-            entry.key[j] = key_of(d);
-            if (entry.there(j)) widest = fmaxf(widest, -d);
-        }
+        for (int j = 0; j < E; ++j) entry.key[j] = key_of(scaled_logit(l[j], top, r.inv));
         uint64_t cut = ~0ull;
-        if (r.k < n || r.p < 1.0f)
-            cut = Grp::cut_of(s, entry, Grp::most_float(s, widest), (uint64_t)r.k, r.k < n, r.p, r.p < 1.0f);
+        if (r.k < n || r.p < 1.0f) cut = Grp::cut_of(s, entry, -scaled_logit(low, top, r.inv), (uint64_t)r.k, r.k < n, r.p, r.p < 1.0f);
         auto weight = [&](int j) -> uint64_t {
             if (!entry.there(j) || !entry.upto(j, cut)) return 0;
             const float e = expf(-distance_of(entry.key[j]));
@@ -528,7 +506,7 @@ __global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a)
             mine += weight(j);
             Grp::pace(j);
         }
-        uint64_t run = Grp::scan(s, mine, &total);
+        uint64_t run = Grp::scan(s.waves, mine, &total);
         const double mark = r.u * (double)total;
         auto beyond = [&](uint64_t v) { return (double)v > mark || v == total; };
         if (beyond(run + mine) && !beyond(run)) {
@@ -549,14 +527,20 @@ __global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a)
 }
 
 constexpr int64_t kGroupRow = 32768;
+constexpr int64_t kFewRows = 512;
 constexpr int64_t kMostGroups = 1 << 20;           // (of a launch, which ends at 2^32 threads)
 
 template <typename T>
 hipError_t launch_group_rows(const SampleArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.rows < kMostGroups ? a.rows : kMostGroups));
+    // a few rows are as long as what a thread does in turn: four entries each; many rows are work, of which a larger workgroup has more in its
+    // scans and barriers
+    const bool few = a.rows <= kFewRows;
     if (a.n <= 256) hipLaunchKernelGGL((sample_row_kernel<T, 64, 4>), grid, dim3(64), 0, s, a);
+    else if (few && a.n <= 1024) hipLaunchKernelGGL((sample_row_kernel<T, 256, 4>), grid, dim3(256), 0, s, a);
     else if (a.n <= 1024) hipLaunchKernelGGL((sample_row_kernel<T, 64, 16>), grid, dim3(64), 0, s, a);
+    else if (few && a.n <= 4096) hipLaunchKernelGGL((sample_row_kernel<T, 1024, 4>), grid, dim3(1024), 0, s, a);
     else if (a.n <= 4096) hipLaunchKernelGGL((sample_row_kernel<T, 256, 16>), grid, dim3(256), 0, s, a);
     else if (a.n <= 16384) hipLaunchKernelGGL((sample_row_kernel<T, 1024, 16>), grid, dim3(1024), 0, s, a);
     else hipLaunchKernelGGL((sample_row_kernel<T, 1024, 32>), grid, dim3(1024), 0, s, a);
@@ -575,15 +559,19 @@ hipError_t launch_short_rows(const SampleArgs &a, hipStream_t s)
 
 // ---- long rows ------------------------------------------------------------------------------------
 
-// Rows are cut into chunks, a workgroup each, and a batch of rows goes through launches: maxima; where a row has top-k or top-p a histogram, the
-// entries of the bins that its cuts lie in as a list, and the cuts; the chunks' weights; the draw.  What a launch needs of the row's other
-// chunks it finds in the workspace.
+// Rows are cut into chunks, a workgroup each, and a batch of rows goes through launches: the maxima; where rows have top-k or top-p a
+// histogram, and the bins that a row's cuts lie in; the weights of what lies before these bins, segment
+// by segment, and the entries in them as a list; the cuts from the list, its share of the weights and the draw, a workgroup per row.
+// What a launch needs of the row's other chunks it finds in the workspace.
 constexpr int kLongThreads = 512;
+constexpr int kLongWaves = kLongThreads / 64;
 constexpr int kLongBins = 2048;
 constexpr int kLongList = 16384;
 constexpr int kLongStage = 1024;                        // places a workgroup collects before it goes to the row's list one by one
 constexpr int64_t kLongRows = 256;                      // of a batch
 constexpr int kMostPieces = 512;                        // chunks of a row
+constexpr int kMostSegments = kMostPieces * kLongWaves; // a segment is a wave's part of a chunk
+constexpr int kMostChunk = 65536;
 constexpr int kLoad = 8;                                // entries a thread takes in a row
 
 struct Piece {
@@ -594,25 +582,38 @@ struct RowBins {                                        // where a row's cuts li
     int32_t k_bin, p_first, p_last;                     // top-k's bin; top-p's is one of these, which depends on what top-k keeps of its own
     uint32_t k_count, k_before;
     uint64_t k_mass_before, p_mass_before;              // weight before k_bin, p_first
+    uint64_t mass;                                      // of the row
     float top, scale;
-    uint64_t cut;
 };
 struct LongArgs {
     SampleArgs a;
     int64_t row0, chunk;
     int32_t rows, pieces;
     Piece *piece;                                       // [rows][pieces]
-    uint64_t *weight;                                   // [rows][pieces]
+    uint64_t *weight;                                   // [rows][pieces][kLongWaves]
     uint64_t *mass;                                     // [rows][kLongBins]
     uint32_t *count, *listed;                           // [rows][kLongBins], [rows]
     uint64_t *list;                                     // [rows][kLongList]
     RowBins *bins;                                      // [rows]
 };
 
+// The entries of a span, kLoad at a time by each of `n` threads, with two loads of each under way; a thread's indices ascend.
 template <typename T, typename F>
-__device__ inline void visit_chunk(const T *x, int64_t begin, int64_t end, int threads, F what)
+__device__ inline void visit_span(const T *x, int64_t begin, int64_t end, int thread, int n, F what)
 {
-    for (int64_t i = begin + (int64_t)threadIdx.x * kLoad; i < end; i += (int64_t)threads * kLoad) {
+    constexpr int U = 2 * 16 / (kLoad * (int)sizeof(T)) > 1 ? 4 : 2;
+    const int64_t step = (int64_t)n * kLoad;
+    int64_t i = begin + (int64_t)thread * kLoad;
+    for (; i + (U - 1) * step + kLoad <= end; i += U * step) {
+        T v[U][kLoad];
+#pragma unroll
+        for (int u = 0; u < U; ++u) __builtin_memcpy(v[u], x + i + u * step, sizeof(v[u]));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < kLoad; ++j) what(logit_of(v[u][j]), i + u * step + j);
+    }
+    for (; i < end; i += step) {
         if (i + kLoad <= end) {
             T v[kLoad];
             __builtin_memcpy(v, x + i, sizeof(v));
@@ -624,58 +625,52 @@ __device__ inline void visit_chunk(const T *x, int64_t begin, int64_t end, int t
     }
 }
 
+__device__ inline Piece joined(const Piece &a, const Piece &b)
+{
+    return Piece{fmaxf(a.top, b.top), fminf(a.low, b.low), a.top > b.top ? a.at : (b.top > a.top ? b.at : min(a.at, b.at))};
+}
+__device__ inline Piece of_wave(const Piece &p)
+{
+    const float top = wave_max(p.top);
+    const uint32_t at = wave_reduce(p.top == top ? p.at : ~0u, ~0u, [](uint32_t a, uint32_t b) { return min(a, b); });
+    return Piece{top, wave_min(p.low), at};
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) long_top_kernel(LongArgs q)
 {
-    __shared__ float tops[kLongThreads / 64], lows[kLongThreads / 64];
-    __shared__ uint32_t ats[kLongThreads / 64];
+    __shared__ Piece lds[kLongWaves];
     const int piece = blockIdx.x, r = blockIdx.y;
     const T *const x = static_cast<const T *>(q.a.logits) + (q.row0 + r) * q.a.ld;
     const int64_t begin = piece * q.chunk, end = min(q.a.n, begin + q.chunk);
-    float top = -INFINITY, low = INFINITY;
-    uint32_t at = ~0u;
-    visit_chunk(x, begin, end, kLongThreads, [&](float v, int64_t i) {
-        if (v > top) { top = v; at = (uint32_t)i; }     // (a thread's indices ascend)
-        if (v > -INFINITY) low = fminf(low, v);
+    Piece p{-INFINITY, INFINITY, ~0u};
+    visit_span(x, begin, end, threadIdx.x, kLongThreads, [&](float v, int64_t i) {
+        p.at = v > p.top ? (uint32_t)i : p.at;
+        p.top = fmaxf(p.top, v);
+        p.low = fminf(p.low, v > -INFINITY ? v : INFINITY);
     });
-    auto join = [&](float t, float l, uint32_t i) {
-        if (t > top || (t == top && i < at)) { top = t; at = i; }
-        low = fminf(low, l);
-    };
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) join(__shfl_xor(top, off, 64), __shfl_xor(low, off, 64), (uint32_t)__shfl_xor((int)at, off, 64));
-    if ((threadIdx.x & 63) == 0) { tops[threadIdx.x >> 6] = top; lows[threadIdx.x >> 6] = low; ats[threadIdx.x >> 6] = at; }
+    p = of_wave(p);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = p;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kLongThreads / 64; ++w) join(tops[w], lows[w], ats[w]);
-        q.piece[(int64_t)r * q.pieces + piece] = Piece{top, low, at};
+        for (int w = 1; w < kLongWaves; ++w) p = joined(p, lds[w]);
+        q.piece[(int64_t)r * q.pieces + piece] = p;
         if (piece == 0) q.listed[r] = 0;
     }
     // the row's histogram is cleared by its workgroups together
-    for (int b = piece * kLongThreads + threadIdx.x; b < kLongBins; b += q.pieces * kLongThreads) {
-        q.count[(int64_t)r * kLongBins + b] = 0;
-        q.mass[(int64_t)r * kLongBins + b] = 0;
-    }
+    if (q.a.top_k || q.a.top_p)
+        for (int b = piece * kLongThreads + threadIdx.x; b < kLongBins; b += q.pieces * kLongThreads) {
+            q.count[(int64_t)r * kLongBins + b] = 0;
+            q.mass[(int64_t)r * kLongBins + b] = 0;
+        }
 }
 
-// The whole row's largest entry, the first place it is at, and the smallest that is not masked
-template <int NT>
-__device__ inline Piece row_top(const LongArgs &q, int r, Piece *lds)
+// The whole row's largest entry, the first place it is at, and the smallest that is not masked: every wave for itself
+__device__ inline Piece row_top(const LongArgs &q, int r)
 {
     Piece p{-INFINITY, INFINITY, ~0u};
-    auto join = [&](const Piece &o) {
-        if (o.top > p.top || (o.top == p.top && o.at < p.at)) { p.top = o.top; p.at = o.at; }
-        p.low = fminf(p.low, o.low);
-    };
-    for (int i = threadIdx.x; i < q.pieces; i += NT) join(q.piece[(int64_t)r * q.pieces + i]);
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1)
-        join(Piece{__shfl_xor(p.top, off, 64), __shfl_xor(p.low, off, 64), (uint32_t)__shfl_xor((int)p.at, off, 64)});
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = p;
-    __syncthreads();
-    for (int w = 0; w < NT / 64; ++w) join(lds[w]);
-    __syncthreads();
-    return p;
+    for (int i = threadIdx.x & 63; i < q.pieces; i += 64) p = joined(p, q.piece[(int64_t)r * q.pieces + i]);
+    return of_wave(p);
 }
 
 // whether a row's cut has to be looked for (a single entry, its largest, is known from the maxima)
@@ -686,22 +681,17 @@ __global__ void __launch_bounds__(kLongThreads) long_histogram_kernel(LongArgs q
 {
     __shared__ uint64_t mass[kLongBins];
     __shared__ uint32_t count[kLongBins];
-    __shared__ Piece lds[kLongThreads / 64];
     const int piece = blockIdx.x, r = blockIdx.y;
     const RowRules rules = rules_of(q.a, q.row0 + r);
-    const Piece p = row_top<kLongThreads>(q, r, lds);
+    const Piece p = row_top(q, r);
     if (!cuts(q, rules, p.top)) return;
     const float scale = bin_scale(-scaled_logit(p.low, p.top, rules.inv), kLongBins);
-    if (piece == 0 && threadIdx.x == 0) {
-        q.bins[r].top = p.top;
-        q.bins[r].scale = scale;
-    }
     for (int b = threadIdx.x; b < kLongBins; b += kLongThreads) { count[b] = 0; mass[b] = 0; }
     __syncthreads();
     const T *const x = static_cast<const T *>(q.a.logits) + (q.row0 + r) * q.a.ld;
     const int64_t begin = piece * q.chunk, end = min(q.a.n, begin + q.chunk);
     const bool use_p = rules.p < 1.0f;
-    visit_chunk(x, begin, end, kLongThreads, [&](float v, int64_t) {
+    visit_span(x, begin, end, threadIdx.x, kLongThreads, [&](float v, int64_t) {
         const uint32_t key = key_of(scaled_logit(v, p.top, rules.inv));
         if (key >= kMaskedKey) return;
         const int b = bin_of(key, scale, kLongBins);
@@ -709,230 +699,165 @@ __global__ void __launch_bounds__(kLongThreads) long_histogram_kernel(LongArgs q
         if (use_p) atomicAdd(reinterpret_cast<unsigned long long *>(&mass[b]), (unsigned long long)weight_of_key(key));
     });
     __syncthreads();
+    uint32_t *const row_count = q.count + (int64_t)r * kLongBins;
+    uint64_t *const row_mass = q.mass + (int64_t)r * kLongBins;
     for (int b = threadIdx.x; b < kLongBins; b += kLongThreads)
         if (count[b]) {
-            atomicAdd(&q.count[(int64_t)r * kLongBins + b], count[b]);
-            if (use_p && mass[b]) atomicAdd(reinterpret_cast<unsigned long long *>(&q.mass[(int64_t)r * kLongBins + b]), (unsigned long long)mass[b]);
+            atomicAdd(&row_count[b], count[b]);
+            if (use_p && mass[b]) atomicAdd(reinterpret_cast<unsigned long long *>(&row_mass[b]), (unsigned long long)mass[b]);
         }
 }
 
-// From the row's histogram the bins that its cuts lie in; then the entries of a chunk in these bins.
-template <typename T>
-__global__ void __launch_bounds__(kLongThreads) long_list_kernel(LongArgs q)
+// The bins that a row's cuts lie in.  (Found by the last workgroup of the row to finish its histogram this took 100 us more: its fence
+// writes the second-level cache back.)
+__global__ void __launch_bounds__(kLongThreads) long_bins_kernel(LongArgs q)
 {
     using Grp = Group<kLongThreads>;
-    __shared__ typename Grp::Shared s;
-    __shared__ uint64_t stage[kLongStage];
-    __shared__ uint32_t staged, base;
+    __shared__ typename Grp::Waves waves;
+    __shared__ uint64_t around[2];
     __shared__ int32_t bin_k, bin_first, bin_last;
-    constexpr int B = kLongBins / kLongThreads;
-    const int piece = blockIdx.x, r = blockIdx.y;
+    const int r = blockIdx.x;
     const RowRules rules = rules_of(q.a, q.row0 + r);
-    float top = -INFINITY;
-    for (int i = 0; i < q.pieces; i += 64) {            // (a wave's worth at a time)
-        const int at = i + (threadIdx.x & 63);
-        top = fmaxf(top, at < q.pieces ? q.piece[(int64_t)r * q.pieces + at].top : -INFINITY);
-    }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    if (!cuts(q, rules, top)) return;
-    const float scale = q.bins[r].scale;
-    uint32_t count[B];
-    uint64_t mass[B], n = 0, w = 0, all_n, all_w;
+    const Piece p = row_top(q, r);
+    if (!cuts(q, rules, p.top)) return;
+    const bool use_p = rules.p < 1.0f;
+    const uint32_t *const row_count = q.count + (int64_t)r * kLongBins;
+    const uint64_t *const row_mass = q.mass + (int64_t)r * kLongBins;
+    constexpr int B = kLongBins / kLongThreads;
+    uint32_t c_of[B];
+    uint64_t m_of[B], n = 0, w = 0, all_n, all_w;
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-        count[b] = q.count[(int64_t)r * kLongBins + threadIdx.x * B + b];
-        mass[b] = q.mass[(int64_t)r * kLongBins + threadIdx.x * B + b];
-        n += count[b];
-        w += mass[b];
+        c_of[b] = row_count[threadIdx.x * B + b];
+        m_of[b] = row_mass[threadIdx.x * B + b];
+        n += c_of[b];
+        w += m_of[b];
     }
-    const uint64_t n_before = Grp::scan(s, n, &all_n), w_before = Grp::scan(s, w, &all_w);
-    if (threadIdx.x == 0) { bin_k = -1; bin_first = bin_last = -1; staged = 0; }
+    const uint64_t n_before = Grp::scan(waves, n, &all_n), w_before = Grp::scan(waves, w, &all_w);
+    if (threadIdx.x == 0) bin_k = bin_first = bin_last = -1;
     __syncthreads();
-    // the last bin that begins below, for `below` of the entries and the weight before it
-    auto last_bin = [&](int32_t *found, auto below) {
+    // every bin with entries and weight before it, by the thread that has it
+    auto bins = [&](auto what) {
         uint64_t c = n_before, m = w_before;
-        int mine = -1;
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-            if (count[b] > 0 && below(c, m)) mine = threadIdx.x * B + b;
-            c += count[b];
-            m += mass[b];
+            what((int)threadIdx.x * B + b, c_of[b], m_of[b], c, m);
+            c += c_of[b];
+            m += m_of[b];
         }
+    };
+    // the last bin that begins below
+    auto last_bin = [&](int32_t *found, auto below) {
+        int mine = -1;
+        bins([&](int b, uint32_t c, uint64_t, uint64_t c0, uint64_t m0) { mine = (c > 0) & below(c0, m0) ? b : mine; });
         if (mine >= 0) atomicMax(found, mine);
         __syncthreads();
     };
-    // weight that top-k keeps, at least and at most
-    uint64_t least = all_w, most = all_w;
     RowBins *const out = &q.bins[r];
-    // a bin's count, and entries and weight before it, by the thread that has it
-    auto of_bin = [&](int bin, auto what) {
-        uint64_t c = n_before, m = w_before;
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-            if ((int)threadIdx.x * B + b == bin) what(count[b], mass[b], c, m);
-            c += count[b];
-            m += mass[b];
-        }
-    };
+    uint64_t least = all_w, most = all_w;               // weight that top-k keeps, at least and at most
     if (rules.k < q.a.n) {
         last_bin(&bin_k, [&](uint64_t c, uint64_t) { return c < (uint64_t)rules.k; });
-        of_bin(bin_k, [&](uint32_t c, uint64_t m, uint64_t c0, uint64_t m0) {
-            s.place[0] = m0;
-            s.place[1] = m0 + m;
-            if (piece == 0) {
-                out->k_count = c;
-                out->k_before = (uint32_t)c0;
-                out->k_mass_before = m0;
-            }
+        bins([&](int b, uint32_t c, uint64_t m, uint64_t c0, uint64_t m0) {
+            if (b != bin_k) return;
+            around[0] = m0;
+            around[1] = m0 + m;
+            out->k_count = c;
+            out->k_before = (uint32_t)c0;
+            out->k_mass_before = m0;
         });
         __syncthreads();
-        least = s.place[0];
-        most = s.place[1];
+        least = around[0];
+        most = around[1];
     }
-    if (rules.p < 1.0f) {
-        last_bin(&bin_first, [&](uint64_t c, uint64_t m) { return begins_below(true, c, m, 0, (double)rules.p * (double)least); });
-        last_bin(&bin_last, [&](uint64_t c, uint64_t m) { return begins_below(true, c, m, 0, (double)rules.p * (double)most); });
-        if (piece == 0) of_bin(bin_first, [&](uint32_t, uint64_t, uint64_t, uint64_t m0) { out->p_mass_before = m0; });
+    if (use_p) {
+        last_bin(&bin_first, [&](uint64_t, uint64_t m) { return begins_below(true, m, 0, (double)rules.p * (double)least); });
+        last_bin(&bin_last, [&](uint64_t, uint64_t m) { return begins_below(true, m, 0, (double)rules.p * (double)most); });
+        bins([&](int b, uint32_t, uint64_t, uint64_t, uint64_t m0) {
+            if (b == bin_first) out->p_mass_before = m0;
+        });
     }
-    const int k_bin = bin_k, p_first = bin_first, p_last = bin_last;
-    if (piece == 0 && threadIdx.x == 0) {
-        out->k_bin = k_bin;
-        out->p_first = p_first;
-        out->p_last = p_last;
+    if (threadIdx.x == 0) {
+        out->k_bin = bin_k;
+        out->p_first = bin_first;
+        out->p_last = bin_last;
+        out->mass = all_w;
+        out->top = p.top;
+        out->scale = bin_scale(-scaled_logit(p.low, p.top, rules.inv), kLongBins);
     }
-    const T *const x = static_cast<const T *>(q.a.logits) + (q.row0 + r) * q.a.ld;
-    const int64_t begin = piece * q.chunk, end = min(q.a.n, begin + q.chunk);
-    visit_chunk(x, begin, end, kLongThreads, [&](float v, int64_t i) {
-        const uint32_t key = key_of(scaled_logit(v, top, rules.inv));
-        if (key >= kMaskedKey) return;
-        const int b = bin_of(key, scale, kLongBins);
-        if (b != k_bin && (b < p_first || b > p_last || p_first < 0)) return;
-        const uint64_t place = (uint64_t)key << 32 | (uint32_t)i;
-        const uint32_t at = atomicAdd(&staged, 1u);
-        if (at < kLongStage) stage[at] = place;
-        else {
-            const uint32_t to = atomicAdd(&q.listed[r], 1u);
-            if (to < kLongList) q.list[(int64_t)r * kLongList + to] = place;
-        }
-    });
-    __syncthreads();
-    const uint32_t own = staged < kLongStage ? staged : kLongStage;
-    if (threadIdx.x == 0) base = atomicAdd(&q.listed[r], own);
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < own; i += kLongThreads)
-        if (base + i < kLongList) q.list[(int64_t)r * kLongList + base + i] = stage[i];
 }
 
-// The cuts, from the list, or from the row itself where its bins hold more entries than the list.
-template <typename T>
-__global__ void __launch_bounds__(1024) long_cut_kernel(LongArgs q)
+// what an entry adds to the draw, its place aside
+__device__ inline uint64_t kept_weight(uint32_t key, const RowRules &rules)
 {
-    using Grp = Group<1024>;
-    __shared__ typename Grp::Shared s;
-    __shared__ Piece lds[1024 / 64];
-    const int r = blockIdx.x;
-    const RowRules rules = rules_of(q.a, q.row0 + r);
-    const Piece p = row_top<1024>(q, r, lds);
-    if (!cuts(q, rules, p.top)) return;
-    const RowBins bins = q.bins[r];
-    const uint32_t listed = q.listed[r];
-    const uint64_t *const list = q.list + (int64_t)r * kLongList;
-    const T *const x = static_cast<const T *>(q.a.logits) + (q.row0 + r) * q.a.ld;
-    uint64_t cut = ~0ull;
-    auto entries_of = [&](int bin) {
-        return [&, bin](auto what) {
-            if (listed <= kLongList) {
-                for (uint32_t i = threadIdx.x; i < listed; i += 1024) {
-                    const uint64_t at = list[i];
-                    const uint32_t key = (uint32_t)(at >> 32);
-                    if (at <= cut && bin_of(key, bins.scale, kLongBins) == bin) what(at, key);
-                }
-            } else {
-                visit_chunk(x, 0, q.a.n, 1024, [&](float v, int64_t i) {
-                    const uint32_t key = key_of(scaled_logit(v, p.top, rules.inv));
-                    const uint64_t at = (uint64_t)key << 32 | (uint32_t)i;
-                    if (key < kMaskedKey && at <= cut && bin_of(key, bins.scale, kLongBins) == bin) what(at, key);
-                });
-            }
-        };
-    };
-    const uint32_t *const count = q.count + (int64_t)r * kLongBins;
-    const uint64_t *const mass = q.mass + (int64_t)r * kLongBins;
-    uint64_t kept = 0;
-    if (rules.k < q.a.n) {
-        cut = Grp::last_below(s, entries_of(bins.k_bin), bins.k_count, false, (uint64_t)rules.k, 0.0, bins.k_before, 0);
-        if (rules.p < 1.0f) {
-            uint64_t w = 0;
-            entries_of(bins.k_bin)([&](uint64_t, uint32_t key) { w += weight_of_key(key); });
-            kept = bins.k_mass_before + Grp::sum(s, w);
-        }
-    } else {
-        uint64_t w = 0;
-        for (int b = threadIdx.x; b < kLongBins; b += 1024) w += mass[b];
-        kept = Grp::sum(s, w);
-    }
-    if (rules.p < 1.0f) {
-        const double limit = (double)rules.p * (double)kept;
-        int bin = bins.p_first;
-        uint64_t before = bins.p_mass_before, m = before;
-        for (int b = bins.p_first; b <= bins.p_last; ++b) {
-            if (count[b] > 0 && begins_below(true, 0, m, 0, limit)) { bin = b; before = m; }
-            m += mass[b];
-        }
-        cut = Grp::last_below(s, entries_of(bin), count[bin], true, 0, limit, 0, before);
-    }
-    if (threadIdx.x == 0) q.bins[r].cut = cut;
+    const float e = expf(-distance_of(key));
+    return (e < rules.least) & (key != 0) ? 0 : weight_of(e);
 }
 
-// what an entry adds to the draw
-__device__ inline uint64_t drawn_weight(float v, int64_t i, float top, const RowRules &rules, uint64_t cut, uint32_t *key_out)
-{
-    const float d = scaled_logit(v, top, rules.inv);
-    const uint32_t key = key_of(d);
-    *key_out = key;
-    if (key >= kMaskedKey || ((uint64_t)key << 32 | (uint32_t)i) > cut) return 0;
-    const float e = expf(d);
-    return e < rules.least && key != 0 ? 0 : weight_of(e);
-}
-
+// The weights of a chunk's segments, as far as they lie before the bins of the row's cuts, and the entries in these bins.
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) long_weight_kernel(LongArgs q)
 {
-    __shared__ Piece lds[kLongThreads / 64];
-    __shared__ uint64_t sums[kLongThreads / 64];
-    const int piece = blockIdx.x, r = blockIdx.y;
+    __shared__ uint64_t stage[kLongStage];
+    __shared__ uint32_t staged, base;
+    const int piece = blockIdx.x, r = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const RowRules rules = rules_of(q.a, q.row0 + r);
-    const Piece p = row_top<kLongThreads>(q, r, lds);
-    if (!(p.top > -INFINITY) || rules.k == 1) return;
-    const uint64_t cut = cuts(q, rules, p.top) ? q.bins[r].cut : ~0ull;
+    const float top = row_top(q, r).top;
+    if (!(top > -INFINITY) || rules.k == 1) return;
     const T *const x = static_cast<const T *>(q.a.logits) + (q.row0 + r) * q.a.ld;
-    const int64_t begin = piece * q.chunk, end = min(q.a.n, begin + q.chunk);
+    const int64_t segment = q.chunk / kLongWaves;
+    const int64_t begin = min(q.a.n, piece * q.chunk + wave * segment), end = min(q.a.n, begin + segment);
     uint64_t w = 0;
-    uint32_t key;
-    visit_chunk(x, begin, end, kLongThreads, [&](float v, int64_t i) { w += drawn_weight(v, i, p.top, rules, cut, &key); });
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) w += __shfl_xor((unsigned long long)w, off, 64);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = w;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < kLongThreads / 64; ++i) w += sums[i];
-        q.weight[(int64_t)r * q.pieces + piece] = w;
+    if (!cuts(q, rules, top)) {
+        visit_span(x, begin, end, lane, 64, [&](float v, int64_t) {
+            const uint32_t key = key_of(scaled_logit(v, top, rules.inv));
+            if (key < kMaskedKey) w += kept_weight(key, rules);
+        });
+    } else {
+        if (threadIdx.x == 0) staged = 0;
+        __syncthreads();
+        const RowBins bins = q.bins[r];
+        const int before = rules.p < 1.0f ? bins.p_first : bins.k_bin;
+        visit_span(x, begin, end, lane, 64, [&](float v, int64_t i) {
+            const uint32_t key = key_of(scaled_logit(v, top, rules.inv));
+            if (key >= kMaskedKey) return;
+            const int b = bin_of(key, bins.scale, kLongBins);
+            if (b < before) w += kept_weight(key, rules);
+            else if (b <= bins.p_last || b == bins.k_bin) {
+                const uint64_t place = (uint64_t)key << 32 | (uint32_t)i;
+                const uint32_t at = atomicAdd(&staged, 1u);
+                if (at < kLongStage) stage[at] = place;
+                else {
+                    const uint32_t to = atomicAdd(&q.listed[r], 1u);
+                    if (to < kLongList) q.list[(int64_t)r * kLongList + to] = place;
+                }
+            }
+        });
+        __syncthreads();
+        const uint32_t own = staged < kLongStage ? staged : kLongStage;
+        if (own > 0) {                                  // (the same in every thread)
+            if (threadIdx.x == 0) base = atomicAdd(&q.listed[r], own);
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < own; i += kLongThreads)
+                if (base + i < kLongList) q.list[(int64_t)r * kLongList + base + i] = stage[i];
+        }
     }
+    w = wave_sum(w);
+    if (lane == 0) q.weight[((int64_t)r * q.pieces + piece) * kLongWaves + wave] = w;
 }
 
+// The cuts, from the list, or from the row itself where its bins hold more entries than the list; then the draw.
 template <typename T>
 __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
 {
     using Grp = Group<1024>;
     __shared__ typename Grp::Shared s;
-    __shared__ Piece lds[1024 / 64];
+    __shared__ uint64_t weight[kMostSegments];
     __shared__ int found;
     __shared__ uint64_t found_before;
     const int r = blockIdx.x;
     const int64_t row = q.row0 + r;
     const RowRules rules = rules_of(q.a, row);
-    const Piece p = row_top<1024>(q, r, lds);
+    const Piece p = row_top(q, r);
     if (!(p.top > -INFINITY) || rules.k == 1) {
         if (threadIdx.x == 0) {
             if (p.top > -INFINITY) {
@@ -942,32 +867,113 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
         }
         return;
     }
-    const uint64_t cut = cuts(q, rules, p.top) ? q.bins[r].cut : ~0ull;
-    uint64_t total;
-    const uint64_t w = (int)threadIdx.x < q.pieces ? q.weight[(int64_t)r * q.pieces + threadIdx.x] : 0;
-    uint64_t run = Grp::scan(s, w, &total);
-    const double mark = rules.u * (double)total;
-    auto beyond = [&](uint64_t v) { return (double)v > mark || v == total; };
-    if (beyond(run + w) && !beyond(run)) {              // (one chunk)
-        found = (int)threadIdx.x;
-        found_before = run;
+    const T *const x = static_cast<const T *>(q.a.logits) + row * q.a.ld;
+    const int64_t segment = q.chunk / kLongWaves;
+    const int segments = q.pieces * kLongWaves;
+    for (int i = threadIdx.x; i < segments; i += 1024) weight[i] = q.weight[(int64_t)r * segments + i];
+    uint64_t cut = ~0ull;
+    if (cuts(q, rules, p.top)) {
+        const RowBins bins = q.bins[r];
+        const uint32_t listed = q.listed[r];
+        const bool whole = listed <= kLongList;
+        const uint64_t *const list = q.list + (int64_t)r * kLongList;
+        auto entries = [&](auto what) {
+            if (whole) {
+                for (uint32_t i = threadIdx.x; i < listed; i += 1024) {
+                    const uint64_t at = list[i];
+                    what(at, (uint32_t)(at >> 32));
+                }
+            } else {
+                for (int64_t i = threadIdx.x; i < q.a.n; i += 1024) {
+                    const uint32_t key = key_of(scaled_logit(logit_of(x[i]), p.top, rules.inv));
+                    if (key < kMaskedKey) what((uint64_t)key << 32 | (uint32_t)i, key);
+                }
+            }
+        };
+        auto of_bin = [&](int bin) {
+            return [&, bin](auto what) {
+                entries([&](uint64_t at, uint32_t key) {
+                    if (at <= cut && bin_of(key, bins.scale, kLongBins) == bin) what(at, key);
+                });
+            };
+        };
+        uint64_t kept = bins.mass;
+        if (rules.k < q.a.n) {
+            cut = Grp::last_below(s, of_bin(bins.k_bin), bins.k_count, false, (uint64_t)rules.k, 0.0, bins.k_before);
+            if (rules.p < 1.0f) {
+                uint64_t w = 0;
+                of_bin(bins.k_bin)([&](uint64_t, uint32_t key) { w += weight_of_key(key); });
+                kept = bins.k_mass_before + Grp::sum(s, w);
+            }
+        }
+        if (rules.p < 1.0f) {
+            const uint32_t *const count = q.count + (int64_t)r * kLongBins;
+            const uint64_t *const mass = q.mass + (int64_t)r * kLongBins;
+            const double limit = (double)rules.p * (double)kept;
+            int bin = bins.p_first;
+            uint64_t before = bins.p_mass_before, m = before;
+            for (int b = bins.p_first; b <= bins.p_last; ++b) {
+                if (count[b] > 0 && begins_below(true, m, 0, limit)) { bin = b; before = m; }
+                m += mass[b];
+            }
+            cut = Grp::last_below(s, of_bin(bin), count[bin], true, 0, limit, before);
+        }
+        // what the cuts' bins add to the segments (the row itself, where the list is not whole: everything)
+        if (!whole)
+            for (int i = threadIdx.x; i < segments; i += 1024) weight[i] = 0;
+        __syncthreads();
+        entries([&](uint64_t at, uint32_t key) {
+            if (at > cut) return;
+            const uint64_t w = kept_weight(key, rules);
+            if (w) atomicAdd(reinterpret_cast<unsigned long long *>(&weight[(uint32_t)at / (uint32_t)segment]), (unsigned long long)w);
+        });
     }
     __syncthreads();
-    // the chunk, a part per thread in the order of the entries
-    const T *const x = static_cast<const T *>(q.a.logits) + row * q.a.ld;
-    const int64_t begin = found * q.chunk, end = min(q.a.n, begin + q.chunk), part = (end - begin + 1023) / 1024;
-    const int64_t from = min(end, begin + part * threadIdx.x), to = min(end, from + part);
-    uint64_t mine = 0, all;
-    uint32_t key;
-    for (int64_t i = from; i < to; ++i) mine += drawn_weight(logit_of(x[i]), i, p.top, rules, cut, &key);
-    run = found_before + Grp::scan(s, mine, &all);
-    if (beyond(run + mine) && !beyond(run)) {
-        for (int64_t i = from; i < to; ++i) {
-            run += drawn_weight(logit_of(x[i]), i, p.top, rules, cut, &key);
-            if (beyond(run)) {
-                q.a.token[row] = (int32_t)i;
-                if (q.a.logprob) q.a.logprob[row] = -distance_of(key) - log_of(total);
+    constexpr int S = kMostSegments / 1024;
+    uint64_t mine = 0, total;
+#pragma unroll
+    for (int i = 0; i < S; ++i) mine += (int)threadIdx.x * S + i < segments ? weight[threadIdx.x * S + i] : 0;
+    uint64_t run = Grp::scan(s.waves, mine, &total);
+    const double mark = rules.u * (double)total;
+    auto beyond = [&](uint64_t v) { return ((double)v > mark) | (v == total); };
+    if (beyond(run + mine) && !beyond(run)) {           // (one thread)
+        for (int i = threadIdx.x * S; i < segments; ++i) {
+            if (beyond(run + weight[i])) {
+                found = i;
+                found_before = run;
                 break;
+            }
+            run += weight[i];
+        }
+    }
+    __syncthreads();
+    // the segment, a part per thread in the order of the entries
+    constexpr int E = kMostChunk / kLongWaves / 1024;
+    const int64_t begin = found * segment, end = min(q.a.n, begin + segment), part = (segment + 1023) / 1024;
+    const int64_t from = min(end, begin + part * threadIdx.x), to = min(end, from + part);
+    uint32_t key[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const float v = logit_of(x[min(from + j, q.a.n - 1)]);
+        key[j] = from + j < to ? key_of(scaled_logit(v, p.top, rules.inv)) : kMaskedKey;
+    }
+    auto drawn = [&](int j) -> uint64_t {
+        return key[j] < kMaskedKey && ((uint64_t)key[j] << 32 | (uint32_t)(from + j)) <= cut ? kept_weight(key[j], rules) : 0;
+    };
+    uint64_t all;
+    mine = 0;
+#pragma unroll
+    for (int j = 0; j < E; ++j) mine += drawn(j);
+    run = found_before + Grp::scan(s.waves, mine, &all);
+    if (beyond(run + mine) && !beyond(run)) {
+        bool open = true;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            run += drawn(j);
+            if (open && beyond(run)) {
+                open = false;
+                q.a.token[row] = (int32_t)(from + j);
+                if (q.a.logprob) q.a.logprob[row] = -distance_of(key[j]) - log_of(total);
             }
         }
     }
@@ -977,7 +983,7 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
 int64_t chunk_of(int64_t rows, int64_t n)
 {
     const int64_t unit = (int64_t)kLongThreads * kLoad;
-    const int64_t pieces = std::max<int64_t>((n + 65535) / 65536, std::min<int64_t>(kMostPieces / rows, n / unit));
+    const int64_t pieces = std::max<int64_t>((n + kMostChunk - 1) / kMostChunk, std::min<int64_t>(kMostPieces / rows, n / unit));
     return ((n + pieces - 1) / pieces + unit - 1) / unit * unit;
 }
 
@@ -994,7 +1000,7 @@ LongLayout long_layout(int64_t rows, int64_t n)
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t here = at; at += align_up(bytes, 256); return here; };
     L.piece = take(L.rows * L.pieces * (int64_t)sizeof(Piece));
-    L.weight = take(L.rows * L.pieces * 8);
+    L.weight = take(L.rows * L.pieces * kLongWaves * 8);
     L.mass = take(L.rows * kLongBins * 8);
     L.count = take(L.rows * kLongBins * 4);
     L.listed = take(L.rows * 4);
@@ -1026,8 +1032,7 @@ hipError_t launch_long_rows(const SampleArgs &a, char *ws, hipStream_t s)
         hipLaunchKernelGGL(long_top_kernel<T>, grid, threads, 0, s, q);
         if (a.top_k || a.top_p) {
             hipLaunchKernelGGL(long_histogram_kernel<T>, grid, threads, 0, s, q);
-            hipLaunchKernelGGL(long_list_kernel<T>, grid, threads, 0, s, q);
-            hipLaunchKernelGGL(long_cut_kernel<T>, each, dim3(1024), 0, s, q);
+            hipLaunchKernelGGL(long_bins_kernel, each, threads, 0, s, q);
         }
         hipLaunchKernelGGL(long_weight_kernel<T>, grid, threads, 0, s, q);
         hipLaunchKernelGGL(long_draw_kernel<T>, each, dim3(1024), 0, s, q);
