@@ -49,7 +49,7 @@ __device__ inline RowRules rules_of(const SampleArgs &a, int64_t row)
     RowRules r;
     const bool greedy = a.temperature && !(t > 0.0f);
     r.k = greedy ? 1 : (a.top_k && k >= 1 && k < a.n ? (int64_t)k : a.n);
-    r.inv = a.temperature && !greedy ? 1.0f / t : 1.0f;
+    r.inv = a.temperature && !greedy ? fminf(1.0f / t, 3.4028235e38f) : 1.0f;
     r.p = a.top_p && p < 1.0f ? p : 1.0f;
     r.least = a.min_p && m > 0.0f ? m : 0.0f;
     r.u = u > 0.0f ? (double)u : 0.0;
@@ -63,21 +63,34 @@ __device__ inline float logit_of(T x)
     const float v = (float)x;
     return v == v ? v : -INFINITY;
 }
-__device__ inline float scaled_logit(float x, float top, float inv)
+// -d: 0 for the largest, infinite (or no number) for what is never drawn
+__device__ inline float distance_from(float top, float x, float inv)
 {
-    const float gap = x - top;
-    return x == top ? 0.0f : (gap == -INFINITY ? -INFINITY : gap * inv);
+    if (top == INFINITY) return x == INFINITY ? 0.0f : INFINITY;
+    return (top - x) * inv;
 }
-__device__ inline uint32_t key_of(float d) { return __float_as_uint(d) & 0x7fffffffu; }
-__device__ inline float distance_of(uint32_t key) { return __uint_as_float(key); }       // -d
+__device__ inline uint32_t key_of(float distance) { return distance < INFINITY ? __float_as_uint(distance) : kMaskedKey; }
+__device__ inline float distance_of(uint32_t key) { return __uint_as_float(key); }
 
-// weight of an entry: exp(d) in multiples of 2^-38 (adding 1.5 * 2^14 leaves the whole number in the low bits of a double)
-__device__ inline uint64_t weight_of(float e)
+// exp(-distance) = 2^(-distance log2 e), the logarithm in two pieces: an exponential of the hardware and eight operations.  (Without what a
+// general one does about results beyond the largest and below the smallest normal number: weights end at 2^-38, and beyond 100, at
+// infinity and where there is no number this is exp(-100), which is no weight.)
+__device__ inline float exp_of(float x)
 {
-    constexpr double kMagic = 1.5 * 16384.0;
-    return (uint64_t)(__double_as_longlong((double)e + kMagic) - __double_as_longlong(kMagic));
+    const float distance = fminf(x, 100.0f);
+    constexpr float kHi = 0x1.715476p+0f, kLo = 0x1.4ae0bep-26f;
+    const float whole = distance * -kHi, n = rintf(whole);
+    const float rest = fmaf(distance, -kLo, fmaf(distance, -kHi, -whole));
+    return ldexpf(__builtin_amdgcn_exp2f((whole - n) + rest), (int)n);
 }
-__device__ inline uint64_t weight_of_key(uint32_t key) { return weight_of(expf(-distance_of(key))); }
+
+// Weight of an entry: its exponential in multiples of 2^-38 (adding 1.5 * 2^14 leaves the whole number in the low bits of a double).  Sums of
+// many leave that offset in and take it off at the end, once per summand.
+constexpr double kOffset = 1.5 * 16384.0;
+__device__ inline uint64_t raw_weight(float e) { return (uint64_t)__double_as_longlong((double)e + kOffset); }
+__device__ inline uint64_t offsets(uint64_t n) { return n * (uint64_t)__double_as_longlong(kOffset); }
+__device__ inline uint64_t weight_of(float e) { return raw_weight(e) - offsets(1); }
+__device__ inline uint64_t weight_of_key(uint32_t key) { return weight_of(exp_of(distance_of(key))); }
 // whether an entry with so many entries, or so much weight, before it is inside top-k, or top-p (the first one always is)
 __device__ inline bool begins_below(bool by_mass, uint64_t before, uint64_t k, double limit)
 {
@@ -120,13 +133,14 @@ __global__ void __launch_bounds__(256) sample_short_kernel(SampleArgs a)
     }
     if (top == -INFINITY) { no_draw(a, row); return; }
     const RowRules r = rules_of(a, row);
-    float d[V], e[V];
+    uint32_t key[V];
+    float e[V];
     uint64_t w[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        d[i] = scaled_logit(l[i], top, r.inv);
-        e[i] = expf(d[i]);
-        w[i] = d[i] > -INFINITY ? weight_of(e[i]) : 0;
+        key[i] = key_of(distance_from(top, l[i], r.inv));
+        e[i] = exp_of(distance_of(key[i]));
+        w[i] = key[i] < kMaskedKey ? weight_of(e[i]) : 0;
     }
     if (r.k < n || r.p < 1.0f) {
         uint64_t before[V], total = 0;                  // weight of what comes before an entry, top-k applied
@@ -137,7 +151,7 @@ __global__ void __launch_bounds__(256) sample_short_kernel(SampleArgs a)
             before[i] = 0;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const bool first = (d[j] > d[i]) | ((d[j] == d[i]) & (j < i));
+                const bool first = (key[j] < key[i]) | ((key[j] == key[i]) & (j < i));
                 rank += first;
                 before[i] += first ? w[j] : 0;
             }
@@ -156,7 +170,7 @@ __global__ void __launch_bounds__(256) sample_short_kernel(SampleArgs a)
     uint64_t total = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        w[i] = (e[i] < r.least) & (d[i] != 0.0f) ? 0 : w[i];
+        w[i] = (e[i] < r.least) & (key[i] != 0) ? 0 : w[i];
         total += w[i];
     }
     const double mark = r.u * (double)total;
@@ -168,7 +182,7 @@ __global__ void __launch_bounds__(256) sample_short_kernel(SampleArgs a)
         run += w[i];
         const bool here = (token < 0) & (((double)run > mark) | (run == total));
         token = here ? i : token;
-        d_token = here ? d[i] : d_token;
+        d_token = here ? -distance_of(key[i]) : d_token;
     }
     a.token[row] = token;
     if (a.logprob) a.logprob[row] = d_token - log_of(total);
@@ -491,12 +505,12 @@ __global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a)
         typename Grp::template Entries<E> entry;
         entry.first = (uint32_t)first;
 #pragma unroll
-        for (int j = 0; j < E; ++j) entry.key[j] = key_of(scaled_logit(l[j], top, r.inv));
+        for (int j = 0; j < E; ++j) entry.key[j] = key_of(distance_from(top, l[j], r.inv));
         uint64_t cut = ~0ull;
-        if (r.k < n || r.p < 1.0f) cut = Grp::cut_of(s, entry, -scaled_logit(low, top, r.inv), (uint64_t)r.k, r.k < n, r.p, r.p < 1.0f);
+        if (r.k < n || r.p < 1.0f) cut = Grp::cut_of(s, entry, distance_from(top, low, r.inv), (uint64_t)r.k, r.k < n, r.p, r.p < 1.0f);
         auto weight = [&](int j) -> uint64_t {
             if (!entry.there(j) || !entry.upto(j, cut)) return 0;
-            const float e = expf(-distance_of(entry.key[j]));
+            const float e = exp_of(distance_of(entry.key[j]));
             return e < r.least && entry.key[j] != 0 ? 0 : weight_of(e);
         };
         uint64_t mine = 0, total;
@@ -580,10 +594,11 @@ struct Piece {
 };
 struct RowBins {                                        // where a row's cuts lie
     int32_t k_bin, p_first, p_last;                     // top-k's bin; top-p's is one of these, which depends on what top-k keeps of its own
+    float near, far, k_near, k_far;                     // distances: kept in any case before `near`; the bins' entries are from `near`, and `k_near`, on
     uint32_t k_count, k_before;
     uint64_t k_mass_before, p_mass_before;              // weight before k_bin, p_first
     uint64_t mass;                                      // of the row
-    float top, scale;
+    float scale;
 };
 struct LongArgs {
     SampleArgs a;
@@ -676,6 +691,14 @@ __device__ inline Piece row_top(const LongArgs &q, int r)
 // whether a row's cut has to be looked for (a single entry, its largest, is known from the maxima)
 __device__ inline bool cuts(const LongArgs &q, const RowRules &r, float top) { return top > -INFINITY && r.k != 1 && (r.k < q.a.n || r.p < 1.0f); }
 
+// `what` with a function from logits to distances: where nothing is infinite it has no case for that
+template <typename F>
+__device__ inline void with_distances(float top, float inv, F what)
+{
+    if (top < INFINITY) what([=](float v) { return (top - v) * inv; });
+    else what([=](float v) { return distance_from(top, v, inv); });
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) long_histogram_kernel(LongArgs q)
 {
@@ -685,27 +708,28 @@ __global__ void __launch_bounds__(kLongThreads) long_histogram_kernel(LongArgs q
     const RowRules rules = rules_of(q.a, q.row0 + r);
     const Piece p = row_top(q, r);
     if (!cuts(q, rules, p.top)) return;
-    const float scale = bin_scale(-scaled_logit(p.low, p.top, rules.inv), kLongBins);
+    const float scale = bin_scale(distance_from(p.top, p.low, rules.inv), kLongBins);
     for (int b = threadIdx.x; b < kLongBins; b += kLongThreads) { count[b] = 0; mass[b] = 0; }
     __syncthreads();
     const T *const x = static_cast<const T *>(q.a.logits) + (q.row0 + r) * q.a.ld;
     const int64_t begin = piece * q.chunk, end = min(q.a.n, begin + q.chunk);
-    const bool use_p = rules.p < 1.0f;
-    visit_span(x, begin, end, threadIdx.x, kLongThreads, [&](float v, int64_t) {
-        const uint32_t key = key_of(scaled_logit(v, p.top, rules.inv));
-        if (key >= kMaskedKey) return;
-        const int b = bin_of(key, scale, kLongBins);
-        atomicAdd(&count[b], 1u);
-        if (use_p) atomicAdd(reinterpret_cast<unsigned long long *>(&mass[b]), (unsigned long long)weight_of_key(key));
+    const bool use_k = rules.k < q.a.n, use_p = rules.p < 1.0f;
+    with_distances(p.top, rules.inv, [&](auto distance) {
+        visit_span(x, begin, end, threadIdx.x, kLongThreads, [&](float v, int64_t) {
+            const float d = distance(v);
+            if (!(d < INFINITY)) return;
+            const int b = (int)fminf(d * scale, (float)(kLongBins - 1));
+            if (use_k) atomicAdd(&count[b], 1u);
+            if (use_p) atomicAdd(reinterpret_cast<unsigned long long *>(&mass[b]), (unsigned long long)weight_of(exp_of(d)));
+        });
     });
     __syncthreads();
     uint32_t *const row_count = q.count + (int64_t)r * kLongBins;
     uint64_t *const row_mass = q.mass + (int64_t)r * kLongBins;
-    for (int b = threadIdx.x; b < kLongBins; b += kLongThreads)
-        if (count[b]) {
-            atomicAdd(&row_count[b], count[b]);
-            if (use_p && mass[b]) atomicAdd(reinterpret_cast<unsigned long long *>(&row_mass[b]), (unsigned long long)mass[b]);
-        }
+    for (int b = threadIdx.x; b < kLongBins; b += kLongThreads) {
+        if (count[b]) atomicAdd(&row_count[b], count[b]);
+        if (mass[b]) atomicAdd(reinterpret_cast<unsigned long long *>(&row_mass[b]), (unsigned long long)mass[b]);
+    }
 }
 
 // The bins that a row's cuts lie in.  (Found by the last workgroup of the row to finish its histogram this took 100 us more: its fence
@@ -717,10 +741,6 @@ __global__ void __launch_bounds__(kLongThreads) long_bins_kernel(LongArgs q)
     __shared__ uint64_t around[2];
     __shared__ int32_t bin_k, bin_first, bin_last;
     const int r = blockIdx.x;
-    const RowRules rules = rules_of(q.a, q.row0 + r);
-    const Piece p = row_top(q, r);
-    if (!cuts(q, rules, p.top)) return;
-    const bool use_p = rules.p < 1.0f;
     const uint32_t *const row_count = q.count + (int64_t)r * kLongBins;
     const uint64_t *const row_mass = q.mass + (int64_t)r * kLongBins;
     constexpr int B = kLongBins / kLongThreads;
@@ -733,10 +753,15 @@ __global__ void __launch_bounds__(kLongThreads) long_bins_kernel(LongArgs q)
         n += c_of[b];
         w += m_of[b];
     }
+    const RowRules rules = rules_of(q.a, q.row0 + r);
+    const Piece p = row_top(q, r);
+    if (!cuts(q, rules, p.top)) return;
+    const bool use_k = rules.k < q.a.n, use_p = rules.p < 1.0f;
+    const float scale = bin_scale(distance_from(p.top, p.low, rules.inv), kLongBins);
     const uint64_t n_before = Grp::scan(waves, n, &all_n), w_before = Grp::scan(waves, w, &all_w);
     if (threadIdx.x == 0) bin_k = bin_first = bin_last = -1;
     __syncthreads();
-    // every bin with entries and weight before it, by the thread that has it
+    // every bin with entries and weight in it and before it, by the thread that has it
     auto bins = [&](auto what) {
         uint64_t c = n_before, m = w_before;
 #pragma unroll
@@ -749,14 +774,14 @@ __global__ void __launch_bounds__(kLongThreads) long_bins_kernel(LongArgs q)
     // the last bin that begins below
     auto last_bin = [&](int32_t *found, auto below) {
         int mine = -1;
-        bins([&](int b, uint32_t c, uint64_t, uint64_t c0, uint64_t m0) { mine = (c > 0) & below(c0, m0) ? b : mine; });
+        bins([&](int b, uint32_t c, uint64_t m, uint64_t c0, uint64_t m0) { mine = below(c, m, c0, m0) ? b : mine; });
         if (mine >= 0) atomicMax(found, mine);
         __syncthreads();
     };
     RowBins *const out = &q.bins[r];
     uint64_t least = all_w, most = all_w;               // weight that top-k keeps, at least and at most
-    if (rules.k < q.a.n) {
-        last_bin(&bin_k, [&](uint64_t c, uint64_t) { return c < (uint64_t)rules.k; });
+    if (use_k) {
+        last_bin(&bin_k, [&](uint32_t c, uint64_t, uint64_t c0, uint64_t) { return (c > 0) & (c0 < (uint64_t)rules.k); });
         bins([&](int b, uint32_t c, uint64_t m, uint64_t c0, uint64_t m0) {
             if (b != bin_k) return;
             around[0] = m0;
@@ -770,27 +795,40 @@ __global__ void __launch_bounds__(kLongThreads) long_bins_kernel(LongArgs q)
         most = around[1];
     }
     if (use_p) {
-        last_bin(&bin_first, [&](uint64_t, uint64_t m) { return begins_below(true, m, 0, (double)rules.p * (double)least); });
-        last_bin(&bin_last, [&](uint64_t, uint64_t m) { return begins_below(true, m, 0, (double)rules.p * (double)most); });
+        // (entries without weight are none that a nucleus ends with)
+        const double limit_least = (double)rules.p * (double)least, limit_most = (double)rules.p * (double)most;
+        last_bin(&bin_first, [&](uint32_t, uint64_t m, uint64_t, uint64_t m0) { return (m > 0) & begins_below(true, m0, 0, limit_least); });
+        last_bin(&bin_last, [&](uint32_t, uint64_t m, uint64_t, uint64_t m0) { return (m > 0) & begins_below(true, m0, 0, limit_most); });
         bins([&](int b, uint32_t, uint64_t, uint64_t, uint64_t m0) {
             if (b == bin_first) out->p_mass_before = m0;
         });
+    }
+    // the least distance that falls into a bin, by bisection, for the ends of the bins
+    if (threadIdx.x < 4) {
+        const int near = use_p ? bin_first : bin_k, far = use_p ? bin_last : bin_k;
+        const int bin = threadIdx.x == 0 ? near : (threadIdx.x == 1 ? far + 1 : (threadIdx.x == 2 ? bin_k : bin_k + 1));
+        uint32_t lo = 0, hi = kMaskedKey;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (bin < kLongBins && bin_of(mid, scale, kLongBins) >= bin) hi = mid;
+            else lo = mid + 1;
+        }
+        (&out->near)[threadIdx.x] = distance_of(lo);
     }
     if (threadIdx.x == 0) {
         out->k_bin = bin_k;
         out->p_first = bin_first;
         out->p_last = bin_last;
         out->mass = all_w;
-        out->top = p.top;
-        out->scale = bin_scale(-scaled_logit(p.low, p.top, rules.inv), kLongBins);
+        out->scale = scale;
     }
 }
 
 // what an entry adds to the draw, its place aside
-__device__ inline uint64_t kept_weight(uint32_t key, const RowRules &rules)
+__device__ inline uint64_t kept_weight(float distance, float least)
 {
-    const float e = expf(-distance_of(key));
-    return (e < rules.least) & (key != 0) ? 0 : weight_of(e);
+    const float e = exp_of(distance);
+    return (e < least) & (distance != 0.0f) ? 0 : weight_of(e);
 }
 
 // The weights of a chunk's segments, as far as they lie before the bins of the row's cuts, and the entries in these bins.
@@ -808,29 +846,32 @@ __global__ void __launch_bounds__(kLongThreads) long_weight_kernel(LongArgs q)
     const int64_t begin = min(q.a.n, piece * q.chunk + wave * segment), end = min(q.a.n, begin + segment);
     uint64_t w = 0;
     if (!cuts(q, rules, top)) {
-        visit_span(x, begin, end, lane, 64, [&](float v, int64_t) {
-            const uint32_t key = key_of(scaled_logit(v, top, rules.inv));
-            if (key < kMaskedKey) w += kept_weight(key, rules);
+        with_distances(top, rules.inv, [&](auto distance) {
+            if (rules.least > 0.0f) {
+                visit_span(x, begin, end, lane, 64, [&](float v, int64_t) { w += kept_weight(distance(v), rules.least); });
+            } else {
+                visit_span(x, begin, end, lane, 64, [&](float v, int64_t) { w += raw_weight(exp_of(distance(v))); });
+            }
         });
+        w = wave_sum(w) - (rules.least > 0.0f ? 0 : offsets((uint64_t)(end - begin)));
     } else {
         if (threadIdx.x == 0) staged = 0;
         __syncthreads();
-        const RowBins bins = q.bins[r];
-        const int before = rules.p < 1.0f ? bins.p_first : bins.k_bin;
-        visit_span(x, begin, end, lane, 64, [&](float v, int64_t i) {
-            const uint32_t key = key_of(scaled_logit(v, top, rules.inv));
-            if (key >= kMaskedKey) return;
-            const int b = bin_of(key, bins.scale, kLongBins);
-            if (b < before) w += kept_weight(key, rules);
-            else if (b <= bins.p_last || b == bins.k_bin) {
-                const uint64_t place = (uint64_t)key << 32 | (uint32_t)i;
-                const uint32_t at = atomicAdd(&staged, 1u);
-                if (at < kLongStage) stage[at] = place;
-                else {
-                    const uint32_t to = atomicAdd(&q.listed[r], 1u);
-                    if (to < kLongList) q.list[(int64_t)r * kLongList + to] = place;
+        const float near = q.bins[r].near, far = q.bins[r].far, k_near = q.bins[r].k_near, k_far = q.bins[r].k_far;
+        with_distances(top, rules.inv, [&](auto distance) {
+            visit_span(x, begin, end, lane, 64, [&](float v, int64_t i) {
+                const float d = distance(v);
+                if (d < near) w += kept_weight(d, rules.least);
+                else if ((d < far) | ((d >= k_near) & (d < k_far))) {
+                    const uint64_t place = (uint64_t)__float_as_uint(d) << 32 | (uint32_t)i;
+                    const uint32_t at = atomicAdd(&staged, 1u);
+                    if (at < kLongStage) stage[at] = place;
+                    else {
+                        const uint32_t to = atomicAdd(&q.listed[r], 1u);
+                        if (to < kLongList) q.list[(int64_t)r * kLongList + to] = place;
+                    }
                 }
-            }
+            });
         });
         __syncthreads();
         const uint32_t own = staged < kLongStage ? staged : kLongStage;
@@ -840,8 +881,8 @@ __global__ void __launch_bounds__(kLongThreads) long_weight_kernel(LongArgs q)
             for (uint32_t i = threadIdx.x; i < own; i += kLongThreads)
                 if (base + i < kLongList) q.list[(int64_t)r * kLongList + base + i] = stage[i];
         }
+        w = wave_sum(w);
     }
-    w = wave_sum(w);
     if (lane == 0) q.weight[((int64_t)r * q.pieces + piece) * kLongWaves + wave] = w;
 }
 
@@ -885,7 +926,7 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
                 }
             } else {
                 for (int64_t i = threadIdx.x; i < q.a.n; i += 1024) {
-                    const uint32_t key = key_of(scaled_logit(logit_of(x[i]), p.top, rules.inv));
+                    const uint32_t key = key_of(distance_from(p.top, logit_of(x[i]), rules.inv));
                     if (key < kMaskedKey) what((uint64_t)key << 32 | (uint32_t)i, key);
                 }
             }
@@ -907,16 +948,18 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
             }
         }
         if (rules.p < 1.0f) {
-            const uint32_t *const count = q.count + (int64_t)r * kLongBins;
             const uint64_t *const mass = q.mass + (int64_t)r * kLongBins;
             const double limit = (double)rules.p * (double)kept;
             int bin = bins.p_first;
             uint64_t before = bins.p_mass_before, m = before;
             for (int b = bins.p_first; b <= bins.p_last; ++b) {
-                if (count[b] > 0 && begins_below(true, m, 0, limit)) { bin = b; before = m; }
-                m += mass[b];
+                const uint64_t own = mass[b];
+                if (own > 0 && begins_below(true, m, 0, limit)) { bin = b; before = m; }
+                m += own;
             }
-            cut = Grp::last_below(s, of_bin(bin), count[bin], true, 0, limit, before);
+            uint64_t n = 0;
+            of_bin(bin)([&](uint64_t, uint32_t) { ++n; });
+            cut = Grp::last_below(s, of_bin(bin), Grp::sum(s, n), true, 0, limit, before);
         }
         // what the cuts' bins add to the segments (the row itself, where the list is not whole: everything)
         if (!whole)
@@ -924,7 +967,7 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
         __syncthreads();
         entries([&](uint64_t at, uint32_t key) {
             if (at > cut) return;
-            const uint64_t w = kept_weight(key, rules);
+            const uint64_t w = kept_weight(distance_of(key), rules.least);
             if (w) atomicAdd(reinterpret_cast<unsigned long long *>(&weight[(uint32_t)at / (uint32_t)segment]), (unsigned long long)w);
         });
     }
@@ -955,10 +998,10 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
 #pragma unroll
     for (int j = 0; j < E; ++j) {
         const float v = logit_of(x[min(from + j, q.a.n - 1)]);
-        key[j] = from + j < to ? key_of(scaled_logit(v, p.top, rules.inv)) : kMaskedKey;
+        key[j] = from + j < to ? key_of(distance_from(p.top, v, rules.inv)) : kMaskedKey;
     }
     auto drawn = [&](int j) -> uint64_t {
-        return key[j] < kMaskedKey && ((uint64_t)key[j] << 32 | (uint32_t)(from + j)) <= cut ? kept_weight(key[j], rules) : 0;
+        return key[j] < kMaskedKey && ((uint64_t)key[j] << 32 | (uint32_t)(from + j)) <= cut ? kept_weight(distance_of(key[j]), rules.least) : 0;
     };
     uint64_t all;
     mine = 0;
