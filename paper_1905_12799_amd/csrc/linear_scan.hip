@@ -4,28 +4,33 @@
 // (a flag, not A = 0, so that infinities and NaN stay before it).  The backward pass is the same recurrence against time:
 // r_t = a_t (dh_t + r_{t+1}) is what step t hands back, the gradients are g_t = dh_t + r_{t+1}, da_t = g_t h_{t-1}.
 //
-// Memory bounds it: two or three operations for every 2 to 4 bytes.  So every array is to be read once, in rows of a cache
-// line and more, with many loads under way:
-// - A workgroup takes a strip of channels of one sequence through time in tiles; a thread takes V channels (16 bytes) of L
-//   steps in a row, lanes side by side in a line of channels, the others further on in time.  A tile stays in registers:
-//   threads compose their steps, a scan over the lanes and one over the waves (through LDS, one barrier) give each the state
-//   it starts from, and it goes through its steps again.  The next tile's loads are issued before that.
-// - With one channel the lanes lie along time, and a thread's steps are what it loads 16 bytes at a time.
-// - Where strips are too few to fill the chip, time is cut into chunks: a launch composes each chunk's steps, a second one goes
-//   through the chunks from the states that the earlier ones' compositions give.  The inputs are read twice then.
+// Memory bounds it: two or three operations for every 2 to 4 bytes.  So every array is read once, in rows of a cache line and
+// more, with many loads under way:
+// - A workgroup takes a tile, a strip of channels through a stretch of time, and keeps it in registers: a thread V channels of
+//   kSteps steps in a row, lanes side by side in a line of channels, the others further on in time.  Threads compose their steps, a
+//   scan over the lanes and one over the waves (through LDS) compose the tile; what comes before it is looked up from the tiles
+//   before (below), and every thread goes through its steps again from the state it then knows.
+// - With one channel that lies step by step, the lanes lie along time, 16 bytes of steps each.
 // - A few steps over many channels (the step of a single token): a thread per channel.
+//
+// Tiles of a sequence publish their compositions, and the state after them once they know it (a composition that is a reset); a
+// tile composes those before it, 32 or 64 at a time, back to the first that is a state.  An item is one 64-bit word that is written
+// and read atomically and is all ones until then, so that no fence is needed (which would write the second-level cache back,
+// 100 us here).  A tile that has waited too long for another goes through all the steps before it by itself, so that no
+// order in which workgroups run can hold up a call.  (Composed by a launch of their own, chunks of time had their inputs read twice:
+// 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us.)
 #include <algorithm>
+#include <type_traits>
 
 #include "element_types.h"
 #include "rls_internal.h"
+#include "wave.h"
 
 namespace rls {
 
 namespace {
 
 constexpr int kScanThreads = 64;
-constexpr int kWaves = 8;                           // of a workgroup that goes through tiles
-constexpr int kMostChunks = 256;
 constexpr int64_t kMostStates = (int64_t)1 << 30;
 
 struct ScanArgs {
@@ -87,14 +92,37 @@ __global__ void __launch_bounds__(kScanThreads) scan_backward_kernel(ScanArgs p)
 
 // ---- tiles --------------------------------------------------------------------------------------
 
-// How the work of a call is cut.  Chunk k's composition is item k + 1 of its sequence, item 0 the state before the first step.
+constexpr int kWaves = 8, kSteps = 16; // of a workgroup, of a thread
+constexpr int kAlongWaves = 4, kAlongParts = 4;     // one channel: parts of 64 x 4 steps that a wave takes
+constexpr int64_t kAlongTile = (int64_t)kAlongWaves * kAlongParts * 256;
+constexpr long long kPatience = 200000;             // ticks of the 100 MHz clock: 2 ms
+
+// How the work of a call is cut.
 struct ScanCut {
     int32_t lanes;                  // side by side along the channels (a power of two); the other 64 / lanes of a wave are further on in time
-    int32_t strips, n_chunks;
-    int64_t chunk;                  // steps
-    float2 *items;                  // [batch][n_chunks][channels] (A, H); of the last chunk no item is needed
-    int32_t *cuts;                  // [batch][strips][n_chunks] whether A is a reset
+    int32_t strips, n_tiles;        // along the channels, along time
+    uint64_t *items;                // [batch][n_tiles][channels]
+    float *start;                   // [batch][channels] the states before the first step (a copy: the last ones may be written over them)
+    long long patience;
 };
+
+// An item: A in the high half, H in the low one.  A state, or a composition that no state goes through, has kCut for A.
+constexpr uint64_t kEmpty = ~0ull;
+constexpr uint32_t kCut = 0xfffffffeu;
+__device__ inline uint64_t item_of(float A, float H, bool cut)
+{
+    const uint32_t a = cut ? kCut : (A == A ? __float_as_uint(A) : 0x7fc00000u);
+    return (uint64_t)a << 32 | __float_as_uint(H);
+}
+__device__ inline void publish(uint64_t *at, uint64_t item) { __hip_atomic_store(at, item, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline uint64_t look(const uint64_t *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+__global__ void __launch_bounds__(256) scan_clear_kernel(ScanCut q, int64_t items, const float *from, int64_t states)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)gridDim.x * 256;
+    for (int64_t k = i; k < items; k += n) q.items[k] = kEmpty;
+    for (int64_t k = i; k < states; k += n) q.start[k] = from ? from[k] : 0.0f;
+}
 
 template <typename T, int N>
 struct Pack {
@@ -114,379 +142,613 @@ __device__ inline void write_pack(T *p, const Pack<T, N> &v)
     __builtin_memcpy(p, &v, sizeof(v));
 }
 
-// WHOLE: the tiles of a sequence one after the other.  COMPOSE: a chunk's composition.  APPLY: the tiles of a chunk.
-enum { WHOLE, COMPOSE, APPLY };
+// The same as they came: elements of 16 bits stay two to a register until they are used
+template <typename T, int V>
+struct Raw {
+    static constexpr int kWords = (V * (int)sizeof(T) + 3) / 4;
+    uint32_t w[kWords];
+    __device__ inline void read(const T *p)
+    {
+        w[kWords - 1] = 0;
+        __builtin_memcpy(w, p, V * sizeof(T));
+    }
+    // elements that are all x
+    __device__ inline void fill(bool where, float x)
+    {
+        T both[4 / sizeof(T)];
+        for (auto &e : both) e = (T)x;
+        uint32_t word;
+        __builtin_memcpy(&word, both, 4);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = where ? word : w[i];
+    }
+    __device__ inline float of(int v) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[v]);
+        else if constexpr (std::is_same_v<T, __bf16>) return __uint_as_float(v & 1 ? w[v / 2] & 0xffff0000u : w[v / 2] << 16);
+        else {
+            const uint16_t half = (uint16_t)(v & 1 ? w[v / 2] >> 16 : w[v / 2]);
+            return (float)__builtin_bit_cast(T, half);
+        }
+    }
+    // (whatever has been made of the elements is made again)
+    __device__ inline void forget()
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
+    }
+};
 
-// V channels x L steps per thread; ALONG: V = 1 and the L steps lie side by side in memory.  Positions i count in the direction of
-// the recurrence, position i is step t = i or steps - 1 - i.
-template <typename T, typename G, int V, int L, bool ALONG, bool BACK, int MODE>
-__global__ void __launch_bounds__(64 * kWaves) scan_tiles_kernel(ScanArgs p, ScanCut q)
+// A composition of steps per channel; bit v of `cut`: no state goes through channel v's.
+template <int V>
+struct Steps {
+    float A[V], H[V];
+    uint32_t cut;
+    static constexpr uint32_t kAll = (1u << V) - 1;
+    __device__ inline void clear()
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
+        cut = 0;
+    }
+    __device__ inline float of(int v, float x) const { return cut >> v & 1u ? H[v] : fmaf(A[v], x, H[v]); }
+    // these steps after others
+    __device__ inline void after(const Steps &o)
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            H[v] = of(v, o.H[v]);
+            A[v] *= o.A[v];
+        }
+        cut |= o.cut;
+    }
+};
+
+// V channels x kSteps steps per thread.  Positions i count in the direction of the recurrence, position i is step t = i or steps - 1 - i.
+template <typename T, typename G, int V, bool BACK, bool RESET>
+__global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, ScanCut q)
 {
-    extern __shared__ __align__(16) float2 totals[];            // [2][kWaves][lanes * V] compositions of the waves
-    __shared__ int wave_cut[2][kWaves];
+    constexpr int L = kSteps;
+    __shared__ float2 totals[2][kWaves][64];                    // compositions of the waves, per channel of the strip
+    __shared__ uint32_t total_cut[2][kWaves][64 / V];
+    __shared__ int gave_up[2][kWaves];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lanes = q.lanes, groups = 64 / lanes;             // of a wave, along time
-    const int at = lane & (lanes - 1), group = wave * groups + lane / lanes;
-    const int64_t tile = (int64_t)kWaves * groups * L;
+    const int at = lane & (lanes - 1), group = wave * groups + lane / lanes, n_groups = kWaves * groups;
+    const int tile = n_groups * L;
     int64_t id = blockIdx.x;
     const int strip = (int)(id % q.strips);
     id /= q.strips;
-    const int64_t n = id % p.batch;
-    const int chunk = (int)(id / p.batch);
+    const int64_t n = id % p.batch, k = id / p.batch;           // (earlier tiles are in earlier workgroups)
     const int64_t C = p.channels, steps = p.steps;
     // the last strip's lanes take the last V channels where theirs would end beyond; they write their own ones only
     const int64_t c_own = ((int64_t)strip * lanes + at) * V, c0 = max(min(c_own, C - V), (int64_t)0);
     const bool idle = c_own >= C, shared = c0 != c_own;
     const bool down = BACK ? !p.reverse : p.reverse != 0;       // positions run against the steps
-    const int64_t i_begin = (int64_t)chunk * q.chunk, i_end = min(steps, i_begin + q.chunk);
+    const int64_t i_begin = k * tile, i = i_begin + (int64_t)group * L;
+    const bool whole = i_begin + tile < steps;                  // (the one after the last position is read too)
     const G *const a = static_cast<const G *>(p.a.data_dev) + n * p.a.batch_stride + c0;
     const T *const b = static_cast<const T *>(p.b.data_dev) + n * p.b.batch_stride + c0;
     T *const h = static_cast<T *>(p.h.data_dev) + n * p.h.batch_stride + c0;
-    G *const da = BACK ? static_cast<G *>(p.da.data_dev) + n * p.da.batch_stride + c0 : nullptr;
-    T *const db = BACK ? static_cast<T *>(p.db.data_dev) + n * p.db.batch_stride + c0 : nullptr;
-    const uint8_t *const reset = p.reset ? p.reset + n * steps : nullptr;
-    auto step_of = [&](int64_t i) { return down ? steps - 1 - i : i; };
+    const uint8_t *const reset = RESET ? p.reset + n * steps : nullptr;
+    auto step_of = [&](int64_t j) { return down ? steps - 1 - j : j; };
 
-    constexpr int N = ALONG ? L : V, M = ALONG ? 1 : L;         // elements of a load, loads of a thread
-    Pack<G, N> a_in[M];
-    Pack<T, N> b_in[M], h_in[M];                                // (backward: h one step earlier in time)
+    Raw<G, V> a_in[L];
+    Raw<T, V> b_in[L], h_in[BACK ? L : 1];                     // (backward: h one step earlier in time)
     uint32_t cut_in;                                            // a bit per step
-    // loads of the steps from position i0 on; positions from i_end on repeat the last one
-    auto load = [&](int64_t i0) {
-        cut_in = 0;
-        if constexpr (ALONG) {
-            auto fetch = [&](const auto *from, int64_t i, auto &pack) {
-                if (i + L <= steps) pack = read_pack<std::remove_cv_t<std::remove_pointer_t<decltype(from)>>, L>(from + (down ? steps - L - i : i));
-                else
+    // a row of each step from position `from` on
+    auto rows_of = [&](const auto *base, int64_t stride, int64_t from, auto &rows) {
+        using E = std::remove_cv_t<std::remove_pointer_t<decltype(base)>>;
+        if (whole) {
+            const E *first = base + step_of(from) * stride;
+            const int64_t next = down ? -stride : stride;
 #pragma unroll
-                    for (int j = 0; j < L; ++j) pack.x[down ? L - 1 - j : j] = from[step_of(min(i + j, steps - 1))];
-            };
-            fetch(a, i0, a_in[0]);
-            fetch(b, i0, b_in[0]);
-            if constexpr (BACK && MODE != COMPOSE) fetch(static_cast<const T *>(h), i0 + 1, h_in[0]);
-            if (reset) {
-#pragma unroll
-                for (int j = 0; j < L; ++j) cut_in |= (reset[step_of(min(i0 + j, steps - 1))] != 0 ? 1u : 0u) << j;
+            for (int j = 0; j < L; ++j) {
+                rows[j].read(first);
+                first += next;
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < L; ++j) {
-                const int64_t t = step_of(min(i0 + j, steps - 1));
-                a_in[j] = read_pack<G, V>(a + t * p.a.step_stride);
-                b_in[j] = read_pack<T, V>(b + t * p.b.step_stride);
-                if constexpr (BACK && MODE != COMPOSE) h_in[j] = read_pack<T, V>(h + step_of(min(i0 + j + 1, steps - 1)) * p.h.step_stride);
-                if (reset) cut_in |= (reset[t] != 0 ? 1u : 0u) << j;
-            }
+            for (int j = 0; j < L; ++j) rows[j].read(base + step_of(min(from + j, steps - 1)) * stride);
         }
     };
-    // element v of step j of a loaded array
-    auto element = [&](const auto *packs, int j, int v) {
-        if constexpr (ALONG) return (float)(down ? packs[0].x[L - 1 - j] : packs[0].x[j]);
-        else return (float)packs[j].x[v];
-    };
-
-    // compositions of steps: A, H per channel, and whether they were cut
-    struct Steps {
-        float A[V], H[V];
-        int cut;
-    };
-    auto nothing = [](Steps &s) {
+    rows_of(a, p.a.step_stride, i, a_in);
+    rows_of(b, p.b.step_stride, i, b_in);
+    cut_in = 0;
+    if constexpr (RESET) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) { s.A[v] = 1.0f; s.H[v] = 0.0f; }
-        s.cut = 0;
-    };
-    auto apply = [](float A, float H, int cut, float x) { return cut ? H : A * x + H; };
-    // s after `first`
-    auto compose = [&](Steps &s, const float (&A)[V], const float (&H)[V], int cut) {
+        for (int j = 0; j < L; ++j) cut_in |= (reset[step_of(min(i + j, steps - 1))] != 0 ? 1u : 0u) << j;
+    }
+    if (!whole) {                                               // steps after the last one change nothing
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            s.H[v] = apply(s.A[v], s.H[v], s.cut, H[v]);
-            s.A[v] = s.A[v] * A[v];
+        for (int j = 0; j < L; ++j) {
+            a_in[j].fill(i + j >= steps, 1.0f);
+            b_in[j].fill(i + j >= steps, 0.0f);
         }
-        s.cut |= cut;
-    };
-    // over the groups of a wave that come before a lane's and, where `own`, its own
-    auto scan_wave = [&](Steps &s) {
+        const int64_t left = steps - i;
+        cut_in &= left >= L ? ~0u : (left > 0 ? (1u << left) - 1 : 0u);
+    }
+    // over the groups of a wave that come before a lane's, and its own
+    auto scan_wave = [&](Steps<V> &s) {
         for (int d = lanes; d < 64; d <<= 1) {
-            Steps o;
+            Steps<V> o;
 #pragma unroll
             for (int v = 0; v < V; ++v) { o.A[v] = __shfl_up(s.A[v], d, 64); o.H[v] = __shfl_up(s.H[v], d, 64); }
             o.cut = __shfl_up(s.cut, d, 64);
-            if (lane >= d) compose(s, o.A, o.H, o.cut);
+            if (lane >= d) s.after(o);
         }
     };
     int turn = 0;
-    // the states before this wave's steps and after those of all waves, from `state` before them all
-    auto scan_waves = [&](const Steps &s, float (&state)[V], float (&before)[V], Steps *whole) {
-        float2 *const t = totals + (size_t)turn * kWaves * lanes * V;
+    // the compositions of the waves before this one and of all; whether any thread gave up
+    auto scan_waves = [&](const Steps<V> &s, Steps<V> &before, Steps<V> &all, bool failed) {
         if (lane >= 64 - lanes) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) t[(wave * lanes + at) * V + v] = make_float2(s.A[v], s.H[v]);
-            if (at == 0) wave_cut[turn][wave] = s.cut;
+            for (int v = 0; v < V; ++v) totals[turn][wave][at * V + v] = make_float2(s.A[v], s.H[v]);
+            total_cut[turn][wave][at] = s.cut;
         }
+        const bool any = __any(failed);
+        if (lane == 0) gave_up[turn][wave] = any;
         __syncthreads();
-#pragma unroll
+        before.clear();
+        all.clear();
+        int bad = 0;
+#pragma unroll 2                                                // (all at once, they are 64 registers)
         for (int w = 0; w < kWaves; ++w) {
-            const int cut = wave_cut[turn][w];
-            if (w == wave) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) before[v] = state[v];
-            }
+            if (w == wave) before = all;
+            Steps<V> o;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float2 x = t[(w * lanes + at) * V + v];
-                state[v] = apply(x.x, x.y, cut, state[v]);
-                if (whole) {
-                    whole->H[v] = apply(x.x, x.y, cut, whole->H[v]);
-                    whole->A[v] = whole->A[v] * x.x;
-                }
+                const float2 x = totals[turn][w][at * V + v];
+                o.A[v] = x.x;
+                o.H[v] = x.y;
             }
-            if (whole) whole->cut |= cut;
+            o.cut = total_cut[turn][w][at];
+            o.after(all);
+            all = o;
+            bad |= gave_up[turn][w];
         }
-        turn ^= 1;                                              // (the other half is read by no wave any more: one barrier a time)
-    };
-    // the steps loaded, from position i0 on, in turn: what(position, j, cut, identity)
-    auto step_values = [&](int64_t i, int j, int v, float &x, float &y) {
-        const bool in = i + j < i_end;
-        const float g = in ? element(a_in, j, v) : 1.0f, e = in ? element(b_in, j, v) : 0.0f;
-        const bool cut = cut_in >> j & 1u && in;
-        x = cut ? 0.0f : g;
-        y = BACK ? (cut ? 0.0f : g * e) : e;
-        return cut;
-    };
-    auto compose_loaded = [&](int64_t i, Steps &s) {
-#pragma unroll
-        for (int j = 0; j < L; ++j) {
-            bool cut = false;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float x, y;
-                cut = step_values(i, j, v, x, y);
-                s.H[v] = cut ? y : x * s.H[v] + y;
-                s.A[v] = s.A[v] * x;
-            }
-            s.cut |= cut;
-        }
+        turn ^= 1;                                              // (no wave reads the other half any more: one barrier a time)
+        return bad != 0;
     };
 
-    float state[V];                                             // before the next tile, the same in every group
-    if (MODE != APPLY) {
+    Steps<V> own, waves_before, of_tile;
+    own.clear();
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+        const bool cut = RESET && (cut_in >> j & 1u);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float x = a_in[j].of(v), y = b_in[j].of(v);
+            own.H[v] = BACK ? (cut ? 0.0f : x * (y + own.H[v])) : (cut ? y : fmaf(x, own.H[v], y));
+            own.A[v] *= x;
+        }
+        if (RESET) own.cut = cut ? Steps<V>::kAll : own.cut;
+    }
+    scan_wave(own);
+    scan_waves(own, waves_before, of_tile, false);
+    uint64_t *const items = q.items + (n * q.n_tiles) * C + c0;
+    const float *const start = q.start + n * C + c0;
+    const bool tells = group == 0 && !idle && k + 1 < q.n_tiles;
+    auto tell = [&](const Steps<V> &s) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (c0 + v >= c_own) publish(items + k * C + v, item_of(s.A[v], s.H[v], s.cut >> v & 1u));
+    };
+    Steps<V> past;                                              // all the steps before the tile
+    past.clear();
+    if (q.n_tiles == 1) {
         const float *const from = BACK ? p.in : p.h0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) state[v] = from && c0 + v < C ? from[n * C + c0 + v] : 0.0f;
-    }
-    float2 *const items = MODE == WHOLE ? nullptr : q.items + n * q.n_chunks * C + c0;
-    int32_t *const cuts = MODE == WHOLE ? nullptr : q.cuts + (n * q.strips + strip) * q.n_chunks;
-    if constexpr (MODE == COMPOSE) {
-        // groups take equal parts of the chunk, whole loads of L steps
-        const int64_t per = (q.chunk / L + (int64_t)kWaves * groups - 1) / ((int64_t)kWaves * groups) * L;
-        const int64_t from = i_begin + per * group, to = min(i_end, from + per);
-        Steps s;
-        nothing(s);
-        for (int64_t i = from; i < to; i += L) {
-            load(i);
-            compose_loaded(i, s);
-        }
-        scan_wave(s);
-        float before[V], none[V];
-        Steps whole;
-        nothing(whole);
+        for (int v = 0; v < V; ++v) past.H[v] = from && c0 + v < C ? from[n * C + c0 + v] : 0.0f;
+    } else if (k == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) none[v] = 0.0f;
-        scan_waves(s, none, before, &whole);
-        if (group == 0 && !idle) {
+        for (int v = 0; v < V; ++v) past.H[v] = c0 + v < C ? start[v] : 0.0f;
+    } else {
+        if (tells) tell(of_tile);
+        // what the tiles before publish, from the nearest ones back, until all that is known is a state
+        bool failed = false;
+        for (int64_t end = k; end > 0; end -= n_groups) {
+            const int64_t other = end - n_groups + group;
+            Steps<V> s, unused, window;
+            s.clear();
+            if (other >= 0) {
+                uint64_t x[V];
+                const long long since = wall_clock64();
+                bool missing;
+                do {
+                    missing = false;
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (c0 + v >= c_own) {
-                    if (chunk == 0) items[v] = make_float2(0.0f, state[v]);
-                    items[(int64_t)(chunk + 1) * C + v] = make_float2(whole.A[v], whole.H[v]);
+                    for (int v = 0; v < V; ++v) {
+                        x[v] = c0 + v < C ? look(items + other * C + v) : 0;
+                        missing |= x[v] == kEmpty;
+                    }
+                } while (missing && wall_clock64() - since < q.patience);
+                failed = missing;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const uint32_t A = (uint32_t)(x[v] >> 32);
+                    s.H[v] = __uint_as_float((uint32_t)x[v]);
+                    s.A[v] = A == kCut ? 0.0f : __uint_as_float(A);
+                    s.cut |= (A == kCut ? 1u : 0u) << v;
                 }
-            if (at == 0) {
-                if (chunk == 0) cuts[0] = 1;
-                cuts[chunk + 1] = whole.cut;
             }
+            scan_wave(s);
+            failed = scan_waves(s, unused, window, failed);
+            if (failed) break;                                  // (the same in every thread)
+            past.after(window);
+            if (__all(past.cut == Steps<V>::kAll)) break;       // (the lanes of a wave have all channels of the strip)
         }
-        return;
-    }
-    if constexpr (MODE == APPLY) {
-        // the state before the chunk: the items up to it, shared among the groups
-        const int per = (chunk + 1 + kWaves * groups - 1) / (kWaves * groups);
-        const int from = per * group, to = min(chunk + 1, from + per);
-        Steps s;
-        nothing(s);
-        for (int k = from; k < to; ++k) {
-            const int cut = cuts[k];
+        if (failed) {                                           // step by step, every thread for its channels
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float2 x = items[(int64_t)k * C + v];
-                s.H[v] = apply(x.x, x.y, cut, s.H[v]);
-                s.A[v] = s.A[v] * x.x;
-            }
-            s.cut |= cut;
-        }
-        scan_wave(s);
-        float before[V];
+            for (int v = 0; v < V; ++v) past.H[v] = c0 + v < C ? start[v] : 0.0f;
+            for (int64_t j = 0; j < i_begin; ++j) {
+                const int64_t t = step_of(j);
+                const Pack<G, V> g = read_pack<G, V>(a + t * p.a.step_stride);
+                const Pack<T, V> e = read_pack<T, V>(b + t * p.b.step_stride);
+                const bool cut = RESET && reset[t] != 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) state[v] = 0.0f;
-        scan_waves(s, state, before, nullptr);
-    }
-    load(i_begin + (int64_t)group * L);
-    for (int64_t i0 = i_begin; i0 < i_end; i0 += tile) {
-        const int64_t i = i0 + (int64_t)group * L;
-        Steps s;
-        nothing(s);
-        compose_loaded(i, s);
-        scan_wave(s);
-        float x[V];
-        scan_waves(s, state, x, nullptr);
-        // the groups before in this wave
-        {
-            Steps o;
-#pragma unroll
-            for (int v = 0; v < V; ++v) { o.A[v] = __shfl_up(s.A[v], lanes, 64); o.H[v] = __shfl_up(s.H[v], lanes, 64); }
-            o.cut = __shfl_up(s.cut, lanes, 64);
-            if (lane >= lanes) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) x[v] = apply(o.A[v], o.H[v], o.cut, x[v]);
-            }
-        }
-        Pack<T, N> out[M];
-        Pack<G, N> out_a[M];
-#pragma unroll
-        for (int j = 0; j < L; ++j) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float y;
-                if constexpr (BACK) {
-                    const bool cut = cut_in >> j & 1u;
-                    const float g = element(b_in, j, v) + x[v];
-                    const float prev = i + j < steps - 1 ? element(h_in, j, v) : (p.h0 && c0 + v < C ? p.h0[n * C + c0 + v] : 0.0f);
-                    const float ga = cut ? 0.0f : g * prev;
-                    x[v] = cut ? 0.0f : element(a_in, j, v) * g;
-                    y = g;
-                    if constexpr (ALONG) out_a[0].x[j] = (G)ga;
-                    else out_a[j].x[v] = (G)ga;
-                } else {
-                    x[v] = cut_in >> j & 1u ? element(b_in, j, v) : element(a_in, j, v) * x[v] + element(b_in, j, v);
-                    y = x[v];
+                for (int v = 0; v < V; ++v) {
+                    const float x = (float)g.x[v], y = (float)e.x[v];
+                    past.H[v] = BACK ? (cut ? 0.0f : x * (y + past.H[v])) : (cut ? y : fmaf(x, past.H[v], y));
                 }
-                if constexpr (ALONG) out[0].x[j] = (T)y;
-                else out[j].x[v] = (T)y;
             }
-            if (i + j == steps - 1 && p.out && !idle) {
+        }
+    }
+    if constexpr (BACK) rows_of(static_cast<const T *>(h), p.h.step_stride, i + 1, h_in);
+    float x[V];                                                 // the state before the thread's steps
+    {
+        Steps<V> o;
+#pragma unroll
+        for (int v = 0; v < V; ++v) { o.A[v] = __shfl_up(own.A[v], lanes, 64); o.H[v] = __shfl_up(own.H[v], lanes, 64); }
+        o.cut = __shfl_up(own.cut, lanes, 64);
+        if (lane < lanes) o.clear();
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            of_tile.H[v] = of_tile.of(v, past.H[v]);
+            x[v] = o.of(v, waves_before.of(v, past.H[v]));
+        }
+        of_tile.cut = Steps<V>::kAll;
+    }
+    if (tells) tell(of_tile);
+    G *const da = BACK ? static_cast<G *>(p.da.data_dev) + n * p.da.batch_stride + c0 : nullptr;
+    T *const to = (BACK ? static_cast<T *>(p.db.data_dev) + n * p.db.batch_stride : static_cast<T *>(p.h.data_dev) + n * p.h.batch_stride) + c0;
+    const int64_t first = step_of(i), next = down ? -1 : 1;
+    T *row = to + first * (BACK ? p.db.step_stride : p.h.step_stride);
+    const int64_t row_next = next * (BACK ? p.db.step_stride : p.h.step_stride);
+    G *row_a = BACK ? da + first * p.da.step_stride : nullptr;
+    const int64_t row_a_next = BACK ? next * p.da.step_stride : 0;
+#pragma unroll
+    for (int j = 0; j < L; ++j) { a_in[j].forget(); b_in[j].forget(); }
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+        if (!whole && i + j >= steps) break;
+        Pack<T, V> out;
+        Pack<G, V> out_a;
+        const bool cut = RESET && (cut_in >> j & 1u);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float g = a_in[j].of(v), e = b_in[j].of(v);
+            if constexpr (BACK) {
+                const float y = e + x[v];
+                float prev = h_in[j].of(v);
+                if (!whole && i + j == steps - 1) prev = p.h0 && c0 + v < C ? p.h0[n * C + c0 + v] : 0.0f;
+                out_a.x[v] = (G)(cut ? 0.0f : y * prev);
+                out.x[v] = (T)y;
+                x[v] = cut ? 0.0f : g * y;
+            } else {
+                x[v] = cut ? e : fmaf(g, x[v], e);
+                out.x[v] = (T)x[v];
+            }
+        }
+        if (!idle) {
+            if (!shared) {
+                write_pack<T, V>(row, out);
+                if constexpr (BACK) write_pack<G, V>(row_a, out_a);
+            } else {
 #pragma unroll
                 for (int v = 0; v < V; ++v)
-                    if (c0 + v >= c_own) p.out[n * C + c0 + v] = x[v];
+                    if (c0 + v >= c_own) {
+                        row[v] = out.x[v];
+                        if constexpr (BACK) row_a[v] = out_a.x[v];
+                    }
             }
         }
-        const int64_t i_next = i0 + tile + (int64_t)group * L;
-        if (i0 + tile < i_end) load(i_next);
-        T *const to = BACK ? db : h;
-        const int64_t stride = BACK ? p.db.step_stride : p.h.step_stride;
-        if constexpr (ALONG) {
-            auto put = [&](auto *where, auto &pack) {
-                using E = std::remove_pointer_t<decltype(where)>;
-                if (down) {
+        row += row_next;
+        if constexpr (BACK) row_a += row_a_next;
+        if (!whole && i + j == steps - 1 && p.out && !idle) {
 #pragma unroll
-                    for (int j = 0; j < L / 2; ++j) { const E y = pack.x[j]; pack.x[j] = pack.x[L - 1 - j]; pack.x[L - 1 - j] = y; }
-                }
-                if (i + L <= i_end) write_pack<E, L>(where + (down ? steps - L - i : i), pack);
-                else
+            for (int v = 0; v < V; ++v)
+                if (c0 + v >= c_own) p.out[n * C + c0 + v] = x[v];
+        }
+    }
+}
+
+// One channel, its steps side by side: a wave takes kAlongParts parts of 64 x 4 steps, a lane four of each.
+template <typename T, typename G, bool BACK, bool RESET>
+__global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p, ScanCut q)
+{
+    constexpr int P = kAlongParts, L = 4;
+    __shared__ float2 totals[kAlongWaves];
+    __shared__ int total_cut[kAlongWaves];
+    __shared__ Steps<1> past_lds;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n = blockIdx.x % p.batch, k = blockIdx.x / p.batch, steps = p.steps;
+    const bool down = BACK ? !p.reverse : p.reverse != 0;
+    const int64_t i_begin = k * kAlongTile, i0 = i_begin + (wave * P * 64 + lane) * L;       // part u begins 64 * L further on
+    const bool whole = i_begin + kAlongTile < steps;
+    const G *const a = static_cast<const G *>(p.a.data_dev) + n * p.a.batch_stride;
+    const T *const b = static_cast<const T *>(p.b.data_dev) + n * p.b.batch_stride;
+    const T *const h = static_cast<const T *>(p.h.data_dev) + n * p.h.batch_stride;
+    const uint8_t *const reset = RESET ? p.reset + n * steps : nullptr;
+    auto step_of = [&](int64_t j) { return down ? steps - 1 - j : j; };
+    // four positions, in their order
+    auto four = [&](const auto *base, int64_t from, auto &x) {
+        using E = std::remove_cv_t<std::remove_pointer_t<decltype(base)>>;
+        if (from + L <= steps) {
+            const Pack<E, L> v = read_pack<E, L>(base + (down ? steps - L - from : from));
 #pragma unroll
-                    for (int j = 0; j < L; ++j)
-                        if (i + j < i_end) where[step_of(i + j)] = pack.x[down ? L - 1 - j : j];
-            };
-            if (!idle) {
-                put(to, out[0]);
-                if constexpr (BACK) put(da, out_a[0]);
-            }
-        } else if (!idle) {
+            for (int j = 0; j < L; ++j) x[j] = (float)(down ? v.x[L - 1 - j] : v.x[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < L; ++j) x[j] = (float)base[step_of(min(from + j, steps - 1))];
+        }
+    };
+    float a_in[P][L], b_in[P][L], h_in[BACK ? P : 1][L];
+    uint32_t cut_in[P];
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+        const int64_t from = i0 + u * 64 * L;
+        four(a, from, a_in[u]);
+        four(b, from, b_in[u]);
+        cut_in[u] = 0;
+        if constexpr (RESET) {
+            float r[L];
+            four(reset, from, r);
+#pragma unroll
+            for (int j = 0; j < L; ++j) cut_in[u] |= (r[j] != 0.0f ? 1u : 0u) << j;
+        }
+        if (!whole) {                               // steps after the last one change nothing
 #pragma unroll
             for (int j = 0; j < L; ++j) {
-                if (i + j >= i_end) break;
-                const int64_t t = step_of(i + j);
-                if (!shared) {
-                    write_pack<T, V>(to + t * stride, out[j]);
-                    if constexpr (BACK) write_pack<G, V>(da + t * p.da.step_stride, out_a[j]);
-                } else {
+                a_in[u][j] = from + j < steps ? a_in[u][j] : 1.0f;
+                b_in[u][j] = from + j < steps ? b_in[u][j] : 0.0f;
+            }
+            const int64_t left = steps - from;
+            cut_in[u] &= left >= L ? ~0u : (left > 0 ? (1u << left) - 1 : 0u);
+        }
+    }
+    auto compose = [&](int u, Steps<1> &s) {
+        s.clear();
 #pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        if (c0 + v >= c_own) {
-                            to[t * stride + v] = out[j].x[v];
-                            if constexpr (BACK) da[t * p.da.step_stride + v] = out_a[j].x[v];
-                        }
-                }
+        for (int j = 0; j < L; ++j) {
+            const bool cut = RESET && (cut_in[u] >> j & 1u);
+            const float x = a_in[u][j], y = b_in[u][j];
+            s.H[0] = BACK ? (cut ? 0.0f : x * (y + s.H[0])) : (cut ? y : fmaf(x, s.H[0], y));
+            s.A[0] *= x;
+            if (RESET) s.cut = cut ? 1u : s.cut;
+        }
+    };
+    // over the lanes before, and the lane's own
+    auto scan_lanes = [&](Steps<1> &s) {
+        auto move = [&](auto ctrl, auto rows) {
+            constexpr int c = decltype(ctrl)::value, m = decltype(rows)::value;
+            Steps<1> o;
+            o.A[0] = lane_move<c, m>(1.0f, s.A[0]);
+            o.H[0] = lane_move<c, m>(0.0f, s.H[0]);
+            o.cut = RESET ? lane_move<c, m>(0u, s.cut) : 0u;
+            s.after(o);
+        };
+        using std::integral_constant;
+        move(integral_constant<int, 0x111>(), integral_constant<int, 0xf>());
+        move(integral_constant<int, 0x112>(), integral_constant<int, 0xf>());
+        move(integral_constant<int, 0x114>(), integral_constant<int, 0xf>());
+        move(integral_constant<int, 0x118>(), integral_constant<int, 0xf>());
+        move(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());
+        move(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());
+    };
+    auto of_last_lane = [&](const Steps<1> &s) {
+        Steps<1> o;
+        o.A[0] = last_lane(s.A[0]);
+        o.H[0] = last_lane(s.H[0]);
+        o.cut = last_lane(s.cut);
+        return o;
+    };
+    Steps<1> own[P], of_wave;                       // per part: the wave's steps up to the lane's
+    of_wave.clear();
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+        compose(u, own[u]);
+        scan_lanes(own[u]);
+        Steps<1> part = of_last_lane(own[u]);
+        own[u].after(of_wave);
+        part.after(of_wave);
+        of_wave = part;
+    }
+    if (lane == 0) {
+        totals[wave] = make_float2(of_wave.A[0], of_wave.H[0]);
+        total_cut[wave] = of_wave.cut;
+    }
+    __syncthreads();
+    Steps<1> before, all;
+    before.clear();
+    all.clear();
+#pragma unroll
+    for (int w = 0; w < kAlongWaves; ++w) {
+        if (w == wave) before = all;
+        Steps<1> o;
+        o.A[0] = totals[w].x;
+        o.H[0] = totals[w].y;
+        o.cut = total_cut[w];
+        o.after(all);
+        all = o;
+    }
+    uint64_t *const items = q.items + n * q.n_tiles;
+    Steps<1> past;
+    past.clear();
+    bool failed = false;
+    if (q.n_tiles == 1) {
+        const float *const from = BACK ? p.in : p.h0;
+        past.H[0] = from ? from[n] : 0.0f;
+    } else if (k == 0) {
+        past.H[0] = q.start[n];
+    } else if (wave == 0) {
+        if (lane == 0) publish(items + k, item_of(all.A[0], all.H[0], all.cut));
+        for (int64_t end = k; end > 0; end -= 64) {
+            const int64_t other = end - 64 + lane;
+            Steps<1> s;
+            s.clear();
+            if (other >= 0) {
+                const long long since = wall_clock64();
+                uint64_t x;
+                do x = look(items + other);
+                while (x == kEmpty && wall_clock64() - since < q.patience);
+                failed = x == kEmpty;
+                const uint32_t A = (uint32_t)(x >> 32);
+                s.H[0] = __uint_as_float((uint32_t)x);
+                s.A[0] = A == kCut ? 0.0f : __uint_as_float(A);
+                s.cut = A == kCut ? 1u : 0u;
+            }
+            failed = __any(failed);
+            if (failed) break;
+            // (item by item the steps may be cut here, also without resets: a state)
+            for (int d = 1; d < 64; d <<= 1) {
+                Steps<1> o;
+                o.A[0] = __shfl_up(s.A[0], d, 64);
+                o.H[0] = __shfl_up(s.H[0], d, 64);
+                o.cut = __shfl_up(s.cut, d, 64);
+                if (lane >= d) s.after(o);
+            }
+            past.after(of_last_lane(s));
+            if (past.cut) break;
+        }
+        if (lane == 0) {
+            past.cut = failed ? 2u : past.cut;
+            past_lds = past;
+        }
+    }
+    if (k > 0) {
+        __syncthreads();
+        past = past_lds;
+        if (past.cut == 2u) {                       // (the same in every thread) step by step
+            past.H[0] = q.start[n];
+            for (int64_t j = 0; j < i_begin; ++j) {
+                const int64_t t = step_of(j);
+                const bool cut = RESET && reset[t] != 0;
+                const float x = (float)a[t], y = (float)b[t];
+                past.H[0] = BACK ? (cut ? 0.0f : x * (y + past.H[0])) : (cut ? y : fmaf(x, past.H[0], y));
             }
         }
+    }
+    if constexpr (BACK) {
+#pragma unroll
+        for (int u = 0; u < P; ++u) four(h, i0 + u * 64 * L + 1, h_in[u]);
+    }
+    if (threadIdx.x == 0 && k + 1 < q.n_tiles) publish(items + k, item_of(0.0f, all.of(0, past.H[0]), true));
+    const float of_waves = before.of(0, past.H[0]);
+    G *const da = BACK ? static_cast<G *>(p.da.data_dev) + n * p.da.batch_stride : nullptr;
+    T *const to = BACK ? static_cast<T *>(p.db.data_dev) + n * p.db.batch_stride : static_cast<T *>(p.h.data_dev) + n * p.h.batch_stride;
+    Steps<1> parts_before;                          // of the wave
+    parts_before.clear();
+#pragma unroll
+    for (int u = 0; u < P; ++u) {
+        const int64_t i = i0 + u * 64 * L;
+        Steps<1> o;
+        o.A[0] = __shfl_up(own[u].A[0], 1, 64);
+        o.H[0] = __shfl_up(own[u].H[0], 1, 64);
+        o.cut = RESET ? __shfl_up(own[u].cut, 1, 64) : 0u;
+        if (lane == 0) o = parts_before;
+        float x = o.of(0, of_waves);
+        parts_before = of_last_lane(own[u]);
+        float y[L], ya[L];
+#pragma unroll
+        for (int j = 0; j < L; ++j) {
+            const bool cut = RESET && (cut_in[u] >> j & 1u);
+            if constexpr (BACK) {
+                y[j] = b_in[u][j] + x;
+                const float prev = i + j < steps - 1 ? h_in[u][j] : (p.h0 ? p.h0[n] : 0.0f);
+                ya[j] = cut ? 0.0f : y[j] * prev;
+                x = cut ? 0.0f : a_in[u][j] * y[j];
+            } else {
+                x = cut ? b_in[u][j] : fmaf(a_in[u][j], x, b_in[u][j]);
+                y[j] = x;
+            }
+            if (i + j == steps - 1 && p.out) p.out[n] = x;
+        }
+        auto put = [&](auto *where, const float (&z)[L]) {
+            using E = std::remove_pointer_t<decltype(where)>;
+            if (i + L <= steps) {
+                Pack<E, L> v;
+#pragma unroll
+                for (int j = 0; j < L; ++j) v.x[j] = (E)(down ? z[L - 1 - j] : z[j]);
+                write_pack<E, L>(where + (down ? steps - L - i : i), v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < L; ++j)
+                    if (i + j < steps) where[step_of(i + j)] = (E)z[j];
+            }
+        };
+        put(to, y);
+        if constexpr (BACK) put(da, ya);
     }
 }
 
 // ---- which way a call takes ----------------------------------------------------------------------
 
 constexpr int64_t kFewSteps = 16;
-constexpr int64_t kFill = 512;                      // workgroups that fill the chip
-constexpr int64_t kAlongSteps = 16, kStripSteps = 4;
+
+thread_local long long g_patience = kPatience;
 
 struct ScanPlan {
     bool tiles, along;
     int vec;                                        // channels of a thread
     ScanCut cut;
-    int64_t bytes;
+    int64_t items, bytes;
 };
 
-ScanPlan plan_scan(int64_t batch, int64_t steps, int64_t channels, int element_bytes, bool unit_steps)
+ScanPlan plan_scan(int64_t batch, int64_t steps, int64_t channels, bool unit_steps)
 {
     ScanPlan r{};
     r.along = channels == 1 && unit_steps;
-    r.vec = channels >= 16 / element_bytes ? 16 / element_bytes : 1;
+    r.vec = channels >= 4 ? 4 : 1;
     int lanes = 1;
-    while (lanes < 128 / element_bytes / r.vec && lanes * r.vec < channels) lanes *= 2;
+    while (lanes < 16 && lanes * r.vec < channels) lanes *= 2;
     r.cut.lanes = lanes;
     r.cut.strips = (int32_t)((channels + lanes * r.vec - 1) / (lanes * r.vec));
-    r.cut.n_chunks = 1;
-    r.cut.chunk = std::max<int64_t>(steps, 1);
-    const int64_t blocks = batch * r.cut.strips;
-    r.tiles = steps > kFewSteps && blocks <= ((int64_t)1 << 22);
+    const int64_t tile = r.along ? kAlongTile : (int64_t)kWaves * (64 / lanes) * kSteps;
+    const int64_t tiles = std::max<int64_t>(1, (steps + tile - 1) / tile);
+    r.tiles = steps > kFewSteps && batch * r.cut.strips <= ((int64_t)1 << 22) / tiles;
     if (!r.tiles) return r;
-    const int64_t tile = (int64_t)kWaves * (64 / lanes) * (r.along ? kAlongSteps : kStripSteps);
-    const int64_t chunks = std::min<int64_t>({kMostChunks, (kFill + blocks - 1) / blocks, (steps + 2 * tile - 1) / (2 * tile)});
-    if (blocks < kFill / 2 && chunks > 1) {
-        r.cut.chunk = ((steps + chunks - 1) / chunks + tile - 1) / tile * tile;
-        r.cut.n_chunks = (int32_t)((steps + r.cut.chunk - 1) / r.cut.chunk);
+    r.cut.n_tiles = (int32_t)tiles;
+    if (tiles > 1) {
+        r.items = batch * tiles * channels;
+        r.bytes = align_up(r.items * 8, 256) + align_up(batch * channels * 4, 256);
     }
-    if (r.cut.n_chunks > 1)
-        r.bytes = align_up(batch * r.cut.n_chunks * channels * 8, 256) + align_up(batch * r.cut.strips * r.cut.n_chunks * 4, 256);
     return r;
 }
 
-template <typename T, typename G, int V, int L, bool ALONG>
-hipError_t launch_tiles(const ScanArgs &p, const ScanCut &q, bool backward, hipStream_t s)
+template <typename T, typename G, bool BACK, bool RESET>
+void launch_tiles(const ScanArgs &p, const ScanPlan &plan, hipStream_t s)
 {
-    const dim3 grid((unsigned)(p.batch * q.strips * q.n_chunks)), threads(64 * kWaves);
-    const size_t lds = (size_t)2 * kWaves * q.lanes * V * sizeof(float2);
-    if (q.n_chunks == 1) {
-        if (backward) hipLaunchKernelGGL((scan_tiles_kernel<T, G, V, L, ALONG, true, WHOLE>), grid, threads, lds, s, p, q);
-        else hipLaunchKernelGGL((scan_tiles_kernel<T, G, V, L, ALONG, false, WHOLE>), grid, threads, lds, s, p, q);
-        return hipGetLastError();
-    }
-    const dim3 all_but_last((unsigned)(p.batch * q.strips * (q.n_chunks - 1)));
-    if (backward) hipLaunchKernelGGL((scan_tiles_kernel<T, G, V, L, ALONG, true, COMPOSE>), all_but_last, threads, lds, s, p, q);
-    else hipLaunchKernelGGL((scan_tiles_kernel<T, G, V, L, ALONG, false, COMPOSE>), all_but_last, threads, lds, s, p, q);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (backward) hipLaunchKernelGGL((scan_tiles_kernel<T, G, V, L, ALONG, true, APPLY>), grid, threads, lds, s, p, q);
-    else hipLaunchKernelGGL((scan_tiles_kernel<T, G, V, L, ALONG, false, APPLY>), grid, threads, lds, s, p, q);
-    return hipGetLastError();
+    const dim3 grid((unsigned)(p.batch * plan.cut.strips * plan.cut.n_tiles));
+    if (plan.along) hipLaunchKernelGGL((scan_along_kernel<T, G, BACK, RESET>), grid, dim3(64 * kAlongWaves), 0, s, p, plan.cut);
+    else if (plan.vec == 1) hipLaunchKernelGGL((scan_strip_kernel<T, G, 1, BACK, RESET>), grid, dim3(64 * kWaves), 0, s, p, plan.cut);
+    else hipLaunchKernelGGL((scan_strip_kernel<T, G, 4, BACK, RESET>), grid, dim3(64 * kWaves), 0, s, p, plan.cut);
 }
 
 template <typename T, typename G>
 hipError_t launch_scan(const ScanArgs &p, const ScanPlan &plan, bool backward, hipStream_t s)
 {
     if (plan.tiles) {
-        if (plan.along) return launch_tiles<T, G, 1, kAlongSteps, true>(p, plan.cut, backward, s);
-        if (plan.vec == 1) return launch_tiles<T, G, 1, kStripSteps, false>(p, plan.cut, backward, s);
-        return launch_tiles<T, G, 16 / sizeof(T), kStripSteps, false>(p, plan.cut, backward, s);
+        if (plan.items > 0) {
+            const int64_t states = p.batch * p.channels, most = std::max(plan.items, states);
+            hipLaunchKernelGGL(scan_clear_kernel, dim3((unsigned)std::min<int64_t>((most + 1023) / 1024, 2048)), dim3(256), 0, s, plan.cut, plan.items,
+                               backward ? p.in : p.h0, states);
+        }
+        if (backward) p.reset ? launch_tiles<T, G, true, true>(p, plan, s) : launch_tiles<T, G, true, false>(p, plan, s);
+        else p.reset ? launch_tiles<T, G, false, true>(p, plan, s) : launch_tiles<T, G, false, false>(p, plan, s);
+        return hipGetLastError();
     }
     const unsigned blocks = (unsigned)((p.batch * p.channels + kScanThreads - 1) / kScanThreads);
     if (backward) hipLaunchKernelGGL((scan_backward_kernel<T, G>), dim3(blocks), dim3(kScanThreads), 0, s, p);
@@ -536,10 +798,11 @@ int32_t plan_call(const rls_scan_shape &shape, bool unit_steps, void *workspace,
         if (!workspace || (uintptr_t)workspace % 256 != 0) return RLS_ERR_WORKSPACE;
         if (bytes < rls_linear_scan_workspace_bytes(shape.batch, shape.steps, shape.channels)) return RLS_ERR_WORKSPACE;
     }
-    *plan = plan_scan(shape.batch, shape.steps, shape.channels, type_bytes(shape.type), unit_steps);
-    if (plan->bytes > 0) {
-        plan->cut.items = static_cast<float2 *>(workspace);
-        plan->cut.cuts = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + align_up(shape.batch * plan->cut.n_chunks * shape.channels * 8, 256));
+    *plan = plan_scan(shape.batch, shape.steps, shape.channels, unit_steps);
+    plan->cut.patience = g_patience;
+    if (plan->items > 0) {
+        plan->cut.items = static_cast<uint64_t *>(workspace);
+        plan->cut.start = reinterpret_cast<float *>(static_cast<char *>(workspace) + align_up(plan->items * 8, 256));
     }
     return RLS_OK;
 }
@@ -552,13 +815,16 @@ using namespace rls;
 
 extern "C" {
 
+int32_t rls_scan_wait_limit(int64_t ticks)
+{
+    g_patience = ticks < 0 ? kPatience : ticks;
+    return RLS_OK;
+}
+
 int64_t rls_linear_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels)
 {
     if (!sizes_fit(batch, steps, channels)) return RLS_ERR_INVALID_ARG;
-    int64_t most = 0;                               // (of any type and any strides)
-    for (int bytes = 2; bytes <= 4; bytes += 2)
-        for (int unit = 0; unit < 2; ++unit) most = std::max(most, plan_scan(batch, steps, channels, bytes, unit != 0).bytes);
-    return most;
+    return std::max(plan_scan(batch, steps, channels, false).bytes, plan_scan(batch, steps, channels, true).bytes);
 }
 
 int32_t rls_linear_scan(const rls_scan_shape *shape, const rls_sequence *a, const rls_sequence *b, const float *h0_dev,

@@ -261,6 +261,22 @@ def test_gradients_against_differences(rls, B, T, C):
             assert abs(slope - float(grad[at])) <= errors + 2.0 ** -18 * abs(slope), (which, at)
 
 
+@pytest.mark.parametrize("B,T,C,dtype", [(1, 3000, 70, "bf16"), (2, 1500, 3, "f32"), (2, 20000, 1, "f32"), (3, 4100, 200, "f32")])
+def test_tiles_that_do_not_wait(rls, B, T, C, dtype):
+    """Tiles that give up at once on what is not there yet go through the steps before them by themselves."""
+    import ctypes
+    a, b, h0, reset = make(B, T, C, TYPES[dtype], torch.float32, 4, with_reset=True)
+    limit = rls.lib().rls_scan_wait_limit
+    limit.argtypes = [ctypes.c_int64]
+    assert limit(0) == 0
+    try:
+        for reverse in (False, True):
+            h, _ = check_forward(rls, a, b, h0, reset, reverse)
+            check_backward(rls, a, h.cpu(), torch.randn(B, T, C, generator=torch.Generator().manual_seed(1)).to(TYPES[dtype]), h0, reset, h0, reverse)
+    finally:
+        assert limit(-1) == 0
+
+
 def test_in_a_graph(rls):
     for B, T, C in ((64, 1, 96), (1, 20000, 24), (2, 30000, 1)):
         a, b = torch.empty(B, T, C).cuda(), torch.empty(B, T, C).cuda()
