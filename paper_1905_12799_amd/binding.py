@@ -155,6 +155,11 @@ def _stream() -> ctypes.c_void_p:
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _raw_stream(t: torch.Tensor) -> int:
+    """The current stream of the tensor's device as a number (making a Stream object of it takes 3 us, a fifth of a short call)."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
 def _ptr(t: Optional[torch.Tensor]) -> ctypes.c_void_p:
     return ctypes.c_void_p(None if t is None else t.data_ptr())
 
@@ -489,21 +494,24 @@ def sample_workspace_bytes(rows: int, n_choices: int) -> int:
     return n
 
 
-def _space(workspace: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[torch.Tensor], ctypes.c_void_p, int]:
-    """Workspace of a call: the caller's, or one of its own where it needs any; with its 256-byte aligned start and what is left of it."""
-    ws = _workspace(need, device) if workspace is None and need > 0 else workspace
-    if ws is None:
-        return None, ctypes.c_void_p(None), 0
-    base = _aligned_ptr(ws)
-    return ws, ctypes.c_void_p(base), max(0, ws.numel() * ws.element_size() - (base - ws.data_ptr()))
+def _space(workspace: Optional[torch.Tensor], need, device) -> Tuple[Optional[torch.Tensor], int, int]:
+    """Workspace of a call: the caller's, or one of its own of need() bytes; with its 256-byte aligned start and what is left of it."""
+    if workspace is None:
+        n = need()
+        if n == 0:
+            return None, 0, 0
+        workspace = _workspace(n, device)
+    base = _aligned_ptr(workspace)
+    return workspace, base, max(0, workspace.numel() * workspace.element_size() - (base - workspace.data_ptr()))
 
 
-def _per_row(t: Optional[torch.Tensor], dtype: torch.dtype, rows: int, name: str) -> Optional[torch.Tensor]:
-    if t is not None:
-        _dev(t, dtype, name)
-        if t.numel() != rows:
-            raise ValueError(f"{name} needs an entry per row")
-    return t
+def _per_row(t: Optional[torch.Tensor], dtype: torch.dtype, rows: int, name: str) -> int:
+    """Address of an array with an entry per row (0 for None)."""
+    if t is None:
+        return 0
+    if t.numel() != rows:
+        raise ValueError(f"{name} needs an entry per row")
+    return _dev(t, dtype, name).data_ptr()
 
 
 def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
@@ -515,16 +523,16 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[to
     if logits.dim() != 2 or not logits.is_cuda or logits.dtype not in _TYPE_OF or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be an fp32, bf16 or fp16 device matrix with unit stride along a row")
     rows, n = logits.shape
-    _per_row(uniform, torch.float32, rows, "uniform")
-    _per_row(temperature, torch.float32, rows, "temperature")
-    _per_row(top_k, torch.int32, rows, "top_k")
-    _per_row(top_p, torch.float32, rows, "top_p")
-    _per_row(min_p, torch.float32, rows, "min_p")
-    token = torch.empty(rows, dtype=torch.int32, device=logits.device) if out is None else _per_row(out, torch.int32, rows, "out")
-    logprob = torch.empty(rows, dtype=torch.float32, device=logits.device) if want_logprob else None
-    ws, base, avail = _space(workspace, sample_workspace_bytes(rows, n), logits.device)
-    _check(lib().rls_sample(_ptr(logits), _TYPE_OF[logits.dtype], rows, n, logits.stride(0) if rows > 1 else n, _ptr(uniform), _ptr(temperature),
-                            _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(token), _ptr(logprob), base, avail, _stream()), "rls_sample")
+    device = logits.device
+    settings = (_per_row(uniform, torch.float32, rows, "uniform"), _per_row(temperature, torch.float32, rows, "temperature"),
+                _per_row(top_k, torch.int32, rows, "top_k"), _per_row(top_p, torch.float32, rows, "top_p"),
+                _per_row(min_p, torch.float32, rows, "min_p"))
+    token = torch.empty(rows, dtype=torch.int32, device=device) if out is None else out
+    to = _per_row(token, torch.int32, rows, "out")
+    logprob = torch.empty(rows, dtype=torch.float32, device=device) if want_logprob else None
+    ws, base, avail = _space(workspace, lambda: sample_workspace_bytes(rows, n), device)
+    _check(lib().rls_sample(logits.data_ptr(), _TYPE_OF[logits.dtype], rows, n, logits.stride(0) if rows > 1 else n, *settings, to,
+                            logprob.data_ptr() if want_logprob else 0, base, avail, _raw_stream(logits)), "rls_sample")
     return token, logprob
 
 
@@ -535,28 +543,28 @@ def linear_scan_workspace_bytes(batch: int, steps: int, channels: int) -> int:
     return n
 
 
-def _sequence(t: torch.Tensor, shape, dtypes, name: str) -> _Sequence:
-    if not t.is_cuda or tuple(t.shape) != tuple(shape) or t.dtype not in dtypes or (shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be a device tensor of shape {tuple(shape)} with unit stride along the channels and of type {dtypes}")
-    return _Sequence(t.data_ptr(), t.stride(0), t.stride(1))
+def _sequence(t: torch.Tensor, shape, dtype: torch.dtype, name: str):
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda or (shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be a device tensor of shape {tuple(shape)} and type {dtype} with unit stride along the channels")
+    return ctypes.byref(_Sequence(t.data_ptr(), t.stride(0), t.stride(1)))
 
 
-def _states(t: Optional[torch.Tensor], shape, name: str) -> Optional[torch.Tensor]:
-    if t is not None:
-        _dev(t, torch.float32, name)
-        if tuple(t.shape) != (shape[0], shape[2]):
-            raise ValueError(f"{name} must be [batch, channels]")
-    return t
+def _states(t: Optional[torch.Tensor], shape, name: str) -> int:
+    if t is None:
+        return 0
+    if t.dim() != 2 or t.shape[0] != shape[0] or t.shape[1] != shape[2]:
+        raise ValueError(f"{name} must be [batch, channels]")
+    return _dev(t, torch.float32, name).data_ptr()
 
 
-def _resets(t: Optional[torch.Tensor], shape) -> Optional[torch.Tensor]:
-    if t is not None:
-        if t.dtype == torch.bool:
-            t = t.view(torch.uint8)
-        _dev(t, torch.uint8, "reset")
-        if tuple(t.shape) != (shape[0], shape[1]):
-            raise ValueError("reset must be [batch, steps]")
-    return t
+def _resets(t: Optional[torch.Tensor], shape) -> int:
+    if t is None:
+        return 0
+    if t.dtype == torch.bool:
+        t = t.view(torch.uint8)
+    if t.dim() != 2 or t.shape[0] != shape[0] or t.shape[1] != shape[1]:
+        raise ValueError("reset must be [batch, steps]")
+    return _dev(t, torch.uint8, "reset").data_ptr()
 
 
 def _scan_shape(a: torch.Tensor, x: torch.Tensor, reverse: bool) -> _ScanShape:
@@ -572,14 +580,14 @@ def linear_scan(a: torch.Tensor, b: torch.Tensor, h0: Optional[torch.Tensor] = N
 
     a may be fp32 beside a b of fewer bits, and either may be an expanded view; reset [batch, steps] (bytes or bools) cuts the carry;
     reverse runs from the last step to the first.  `last` may be h0 itself, for a state that is updated in place."""
-    shape = _scan_shape(a, b, reverse)
-    B, T, C = b.shape
-    h = torch.empty((B, T, C), dtype=b.dtype, device=b.device) if out is None else out
-    last = torch.empty((B, C), dtype=torch.float32, device=b.device) if last is None else _states(last, b.shape, "last")
-    ws, base, avail = _space(workspace, linear_scan_workspace_bytes(B, T, C), b.device)
-    args = [_sequence(a, b.shape, (a.dtype,), "a"), _sequence(b, b.shape, (b.dtype,), "b"), _sequence(h, b.shape, (b.dtype,), "out")]
-    _check(lib().rls_linear_scan(ctypes.byref(shape), ctypes.byref(args[0]), ctypes.byref(args[1]), _ptr(_states(h0, b.shape, "h0")),
-                                 _ptr(_resets(reset, b.shape)), ctypes.byref(args[2]), _ptr(last), base, avail, _stream()), "rls_linear_scan")
+    shape, size = _scan_shape(a, b, reverse), b.shape
+    B, T, C = size
+    h = torch.empty(size, dtype=b.dtype, device=b.device) if out is None else out
+    last = torch.empty((B, C), dtype=torch.float32, device=b.device) if last is None else last
+    ws, base, avail = _space(workspace, lambda: linear_scan_workspace_bytes(B, T, C), b.device)
+    _check(lib().rls_linear_scan(ctypes.byref(shape), _sequence(a, size, a.dtype, "a"), _sequence(b, size, b.dtype, "b"), _states(h0, size, "h0"),
+                                 _resets(reset, size), _sequence(h, size, b.dtype, "out"), _states(last, size, "last"), base, avail,
+                                 _raw_stream(b)), "rls_linear_scan")
     return h, last
 
 
@@ -589,17 +597,16 @@ def linear_scan_backward(a: torch.Tensor, h: torch.Tensor, dh: torch.Tensor, h0:
     """Gradients of linear_scan from its gates, the states it returned and the gradients by them: (da in a's type, db in h's, dh0 in fp32).
 
     Where a or b was an expanded view, da or db is the gradient of every element: its sum along the expanded axes is the input's."""
-    shape = _scan_shape(a, h, reverse)
-    B, T, C = h.shape
+    shape, size = _scan_shape(a, h, reverse), h.shape
+    B, T, C = size
     da = torch.empty((B, T, C), dtype=a.dtype, device=h.device)
     db = torch.empty((B, T, C), dtype=h.dtype, device=h.device)
     dh0 = torch.empty((B, C), dtype=torch.float32, device=h.device)
-    ws, base, avail = _space(workspace, linear_scan_workspace_bytes(B, T, C), h.device)
-    args = [_sequence(a, h.shape, (a.dtype,), "a"), _sequence(h, h.shape, (h.dtype,), "h"), _sequence(dh, h.shape, (h.dtype,), "dh"),
-            _sequence(da, h.shape, (a.dtype,), "da"), _sequence(db, h.shape, (h.dtype,), "db")]
-    _check(lib().rls_linear_scan_backward(ctypes.byref(shape), ctypes.byref(args[0]), ctypes.byref(args[1]), ctypes.byref(args[2]),
-                                          _ptr(_states(h0, h.shape, "h0")), _ptr(_resets(reset, h.shape)), _ptr(_states(dh_last, h.shape, "dh_last")),
-                                          ctypes.byref(args[3]), ctypes.byref(args[4]), _ptr(dh0), base, avail, _stream()),
+    ws, base, avail = _space(workspace, lambda: linear_scan_workspace_bytes(B, T, C), h.device)
+    _check(lib().rls_linear_scan_backward(ctypes.byref(shape), _sequence(a, size, a.dtype, "a"), _sequence(h, size, h.dtype, "h"),
+                                          _sequence(dh, size, h.dtype, "dh"), _states(h0, size, "h0"), _resets(reset, size),
+                                          _states(dh_last, size, "dh_last"), _sequence(da, size, a.dtype, "da"),
+                                          _sequence(db, size, h.dtype, "db"), dh0.data_ptr(), base, avail, _raw_stream(h)),
            "rls_linear_scan_backward")
     return da, db, dh0
 
@@ -632,8 +639,9 @@ class AdamW:
             master = [p.detach().float() for p in self.params]
         self.master = self._list(master, torch.float32, shapes, "master") if master else None
         self._tensors = (_AdamwTensor * max(1, len(self.params)))()
+        self._each, self._forms = list(self._tensors)[:len(self.params)], [(p.shape, p.dtype) for p in self.params]
         for i, p in enumerate(self.params):
-            t = self._tensors[i]
+            t = self._each[i]
             t.n, t.param_type, t.param_dev = p.numel(), _TYPE_OF[p.dtype], p.data_ptr()
             t.m_dev, t.v_dev = self.exp_avg[i].data_ptr(), self.exp_avg_sq[i].data_ptr()
             t.master_dev = self.master[i].data_ptr() if self.master and p.dtype != torch.float32 else None
@@ -657,13 +665,14 @@ class AdamW:
         """One step with these gradients (fp32 or the parameter's type), times grad_scale (one fp32 on the device) where given."""
         if len(grads) != len(self.params):
             raise ValueError("step needs a gradient per parameter")
-        for t, p, g in zip(self._tensors, self.params, grads):
-            if g.shape != p.shape or not g.is_cuda or g.dtype not in (torch.float32, p.dtype) or not g.is_contiguous():
+        for t, (shape, dtype), g in zip(self._each, self._forms, grads):
+            if g.shape != shape or not g.is_cuda or (g.dtype != dtype and g.dtype != torch.float32) or not g.is_contiguous():
                 raise ValueError("a gradient must be a contiguous device tensor of its parameter's shape, in fp32 or the parameter's type")
             t.grad_dev, t.grad_type = g.data_ptr(), _TYPE_OF[g.dtype]
         if grad_scale is not None and _dev(grad_scale, torch.float32, "grad_scale").numel() != 1:
             raise ValueError("grad_scale must hold one number")
         options = _AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, self.step_count + 1, ctypes.c_uint64(self.seed).value, self.state_bits,
                                 None if grad_scale is None else grad_scale.data_ptr())
-        _check(lib().rls_adamw_step(self._tensors, len(self.params), ctypes.byref(options), _stream()), "rls_adamw_step")
+        stream = _raw_stream(self.params[0]) if self.params else 0
+        _check(lib().rls_adamw_step(self._tensors, len(self.params), ctypes.byref(options), stream), "rls_adamw_step")
         self.step_count += 1

@@ -7,14 +7,14 @@
 // Memory bounds it: two or three operations for every 2 to 4 bytes.  So every array is read once, in rows of a cache line and
 // more, with many loads under way:
 // - A workgroup takes a tile, a strip of channels through a stretch of time, and keeps it in registers: a thread V channels of
-//   kSteps steps in a row, lanes side by side in a line of channels, the others further on in time.  Threads compose their steps, a
+//   8 or 16 steps in a row, lanes side by side in a line of channels, the others further on in time.  Threads compose their steps, a
 //   scan over the lanes and one over the waves (through LDS) compose the tile; what comes before it is looked up from the tiles
 //   before (below), and every thread goes through its steps again from the state it then knows.
 // - With one channel that lies step by step, the lanes lie along time, 16 bytes of steps each.
 // - A few steps over many channels (the step of a single token): a thread per channel.
 //
 // Tiles of a sequence publish their compositions, and the state after them once they know it (a composition that is a reset); a
-// tile composes those before it, 32 or 64 at a time, back to the first that is a state.  An item is one 64-bit word that is written
+// tile composes those before it, 8 to 64 at a time, back to the first that is a state.  An item is one 64-bit word that is written
 // and read atomically and is all ones until then, so that no fence is needed (which would write the second-level cache back,
 // 100 us here).  A tile that has waited too long for another goes through all the steps before it by itself, so that no
 // order in which workgroups run can hold up a call.  (Composed by a launch of their own, chunks of time had their inputs read twice:
@@ -92,8 +92,9 @@ __global__ void __launch_bounds__(kScanThreads) scan_backward_kernel(ScanArgs p)
 
 // ---- tiles --------------------------------------------------------------------------------------
 
-constexpr int kWaves = 8, kSteps = 16; // of a workgroup, of a thread
-constexpr int kAlongWaves = 4, kAlongParts = 4;     // one channel: parts of 64 x 4 steps that a wave takes
+constexpr int kWaves = 4, kStripLanes = 32;      // of a workgroup; of a strip at most
+constexpr int kSteps = 16, kWideSteps = 8;          // of a thread: of two bytes each, of four (16 of those spill registers and are as fast)
+constexpr int kAlongWaves = 8, kAlongParts = 2;     // one channel: parts of 64 x 4 steps that a wave takes
 constexpr int64_t kAlongTile = (int64_t)kAlongWaves * kAlongParts * 256;
 constexpr long long kPatience = 200000;             // ticks of the 100 MHz clock: 2 ms
 
@@ -101,7 +102,7 @@ constexpr long long kPatience = 200000;             // ticks of the 100 MHz cloc
 struct ScanCut {
     int32_t lanes;                  // side by side along the channels (a power of two); the other 64 / lanes of a wave are further on in time
     int32_t strips, n_tiles;        // along the channels, along time
-    uint64_t *items;                // [batch][n_tiles][channels]
+    uint64_t *items;                // [batch][n_tiles][strips][channels of a thread][lanes]: what a wave reads at a time lies side by side (32 bytes a lane, four times as much came)
     float *start;                   // [batch][channels] the states before the first step (a copy: the last ones may be written over them)
     long long patience;
 };
@@ -204,13 +205,13 @@ struct Steps {
     }
 };
 
-// V channels x kSteps steps per thread.  Positions i count in the direction of the recurrence, position i is step t = i or steps - 1 - i.
+// V channels x kSteps or kWideSteps steps per thread.  Positions i count in the direction of the recurrence, position i is step t = i or steps - 1 - i.
 template <typename T, typename G, int V, bool BACK, bool RESET>
 __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, ScanCut q)
 {
-    constexpr int L = kSteps;
-    __shared__ float2 totals[2][kWaves][64];                    // compositions of the waves, per channel of the strip
-    __shared__ uint32_t total_cut[2][kWaves][64 / V];
+    constexpr int L = sizeof(T) == 4 ? kWideSteps : kSteps;
+    __shared__ float2 totals[2][kWaves][kStripLanes * V];       // compositions of the waves, per channel of the strip
+    __shared__ uint32_t total_cut[2][kWaves][kStripLanes];
     __shared__ int gave_up[2][kWaves];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -327,13 +328,13 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
     }
     scan_wave(own);
     scan_waves(own, waves_before, of_tile, false);
-    uint64_t *const items = q.items + (n * q.n_tiles) * C + c0;
+    const int64_t row = (int64_t)q.strips * V * lanes;          // items of a tile of time
+    uint64_t *const items = q.items + n * q.n_tiles * row + (int64_t)strip * V * lanes + at;
     const float *const start = q.start + n * C + c0;
-    const bool tells = group == 0 && !idle && k + 1 < q.n_tiles;
+    const bool tells = group == 0 && k + 1 < q.n_tiles;
     auto tell = [&](const Steps<V> &s) {
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (c0 + v >= c_own) publish(items + k * C + v, item_of(s.A[v], s.H[v], s.cut >> v & 1u));
+        for (int v = 0; v < V; ++v) publish(items + k * row + v * lanes, item_of(s.A[v], s.H[v], s.cut >> v & 1u));
     };
     Steps<V> past;                                              // all the steps before the tile
     past.clear();
@@ -360,9 +361,10 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
                     missing = false;
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        x[v] = c0 + v < C ? look(items + other * C + v) : 0;
+                        x[v] = look(items + other * row + v * lanes);
                         missing |= x[v] == kEmpty;
                     }
+                    if (missing) __builtin_amdgcn_s_sleep(4);
                 } while (missing && wall_clock64() - since < q.patience);
                 failed = missing;
 #pragma unroll
@@ -414,10 +416,10 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
     G *const da = BACK ? static_cast<G *>(p.da.data_dev) + n * p.da.batch_stride + c0 : nullptr;
     T *const to = (BACK ? static_cast<T *>(p.db.data_dev) + n * p.db.batch_stride : static_cast<T *>(p.h.data_dev) + n * p.h.batch_stride) + c0;
     const int64_t first = step_of(i), next = down ? -1 : 1;
-    T *row = to + first * (BACK ? p.db.step_stride : p.h.step_stride);
-    const int64_t row_next = next * (BACK ? p.db.step_stride : p.h.step_stride);
-    G *row_a = BACK ? da + first * p.da.step_stride : nullptr;
-    const int64_t row_a_next = BACK ? next * p.da.step_stride : 0;
+    T *out_row = to + first * (BACK ? p.db.step_stride : p.h.step_stride);
+    const int64_t out_next = next * (BACK ? p.db.step_stride : p.h.step_stride);
+    G *out_row_a = BACK ? da + first * p.da.step_stride : nullptr;
+    const int64_t out_next_a = BACK ? next * p.da.step_stride : 0;
 #pragma unroll
     for (int j = 0; j < L; ++j) { a_in[j].forget(); b_in[j].forget(); }
 #pragma unroll
@@ -443,19 +445,19 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
         }
         if (!idle) {
             if (!shared) {
-                write_pack<T, V>(row, out);
-                if constexpr (BACK) write_pack<G, V>(row_a, out_a);
+                write_pack<T, V>(out_row, out);
+                if constexpr (BACK) write_pack<G, V>(out_row_a, out_a);
             } else {
 #pragma unroll
                 for (int v = 0; v < V; ++v)
                     if (c0 + v >= c_own) {
-                        row[v] = out.x[v];
-                        if constexpr (BACK) row_a[v] = out_a.x[v];
+                        out_row[v] = out.x[v];
+                        if constexpr (BACK) out_row_a[v] = out_a.x[v];
                     }
             }
         }
-        row += row_next;
-        if constexpr (BACK) row_a += row_a_next;
+        out_row += out_next;
+        if constexpr (BACK) out_row_a += out_next_a;
         if (!whole && i + j == steps - 1 && p.out && !idle) {
 #pragma unroll
             for (int v = 0; v < V; ++v)
@@ -602,8 +604,10 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
             if (other >= 0) {
                 const long long since = wall_clock64();
                 uint64_t x;
-                do x = look(items + other);
-                while (x == kEmpty && wall_clock64() - since < q.patience);
+                do {
+                    x = look(items + other);
+                    if (x == kEmpty) __builtin_amdgcn_s_sleep(4);
+                } while (x == kEmpty && wall_clock64() - since < q.patience);
                 failed = x == kEmpty;
                 const uint32_t A = (uint32_t)(x >> 32);
                 s.H[0] = __uint_as_float((uint32_t)x);
@@ -707,22 +711,22 @@ struct ScanPlan {
     int64_t items, bytes;
 };
 
-ScanPlan plan_scan(int64_t batch, int64_t steps, int64_t channels, bool unit_steps)
+ScanPlan plan_scan(int64_t batch, int64_t steps, int64_t channels, bool wide, bool unit_steps)
 {
     ScanPlan r{};
     r.along = channels == 1 && unit_steps;
     r.vec = channels >= 4 ? 4 : 1;
     int lanes = 1;
-    while (lanes < 16 && lanes * r.vec < channels) lanes *= 2;
+    while (lanes < kStripLanes && lanes * r.vec < channels) lanes *= 2;
     r.cut.lanes = lanes;
     r.cut.strips = (int32_t)((channels + lanes * r.vec - 1) / (lanes * r.vec));
-    const int64_t tile = r.along ? kAlongTile : (int64_t)kWaves * (64 / lanes) * kSteps;
+    const int64_t tile = r.along ? kAlongTile : (int64_t)kWaves * (64 / lanes) * (wide ? kWideSteps : kSteps);
     const int64_t tiles = std::max<int64_t>(1, (steps + tile - 1) / tile);
     r.tiles = steps > kFewSteps && batch * r.cut.strips <= ((int64_t)1 << 22) / tiles;
     if (!r.tiles) return r;
     r.cut.n_tiles = (int32_t)tiles;
     if (tiles > 1) {
-        r.items = batch * tiles * channels;
+        r.items = batch * tiles * r.cut.strips * lanes * r.vec;
         r.bytes = align_up(r.items * 8, 256) + align_up(batch * channels * 4, 256);
     }
     return r;
@@ -798,7 +802,7 @@ int32_t plan_call(const rls_scan_shape &shape, bool unit_steps, void *workspace,
         if (!workspace || (uintptr_t)workspace % 256 != 0) return RLS_ERR_WORKSPACE;
         if (bytes < rls_linear_scan_workspace_bytes(shape.batch, shape.steps, shape.channels)) return RLS_ERR_WORKSPACE;
     }
-    *plan = plan_scan(shape.batch, shape.steps, shape.channels, unit_steps);
+    *plan = plan_scan(shape.batch, shape.steps, shape.channels, shape.type == RLS_F32, unit_steps);
     plan->cut.patience = g_patience;
     if (plan->items > 0) {
         plan->cut.items = static_cast<uint64_t *>(workspace);
@@ -824,7 +828,9 @@ int32_t rls_scan_wait_limit(int64_t ticks)
 int64_t rls_linear_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels)
 {
     if (!sizes_fit(batch, steps, channels)) return RLS_ERR_INVALID_ARG;
-    return std::max(plan_scan(batch, steps, channels, false).bytes, plan_scan(batch, steps, channels, true).bytes);
+    int64_t most = 0;                               // (of any type and any strides)
+    for (int form = 0; form < 4; ++form) most = std::max(most, plan_scan(batch, steps, channels, (form & 1) != 0, (form & 2) != 0).bytes);
+    return most;
 }
 
 int32_t rls_linear_scan(const rls_scan_shape *shape, const rls_sequence *a, const rls_sequence *b, const float *h0_dev,
