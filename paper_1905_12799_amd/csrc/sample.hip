@@ -194,7 +194,9 @@ template <int NT>
 struct Group {
     static constexpr int kWaves = NT / 64;
     static constexpr int kBins = NT == 64 ? 256 : 1024;
-    static constexpr int kList = 128;                   // places that are counted against each other (1000 in 1000 threads take 12 us)
+    // places that are counted against each other, by so many threads each (1000 by 1000 threads took 12 us, 256 by 1024 take one)
+    static constexpr int kList = NT == 64 ? 128 : 256;
+    static constexpr int kShare = NT > kList ? NT / kList : 1;
     static constexpr int kBinsOfThread = kBins / NT;
 
     struct Waves {
@@ -203,7 +205,7 @@ struct Group {
     struct Shared {
         uint64_t mass[kBins];
         uint32_t count[kBins];
-        uint64_t place[kList], weight[kList];
+        uint64_t place[kList], weight[kList], run[kList];
         Waves waves;
         uint64_t found_before;
         uint32_t found_bin, found_n, listed;
@@ -319,6 +321,16 @@ struct Group {
         }
         sync();
     }
+    // entries or weight of the list's places from..to that come before `at`
+    static __device__ inline uint64_t smaller(const Shared &s, uint64_t at, uint32_t from, uint32_t to, bool by_mass)
+    {
+        uint64_t run = 0;
+        for (uint32_t o = from; o < to; ++o) {
+            const uint64_t add = by_mass ? s.weight[o] : 1;
+            run += s.place[o] < at ? add : 0;
+        }
+        return run;
+    }
     // Among the n entries that `visit` hands to a function of place and key, the last place that begins below (see find_bin).  Where they fit the
     // list they are counted against each other; more are cut into bins of places first, again and again.
     template <typename Visit>
@@ -366,14 +378,20 @@ struct Group {
         sync();
         const uint32_t listed = s.listed;
         uint64_t cut = 0;
-        for (uint32_t i = threadIdx.x; i < listed; i += NT) {
-            const uint64_t at = s.place[i];
-            uint64_t run = before;
-            for (uint32_t o = 0; o < listed; ++o) {
-                const uint64_t add = by_mass ? s.weight[o] : 1;
-                run += s.place[o] < at ? add : 0;
+        if constexpr (kShare == 1) {
+            for (uint32_t i = threadIdx.x; i < listed; i += NT) {
+                const uint64_t at = s.place[i], run = before + smaller(s, at, 0, listed, by_mass);
+                if (begins_below(by_mass, run, k, limit)) cut = cut > at ? cut : at;
             }
-            if (begins_below(by_mass, run, k, limit)) cut = cut > at ? cut : at;
+        } else {
+            const uint32_t i = threadIdx.x % kList, share = threadIdx.x / kList, part = (listed + kShare - 1) / kShare;
+            if (share == 0) s.run[i] = before;
+            __syncthreads();
+            const uint64_t at = s.place[i];
+            if (i < listed)
+                atomicAdd(reinterpret_cast<unsigned long long *>(&s.run[i]), (unsigned long long)smaller(s, at, share * part, min(listed, share * part + part), by_mass));
+            __syncthreads();
+            if (share == 0 && i < listed && begins_below(by_mass, s.run[i], k, limit)) cut = at;
         }
         return most(s, cut);
     }
@@ -554,6 +572,7 @@ hipError_t launch_group_rows(const SampleArgs &a, hipStream_t s)
     if (a.n <= 256) hipLaunchKernelGGL((sample_row_kernel<T, 64, 4>), grid, dim3(64), 0, s, a);
     else if (few && a.n <= 1024) hipLaunchKernelGGL((sample_row_kernel<T, 256, 4>), grid, dim3(256), 0, s, a);
     else if (a.n <= 1024) hipLaunchKernelGGL((sample_row_kernel<T, 64, 16>), grid, dim3(64), 0, s, a);
+    else if (few && a.n <= 2048) hipLaunchKernelGGL((sample_row_kernel<T, 512, 4>), grid, dim3(512), 0, s, a);
     else if (few && a.n <= 4096) hipLaunchKernelGGL((sample_row_kernel<T, 1024, 4>), grid, dim3(1024), 0, s, a);
     else if (a.n <= 4096) hipLaunchKernelGGL((sample_row_kernel<T, 256, 16>), grid, dim3(256), 0, s, a);
     else if (a.n <= 16384) hipLaunchKernelGGL((sample_row_kernel<T, 1024, 16>), grid, dim3(1024), 0, s, a);
@@ -574,13 +593,15 @@ hipError_t launch_short_rows(const SampleArgs &a, hipStream_t s)
 // ---- long rows ------------------------------------------------------------------------------------
 
 // Rows are cut into chunks, a workgroup each, and a batch of rows goes through launches: the maxima; where rows have top-k or top-p a
-// histogram, and the bins that a row's cuts lie in; the weights of what lies before these bins, segment
+// histogram (of entries for top-k, of weights for top-p), and the bins that a row's cuts lie in; the weights of what lies before these bins, segment
 // by segment, and the entries in them as a list; the cuts from the list, its share of the weights and the draw, a workgroup per row.
 // What a launch needs of the row's other chunks it finds in the workspace.
 constexpr int kLongThreads = 512;
 constexpr int kLongWaves = kLongThreads / 64;
 constexpr int kLongBins = 2048;
 constexpr int kLongList = 16384;
+constexpr int64_t kListedK = 4096;                      // top-k of so many at most: all it keeps goes through the list, weights and top-p with it
+constexpr uint32_t kLdsList = 2048;                     // entries of it that the draw holds in LDS
 constexpr int kLongStage = 1024;                        // places a workgroup collects before it goes to the row's list one by one
 constexpr int64_t kLongRows = 256;                      // of a batch
 constexpr int kMostPieces = 512;                        // chunks of a row
@@ -612,7 +633,8 @@ struct LongArgs {
     RowBins *bins;                                      // [rows]
 };
 
-// The entries of a span, kLoad at a time by each of `n` threads, with two loads of each under way; a thread's indices ascend.
+// The entries of a span, kLoad at a time by each of `n` threads, with two loads of each under way; a thread's indices ascend.  (NaN comes as it is: no
+// comparison takes it for a largest or smallest one, and its distance is none.)
 template <typename T, typename F>
 __device__ inline void visit_span(const T *x, int64_t begin, int64_t end, int thread, int n, F what)
 {
@@ -626,16 +648,16 @@ __device__ inline void visit_span(const T *x, int64_t begin, int64_t end, int th
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < kLoad; ++j) what(logit_of(v[u][j]), i + u * step + j);
+            for (int j = 0; j < kLoad; ++j) what((float)v[u][j], i + u * step + j);
     }
     for (; i < end; i += step) {
         if (i + kLoad <= end) {
             T v[kLoad];
             __builtin_memcpy(v, x + i, sizeof(v));
 #pragma unroll
-            for (int j = 0; j < kLoad; ++j) what(logit_of(v[j]), i + j);
+            for (int j = 0; j < kLoad; ++j) what((float)v[j], i + j);
         } else {
-            for (int64_t j = i; j < end; ++j) what(logit_of(x[j]), j);
+            for (int64_t j = i; j < end; ++j) what((float)x[j], j);
         }
     }
 }
@@ -688,6 +710,8 @@ __device__ inline Piece row_top(const LongArgs &q, int r)
     return of_wave(p);
 }
 
+// whether all that top-k keeps goes through the list: its histogram needs no weights then
+__device__ inline bool k_by_list(const LongArgs &q, const RowRules &r) { return r.k < q.a.n && r.k <= kListedK; }
 // whether a row's cut has to be looked for (a single entry, its largest, is known from the maxima)
 __device__ inline bool cuts(const LongArgs &q, const RowRules &r, float top) { return top > -INFINITY && r.k != 1 && (r.k < q.a.n || r.p < 1.0f); }
 
@@ -713,7 +737,7 @@ __global__ void __launch_bounds__(kLongThreads) long_histogram_kernel(LongArgs q
     __syncthreads();
     const T *const x = static_cast<const T *>(q.a.logits) + (q.row0 + r) * q.a.ld;
     const int64_t begin = piece * q.chunk, end = min(q.a.n, begin + q.chunk);
-    const bool use_k = rules.k < q.a.n, use_p = rules.p < 1.0f;
+    const bool use_k = rules.k < q.a.n, use_p = rules.p < 1.0f && !k_by_list(q, rules);
     with_distances(p.top, rules.inv, [&](auto distance) {
         visit_span(x, begin, end, threadIdx.x, kLongThreads, [&](float v, int64_t) {
             const float d = distance(v);
@@ -756,7 +780,7 @@ __global__ void __launch_bounds__(kLongThreads) long_bins_kernel(LongArgs q)
     const RowRules rules = rules_of(q.a, q.row0 + r);
     const Piece p = row_top(q, r);
     if (!cuts(q, rules, p.top)) return;
-    const bool use_k = rules.k < q.a.n, use_p = rules.p < 1.0f;
+    const bool use_k = rules.k < q.a.n, by_list = k_by_list(q, rules), use_p = rules.p < 1.0f && !by_list;
     const float scale = bin_scale(distance_from(p.top, p.low, rules.inv), kLongBins);
     const uint64_t n_before = Grp::scan(waves, n, &all_n), w_before = Grp::scan(waves, w, &all_w);
     if (threadIdx.x == 0) bin_k = bin_first = bin_last = -1;
@@ -813,7 +837,7 @@ __global__ void __launch_bounds__(kLongThreads) long_bins_kernel(LongArgs q)
             if (bin < kLongBins && bin_of(mid, scale, kLongBins) >= bin) hi = mid;
             else lo = mid + 1;
         }
-        (&out->near)[threadIdx.x] = distance_of(lo);
+        (&out->near)[threadIdx.x] = by_list && threadIdx.x == 0 ? 0.0f : distance_of(lo);
     }
     if (threadIdx.x == 0) {
         out->k_bin = bin_k;
@@ -892,7 +916,7 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
 {
     using Grp = Group<1024>;
     __shared__ typename Grp::Shared s;
-    __shared__ uint64_t weight[kMostSegments];
+    __shared__ uint64_t weight[kMostSegments], held[kLdsList];
     __shared__ int found;
     __shared__ uint64_t found_before;
     const int r = blockIdx.x;
@@ -917,56 +941,57 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
         const RowBins bins = q.bins[r];
         const uint32_t listed = q.listed[r];
         const bool whole = listed <= kLongList;
+        const bool near = listed <= kLdsList;
         const uint64_t *const list = q.list + (int64_t)r * kLongList;
-        auto entries = [&](auto what) {
-            if (whole) {
-                for (uint32_t i = threadIdx.x; i < listed; i += 1024) {
-                    const uint64_t at = list[i];
-                    what(at, (uint32_t)(at >> 32));
-                }
-            } else {
-                for (int64_t i = threadIdx.x; i < q.a.n; i += 1024) {
-                    const uint32_t key = key_of(distance_from(p.top, logit_of(x[i]), rules.inv));
-                    if (key < kMaskedKey) what((uint64_t)key << 32 | (uint32_t)i, key);
-                }
+        if (near)
+            for (uint32_t i = threadIdx.x; i < listed; i += 1024) held[i] = list[i];        // (a thread reads its own ones)
+        // those up to the cut, of one bin (or all)
+        auto entries = [&](int bin, auto what) {
+            const int64_t n = whole ? (int64_t)listed : q.a.n;
+            for (int64_t i = threadIdx.x; i < n; i += 1024) {
+                uint64_t at;
+                if (near) at = held[i];
+                else if (whole) at = list[i];
+                else at = (uint64_t)key_of(distance_from(p.top, logit_of(x[i]), rules.inv)) << 32 | (uint32_t)i;
+                const uint32_t key = (uint32_t)(at >> 32);
+                if (key < kMaskedKey && at <= cut && (bin < 0 || bin_of(key, bins.scale, kLongBins) == bin)) what(at, key);
             }
         };
-        auto of_bin = [&](int bin) {
-            return [&, bin](auto what) {
-                entries([&](uint64_t at, uint32_t key) {
-                    if (at <= cut && bin_of(key, bins.scale, kLongBins) == bin) what(at, key);
-                });
-            };
-        };
-        uint64_t kept = bins.mass;
-        if (rules.k < q.a.n) {
-            cut = Grp::last_below(s, of_bin(bins.k_bin), bins.k_count, false, (uint64_t)rules.k, 0.0, bins.k_before);
-            if (rules.p < 1.0f) {
+        // top-k's cut, then top-p's.  (One place that looks for both: twice, the code does not fit the instruction cache.)
+        for (int by_mass = rules.k < q.a.n ? 0 : 1; by_mass < (rules.p < 1.0f ? 2 : 1); ++by_mass) {
+            int bin = bins.k_bin;
+            uint64_t n = bins.k_count, before = bins.k_before;
+            double limit = 0.0;
+            if (by_mass) {
                 uint64_t w = 0;
-                of_bin(bins.k_bin)([&](uint64_t, uint32_t key) { w += weight_of_key(key); });
-                kept = bins.k_mass_before + Grp::sum(s, w);
+                if (rules.k < q.a.n) {
+                    entries(k_by_list(q, rules) ? -1 : bins.k_bin, [&](uint64_t, uint32_t key) { w += weight_of_key(key); });
+                    w = Grp::sum(s, w);
+                }
+                n = whole ? (uint64_t)listed : (uint64_t)q.a.n;         // (at most)
+                bin = -1;
+                before = 0;
+                if (k_by_list(q, rules)) limit = (double)rules.p * (double)w;
+                else {
+                    limit = (double)rules.p * (double)(rules.k < q.a.n ? bins.k_mass_before + w : bins.mass);
+                    const uint64_t *const mass = q.mass + (int64_t)r * kLongBins;
+                    bin = bins.p_first;
+                    before = bins.p_mass_before;
+                    uint64_t m = before;
+                    for (int b = bins.p_first; b <= bins.p_last; ++b) {
+                        const uint64_t own = mass[b];
+                        if (own > 0 && begins_below(true, m, 0, limit)) { bin = b; before = m; }
+                        m += own;
+                    }
+                }
             }
+            cut = Grp::last_below(s, [&](auto what) { entries(bin, what); }, n, by_mass != 0, (uint64_t)rules.k, limit, before);
         }
-        if (rules.p < 1.0f) {
-            const uint64_t *const mass = q.mass + (int64_t)r * kLongBins;
-            const double limit = (double)rules.p * (double)kept;
-            int bin = bins.p_first;
-            uint64_t before = bins.p_mass_before, m = before;
-            for (int b = bins.p_first; b <= bins.p_last; ++b) {
-                const uint64_t own = mass[b];
-                if (own > 0 && begins_below(true, m, 0, limit)) { bin = b; before = m; }
-                m += own;
-            }
-            uint64_t n = 0;
-            of_bin(bin)([&](uint64_t, uint32_t) { ++n; });
-            cut = Grp::last_below(s, of_bin(bin), Grp::sum(s, n), true, 0, limit, before);
-        }
-        // what the cuts' bins add to the segments (the row itself, where the list is not whole: everything)
+        // what the list adds to the segments (the row itself, where the list is not whole: everything)
         if (!whole)
             for (int i = threadIdx.x; i < segments; i += 1024) weight[i] = 0;
         __syncthreads();
-        entries([&](uint64_t at, uint32_t key) {
-            if (at > cut) return;
+        entries(-1, [&](uint64_t at, uint32_t key) {
             const uint64_t w = kept_weight(distance_of(key), rules.least);
             if (w) atomicAdd(reinterpret_cast<unsigned long long *>(&weight[(uint32_t)at / (uint32_t)segment]), (unsigned long long)w);
         });
