@@ -11,6 +11,8 @@
 //   before each; where a bin holds more than fit the list in LDS, it is cut into bins of places, again and again.
 // - longer rows are cut into chunks, a workgroup each; a launch for each of the passes.
 #include <algorithm>
+#include <type_traits>
+#include <utility>
 
 #include "element_types.h"
 #include "rls_internal.h"
@@ -186,6 +188,109 @@ __global__ void __launch_bounds__(256) sample_short_kernel(SampleArgs a)
     }
     a.token[row] = token;
     if (a.logprob) a.logprob[row] = d_token - log_of(total);
+}
+
+// ---- rows of up to 64 entries ----------------------------------------------------------------------
+
+constexpr int kLaneRow = 64;
+
+// 16 lanes take a row, four entries each; for a cut every entry is counted against those of the 15 other lanes, which go round.  (A wave per
+// row: 524288 x 20 entries 330 us, bound by how many workgroups begin.)
+template <typename T>
+__global__ void __launch_bounds__(256) sample_lanes_kernel(SampleArgs a)
+{
+    constexpr int E = 4;
+    const int lane = threadIdx.x & 15, n = (int)a.n, first = lane * E;
+    const int64_t at = (int64_t)blockIdx.x * (256 / 16) + (threadIdx.x >> 4), row = min(at, a.rows - 1);
+    const RowRules r = rules_of(a, row);
+    const T *const x = static_cast<const T *>(a.logits) + row * a.ld;
+    float l[E], top = -INFINITY;
+    if (first + E <= n) {
+        T v[E];
+        __builtin_memcpy(v, x + first, sizeof(v));
+#pragma unroll
+        for (int j = 0; j < E; ++j) l[j] = logit_of(v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            l[j] = logit_of(x[min(first + j, n - 1)]);
+            l[j] = first + j < n ? l[j] : -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) top = fmaxf(top, l[j]);
+    top = row_reduce(top, [](float u, float v) { return fmaxf(u, v); });
+    uint32_t key[E];
+    uint64_t w[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        key[j] = key_of(distance_from(top, l[j], r.inv));
+        w[j] = key[j] < kMaskedKey ? weight_of_key(key[j]) : 0;
+    }
+    auto add = [](uint64_t u, uint64_t v) { return u + v; };
+    const bool cut = (r.k < n) | (r.p < 1.0f);
+    if (__any(cut)) {
+        const bool by_mass = __any(r.p < 1.0f);
+        uint32_t rank[E] = {0, 0, 0, 0};
+        uint64_t before[E] = {0, 0, 0, 0};              // weight of what comes before an entry
+        auto against = [&](auto turn) {
+            constexpr int s = decltype(turn)::value;
+            const bool earlier = lane >= s && s > 0;    // (row_ror:s brings the entries of lane - s, or of lane + 16 - s)
+#pragma unroll
+            for (int o = 0; o < E; ++o) {
+                const uint32_t key_o = s == 0 ? key[o] : lane_move<0x120 + (s ? s : 1), 0xf>(key[o], key[o]);
+                const uint64_t w_o = !by_mass ? 0 : (s == 0 ? w[o] : lane_move<0x120 + (s ? s : 1), 0xf>(w[o], w[o]));
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    const bool ties = s == 0 ? o < j : earlier;
+                    const bool comes_first = key_o < key[j] + (ties ? 1u : 0u);
+                    rank[j] += comes_first ? 1u : 0u;
+                    if (by_mass) before[j] += comes_first ? w_o : 0;
+                }
+            }
+        };
+        [&]<int... S>(std::integer_sequence<int, S...>) { (against(std::integral_constant<int, S>()), ...); }(std::make_integer_sequence<int, 16>());
+        uint64_t kept = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            w[j] = (int64_t)rank[j] < r.k ? w[j] : 0;   // (where an entry is inside top-k so is everything before it)
+            kept += w[j];
+        }
+        if (by_mass) {
+            const double limit = (double)r.p * (double)row_reduce(kept, add);
+#pragma unroll
+            for (int j = 0; j < E; ++j) w[j] = (r.p < 1.0f) & (before[j] > 0) & ((double)before[j] >= limit) ? 0 : w[j];
+        }
+    }
+    uint64_t mine = 0;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const float e = exp_of(distance_of(key[j]));
+        w[j] = (e < r.least) & (key[j] != 0) ? 0 : w[j];
+        mine += w[j];
+    }
+    uint64_t run = row_scan(mine, (uint64_t)0, add);
+    const uint64_t total = row_reduce(mine, add);
+    const double mark = r.u * (double)total;
+    auto beyond = [&](uint64_t v) { return ((double)v > mark) | (v == total); };
+    run -= mine;
+    int token = -1;
+    uint32_t key_token = 0;
+    const bool here = beyond(run + mine) & !beyond(run);
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        run += w[j];
+        const bool now = (token < 0) & beyond(run);
+        token = now ? first + j : token;
+        key_token = now ? key[j] : key_token;
+    }
+    if (at >= a.rows) return;
+    if (!(top > -INFINITY)) {
+        if (lane == 0) no_draw(a, row);
+    } else if (here) {
+        a.token[row] = token;
+        if (a.logprob) a.logprob[row] = -distance_of(key_token) - log_of(total);
+    }
 }
 
 // ---- a workgroup's tools --------------------------------------------------------------------------
@@ -558,7 +663,7 @@ __global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a)
     }
 }
 
-constexpr int64_t kGroupRow = 32768;
+constexpr int64_t kGroupRow = 16384;
 constexpr int64_t kFewRows = 512;
 constexpr int64_t kMostGroups = 1 << 20;           // (of a launch, which ends at 2^32 threads)
 
@@ -569,14 +674,13 @@ hipError_t launch_group_rows(const SampleArgs &a, hipStream_t s)
     // a few rows are as long as what a thread does in turn: four entries each; many rows are work, of which a larger workgroup has more in its
     // scans and barriers
     const bool few = a.rows <= kFewRows;
-    if (a.n <= 256) hipLaunchKernelGGL((sample_row_kernel<T, 64, 4>), grid, dim3(64), 0, s, a);
-    else if (few && a.n <= 1024) hipLaunchKernelGGL((sample_row_kernel<T, 256, 4>), grid, dim3(256), 0, s, a);
-    else if (a.n <= 1024) hipLaunchKernelGGL((sample_row_kernel<T, 64, 16>), grid, dim3(64), 0, s, a);
-    else if (few && a.n <= 2048) hipLaunchKernelGGL((sample_row_kernel<T, 512, 4>), grid, dim3(512), 0, s, a);
-    else if (few && a.n <= 4096) hipLaunchKernelGGL((sample_row_kernel<T, 1024, 4>), grid, dim3(1024), 0, s, a);
-    else if (a.n <= 4096) hipLaunchKernelGGL((sample_row_kernel<T, 256, 16>), grid, dim3(256), 0, s, a);
-    else if (a.n <= 16384) hipLaunchKernelGGL((sample_row_kernel<T, 1024, 16>), grid, dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL((sample_row_kernel<T, 1024, 32>), grid, dim3(1024), 0, s, a);
+    auto launch = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a); };
+    if (a.n <= 256) launch(sample_row_kernel<T, 64, 4>, 64);
+    else if (a.n <= 1024) few ? launch(sample_row_kernel<T, 256, 4>, 256) : a.n <= 512 ? launch(sample_row_kernel<T, 64, 8>, 64) : launch(sample_row_kernel<T, 64, 16>, 64);
+    else if (a.n <= 2048) few ? launch(sample_row_kernel<T, 512, 4>, 512) : launch(sample_row_kernel<T, 128, 16>, 128);
+    else if (a.n <= 4096) few ? launch(sample_row_kernel<T, 1024, 4>, 1024) : launch(sample_row_kernel<T, 256, 16>, 256);
+    else if (a.n <= 8192) few ? launch(sample_row_kernel<T, 1024, 8>, 1024) : launch(sample_row_kernel<T, 512, 16>, 512);
+    else launch(sample_row_kernel<T, 1024, 16>, 1024);
     return hipGetLastError();
 }
 
@@ -1114,6 +1218,10 @@ template <typename T>
 hipError_t launch_sample(const SampleArgs &a, char *ws, hipStream_t s)
 {
     if (a.n <= kThreadRow) return launch_short_rows<T>(a, s);
+    if (a.n <= kLaneRow) {
+        hipLaunchKernelGGL(sample_lanes_kernel<T>, dim3((unsigned)((a.rows + 15) / 16)), dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
     if (a.n <= kGroupRow) return launch_group_rows<T>(a, s);
     return launch_long_rows<T>(a, ws, s);
 }

@@ -41,6 +41,24 @@ __device__ inline uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_am
 __device__ inline float last_lane(float x) { return __uint_as_float(last_lane(__float_as_uint(x))); }
 __device__ inline uint64_t last_lane(uint64_t x) { return (uint64_t)last_lane((uint32_t)(x >> 32)) << 32 | last_lane((uint32_t)x); }
 
+// The same over rows of 16 lanes, each by itself: a scan, and a join that all lanes of the row get
+template <typename T, typename F>
+__device__ inline T row_scan(T x, T none, F join)
+{
+    x = join(lane_move<0x111, 0xf>(none, x), x);
+    x = join(lane_move<0x112, 0xf>(none, x), x);
+    x = join(lane_move<0x114, 0xf>(none, x), x);
+    return join(lane_move<0x118, 0xf>(none, x), x);
+}
+template <typename T, typename F>
+__device__ inline T row_reduce(T x, F join)
+{
+    x = join(lane_move<0x128, 0xf>(x, x), x);           // row_ror:8, 4, 2, 1
+    x = join(lane_move<0x124, 0xf>(x, x), x);
+    x = join(lane_move<0x122, 0xf>(x, x), x);
+    return join(lane_move<0x121, 0xf>(x, x), x);
+}
+
 // over all lanes of a wave, all of them active; the same in every lane
 template <typename T, typename F>
 __device__ inline T wave_reduce(T x, T none, F join)

@@ -60,12 +60,12 @@ def reference(d, order, u, k, p, min_p):
     return int(token), float(d[token] - np.log(total))
 
 
-def check(rls, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, device_logits=None):
+def check(rls, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, device_logits=None, every=1):
     dev = lambda t: None if t is None else t.cuda()      # noqa: E731
     token, logprob = rls.sample(device_logits if device_logits is not None else logits.cuda(), dev(uniform), dev(temperature), dev(top_k), dev(top_p), dev(min_p))
     token, logprob = token.cpu().numpy(), logprob.cpu().numpy()
     x = logits.float().numpy()
-    for r in range(x.shape[0]):
+    for r in range(0, x.shape[0], every):
         t = 1.0 if temperature is None else float(temperature[r])
         if not np.any(x[r] > -np.inf):
             assert token[r] == -1 and logprob[r] == -np.inf
@@ -108,6 +108,16 @@ def test_long_rows(rls, rows, n, dtype, which):
     gen = torch.Generator().manual_seed(n)
     logits = (torch.randn(rows, n, generator=gen) * 2.0).to(TYPES[dtype])
     check(rls, logits, torch.rand(rows, generator=gen), **settings(rows, n, which, gen))
+
+
+@pytest.mark.parametrize("which", ["", "k", "p", "tkpm"])
+@pytest.mark.parametrize("n", [20, 64, 65, 200, 400, 900, 1500, 3000, 6000, 12000])
+def test_many_rows(rls, n, which):
+    """More rows than the widest workgroups are for; one in 29 is looked at."""
+    gen = torch.Generator().manual_seed(n)
+    rows = 700
+    logits = (torch.randn(rows, n, generator=gen) * 2.0).to(torch.bfloat16 if n % 200 else torch.float32)
+    check(rls, logits, torch.rand(rows, generator=gen), every=29, **settings(rows, n, which, gen))
 
 
 @pytest.mark.parametrize("n", [3, 8, 40, 700, 5000, 140000, 400001])
