@@ -156,8 +156,11 @@ def _stream() -> ctypes.c_void_p:
 
 
 def _raw_stream(t: torch.Tensor) -> int:
-    """The current stream of the tensor's device as a number (making a Stream object of it takes 3 us, a fifth of a short call)."""
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+    """The current stream as a number (making a Stream object of it takes 3 us, a fifth of a short call)."""
+    device = t.device.index
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors are on device {device}, which is not the current one")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _ptr(t: Optional[torch.Tensor]) -> ctypes.c_void_p:
@@ -501,6 +504,8 @@ def _space(workspace: Optional[torch.Tensor], need, device) -> Tuple[Optional[to
         if n == 0:
             return None, 0, 0
         workspace = _workspace(n, device)
+    elif not workspace.is_cuda:
+        raise ValueError("workspace must be a device tensor")
     base = _aligned_ptr(workspace)
     return workspace, base, max(0, workspace.numel() * workspace.element_size() - (base - workspace.data_ptr()))
 

@@ -700,7 +700,10 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
 
 // ---- which way a call takes ----------------------------------------------------------------------
 
-constexpr int64_t kFewSteps = 16;
+// Up to so many steps a thread goes through a channel by itself; a thread | tiles, in bf16, forward: 64 x 16 x 4096 12 | 25 us, 4 x 64 x 4096 19 | 13.
+// Many channels hide a thread's waits for longer: 1024 x 32 x 1024 53 | 90 us, 1024 x 64 x 1024 168 | 122, and one channel's tile is
+// 4096 steps: 100000 x 64 x 1 181 | 543, 100000 x 200 x 1 744 | 550.
+int64_t few_steps(int64_t states, bool along) { return along && states >= (1 << 16) ? 128 : (states >= (1 << 17) ? 32 : 16); }
 
 thread_local long long g_patience = kPatience;
 
@@ -722,7 +725,7 @@ ScanPlan plan_scan(int64_t batch, int64_t steps, int64_t channels, bool wide, bo
     r.cut.strips = (int32_t)((channels + lanes * r.vec - 1) / (lanes * r.vec));
     const int64_t tile = r.along ? kAlongTile : (int64_t)kWaves * (64 / lanes) * (wide ? kWideSteps : kSteps);
     const int64_t tiles = std::max<int64_t>(1, (steps + tile - 1) / tile);
-    r.tiles = steps > kFewSteps && batch * r.cut.strips <= ((int64_t)1 << 22) / tiles;
+    r.tiles = steps > few_steps(batch * channels, r.along) && batch * r.cut.strips <= ((int64_t)1 << 22) / tiles;
     if (!r.tiles) return r;
     r.cut.n_tiles = (int32_t)tiles;
     if (tiles > 1) {

@@ -110,7 +110,7 @@ def check_backward(rls, a, h, dh, h0, reset, dlast, reverse, a_dev=None, dh_dev=
 
 
 SIZES = [(1, 1, 1), (3, 1, 5), (64, 1, 130), (2, 2, 64), (1, 7, 3), (3, 63, 65), (2, 64, 128), (1, 129, 257), (5, 300, 33), (1, 1025, 48), (2, 4099, 19),
-         (1, 20001, 8), (300, 40, 70), (2, 513, 1024)]
+         (1, 20001, 8), (300, 40, 70), (2, 513, 1024), (130, 24, 1030), (70000, 60, 1)]
 
 
 @pytest.mark.parametrize("B,T,C", SIZES)
