@@ -18,7 +18,8 @@
 // and read atomically and is all ones until then, so that no fence is needed (which would write the second-level cache back,
 // 100 us here).  A tile that has waited too long for another goes through all the steps before it by itself, so that no
 // order in which workgroups run can hold up a call.  (Composed by a launch of their own, chunks of time had their inputs read twice:
-// 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us.)
+// 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us; now 61 and 140, the floors 42 and 104.  The backward pass of
+// 8 x 4093 x 2048 in bf16 takes 154 us, 4.4 TB/s.  A launch that clears the items first is 5 us of it, with the gap after it 10.)
 #include <algorithm>
 #include <type_traits>
 
@@ -92,9 +93,11 @@ __global__ void __launch_bounds__(kScanThreads) scan_backward_kernel(ScanArgs p)
 
 // ---- tiles --------------------------------------------------------------------------------------
 
-constexpr int kWaves = 4, kStripLanes = 32;      // of a workgroup; of a strip at most
+// Of a workgroup; of a strip at most.  (8 waves: 1 x 65521 x 1024 forward 140 -> 144 us, 8 x 4093 x 2048 backward 156 -> 166; strips of
+// 16 lanes: 138, 168.  A tile's fixed costs - a barrier, a look at the tiles before, 2 to 4 us each - hide behind another workgroup's loads.)
+constexpr int kWaves = 4, kStripLanes = 32;
 constexpr int kSteps = 16, kWideSteps = 8;          // of a thread: of two bytes each, of four (16 of those spill registers and are as fast)
-constexpr int kAlongWaves = 8, kAlongParts = 2;     // one channel: parts of 64 x 4 steps that a wave takes
+constexpr int kAlongWaves = 8, kAlongParts = 2;     // one channel: parts of 64 x 4 steps that a wave takes (4 and 4: 64 x 262144 70 us, 8 and 4: 69, 8 and 2: 61)
 constexpr int64_t kAlongTile = (int64_t)kAlongWaves * kAlongParts * 256;
 constexpr long long kPatience = 200000;             // ticks of the 100 MHz clock: 2 ms
 
