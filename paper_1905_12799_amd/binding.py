@@ -115,7 +115,7 @@ def lib() -> ctypes.CDLL:
         L.rls_sample_workspace_bytes.argtypes = [i64, i64]
         L.rls_sample.restype = i32
         L.rls_sample.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
-        seq = ctypes.POINTER(_Sequence)
+        seq = vp                                         # addresses within one array: see _sequences
         L.rls_linear_scan_workspace_bytes.restype = i64
         L.rls_linear_scan_workspace_bytes.argtypes = [i64, i64, i64]
         L.rls_linear_scan.restype = i32
@@ -548,10 +548,16 @@ def linear_scan_workspace_bytes(batch: int, steps: int, channels: int) -> int:
     return n
 
 
-def _sequence(t: torch.Tensor, shape, dtype: torch.dtype, name: str):
-    if t.dtype != dtype or t.shape != shape or not t.is_cuda or (shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be a device tensor of shape {tuple(shape)} and type {dtype} with unit stride along the channels")
-    return ctypes.byref(_Sequence(t.data_ptr(), t.stride(0), t.stride(1)))
+def _sequences(shape, *named):
+    """rls_sequence structs of (tensor, type, name) side by side in one array, and their addresses; the array has to outlive the call."""
+    numbers = []
+    for t, dtype, name in named:
+        if t.dtype != dtype or t.shape != shape or not t.is_cuda or (shape[2] > 1 and t.stride(2) != 1):
+            raise ValueError(f"{name} must be a device tensor of shape {tuple(shape)} and type {dtype} with unit stride along the channels")
+        numbers += (t.data_ptr(), t.stride(0), t.stride(1))
+    held = (ctypes.c_int64 * len(numbers))(*numbers)
+    base = ctypes.addressof(held)
+    return held, range(base, base + ctypes.sizeof(held), ctypes.sizeof(_Sequence))
 
 
 def _states(t: Optional[torch.Tensor], shape, name: str) -> int:
@@ -590,9 +596,9 @@ def linear_scan(a: torch.Tensor, b: torch.Tensor, h0: Optional[torch.Tensor] = N
     h = torch.empty(size, dtype=b.dtype, device=b.device) if out is None else out
     last = torch.empty((B, C), dtype=torch.float32, device=b.device) if last is None else last
     ws, base, avail = _space(workspace, lambda: linear_scan_workspace_bytes(B, T, C), b.device)
-    _check(lib().rls_linear_scan(ctypes.byref(shape), _sequence(a, size, a.dtype, "a"), _sequence(b, size, b.dtype, "b"), _states(h0, size, "h0"),
-                                 _resets(reset, size), _sequence(h, size, b.dtype, "out"), _states(last, size, "last"), base, avail,
-                                 _raw_stream(b)), "rls_linear_scan")
+    held, at = _sequences(size, (a, a.dtype, "a"), (b, b.dtype, "b"), (h, b.dtype, "out"))
+    _check(lib().rls_linear_scan(ctypes.byref(shape), at[0], at[1], _states(h0, size, "h0"), _resets(reset, size), at[2], _states(last, size, "last"),
+                                 base, avail, _raw_stream(b)), "rls_linear_scan")
     return h, last
 
 
@@ -608,10 +614,9 @@ def linear_scan_backward(a: torch.Tensor, h: torch.Tensor, dh: torch.Tensor, h0:
     db = torch.empty((B, T, C), dtype=h.dtype, device=h.device)
     dh0 = torch.empty((B, C), dtype=torch.float32, device=h.device)
     ws, base, avail = _space(workspace, lambda: linear_scan_workspace_bytes(B, T, C), h.device)
-    _check(lib().rls_linear_scan_backward(ctypes.byref(shape), _sequence(a, size, a.dtype, "a"), _sequence(h, size, h.dtype, "h"),
-                                          _sequence(dh, size, h.dtype, "dh"), _states(h0, size, "h0"), _resets(reset, size),
-                                          _states(dh_last, size, "dh_last"), _sequence(da, size, a.dtype, "da"),
-                                          _sequence(db, size, h.dtype, "db"), dh0.data_ptr(), base, avail, _raw_stream(h)),
+    held, at = _sequences(size, (a, a.dtype, "a"), (h, h.dtype, "h"), (dh, h.dtype, "dh"), (da, a.dtype, "da"), (db, h.dtype, "db"))
+    _check(lib().rls_linear_scan_backward(ctypes.byref(shape), at[0], at[1], at[2], _states(h0, size, "h0"), _resets(reset, size),
+                                          _states(dh_last, size, "dh_last"), at[3], at[4], dh0.data_ptr(), base, avail, _raw_stream(h)),
            "rls_linear_scan_backward")
     return da, db, dh0
 

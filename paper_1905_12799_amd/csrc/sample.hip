@@ -432,6 +432,7 @@ struct Group {
     static __device__ inline uint64_t smaller(const Shared &s, uint64_t at, uint32_t from, uint32_t to, bool by_mass)
     {
         uint64_t run = 0;
+#pragma unroll 8
         for (uint32_t o = from; o < to; ++o) {
             const uint64_t add = by_mass ? s.weight[o] : 1;
             run += s.place[o] < at ? add : 0;
@@ -935,15 +936,16 @@ __global__ void __launch_bounds__(kLongThreads) long_bins_kernel(LongArgs q)
             if (b == bin_first) out->p_mass_before = m0;
         });
     }
-    // the least distance that falls into a bin, by bisection, for the ends of the bins
+    // the least distance that falls into a bin, for the ends of the bins: next to the bin's number over the scale
     if (threadIdx.x < 4) {
         const int near = use_p ? bin_first : bin_k, far = use_p ? bin_last : bin_k;
         const int bin = threadIdx.x == 0 ? near : (threadIdx.x == 1 ? far + 1 : (threadIdx.x == 2 ? bin_k : bin_k + 1));
-        uint32_t lo = 0, hi = kMaskedKey;
-        while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (bin < kLongBins && bin_of(mid, scale, kLongBins) >= bin) hi = mid;
-            else lo = mid + 1;
+        uint32_t lo = 0;
+        if (bin >= kLongBins) lo = kMaskedKey;
+        else if (bin > 0) {
+            lo = min(__float_as_uint((float)bin / scale), kMaskedKey - 1);
+            while (lo > 0 && bin_of(lo - 1, scale, kLongBins) >= bin) --lo;
+            while (lo < kMaskedKey && bin_of(lo, scale, kLongBins) < bin) ++lo;
         }
         (&out->near)[threadIdx.x] = by_list && threadIdx.x == 0 ? 0.0f : distance_of(lo);
     }

@@ -264,3 +264,24 @@ def test_on_another_stream_and_in_a_graph(rls):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(p[0], state[0]) and torch.equal(a.exp_avg[0], state[1]) and torch.equal(a.exp_avg_sq[0], state[2])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_tensor_beyond_32_bits(rls, bits):
+    """2^31 + 300 elements: the last ones, and some in between, against the formula."""
+    n = (1 << 31) + 300
+    p = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    for at in (0, 1 << 30, (1 << 31) - 5, n - 300):
+        g[at:at + 300] = torch.linspace(-1, 1, 300, device="cuda").to(torch.bfloat16)
+    opt = rls.AdamW([p], state_bits=bits)
+    opt.step([g], lr=0.25, eps=1.0, weight_decay=0.0)
+    for at in (0, 1 << 30, (1 << 31) - 5, n - 300):
+        x = g[at:at + 300].double()
+        want = 0.5 - 0.25 * x / (x.abs() + 1.0)
+        assert (p[at:at + 300].double() - want).abs().max() <= 2.0 ** -8 * 0.65 + 2.0 ** -18
+    assert (p[1 << 20:1 << 21] == 0.5).all()
+    if bits == 32:
+        assert (opt.exp_avg[0][n - 300:].double() - 0.1 * g[n - 300:].double()).abs().max() <= 2.0 ** -24
+    else:
+        assert (opt.exp_avg[0][n - 300:] != 0).sum() > 250

@@ -269,3 +269,27 @@ def test_in_a_graph(rls, rows, n):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("rows,n,part", [((1 << 20) + 5000, 65, 300), (300, 20000, 7), (600, 16385, 300), (40000, 33, 100)])
+def test_rows_do_not_depend_on_each_other(rls, rows, n, part):
+    """More rows than a launch, or a batch of long rows, takes at a time: the last ones get what they get by themselves."""
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    logits = (torch.randn(rows, n, generator=gen, device="cuda") * 2).to(torch.bfloat16)
+    u, p = torch.rand(rows, generator=gen, device="cuda"), 0.3 + 0.6 * torch.rand(rows, generator=gen, device="cuda")
+    k = torch.randint(1, 60, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    token, logprob = rls.sample(logits, u, top_k=k, top_p=p)
+    for at in (slice(0, part), slice(rows // 2, rows // 2 + part), slice(rows - part, rows)):
+        own, own_lp = rls.sample(logits[at], u[at].contiguous(), top_k=k[at].contiguous(), top_p=p[at].contiguous())
+        assert torch.equal(token[at], own) and torch.equal(logprob[at], own_lp)
+
+
+@pytest.mark.parametrize("n", [7, 50, 3000, 40000])
+def test_offsets_beyond_32_bits(rls, n):
+    """Rows 2^30 elements apart: the last one starts past 2^32 bytes."""
+    gen = torch.Generator().manual_seed(n)
+    whole = torch.empty(3 << 30, dtype=torch.float16, device="cuda")
+    view = whole.view(3, 1 << 30)[:, (1 << 30) - n:]
+    logits = (torch.randn(3, n, generator=gen) * 2).half()
+    view.copy_(logits)
+    check(rls, logits, torch.rand(3, generator=gen), device_logits=view, **settings(3, n, "tkp", gen))

@@ -305,3 +305,33 @@ def test_same_result_every_time(rls):
         for _ in range(3):
             again = rls.linear_scan(dev(a), dev(b), dev(h0))
             assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("T,C", [(12, 70), (70, 70), (70, 2)])
+def test_offsets_beyond_32_bits(rls, T, C):
+    """Steps 2^26 elements apart: the last ones lie past 2^32 bytes."""
+    a, b, h0, _ = make(1, T, C, torch.bfloat16, torch.float32, T)
+    apart = (1 << 26) if T > 60 else (1 << 28)
+    whole = torch.empty(T * apart, dtype=torch.bfloat16, device="cuda")
+    far = whole.view(1, T, apart)[:, :, apart - C:]
+    far.copy_(b)
+    h, _ = check_forward(rls, a, b, h0, None, False, b_dev=far)
+    dh = torch.randn(1, T, C, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
+    far.copy_(dh)
+    check_backward(rls, a, h.cpu(), dh, h0, None, None, False, dh_dev=far)
+    out = far                                            # written through as well
+    h2, _ = rls.linear_scan(dev(a), dev(b), dev(h0), out=out)
+    assert torch.equal(h2, h)
+
+
+def test_nothing_around_the_outputs_is_written(rls):
+    """Odd sizes inside larger arrays, both passes: the border keeps what it held."""
+    for B, T, C in ((2, 300, 67), (1, 1000, 3), (2, 5000, 1), (3, 20, 130)):
+        a, b, h0, _ = make(B, T, C, torch.bfloat16, torch.bfloat16, 8)
+        border = torch.full((B + 2, T + 2, C + 4), 3.0, dtype=torch.bfloat16).cuda()
+        out = border[1:1 + B, 1:1 + T, 2:2 + C]
+        want, _ = rls.linear_scan(dev(a), dev(b), dev(h0))
+        rls.linear_scan(dev(a), dev(b), dev(h0), out=out)
+        assert torch.equal(out, want)
+        border[1:1 + B, 1:1 + T, 2:2 + C] = 3.0
+        assert (border == 3).all()
