@@ -814,8 +814,16 @@ __global__ void __launch_bounds__(kLongThreads) long_top_kernel(LongArgs q)
 // The whole row's largest entry, the first place it is at, and the smallest that is not masked: every wave for itself
 __device__ inline Piece row_top(const LongArgs &q, int r)
 {
-    Piece p{-INFINITY, INFINITY, ~0u};
-    for (int i = threadIdx.x & 63; i < q.pieces; i += 64) p = joined(p, q.piece[(int64_t)r * q.pieces + i]);
+    constexpr int U = kMostPieces / 64;                 // (all reads under way together)
+    const Piece *const pieces = q.piece + (int64_t)r * q.pieces;
+    const int lane = threadIdx.x & 63;
+    Piece v[U], p{-INFINITY, INFINITY, ~0u};
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (64 * u < q.pieces) v[u] = pieces[min(64 * u + lane, q.pieces - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (64 * u < q.pieces) p = joined(p, v[u]);     // (one that is read twice changes nothing)
     return of_wave(p);
 }
 
@@ -1045,7 +1053,16 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
     const T *const x = static_cast<const T *>(q.a.logits) + row * q.a.ld;
     const int64_t segment = q.chunk / kLongWaves;
     const int segments = q.pieces * kLongWaves;
-    for (int i = threadIdx.x; i < segments; i += 1024) weight[i] = q.weight[(int64_t)r * segments + i];
+    {
+        constexpr int U = kMostSegments / 1024;
+        uint64_t v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (1024 * u < segments) v[u] = q.weight[(int64_t)r * segments + min(1024 * u + (int)threadIdx.x, segments - 1)];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (1024 * u + (int)threadIdx.x < segments) weight[1024 * u + threadIdx.x] = v[u];
+    }
     uint64_t cut = ~0ull;
     if (cuts(q, rules, p.top)) {
         const RowBins bins = q.bins[r];
