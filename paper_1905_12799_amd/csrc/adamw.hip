@@ -2,7 +2,7 @@
 //
 // Every array is read once and written once: 28 bytes a parameter with fp32 throughout, 16 in bf16 with master weights and
 // 8-bit moments, for some fifteen operations, so memory bounds it: 63 million parameters in fp32 take 344 us (5.1 TB/s, the rate of a
-// large copy), 185 million in bf16 with 8-bit moments 633 us (4.7 TB/s).  One launch takes the tensors of one kind, up to kTensors
+// large copy), 185 million in bf16 with 8-bit moments 633 to 645 us (4.6 TB/s).  One launch takes the tensors of one kind, up to kTensors
 // of them: their addresses travel as kernel arguments, and a workgroup finds its own by bisection of the first workgroups'
 // numbers.  (A launch per tensor would cost a network of small layers its launches: 2 us each.)
 //

@@ -19,7 +19,7 @@
 // 100 us here).  A tile that has waited too long for another goes through all the steps before it by itself, so that no
 // order in which workgroups run can hold up a call.  (Composed by a launch of their own, chunks of time had their inputs read twice:
 // 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us; now 61 and 140, the floors 42 and 104.  The backward pass of
-// 8 x 4093 x 2048 in bf16 takes 154 us, 4.4 TB/s.  A launch that clears the items first is 5 us of it, with the gap after it 10.)
+// 8 x 4093 x 2048 in bf16 takes 153 us, 4.4 TB/s.  A launch that clears the items first is 5 us of it, with the gap after it 10.)
 #include <algorithm>
 #include <type_traits>
 

@@ -10,8 +10,8 @@
 //   them.  A cut is found by a histogram over d (counts and weights in LDS) and, in the bin it lies in, by counting the places
 //   before each; where a bin holds more than fit the list in LDS, it is cut into bins of places, again and again.
 // - longer rows are cut into chunks, a workgroup each; a launch for each of the passes.
-// What it takes, of that the reading of the logits at the rate of a large copy: 524288 x 3 10 us (2), 524288 x 20 76 (8), 8 x 2000 with
-// top-k and top-p 12, 2048 x 8000 45 (13), 64 x 128003 in bf16 with every rule 47 (3), 64 x 262144 with top-p 75 (13), 1 x 8388608 26 (7).
+// What it takes, of that the reading of the logits at the rate of a large copy: 524288 x 3 10 us (2), 524288 x 20 78 (8), 8 x 2000 with
+// top-k and top-p 12, 2048 x 8000 44 (13), 64 x 128003 in bf16 with every rule 46 (3), 64 x 262144 with top-p 73 (13), 1 x 8388608 24 (7).
 #include <algorithm>
 #include <type_traits>
 #include <utility>
