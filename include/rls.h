@@ -294,7 +294,7 @@ int32_t rls_apply_actions(const int32_t *cfg_dev, const int8_t *action_dev, int6
 /*
  * One draw per row of logits: the search agent's action in a knob (Sec. 4.1, "Action space"), a candidate out of a
  * trajectory's scores, an entry of a vocabulary.  For a row x with largest logit x_max:
- *   d_i = (x_i - x_max) * (1 / temperature) in fp32, e_i = exp(d_i) in fp32 (0 beyond -100),
+ *   d_i = (x_i - x_max) * min(1 / temperature, largest fp32 number) in fp32, e_i = exp(d_i) in fp32 (0 beyond -100),
  *   w_i = e_i rounded to a multiple of 2^-38, as a whole number of them; sums of w are exact, whatever their order
  *   top-k:  the k first entries in the order of descending d, equal ones by ascending index
  *   top-p:  of these the ones before which, in that order, the sum of w is less than p times the sum over all of them
