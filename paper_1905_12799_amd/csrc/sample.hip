@@ -10,7 +10,7 @@
 //   them.  A cut is found by a histogram over d (counts and weights in LDS) and, in the bin it lies in, by counting the places
 //   before each; where a bin holds more than fit the list in LDS, it is cut into bins of places, again and again.
 // - longer rows are cut into chunks, a workgroup each; a launch for each of the passes.
-// What it takes, of that the reading of the logits at the rate of a large copy: 524288 x 3 10 us (2), 524288 x 20 78 (8), 8 x 2000 with
+// What it takes, of that the reading of the logits at the rate of a large copy: 524288 x 3 10 us (2), 524288 x 20 52 (8), 8 x 2000 with
 // top-k and top-p 12, 2048 x 8000 44 (13), 64 x 128003 in bf16 with every rule 46 (3), 64 x 262144 with top-p 73 (13), 1 x 8388608 24 (7).
 #include <algorithm>
 #include <type_traits>
@@ -196,12 +196,13 @@ __global__ void __launch_bounds__(256) sample_short_kernel(SampleArgs a)
 
 constexpr int kLaneRow = 64;
 
-// 16 lanes take a row, four entries each; for a cut every entry is counted against those of the 15 other lanes, which go round.  (A wave per
-// row: 524288 x 20 entries 330 us, bound by how many workgroups begin.)
-template <typename T>
+// 16 lanes take a row, two to four entries each; for a cut every entry is counted against those of the 15 other lanes, which go round: 16 E^2
+// pairs a lane, whose comparisons and additions are what bounds it.  524288 rows of 20, 40 and 64 entries without a cut 52, 63 and 72 us (reading
+// the logits 8, 16 and 26), with top-k 91, 139 and 199, with top-p 133, 213 and 300; with four entries a lane for every length, 64-bit weights and
+// ranks beside them top-k took 575 and top-p 625 at each.  (A wave per row: 524288 x 20 entries without a cut 330 us.)
+template <typename T, int E>
 __global__ void __launch_bounds__(256) sample_lanes_kernel(SampleArgs a)
 {
-    constexpr int E = 4;
     const int lane = threadIdx.x & 15, n = (int)a.n, first = lane * E;
     const int64_t at = (int64_t)blockIdx.x * (256 / 16) + (threadIdx.x >> 4), row = min(at, a.rows - 1);
     const RowRules r = rules_of(a, row);
@@ -209,7 +210,8 @@ __global__ void __launch_bounds__(256) sample_lanes_kernel(SampleArgs a)
     float l[E], top = -INFINITY;
     if (first + E <= n) {
         T v[E];
-        __builtin_memcpy(v, x + first, sizeof(v));
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = x[first + j];
 #pragma unroll
         for (int j = 0; j < E; ++j) l[j] = logit_of(v[j]);
     } else {
@@ -233,35 +235,56 @@ __global__ void __launch_bounds__(256) sample_lanes_kernel(SampleArgs a)
     const bool cut = (r.k < n) | (r.p < 1.0f);
     if (__any(cut)) {
         const bool by_mass = __any(r.p < 1.0f);
-        uint32_t rank[E] = {0, 0, 0, 0};
-        uint64_t before[E] = {0, 0, 0, 0};              // weight of what comes before an entry
-        auto against = [&](auto turn) {
+        // What comes before an entry.  By weight, a number of 64 bits takes both sums: the weights, whole numbers whose sum is 2^44 at
+        // most, and in the eight bits below them how many there are.  (Only its upper word is set to nothing where an entry does not
+        // come first: what is left is less than 2^-1022, which adds nothing to 1/256 and more.)
+        constexpr double kOne = 1.0 / 256.0;
+        uint32_t rank[E] = {};
+        double mass[E], before[E] = {};
+#pragma unroll
+        for (int j = 0; j < E; ++j) mass[j] = (double)w[j] + kOne;
+        auto against = [&](auto turn, auto weighed) {
             constexpr int s = decltype(turn)::value;
+            constexpr bool kMass = decltype(weighed)::value;
             const bool earlier = lane >= s && s > 0;    // (row_ror:s brings the entries of lane - s, or of lane + 16 - s)
+            uint32_t below[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) below[j] = key[j] + (earlier ? 1u : 0u);
 #pragma unroll
             for (int o = 0; o < E; ++o) {
                 const uint32_t key_o = s == 0 ? key[o] : lane_move<0x120 + (s ? s : 1), 0xf>(key[o], key[o]);
-                const uint64_t w_o = !by_mass ? 0 : (s == 0 ? w[o] : lane_move<0x120 + (s ? s : 1), 0xf>(w[o], w[o]));
+                const uint64_t bits = (uint64_t)__double_as_longlong(mass[o]);
+                const uint64_t moved = !kMass || s == 0 ? bits : lane_move<0x120 + (s ? s : 1), 0xf>(bits, bits);
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    const bool ties = s == 0 ? o < j : earlier;
-                    const bool comes_first = key_o < key[j] + (ties ? 1u : 0u);
-                    rank[j] += comes_first ? 1u : 0u;
-                    if (by_mass) before[j] += comes_first ? w_o : 0;
+                    const bool comes_first = key_o < (s == 0 && o < j ? key[j] + 1u : below[j]);
+                    if constexpr (kMass) before[j] += __hiloint2double(comes_first ? (int)(moved >> 32) : 0, (int)moved);
+                    else rank[j] += comes_first ? 1u : 0u;
                 }
             }
         };
-        [&]<int... S>(std::integer_sequence<int, S...>) { (against(std::integral_constant<int, S>()), ...); }(std::make_integer_sequence<int, 16>());
+        auto all_turns = [&]<int... S>(std::integer_sequence<int, S...>, auto weighed) { (against(std::integral_constant<int, S>(), weighed), ...); };
+        if (by_mass) {
+            all_turns(std::make_integer_sequence<int, 16>(), std::true_type());
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const double weight = trunc(before[j]);
+                rank[j] = (uint32_t)((before[j] - weight) * 256.0);
+                before[j] = weight;
+            }
+        } else {
+            all_turns(std::make_integer_sequence<int, 16>(), std::false_type());
+        }
         uint64_t kept = 0;
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            w[j] = (int64_t)rank[j] < r.k ? w[j] : 0;   // (where an entry is inside top-k so is everything before it)
+            w[j] = rank[j] < (uint32_t)r.k ? w[j] : 0;  // (where an entry is inside top-k so is everything before it)
             kept += w[j];
         }
         if (by_mass) {
             const double limit = (double)r.p * (double)row_reduce(kept, add);
 #pragma unroll
-            for (int j = 0; j < E; ++j) w[j] = (r.p < 1.0f) & (before[j] > 0) & ((double)before[j] >= limit) ? 0 : w[j];
+            for (int j = 0; j < E; ++j) w[j] = (r.p < 1.0f) & (before[j] > 0.0) & (before[j] >= limit) ? 0 : w[j];
         }
     }
     uint64_t mine = 0;
@@ -1242,7 +1265,8 @@ hipError_t launch_sample(const SampleArgs &a, char *ws, hipStream_t s)
 {
     if (a.n <= kThreadRow) return launch_short_rows<T>(a, s);
     if (a.n <= kLaneRow) {
-        hipLaunchKernelGGL(sample_lanes_kernel<T>, dim3((unsigned)((a.rows + 15) / 16)), dim3(256), 0, s, a);
+        auto *const kernel = a.n <= 32 ? sample_lanes_kernel<T, 2> : a.n <= 48 ? sample_lanes_kernel<T, 3> : sample_lanes_kernel<T, 4>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((a.rows + 15) / 16)), dim3(256), 0, s, a);
         return hipGetLastError();
     }
     if (a.n <= kGroupRow) return launch_group_rows<T>(a, s);

@@ -120,6 +120,19 @@ def test_many_rows(rls, n, which):
     check(rls, logits, torch.rand(rows, generator=gen), every=29, **settings(rows, n, which, gen))
 
 
+@pytest.mark.parametrize("which", ["", "k", "p", "tkpm"])
+@pytest.mark.parametrize("n", [17, 31, 32, 33, 47, 48, 49])
+@pytest.mark.parametrize("values", [4, 1000])
+def test_rows_of_a_few_entries_a_lane(rls, n, which, values):
+    """Around the lengths at which a lane takes one entry more, with and without ties, and masked entries."""
+    gen = torch.Generator().manual_seed(n + values)
+    rows = 90
+    logits = torch.randint(0, values, (rows, n), generator=gen).float() * (6.0 / values)
+    logits[::3, 1::2] = float("-inf")
+    logits[5] = float("-inf")
+    check(rls, logits, torch.rand(rows, generator=gen), **settings(rows, n, which, gen))
+
+
 @pytest.mark.parametrize("n", [3, 8, 40, 700, 5000, 140000, 400001])
 def test_ties_go_to_the_lowest_index(rls, n):
     """Logits of a few values: top-k cuts through entries that are equal, which keep the order of their indices."""
