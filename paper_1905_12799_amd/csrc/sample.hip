@@ -110,6 +110,13 @@ __device__ inline float bin_scale(float widest, int bins)
 __device__ inline int bin_of(uint32_t key, float scale, int bins) { return (int)fminf(distance_of(key) * scale, (float)(bins - 1)); }
 __device__ inline float log_of(uint64_t total) { return logf((float)((double)total * 0x1p-38)); }
 
+// Weight and count of the entries before one, up to 64 of them, as one number of 64 bits: the weights, whole numbers whose sum is 2^44 at
+// most, and in the eight bits below them how many there are.  (Where an entry is not counted only its upper word is set to nothing: what
+// is left is less than 2^-1022, which adds nothing to 1/256 and more.)
+__device__ inline double counted_mass(uint64_t w) { return (double)w + 1.0 / 256.0; }
+__device__ inline double mass_if(bool counted, uint64_t bits) { return __hiloint2double(counted ? (int)(bits >> 32) : 0, (int)bits); }
+__device__ inline uint32_t count_of(double mass) { return (uint32_t)((mass - trunc(mass)) * 256.0); }
+
 __device__ inline void no_draw(const SampleArgs &a, int64_t row)
 {
     a.token[row] = -1;
@@ -147,18 +154,18 @@ __global__ void __launch_bounds__(256) sample_short_kernel(SampleArgs a)
         w[i] = key[i] < kMaskedKey ? weight_of(e[i]) : 0;
     }
     if (r.k < n || r.p < 1.0f) {
-        uint64_t before[V], total = 0;                  // weight of what comes before an entry, top-k applied
+        uint64_t mass[V], total = 0;
+        double before[V];
         uint32_t in = 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            int rank = 0;
-            before[i] = 0;
+        for (int i = 0; i < V; ++i) mass[i] = (uint64_t)__double_as_longlong(counted_mass(w[i]));
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const bool first = (key[j] < key[i]) | ((key[j] == key[i]) & (j < i));
-                rank += first;
-                before[i] += first ? w[j] : 0;
-            }
+        for (int i = 0; i < V; ++i) {
+            before[i] = 0.0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) before[i] += j == i ? 0.0 : mass_if(key[j] < key[i] + (j < i ? 1u : 0u), mass[j]);
+            const int rank = (int)count_of(before[i]);
+            before[i] = trunc(before[i]);
             // (where an entry is inside top-k so is everything before it)
             in |= (rank < r.k ? 1u : 0u) << i;
             total += rank < r.k ? w[i] : 0;
@@ -167,7 +174,7 @@ __global__ void __launch_bounds__(256) sample_short_kernel(SampleArgs a)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             // (a selection, no branches: hipcc 7.2 loses the assignment of an element of an array in registers behind nested conditions)
-            const bool out = ((in >> i & 1u) == 0) | ((r.p < 1.0f) & (before[i] > 0) & ((double)before[i] >= limit));
+            const bool out = ((in >> i & 1u) == 0) | ((r.p < 1.0f) & (before[i] > 0.0) & (before[i] >= limit));
             w[i] = out ? 0 : w[i];
         }
     }
@@ -235,14 +242,11 @@ __global__ void __launch_bounds__(256) sample_lanes_kernel(SampleArgs a)
     const bool cut = (r.k < n) | (r.p < 1.0f);
     if (__any(cut)) {
         const bool by_mass = __any(r.p < 1.0f);
-        // What comes before an entry.  By weight, a number of 64 bits takes both sums: the weights, whole numbers whose sum is 2^44 at
-        // most, and in the eight bits below them how many there are.  (Only its upper word is set to nothing where an entry does not
-        // come first: what is left is less than 2^-1022, which adds nothing to 1/256 and more.)
-        constexpr double kOne = 1.0 / 256.0;
+        // (what comes before an entry: by weight, both sums in one number)
         uint32_t rank[E] = {};
         double mass[E], before[E] = {};
 #pragma unroll
-        for (int j = 0; j < E; ++j) mass[j] = (double)w[j] + kOne;
+        for (int j = 0; j < E; ++j) mass[j] = counted_mass(w[j]);
         auto against = [&](auto turn, auto weighed) {
             constexpr int s = decltype(turn)::value;
             constexpr bool kMass = decltype(weighed)::value;
@@ -258,7 +262,7 @@ __global__ void __launch_bounds__(256) sample_lanes_kernel(SampleArgs a)
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
                     const bool comes_first = key_o < (s == 0 && o < j ? key[j] + 1u : below[j]);
-                    if constexpr (kMass) before[j] += __hiloint2double(comes_first ? (int)(moved >> 32) : 0, (int)moved);
+                    if constexpr (kMass) before[j] += mass_if(comes_first, moved);
                     else rank[j] += comes_first ? 1u : 0u;
                 }
             }
@@ -268,9 +272,8 @@ __global__ void __launch_bounds__(256) sample_lanes_kernel(SampleArgs a)
             all_turns(std::make_integer_sequence<int, 16>(), std::true_type());
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const double weight = trunc(before[j]);
-                rank[j] = (uint32_t)((before[j] - weight) * 256.0);
-                before[j] = weight;
+                rank[j] = count_of(before[j]);
+                before[j] = trunc(before[j]);
             }
         } else {
             all_turns(std::make_integer_sequence<int, 16>(), std::false_type());
