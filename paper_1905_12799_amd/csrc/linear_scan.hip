@@ -330,6 +330,13 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
         if (RESET) own.cut = cut ? Steps<V>::kAll : own.cut;
     }
     scan_wave(own);
+    Steps<V> past;                                              // all the steps before the tile
+    past.clear();
+    if (q.n_tiles == 1) {                                       // (before the barrier: the last state may be written over it, by another wave)
+        const float *const from = BACK ? p.in : p.h0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) past.H[v] = from && c0 + v < C ? from[n * C + c0 + v] : 0.0f;
+    }
     scan_waves(own, waves_before, of_tile, false);
     const int64_t row = (int64_t)q.strips * V * lanes;          // items of a tile of time
     uint64_t *const items = q.items + n * q.n_tiles * row + (int64_t)strip * V * lanes + at;
@@ -339,15 +346,11 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
 #pragma unroll
         for (int v = 0; v < V; ++v) publish(items + k * row + v * lanes, item_of(s.A[v], s.H[v], s.cut >> v & 1u));
     };
-    Steps<V> past;                                              // all the steps before the tile
-    past.clear();
-    if (q.n_tiles == 1) {
-        const float *const from = BACK ? p.in : p.h0;
+    if (k == 0) {
+        if (q.n_tiles > 1) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) past.H[v] = from && c0 + v < C ? from[n * C + c0 + v] : 0.0f;
-    } else if (k == 0) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) past.H[v] = c0 + v < C ? start[v] : 0.0f;
+            for (int v = 0; v < V; ++v) past.H[v] = c0 + v < C ? start[v] : 0.0f;
+        }
     } else {
         if (tells) tell(of_tile);
         // what the tiles before publish, from the nearest ones back, until all that is known is a state
@@ -575,6 +578,12 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
         totals[wave] = make_float2(of_wave.A[0], of_wave.H[0]);
         total_cut[wave] = of_wave.cut;
     }
+    Steps<1> past;
+    past.clear();
+    if (q.n_tiles == 1) {                           // (before the barrier: the last state may be written over it, by another wave)
+        const float *const from = BACK ? p.in : p.h0;
+        past.H[0] = from ? from[n] : 0.0f;
+    }
     __syncthreads();
     Steps<1> before, all;
     before.clear();
@@ -590,14 +599,9 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
         all = o;
     }
     uint64_t *const items = q.items + n * q.n_tiles;
-    Steps<1> past;
-    past.clear();
     bool failed = false;
-    if (q.n_tiles == 1) {
-        const float *const from = BACK ? p.in : p.h0;
-        past.H[0] = from ? from[n] : 0.0f;
-    } else if (k == 0) {
-        past.H[0] = q.start[n];
+    if (k == 0) {
+        if (q.n_tiles > 1) past.H[0] = q.start[n];
     } else if (wave == 0) {
         if (lane == 0) publish(items + k, item_of(all.A[0], all.H[0], all.cut));
         for (int64_t end = k; end > 0; end -= 64) {
