@@ -52,7 +52,7 @@ int32_t rls_matrix_step(int32_t bf16, const void *a_dev, const void *b_dev, cons
                         void *stream);
 
 /* The tiles of a linear scan that is cut along time look up what the tiles before them publish; one that has waited too long for another (2 ms) goes
- * through all the steps before it by itself.  This sets the limit, in ticks of the 100 MHz clock, for the calls of the host thread that sets
+ * through all the tiles before it by itself, to the same result.  This sets the limit, in ticks of the 100 MHz clock, for the calls of the host thread that sets
  * it.  0 makes every tile do that whose first look finds something missing, for tests; a negative value restores the default. */
 int32_t rls_scan_wait_limit(int64_t ticks);
 

@@ -13,10 +13,12 @@
 // - With one channel that lies step by step, the lanes lie along time, 16 bytes of steps each.
 // - A few steps over many channels (the step of a single token): a thread per channel.
 //
-// Tiles of a sequence publish their compositions, and the state after them once they know it (a composition that is a reset); a
-// tile composes those before it, 8 to 64 at a time, back to the first that is a state.  An item is one 64-bit word that is written
+// Tiles of a sequence publish their compositions, and the state after them once they know it (a composition that is a reset); a tile
+// looks at those before it, a window of 8 to 256 at a time, back to the nearest state, and takes that state through the compositions
+// after it, one by one.  That is how each of them gets its own state, so the result does not depend on where a tile finds one (a single-pass
+// scan with look-back, Merrill and Garland 2016; they let compositions join as they come).  An item is one 64-bit word that is written
 // and read atomically and is all ones until then, so that no fence is needed (which would write the second-level cache back,
-// 100 us here).  A tile that has waited too long for another goes through all the steps before it by itself, so that no
+// 100 us here).  A tile that has waited too long for another goes through all the tiles before it by itself, in the same way, so that no
 // order in which workgroups run can hold up a call.  (Composed by a launch of their own, chunks of time had their inputs read twice:
 // 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us; now 61 and 140, the floors 42 and 104.  The backward pass of
 // 8 x 4093 x 2048 in bf16 takes 153 us, 4.4 TB/s.  A launch that clears the items first is 5 us of it, with the gap after it 10.)
@@ -100,6 +102,7 @@ constexpr int kSteps = 16, kWideSteps = 8;          // of a thread: of two bytes
 constexpr int kAlongWaves = 8, kAlongParts = 2;     // one channel: parts of 64 x 4 steps that a wave takes (4 and 4: 64 x 262144 70 us, 8 and 4: 69, 8 and 2: 61)
 constexpr int64_t kAlongTile = (int64_t)kAlongWaves * kAlongParts * 256;
 constexpr long long kPatience = 200000;             // ticks of the 100 MHz clock: 2 ms
+constexpr int kWindows = 4;                         // that a look keeps; further back it begins anew, where states have come nearer by then
 
 // How the work of a call is cut.
 struct ScanCut {
@@ -120,6 +123,13 @@ __device__ inline uint64_t item_of(float A, float H, bool cut)
 }
 __device__ inline void publish(uint64_t *at, uint64_t item) { __hip_atomic_store(at, item, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ inline uint64_t look(const uint64_t *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline bool is_state(uint64_t item) { return (uint32_t)(item >> 32) == kCut; }
+// a state after the steps of an item
+__device__ inline float through(uint64_t item, float x)
+{
+    const float H = __uint_as_float((uint32_t)item);
+    return is_state(item) ? H : fmaf(__uint_as_float((uint32_t)(item >> 32)), x, H);
+}
 
 __global__ void __launch_bounds__(256) scan_clear_kernel(ScanCut q, int64_t items, const float *from, int64_t states)
 {
@@ -215,6 +225,8 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
     constexpr int L = sizeof(T) == 4 ? kWideSteps : kSteps;
     __shared__ float2 totals[2][kWaves][kStripLanes * V];       // compositions of the waves, per channel of the strip
     __shared__ uint32_t total_cut[2][kWaves][kStripLanes];
+    __shared__ uint64_t seen[kWindows][kWaves * 64 * V];        // items of the tiles before: [n_groups][V][lanes]
+    __shared__ uint32_t states_at[2][kWaves][V];                // a bit per lane of the strip
     __shared__ int gave_up[2][kWaves];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -273,6 +285,16 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
         const int64_t left = steps - i;
         cut_in &= left >= L ? ~0u : (left > 0 ? (1u << left) - 1 : 0u);
     }
+    // one step more
+    auto append = [&](Steps<V> &s, const Raw<G, V> &gate, const Raw<T, V> &input, bool cut) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float x = gate.of(v), y = input.of(v);
+            s.H[v] = BACK ? (cut ? 0.0f : x * (y + s.H[v])) : (cut ? y : fmaf(x, s.H[v], y));
+            s.A[v] *= x;
+        }
+        if (RESET) s.cut = cut ? Steps<V>::kAll : s.cut;
+    };
     // over the groups of a wave that come before a lane's, and its own
     auto scan_wave = [&](Steps<V> &s) {
         for (int d = lanes; d < 64; d <<= 1) {
@@ -283,20 +305,17 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
             if (lane >= d) s.after(o);
         }
     };
-    int turn = 0;
-    // the compositions of the waves before this one and of all; whether any thread gave up
-    auto scan_waves = [&](const Steps<V> &s, Steps<V> &before, Steps<V> &all, bool failed) {
+    int turn = 0;                                               // (no wave reads the other half any more: one barrier a time)
+    // the compositions of the waves before this one and of all
+    auto scan_waves = [&](const Steps<V> &s, Steps<V> &before, Steps<V> &all) {
         if (lane >= 64 - lanes) {
 #pragma unroll
             for (int v = 0; v < V; ++v) totals[turn][wave][at * V + v] = make_float2(s.A[v], s.H[v]);
             total_cut[turn][wave][at] = s.cut;
         }
-        const bool any = __any(failed);
-        if (lane == 0) gave_up[turn][wave] = any;
         __syncthreads();
         before.clear();
         all.clear();
-        int bad = 0;
 #pragma unroll 2                                                // (all at once, they are 64 registers)
         for (int w = 0; w < kWaves; ++w) {
             if (w == wave) before = all;
@@ -310,34 +329,10 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
             o.cut = total_cut[turn][w][at];
             o.after(all);
             all = o;
-            bad |= gave_up[turn][w];
         }
-        turn ^= 1;                                              // (no wave reads the other half any more: one barrier a time)
-        return bad != 0;
+        turn ^= 1;
     };
 
-    Steps<V> own, waves_before, of_tile;
-    own.clear();
-#pragma unroll
-    for (int j = 0; j < L; ++j) {
-        const bool cut = RESET && (cut_in >> j & 1u);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float x = a_in[j].of(v), y = b_in[j].of(v);
-            own.H[v] = BACK ? (cut ? 0.0f : x * (y + own.H[v])) : (cut ? y : fmaf(x, own.H[v], y));
-            own.A[v] *= x;
-        }
-        if (RESET) own.cut = cut ? Steps<V>::kAll : own.cut;
-    }
-    scan_wave(own);
-    Steps<V> past;                                              // all the steps before the tile
-    past.clear();
-    if (q.n_tiles == 1) {                                       // (before the barrier: the last state may be written over it, by another wave)
-        const float *const from = BACK ? p.in : p.h0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) past.H[v] = from && c0 + v < C ? from[n * C + c0 + v] : 0.0f;
-    }
-    scan_waves(own, waves_before, of_tile, false);
     const int64_t row = (int64_t)q.strips * V * lanes;          // items of a tile of time
     uint64_t *const items = q.items + n * q.n_tiles * row + (int64_t)strip * V * lanes + at;
     const float *const start = q.start + n * C + c0;
@@ -346,60 +341,112 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
 #pragma unroll
         for (int v = 0; v < V; ++v) publish(items + k * row + v * lanes, item_of(s.A[v], s.H[v], s.cut >> v & 1u));
     };
-    if (k == 0) {
-        if (q.n_tiles > 1) {
+    // The states before the tile, from what the tiles before it publish; false if one of them is missing for too long (the same in every thread)
+    auto look_back = [&](float (&x)[V]) {
+        const uint32_t all_lanes = lanes == 32 ? ~0u : (1u << lanes) - 1;
+        uint32_t known[V];                                      // a bit per lane: a state is among what was seen
+        int64_t end = k;
+        int windows = 0;
+        for (int flip = 0;; flip ^= 1) {
+            if (windows == 0) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) past.H[v] = c0 + v < C ? start[v] : 0.0f;
-        }
-    } else {
-        if (tells) tell(of_tile);
-        // what the tiles before publish, from the nearest ones back, until all that is known is a state
-        bool failed = false;
-        for (int64_t end = k; end > 0; end -= n_groups) {
+                for (int v = 0; v < V; ++v) known[v] = 0;
+            }
             const int64_t other = end - n_groups + group;
-            Steps<V> s, unused, window;
-            s.clear();
+            uint64_t item[V];
+            bool missing = false;
+#pragma unroll
+            for (int v = 0; v < V; ++v) item[v] = item_of(1.0f, 0.0f, false);
             if (other >= 0) {
-                uint64_t x[V];
                 const long long since = wall_clock64();
-                bool missing;
                 do {
                     missing = false;
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        x[v] = look(items + other * row + v * lanes);
-                        missing |= x[v] == kEmpty;
+                        item[v] = look(items + other * row + v * lanes);
+                        missing |= item[v] == kEmpty;
                     }
                     if (missing) __builtin_amdgcn_s_sleep(4);
                 } while (missing && wall_clock64() - since < q.patience);
-                failed = missing;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const uint32_t A = (uint32_t)(x[v] >> 32);
-                    s.H[v] = __uint_as_float((uint32_t)x[v]);
-                    s.A[v] = A == kCut ? 0.0f : __uint_as_float(A);
-                    s.cut |= (A == kCut ? 1u : 0u) << v;
-                }
             }
-            scan_wave(s);
-            failed = scan_waves(s, unused, window, failed);
-            if (failed) break;                                  // (the same in every thread)
-            past.after(window);
-            if (__all(past.cut == Steps<V>::kAll)) break;       // (the lanes of a wave have all channels of the strip)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                seen[windows][(group * V + v) * lanes + at] = item[v];
+                uint64_t states = __ballot(is_state(item[v]));
+                for (int d = 32; d >= lanes; d >>= 1) states |= states >> d;
+                if (lane == 0) states_at[flip][wave][v] = (uint32_t)states & all_lanes;
+            }
+            const bool any = __any(missing);
+            if (lane == 0) gave_up[flip][wave] = any;
+            __syncthreads();
+            bool all_known = true;
+            int failed = 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) known[v] |= (uint32_t)__builtin_amdgcn_readfirstlane((int)states_at[flip][w][v]);
+                all_known &= known[v] == all_lanes;
+            }
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) failed |= gave_up[flip][w];
+            if (failed) return false;
+            ++windows;
+            if (all_known) break;                               // (tile 0 publishes nothing but its state)
+            end -= n_groups;
+            if (windows == kWindows) {
+                windows = 0;
+                end = k;
+                __builtin_amdgcn_s_sleep(16);
+            }
         }
-        if (failed) {                                           // step by step, every thread for its channels
 #pragma unroll
-            for (int v = 0; v < V; ++v) past.H[v] = c0 + v < C ? start[v] : 0.0f;
-            for (int64_t j = 0; j < i_begin; ++j) {
-                const int64_t t = step_of(j);
-                const Pack<G, V> g = read_pack<G, V>(a + t * p.a.step_stride);
-                const Pack<T, V> e = read_pack<T, V>(b + t * p.b.step_stride);
-                const bool cut = RESET && reset[t] != 0;
+        for (int v = 0; v < V; ++v) x[v] = 0.0f;                // (a state takes its place)
+        for (int w = windows - 1; w >= 0; --w) {
+            const uint64_t *const of_window = &seen[w][at];
+#pragma unroll 4
+            for (int g = 0; g < n_groups; ++g) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float x = (float)g.x[v], y = (float)e.x[v];
-                    past.H[v] = BACK ? (cut ? 0.0f : x * (y + past.H[v])) : (cut ? y : fmaf(x, past.H[v], y));
+                for (int v = 0; v < V; ++v) x[v] = through(of_window[(g * V + v) * lanes], x[v]);
+            }
+        }
+        return true;
+    };
+
+    Steps<V> own, waves_before, of_tile;
+    float past[V];                                              // the states before the tile
+#pragma unroll
+    for (int v = 0; v < V; ++v) past[v] = 0.0f;
+    if (k == 0) {                                               // (before any barrier: the last state may be written over it, by another wave)
+        const float *const from = q.n_tiles > 1 ? q.start : (BACK ? p.in : p.h0);
+#pragma unroll
+        for (int v = 0; v < V; ++v) past[v] = from && c0 + v < C ? from[n * C + c0 + v] : 0.0f;
+    }
+    own.clear();
+#pragma unroll
+    for (int j = 0; j < L; ++j) append(own, a_in[j], b_in[j], RESET && (cut_in >> j & 1u));
+    scan_wave(own);
+    scan_waves(own, waves_before, of_tile);
+    if (k > 0) {
+        if (tells) tell(of_tile);
+        if (!look_back(past)) {                                 // through all the tiles before, all of the workgroup together
+#pragma unroll
+            for (int v = 0; v < V; ++v) past[v] = c0 + v < C ? start[v] : 0.0f;
+            for (int64_t j0 = (int64_t)group * L; j0 < i_begin; j0 += tile) {
+                Steps<V> s, unused, other;
+                s.clear();
+#pragma unroll 2
+                for (int j = 0; j < L; ++j) {
+                    const int64_t t = step_of(j0 + j);
+                    Raw<G, V> gate;
+                    Raw<T, V> input;
+                    gate.read(a + t * p.a.step_stride);
+                    input.read(b + t * p.b.step_stride);
+                    append(s, gate, input, RESET && reset[t] != 0);
                 }
+                scan_wave(s);
+                scan_waves(s, unused, other);
+#pragma unroll
+                for (int v = 0; v < V; ++v) past[v] = other.of(v, past[v]);
             }
         }
     }
@@ -413,8 +460,8 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
         if (lane < lanes) o.clear();
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            of_tile.H[v] = of_tile.of(v, past.H[v]);
-            x[v] = o.of(v, waves_before.of(v, past.H[v]));
+            of_tile.H[v] = of_tile.of(v, past[v]);
+            x[v] = o.of(v, waves_before.of(v, past[v]));
         }
         of_tile.cut = Steps<V>::kAll;
     }
@@ -479,13 +526,13 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
     constexpr int P = kAlongParts, L = 4;
     __shared__ float2 totals[kAlongWaves];
     __shared__ int total_cut[kAlongWaves];
-    __shared__ Steps<1> past_lds;
+    __shared__ uint64_t seen[kWindows][64];         // items of the tiles before (the first wave's)
+    __shared__ float found;
+    __shared__ bool gave_up;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n = blockIdx.x % p.batch, k = blockIdx.x / p.batch, steps = p.steps;
     const bool down = BACK ? !p.reverse : p.reverse != 0;
-    const int64_t i_begin = k * kAlongTile, i0 = i_begin + (wave * P * 64 + lane) * L;       // part u begins 64 * L further on
-    const bool whole = i_begin + kAlongTile < steps;
     const G *const a = static_cast<const G *>(p.a.data_dev) + n * p.a.batch_stride;
     const T *const b = static_cast<const T *>(p.b.data_dev) + n * p.b.batch_stride;
     const T *const h = static_cast<const T *>(p.h.data_dev) + n * p.h.batch_stride;
@@ -505,28 +552,6 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
     };
     float a_in[P][L], b_in[P][L], h_in[BACK ? P : 1][L];
     uint32_t cut_in[P];
-#pragma unroll
-    for (int u = 0; u < P; ++u) {
-        const int64_t from = i0 + u * 64 * L;
-        four(a, from, a_in[u]);
-        four(b, from, b_in[u]);
-        cut_in[u] = 0;
-        if constexpr (RESET) {
-            float r[L];
-            four(reset, from, r);
-#pragma unroll
-            for (int j = 0; j < L; ++j) cut_in[u] |= (r[j] != 0.0f ? 1u : 0u) << j;
-        }
-        if (!whole) {                               // steps after the last one change nothing
-#pragma unroll
-            for (int j = 0; j < L; ++j) {
-                a_in[u][j] = from + j < steps ? a_in[u][j] : 1.0f;
-                b_in[u][j] = from + j < steps ? b_in[u][j] : 0.0f;
-            }
-            const int64_t left = steps - from;
-            cut_in[u] &= left >= L ? ~0u : (left > 0 ? (1u << left) - 1 : 0u);
-        }
-    }
     auto compose = [&](int u, Steps<1> &s) {
         s.clear();
 #pragma unroll
@@ -563,101 +588,135 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
         o.cut = last_lane(s.cut);
         return o;
     };
-    Steps<1> own[P], of_wave;                       // per part: the wave's steps up to the lane's
-    of_wave.clear();
-#pragma unroll
-    for (int u = 0; u < P; ++u) {
-        compose(u, own[u]);
-        scan_lanes(own[u]);
-        Steps<1> part = of_last_lane(own[u]);
-        own[u].after(of_wave);
-        part.after(of_wave);
-        of_wave = part;
-    }
-    if (lane == 0) {
-        totals[wave] = make_float2(of_wave.A[0], of_wave.H[0]);
-        total_cut[wave] = of_wave.cut;
-    }
-    Steps<1> past;
-    past.clear();
-    if (q.n_tiles == 1) {                           // (before the barrier: the last state may be written over it, by another wave)
-        const float *const from = BACK ? p.in : p.h0;
-        past.H[0] = from ? from[n] : 0.0f;
-    }
-    __syncthreads();
-    Steps<1> before, all;
-    before.clear();
-    all.clear();
-#pragma unroll
-    for (int w = 0; w < kAlongWaves; ++w) {
-        if (w == wave) before = all;
-        Steps<1> o;
-        o.A[0] = totals[w].x;
-        o.H[0] = totals[w].y;
-        o.cut = total_cut[w];
-        o.after(all);
-        all = o;
-    }
     uint64_t *const items = q.items + n * q.n_tiles;
-    bool failed = false;
-    if (k == 0) {
-        if (q.n_tiles > 1) past.H[0] = q.start[n];
-    } else if (wave == 0) {
-        if (lane == 0) publish(items + k, item_of(all.A[0], all.H[0], all.cut));
-        for (int64_t end = k; end > 0; end -= 64) {
+    // The state before the tile, from what the tiles before it publish (by one wave); false if one of them is missing for too long
+    auto look_back = [&](float &x) {
+        int64_t end = k;
+        int windows = 0, first;
+        for (;;) {
             const int64_t other = end - 64 + lane;
-            Steps<1> s;
-            s.clear();
+            uint64_t item = item_of(1.0f, 0.0f, false);
+            bool missing = false;
             if (other >= 0) {
                 const long long since = wall_clock64();
-                uint64_t x;
                 do {
-                    x = look(items + other);
-                    if (x == kEmpty) __builtin_amdgcn_s_sleep(4);
-                } while (x == kEmpty && wall_clock64() - since < q.patience);
-                failed = x == kEmpty;
-                const uint32_t A = (uint32_t)(x >> 32);
-                s.H[0] = __uint_as_float((uint32_t)x);
-                s.A[0] = A == kCut ? 0.0f : __uint_as_float(A);
-                s.cut = A == kCut ? 1u : 0u;
+                    item = look(items + other);
+                    missing = item == kEmpty;
+                    if (missing) __builtin_amdgcn_s_sleep(4);
+                } while (missing && wall_clock64() - since < q.patience);
             }
-            failed = __any(failed);
-            if (failed) break;
-            // (item by item the steps may be cut here, also without resets: a state)
-            for (int d = 1; d < 64; d <<= 1) {
-                Steps<1> o;
-                o.A[0] = __shfl_up(s.A[0], d, 64);
-                o.H[0] = __shfl_up(s.H[0], d, 64);
-                o.cut = __shfl_up(s.cut, d, 64);
-                if (lane >= d) s.after(o);
+            if (__any(missing)) return false;
+            seen[windows++][lane] = item;
+            const uint64_t states = __ballot(is_state(item));
+            if (states != 0) {                      // (tile 0 publishes nothing but its state)
+                first = 63 - __clzll((long long)states);
+                break;
             }
-            past.after(of_last_lane(s));
-            if (past.cut) break;
+            end -= 64;
+            if (windows == kWindows) {
+                windows = 0;
+                end = k;
+                __builtin_amdgcn_s_sleep(16);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();            // (a wave's accesses to LDS stay in their order)
+        x = 0.0f;                                   // (a state takes its place)
+        for (int w = windows - 1; w >= 0; --w, first = 0) {
+#pragma unroll 4
+            for (int l = first; l < 64; ++l) x = through(seen[w][l], x);
+        }
+        return true;
+    };
+    Steps<1> own[P], before, all;                   // per part: the wave's steps up to the lane's; the waves before; the tile
+    float past = 0.0f;                              // the state before the tile
+    if (k == 0) {                                   // (before any barrier: the last state may be written over it, by another wave)
+        const float *const from = q.n_tiles > 1 ? q.start : (BACK ? p.in : p.h0);
+        past = from ? from[n] : 0.0f;
+    }
+    int64_t i0;                                     // the lane's first position; part u begins 64 * L further on
+    bool known = k == 0;
+    // once, or through all the tiles before the own one first
+    for (int64_t here = k;;) {
+        const int64_t i_begin = here * kAlongTile;
+        const bool whole = i_begin + kAlongTile < steps;
+        i0 = i_begin + (wave * P * 64 + lane) * L;
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            const int64_t from = i0 + u * 64 * L;
+            four(a, from, a_in[u]);
+            four(b, from, b_in[u]);
+            cut_in[u] = 0;
+            if constexpr (RESET) {
+                float r[L];
+                four(reset, from, r);
+#pragma unroll
+                for (int j = 0; j < L; ++j) cut_in[u] |= (r[j] != 0.0f ? 1u : 0u) << j;
+            }
+            if (!whole) {                           // steps after the last one change nothing
+#pragma unroll
+                for (int j = 0; j < L; ++j) {
+                    a_in[u][j] = from + j < steps ? a_in[u][j] : 1.0f;
+                    b_in[u][j] = from + j < steps ? b_in[u][j] : 0.0f;
+                }
+                const int64_t left = steps - from;
+                cut_in[u] &= left >= L ? ~0u : (left > 0 ? (1u << left) - 1 : 0u);
+            }
+        }
+        Steps<1> of_wave;
+        of_wave.clear();
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            compose(u, own[u]);
+            scan_lanes(own[u]);
+            Steps<1> part = of_last_lane(own[u]);
+            own[u].after(of_wave);
+            part.after(of_wave);
+            of_wave = part;
         }
         if (lane == 0) {
-            past.cut = failed ? 2u : past.cut;
-            past_lds = past;
+            totals[wave] = make_float2(of_wave.A[0], of_wave.H[0]);
+            total_cut[wave] = of_wave.cut;
         }
-    }
-    if (k > 0) {
         __syncthreads();
-        past = past_lds;
-        if (past.cut == 2u) {                       // (the same in every thread) step by step
-            past.H[0] = q.start[n];
-            for (int64_t j = 0; j < i_begin; ++j) {
-                const int64_t t = step_of(j);
-                const bool cut = RESET && reset[t] != 0;
-                const float x = (float)a[t], y = (float)b[t];
-                past.H[0] = BACK ? (cut ? 0.0f : x * (y + past.H[0])) : (cut ? y : fmaf(x, past.H[0], y));
+        before.clear();
+        all.clear();
+#pragma unroll
+        for (int w = 0; w < kAlongWaves; ++w) {
+            if (w == wave) before = all;
+            Steps<1> o;
+            o.A[0] = totals[w].x;
+            o.H[0] = totals[w].y;
+            o.cut = total_cut[w];
+            o.after(all);
+            all = o;
+        }
+        if (here == k && known) break;
+        if (here == k && wave == 0) {
+            if (lane == 0) publish(items + k, item_of(all.A[0], all.H[0], all.cut));
+            float x = 0.0f;
+            const bool there = look_back(x);
+            if (lane == 0) {
+                found = x;
+                gave_up = !there;
             }
+        }
+        __syncthreads();                            // (nor are the totals read any more)
+        if (here < k) {
+            past = all.of(0, past);
+            known = ++here == k;
+        } else {
+            past = found;
+            if (!gave_up) break;                    // (the same in every thread)
+            here = 0;
+            past = q.start[n];
         }
     }
     if constexpr (BACK) {
 #pragma unroll
         for (int u = 0; u < P; ++u) four(h, i0 + u * 64 * L + 1, h_in[u]);
     }
-    if (threadIdx.x == 0 && k + 1 < q.n_tiles) publish(items + k, item_of(0.0f, all.of(0, past.H[0]), true));
-    const float of_waves = before.of(0, past.H[0]);
+    if (threadIdx.x == 0 && k + 1 < q.n_tiles) publish(items + k, item_of(0.0f, all.of(0, past), true));
+    const float of_waves = before.of(0, past);
     G *const da = BACK ? static_cast<G *>(p.da.data_dev) + n * p.da.batch_stride : nullptr;
     T *const to = BACK ? static_cast<T *>(p.db.data_dev) + n * p.db.batch_stride : static_cast<T *>(p.h.data_dev) + n * p.h.batch_stride;
     Steps<1> parts_before;                          // of the wave
