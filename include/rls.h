@@ -345,6 +345,9 @@ typedef struct {
  *   h           (written) every state, rounded to `type`;  h_last_dev [batch][channels] fp32 (written) or null, the state
  *               after the last step in fp32; it may be h0_dev's memory: with steps = 1 the step of a single token
  * steps = 0 leaves h alone and copies h0 (or 0) to h_last.
+ * Gates may be anything: long sequences are cut into tiles that are composed, but where a product of gates, or what is added up under it, passes the
+ * largest number the steps are taken one by one.  From a state that is not finite on, up to the next reset, no state is finite
+ * (infinities and NaN are not told apart); a term smaller than 2^-126 times the state that it comes from may be left out.
  */
 int64_t rls_linear_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels);
 int32_t rls_linear_scan(const rls_scan_shape *shape, const rls_sequence *a, const rls_sequence *b, const float *h0_dev,

@@ -19,7 +19,11 @@
 // scan with look-back, Merrill and Garland 2016; they let compositions join as they come).  An item is one 64-bit word that is written
 // and read atomically and is all ones until then, so that no fence is needed (which would write the second-level cache back,
 // 100 us here).  A tile that has waited too long for another goes through all the tiles before it by itself, in the same way, so that no
-// order in which workgroups run can hold up a call.  (Composed by a launch of their own, chunks of time had their inputs read twice:
+// order in which workgroups run can hold up a call.
+//
+// Products of gates above 1, and what is added up under them, can pass the largest number where the states themselves do not (gates of 4
+// over a state of 0), or be no number.  A composition of that kind is not used: the tile's steps are taken one by one from the
+// state before it, thread after thread, and the tile publishes that a state will follow and nothing else.  (Composed by a launch of their own, chunks of time had their inputs read twice:
 // 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us; now 61 and 140, the floors 42 and 104.  The backward pass of
 // 8 x 4093 x 2048 in bf16 takes 153 us, 4.4 TB/s.  A launch that clears the items first is 5 us of it, with the gap after it 10.)
 #include <algorithm>
@@ -113,22 +117,28 @@ struct ScanCut {
     long long patience;
 };
 
-// An item: A in the high half, H in the low one.  A state, or a composition that no state goes through, has kCut for A.
+// An item: A in the high half, H in the low one.  A state, or a composition that no state goes through, has kCut for A; kLater says that there is
+// no composition, but that a state will follow.
 constexpr uint64_t kEmpty = ~0ull;
-constexpr uint32_t kCut = 0xfffffffeu;
+constexpr uint32_t kNone = 0xffffffffu, kLater = 0xfffffffeu, kCut = 0xfffffffdu;
+__device__ inline uint32_t gate_of(uint64_t item) { return (uint32_t)(item >> 32); }
+__device__ inline bool is_state(uint64_t item) { return gate_of(item) == kCut; }
+__device__ inline uint64_t state_item(float H) { return (uint64_t)kCut << 32 | __float_as_uint(H); }
+__device__ inline bool finite(float x) { return fabsf(x) < INFINITY; }
 __device__ inline uint64_t item_of(float A, float H, bool cut)
 {
-    const uint32_t a = cut ? kCut : (A == A ? __float_as_uint(A) : 0x7fc00000u);
+    const uint32_t a = fabsf(H) + (cut ? 0.0f : fabsf(A)) < INFINITY ? (cut ? kCut : __float_as_uint(A)) : kLater;
     return (uint64_t)a << 32 | __float_as_uint(H);
 }
+// whether a state that compositions give has been lost on the way: it is not finite, and no state before them is to blame
+__device__ inline bool lost(float x, float past, bool cut) { return !finite(x) && (cut || finite(past)); }
 __device__ inline void publish(uint64_t *at, uint64_t item) { __hip_atomic_store(at, item, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ inline uint64_t look(const uint64_t *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ inline bool is_state(uint64_t item) { return (uint32_t)(item >> 32) == kCut; }
 // a state after the steps of an item
 __device__ inline float through(uint64_t item, float x)
 {
     const float H = __uint_as_float((uint32_t)item);
-    return is_state(item) ? H : fmaf(__uint_as_float((uint32_t)(item >> 32)), x, H);
+    return is_state(item) ? H : fmaf(__uint_as_float(gate_of(item)), x, H);
 }
 
 __global__ void __launch_bounds__(256) scan_clear_kernel(ScanCut q, int64_t items, const float *from, int64_t states)
@@ -193,8 +203,8 @@ struct Raw {
     }
 };
 
-// A composition of steps per channel; bit v of `cut`: no state goes through channel v's.
-template <int V>
+// A composition of steps per channel; bit v of `cut`: no state goes through channel v's (nowhere, without resets).
+template <int V, bool RESET>
 struct Steps {
     float A[V], H[V];
     uint32_t cut;
@@ -205,7 +215,16 @@ struct Steps {
         for (int v = 0; v < V; ++v) { A[v] = 1.0f; H[v] = 0.0f; }
         cut = 0;
     }
-    __device__ inline float of(int v, float x) const { return cut >> v & 1u ? H[v] : fmaf(A[v], x, H[v]); }
+    __device__ inline bool is_cut(int v) const { return RESET && (cut >> v & 1u); }
+    __device__ inline float of(int v, float x) const { return is_cut(v) ? H[v] : fmaf(A[v], x, H[v]); }
+    // not finite (or next to the largest number) where an A or H is not
+    __device__ inline float size() const
+    {
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum += fabsf(A[v]) + fabsf(H[v]);
+        return sum;
+    }
     // these steps after others
     __device__ inline void after(const Steps &o)
     {
@@ -214,20 +233,21 @@ struct Steps {
             H[v] = of(v, o.H[v]);
             A[v] *= o.A[v];
         }
-        cut |= o.cut;
+        if (RESET) cut |= o.cut;
     }
 };
 
 // V channels x kSteps or kWideSteps steps per thread.  Positions i count in the direction of the recurrence, position i is step t = i or steps - 1 - i.
 template <typename T, typename G, int V, bool BACK, bool RESET>
-__global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, ScanCut q)
+__global__ void __launch_bounds__(64 * kWaves, 2) scan_strip_kernel(ScanArgs p, ScanCut q)
 {
     constexpr int L = sizeof(T) == 4 ? kWideSteps : kSteps;
     __shared__ float2 totals[2][kWaves][kStripLanes * V];       // compositions of the waves, per channel of the strip
     __shared__ uint32_t total_cut[2][kWaves][kStripLanes];
     __shared__ uint64_t seen[kWindows][kWaves * 64 * V];        // items of the tiles before: [n_groups][V][lanes]
     __shared__ uint32_t states_at[2][kWaves][V];                // a bit per lane of the strip
-    __shared__ int gave_up[2][kWaves];
+    __shared__ int gave_up[2][kWaves], large[2][kWaves];
+    __shared__ float chain[kStripLanes * V];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lanes = q.lanes, groups = 64 / lanes;             // of a wave, along time
@@ -286,61 +306,70 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
         cut_in &= left >= L ? ~0u : (left > 0 ? (1u << left) - 1 : 0u);
     }
     // one step more
-    auto append = [&](Steps<V> &s, const Raw<G, V> &gate, const Raw<T, V> &input, bool cut) {
+    auto append = [&](Steps<V, RESET> &s, const Raw<G, V> &gate, const Raw<T, V> &input, bool cut) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float x = gate.of(v), y = input.of(v);
             s.H[v] = BACK ? (cut ? 0.0f : x * (y + s.H[v])) : (cut ? y : fmaf(x, s.H[v], y));
             s.A[v] *= x;
         }
-        if (RESET) s.cut = cut ? Steps<V>::kAll : s.cut;
+        if (RESET) s.cut = cut ? Steps<V, RESET>::kAll : s.cut;
     };
     // over the groups of a wave that come before a lane's, and its own
-    auto scan_wave = [&](Steps<V> &s) {
+    auto scan_wave = [&](Steps<V, RESET> &s) {
         for (int d = lanes; d < 64; d <<= 1) {
-            Steps<V> o;
+            Steps<V, RESET> o;
 #pragma unroll
             for (int v = 0; v < V; ++v) { o.A[v] = __shfl_up(s.A[v], d, 64); o.H[v] = __shfl_up(s.H[v], d, 64); }
-            o.cut = __shfl_up(s.cut, d, 64);
+            o.cut = RESET ? __shfl_up(s.cut, d, 64) : 0u;
             if (lane >= d) s.after(o);
         }
     };
     int turn = 0;                                               // (no wave reads the other half any more: one barrier a time)
-    // the compositions of the waves before this one and of all
-    auto scan_waves = [&](const Steps<V> &s, Steps<V> &before, Steps<V> &all) {
+    // The compositions of the waves before this one and of all; whether any composition on the way cannot be used (the same in every thread: every wave
+    // has all channels of the strip).  Without resets what is not finite stays so, and is seen at the end.
+    auto scan_waves = [&](const Steps<V, RESET> &s, Steps<V, RESET> &before, Steps<V, RESET> &all) {
+        if constexpr (RESET) {
+            const bool any = __any(!(s.size() < INFINITY));
+            if (lane == 0) large[turn][wave] = any;
+        }
         if (lane >= 64 - lanes) {
 #pragma unroll
             for (int v = 0; v < V; ++v) totals[turn][wave][at * V + v] = make_float2(s.A[v], s.H[v]);
-            total_cut[turn][wave][at] = s.cut;
+            if (RESET) total_cut[turn][wave][at] = s.cut;
         }
         __syncthreads();
         before.clear();
         all.clear();
+        float size = 0.0f;
+        int odd = 0;
 #pragma unroll 2                                                // (all at once, they are 64 registers)
         for (int w = 0; w < kWaves; ++w) {
             if (w == wave) before = all;
-            Steps<V> o;
+            Steps<V, RESET> o;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float2 x = totals[turn][w][at * V + v];
                 o.A[v] = x.x;
                 o.H[v] = x.y;
             }
-            o.cut = total_cut[turn][w][at];
+            o.cut = RESET ? total_cut[turn][w][at] : 0u;
             o.after(all);
             all = o;
+            if constexpr (RESET) {
+                size += all.size();
+                odd |= large[turn][w];
+            }
         }
+        if (!RESET) size = all.size();
         turn ^= 1;
+        return odd != 0 || __any(!(size < INFINITY)) != 0;
     };
 
     const int64_t row = (int64_t)q.strips * V * lanes;          // items of a tile of time
     uint64_t *const items = q.items + n * q.n_tiles * row + (int64_t)strip * V * lanes + at;
     const float *const start = q.start + n * C + c0;
     const bool tells = group == 0 && k + 1 < q.n_tiles;
-    auto tell = [&](const Steps<V> &s) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) publish(items + k * row + v * lanes, item_of(s.A[v], s.H[v], s.cut >> v & 1u));
-    };
     // The states before the tile, from what the tiles before it publish; false if one of them is missing for too long (the same in every thread)
     auto look_back = [&](float (&x)[V]) {
         const uint32_t all_lanes = lanes == 32 ? ~0u : (1u << lanes) - 1;
@@ -359,15 +388,18 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
             for (int v = 0; v < V; ++v) item[v] = item_of(1.0f, 0.0f, false);
             if (other >= 0) {
                 const long long since = wall_clock64();
-                do {
-                    missing = false;
+                for (;;) {
+                    uint32_t most = 0;
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
                         item[v] = look(items + other * row + v * lanes);
-                        missing |= item[v] == kEmpty;
+                        most = max(most, gate_of(item[v]));
                     }
-                    if (missing) __builtin_amdgcn_s_sleep(4);
-                } while (missing && wall_clock64() - since < q.patience);
+                    missing = most == kNone;
+                    // (a tile that says "later" is running: for it there is no limit)
+                    if (most < kLater || (missing && wall_clock64() - since >= q.patience)) break;
+                    __builtin_amdgcn_s_sleep(4);
+                }
             }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -409,10 +441,54 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
                 for (int v = 0; v < V; ++v) x[v] = through(of_window[(g * V + v) * lanes], x[v]);
             }
         }
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum += fabsf(x[v]);
+        bool good = sum < INFINITY;
+        while (__builtin_expect(!good, 0)) {                                         // the state that the tile before has (it is running, as all are that published something)
+            good = true;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const uint64_t item = look(items + (k - 1) * row + v * lanes);
+                x[v] = __uint_as_float((uint32_t)item);
+                good &= is_state(item);
+            }
+            if (!good) __builtin_amdgcn_s_sleep(4);
+        }
         return true;
     };
+    // The states before each thread and after the tile, step by step, from position `first` of the thread on.  (All of the workgroup together.  Rare, so
+    // the rows are read again: kept for this as well they are registers of every call.)
+    auto one_by_one = [&](const float (&from)[V], int64_t first, float (&x)[V], float (&end)[V]) {
+        for (int g = 0; g < n_groups; ++g) {
+            __syncthreads();
+            if (group != g) continue;
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = end[v] = g == 0 ? from[v] : chain[at * V + v];
+#pragma unroll 1
+            for (int j = 0; j < L; ++j) {
+                if (first + j >= steps) break;
+                const int64_t t = step_of(first + j);
+                Raw<G, V> gate;
+                Raw<T, V> input;
+                gate.read(a + t * p.a.step_stride);
+                input.read(b + t * p.b.step_stride);
+                const bool cut = RESET && reset[t] != 0;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float e = gate.of(v), y = input.of(v);
+                    end[v] = BACK ? (cut ? 0.0f : e * (y + end[v])) : (cut ? y : fmaf(e, end[v], y));
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) chain[at * V + v] = end[v];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < V; ++v) end[v] = chain[at * V + v];
+    };
 
-    Steps<V> own, waves_before, of_tile;
+    Steps<V, RESET> own, waves_before, of_tile;
     float past[V];                                              // the states before the tile
 #pragma unroll
     for (int v = 0; v < V; ++v) past[v] = 0.0f;
@@ -425,14 +501,17 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
 #pragma unroll
     for (int j = 0; j < L; ++j) append(own, a_in[j], b_in[j], RESET && (cut_in >> j & 1u));
     scan_wave(own);
-    scan_waves(own, waves_before, of_tile);
+    const bool odd = scan_waves(own, waves_before, of_tile);
     if (k > 0) {
-        if (tells) tell(of_tile);
-        if (!look_back(past)) {                                 // through all the tiles before, all of the workgroup together
+        if (tells) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) publish(items + k * row + v * lanes, item_of(of_tile.A[v], of_tile.H[v], of_tile.is_cut(v)));
+        }
+        if (__builtin_expect(!look_back(past), 0)) {                                 // through all the tiles before, all of the workgroup together
 #pragma unroll
             for (int v = 0; v < V; ++v) past[v] = c0 + v < C ? start[v] : 0.0f;
             for (int64_t j0 = (int64_t)group * L; j0 < i_begin; j0 += tile) {
-                Steps<V> s, unused, other;
+                Steps<V, RESET> s, unused, other;
                 s.clear();
 #pragma unroll 2
                 for (int j = 0; j < L; ++j) {
@@ -444,28 +523,41 @@ __global__ void __launch_bounds__(64 * kWaves) scan_strip_kernel(ScanArgs p, Sca
                     append(s, gate, input, RESET && reset[t] != 0);
                 }
                 scan_wave(s);
-                scan_waves(s, unused, other);
+                float x[V], end[V];
+                const bool strange = scan_waves(s, unused, other);
+                if (strange)
+                    one_by_one(past, j0, x, end);
 #pragma unroll
-                for (int v = 0; v < V; ++v) past[v] = other.of(v, past[v]);
+                for (int v = 0; v < V; ++v) {
+                    const float then = other.of(v, past[v]);
+                    past[v] = strange && lost(then, past[v], other.is_cut(v)) ? end[v] : then;
+                }
             }
         }
     }
-    if constexpr (BACK) rows_of(static_cast<const T *>(h), p.h.step_stride, i + 1, h_in);
-    float x[V];                                                 // the state before the thread's steps
-    {
-        Steps<V> o;
 #pragma unroll
-        for (int v = 0; v < V; ++v) { o.A[v] = __shfl_up(own.A[v], lanes, 64); o.H[v] = __shfl_up(own.H[v], lanes, 64); }
-        o.cut = __shfl_up(own.cut, lanes, 64);
-        if (lane < lanes) o.clear();
+    for (int v = 0; v < V; ++v) {
+        const float then = of_tile.of(v, past[v]);
+        if (tells && !(odd && lost(then, past[v], of_tile.is_cut(v)))) publish(items + k * row + v * lanes, state_item(then));
+    }
+    float x[V];                                                 // the state before the thread's steps
+    Steps<V, RESET> before;
+#pragma unroll
+    for (int v = 0; v < V; ++v) { before.A[v] = __shfl_up(own.A[v], lanes, 64); before.H[v] = __shfl_up(own.H[v], lanes, 64); }
+    before.cut = RESET ? __shfl_up(own.cut, lanes, 64) : 0u;
+    if (lane < lanes) before.clear();
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] = before.of(v, waves_before.of(v, past[v]));
+    if (__builtin_expect(odd, 0)) {
+        float y[V], end[V];
+        one_by_one(past, i, y, end);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            of_tile.H[v] = of_tile.of(v, past[v]);
-            x[v] = o.of(v, waves_before.of(v, past[v]));
+            if (tells && lost(of_tile.of(v, past[v]), past[v], of_tile.is_cut(v))) publish(items + k * row + v * lanes, state_item(end[v]));
+            x[v] = lost(x[v], past[v], before.is_cut(v) || waves_before.is_cut(v)) ? y[v] : x[v];
         }
-        of_tile.cut = Steps<V>::kAll;
     }
-    if (tells) tell(of_tile);
+    if constexpr (BACK) rows_of(static_cast<const T *>(h), p.h.step_stride, i + 1, h_in);
     G *const da = BACK ? static_cast<G *>(p.da.data_dev) + n * p.da.batch_stride + c0 : nullptr;
     T *const to = (BACK ? static_cast<T *>(p.db.data_dev) + n * p.db.batch_stride : static_cast<T *>(p.h.data_dev) + n * p.h.batch_stride) + c0;
     const int64_t first = step_of(i), next = down ? -1 : 1;
@@ -527,8 +619,9 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
     __shared__ float2 totals[kAlongWaves];
     __shared__ int total_cut[kAlongWaves];
     __shared__ uint64_t seen[kWindows][64];         // items of the tiles before (the first wave's)
-    __shared__ float found;
+    __shared__ float found, chain;
     __shared__ bool gave_up;
+    __shared__ int large[kAlongWaves];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t n = blockIdx.x % p.batch, k = blockIdx.x / p.batch, steps = p.steps;
@@ -552,7 +645,7 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
     };
     float a_in[P][L], b_in[P][L], h_in[BACK ? P : 1][L];
     uint32_t cut_in[P];
-    auto compose = [&](int u, Steps<1> &s) {
+    auto compose = [&](int u, Steps<1, RESET> &s) {
         s.clear();
 #pragma unroll
         for (int j = 0; j < L; ++j) {
@@ -564,10 +657,10 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
         }
     };
     // over the lanes before, and the lane's own
-    auto scan_lanes = [&](Steps<1> &s) {
+    auto scan_lanes = [&](Steps<1, RESET> &s) {
         auto move = [&](auto ctrl, auto rows) {
             constexpr int c = decltype(ctrl)::value, m = decltype(rows)::value;
-            Steps<1> o;
+            Steps<1, RESET> o;
             o.A[0] = lane_move<c, m>(1.0f, s.A[0]);
             o.H[0] = lane_move<c, m>(0.0f, s.H[0]);
             o.cut = RESET ? lane_move<c, m>(0u, s.cut) : 0u;
@@ -581,8 +674,8 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
         move(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());
         move(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());
     };
-    auto of_last_lane = [&](const Steps<1> &s) {
-        Steps<1> o;
+    auto of_last_lane = [&](const Steps<1, RESET> &s) {
+        Steps<1, RESET> o;
         o.A[0] = last_lane(s.A[0]);
         o.H[0] = last_lane(s.H[0]);
         o.cut = last_lane(s.cut);
@@ -599,11 +692,13 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
             bool missing = false;
             if (other >= 0) {
                 const long long since = wall_clock64();
-                do {
+                for (;;) {
                     item = look(items + other);
-                    missing = item == kEmpty;
-                    if (missing) __builtin_amdgcn_s_sleep(4);
-                } while (missing && wall_clock64() - since < q.patience);
+                    missing = gate_of(item) == kNone;
+                    // (a tile that says "later" is running: for it there is no limit)
+                    if (gate_of(item) < kLater || (missing && wall_clock64() - since >= q.patience)) break;
+                    __builtin_amdgcn_s_sleep(4);
+                }
             }
             if (__any(missing)) return false;
             seen[windows++][lane] = item;
@@ -625,16 +720,46 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
 #pragma unroll 4
             for (int l = first; l < 64; ++l) x = through(seen[w][l], x);
         }
+        while (__builtin_expect(!finite(x), 0)) {                        // the state that the tile before has (it is running, as all are that published something)
+            const uint64_t item = look(items + k - 1);
+            x = __uint_as_float((uint32_t)item);
+            if (is_state(item)) break;
+            x = INFINITY;
+            __builtin_amdgcn_s_sleep(4);
+        }
         return true;
     };
-    Steps<1> own[P], before, all;                   // per part: the wave's steps up to the lane's; the waves before; the tile
+    // The states before a lane's steps of each part, and after the tile, step by step: lane after lane.  (All of the workgroup together.)
+    auto one_by_one = [&](float from, float (&x)[P]) {
+        for (int w = 0; w < kAlongWaves; ++w) {
+            __syncthreads();
+            if (wave != w) continue;
+            float y = w == 0 ? from : chain;
+#pragma unroll
+            for (int u = 0; u < P; ++u)
+                for (int l = 0; l < 64; ++l) {
+                    x[u] = lane == l ? y : x[u];
+                    float z = y;
+#pragma unroll
+                    for (int j = 0; j < L; ++j) {
+                        const bool cut = RESET && (cut_in[u] >> j & 1u);
+                        z = BACK ? (cut ? 0.0f : a_in[u][j] * (b_in[u][j] + z)) : (cut ? b_in[u][j] : fmaf(a_in[u][j], z, b_in[u][j]));
+                    }
+                    y = __shfl(z, l, 64);
+                }
+            if (lane == 0) chain = y;
+        }
+        __syncthreads();
+        return chain;
+    };
+    Steps<1, RESET> own[P], before, all;                   // per part: the wave's steps up to the lane's; the waves before; the tile
     float past = 0.0f;                              // the state before the tile
     if (k == 0) {                                   // (before any barrier: the last state may be written over it, by another wave)
         const float *const from = q.n_tiles > 1 ? q.start : (BACK ? p.in : p.h0);
         past = from ? from[n] : 0.0f;
     }
     int64_t i0;                                     // the lane's first position; part u begins 64 * L further on
-    bool known = k == 0;
+    bool known = k == 0, odd;
     // once, or through all the tiles before the own one first
     for (int64_t here = k;;) {
         const int64_t i_begin = here * kAlongTile;
@@ -662,16 +787,23 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
                 cut_in[u] &= left >= L ? ~0u : (left > 0 ? (1u << left) - 1 : 0u);
             }
         }
-        Steps<1> of_wave;
+        Steps<1, RESET> of_wave;
         of_wave.clear();
 #pragma unroll
         for (int u = 0; u < P; ++u) {
             compose(u, own[u]);
             scan_lanes(own[u]);
-            Steps<1> part = of_last_lane(own[u]);
+            Steps<1, RESET> part = of_last_lane(own[u]);
             own[u].after(of_wave);
             part.after(of_wave);
             of_wave = part;
+        }
+        if constexpr (RESET) {                      // (without resets what is not finite stays so, and is seen at the end)
+            float size = 0.0f;
+#pragma unroll
+            for (int u = 0; u < P; ++u) size += own[u].size();
+            const bool any = __any(!(size < INFINITY));
+            if (lane == 0) large[wave] = any;
         }
         if (lane == 0) {
             totals[wave] = make_float2(of_wave.A[0], of_wave.H[0]);
@@ -680,19 +812,27 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
         __syncthreads();
         before.clear();
         all.clear();
+        float size = 0.0f;
+        int not_small = 0;
 #pragma unroll
         for (int w = 0; w < kAlongWaves; ++w) {
             if (w == wave) before = all;
-            Steps<1> o;
+            Steps<1, RESET> o;
             o.A[0] = totals[w].x;
             o.H[0] = totals[w].y;
             o.cut = total_cut[w];
             o.after(all);
             all = o;
+            if constexpr (RESET) {
+                size += all.size();
+                not_small |= large[w];
+            }
         }
+        if (!RESET) size = all.size();
+        odd = not_small != 0 || !(size < INFINITY);         // a composition on the way cannot be used (the same in every thread)
         if (here == k && known) break;
         if (here == k && wave == 0) {
-            if (lane == 0) publish(items + k, item_of(all.A[0], all.H[0], all.cut));
+            if (lane == 0) publish(items + k, item_of(all.A[0], all.H[0], all.is_cut(0)));
             float x = 0.0f;
             const bool there = look_back(x);
             if (lane == 0) {
@@ -702,7 +842,10 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
         }
         __syncthreads();                            // (nor are the totals read any more)
         if (here < k) {
-            past = all.of(0, past);
+            const float then = all.of(0, past);
+            float x[P], end = 0.0f;
+            if (odd) end = one_by_one(past, x);
+            past = odd && lost(then, past, all.is_cut(0)) ? end : then;
             known = ++here == k;
         } else {
             past = found;
@@ -715,22 +858,40 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
 #pragma unroll
         for (int u = 0; u < P; ++u) four(h, i0 + u * 64 * L + 1, h_in[u]);
     }
-    if (threadIdx.x == 0 && k + 1 < q.n_tiles) publish(items + k, item_of(0.0f, all.of(0, past), true));
+    const float after = all.of(0, past);
+    const bool late = odd && lost(after, past, all.is_cut(0));
+    if (threadIdx.x == 0 && k + 1 < q.n_tiles && !late) publish(items + k, state_item(after));
     const float of_waves = before.of(0, past);
     G *const da = BACK ? static_cast<G *>(p.da.data_dev) + n * p.da.batch_stride : nullptr;
     T *const to = BACK ? static_cast<T *>(p.db.data_dev) + n * p.db.batch_stride : static_cast<T *>(p.h.data_dev) + n * p.h.batch_stride;
-    Steps<1> parts_before;                          // of the wave
-    parts_before.clear();
+    float first[P];                                 // the state before the lane's steps of a part
+    uint32_t cuts = RESET && before.cut ? (1u << P) - 1 : 0u;        // a bit per part: no state goes through what comes before it in the tile
+    {
+        Steps<1, RESET> parts_before;               // of the wave
+        parts_before.clear();
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            Steps<1, RESET> o;
+            o.A[0] = __shfl_up(own[u].A[0], 1, 64);
+            o.H[0] = __shfl_up(own[u].H[0], 1, 64);
+            o.cut = RESET ? __shfl_up(own[u].cut, 1, 64) : 0u;
+            if (lane == 0) o = parts_before;
+            first[u] = o.of(0, of_waves);
+            if (RESET) cuts |= o.cut << u;
+            parts_before = of_last_lane(own[u]);
+        }
+    }
+    if (__builtin_expect(odd, 0)) {
+        float y[P];
+        const float end = one_by_one(past, y);
+        if (threadIdx.x == 0 && k + 1 < q.n_tiles && late) publish(items + k, state_item(end));
+#pragma unroll
+        for (int u = 0; u < P; ++u) first[u] = lost(first[u], past, cuts >> u & 1u) ? y[u] : first[u];
+    }
 #pragma unroll
     for (int u = 0; u < P; ++u) {
         const int64_t i = i0 + u * 64 * L;
-        Steps<1> o;
-        o.A[0] = __shfl_up(own[u].A[0], 1, 64);
-        o.H[0] = __shfl_up(own[u].H[0], 1, 64);
-        o.cut = RESET ? __shfl_up(own[u].cut, 1, 64) : 0u;
-        if (lane == 0) o = parts_before;
-        float x = o.of(0, of_waves);
-        parts_before = of_last_lane(own[u]);
+        float x = first[u];
         float y[L], ya[L];
 #pragma unroll
         for (int j = 0; j < L; ++j) {
