@@ -346,8 +346,9 @@ typedef struct {
  *               after the last step in fp32; it may be h0_dev's memory: with steps = 1 the step of a single token
  * steps = 0 leaves h alone and copies h0 (or 0) to h_last.
  * Gates may be anything: long sequences are cut into tiles that are composed, but where a product of gates, or what is added up under it, passes the
- * largest number the steps are taken one by one.  From a state that is not finite on, up to the next reset, no state is finite
- * (infinities and NaN are not told apart); a term smaller than 2^-126 times the state that it comes from may be left out.
+ * largest number the steps are taken one by one.  An input that is not finite makes every state from there on, up to the next reset, not
+ * finite (infinite or NaN); after finite inputs whose states pass the largest number, later ones may be either.  A term smaller
+ * than 2^-126 times the state that it comes from may be left out.
  */
 int64_t rls_linear_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels);
 int32_t rls_linear_scan(const rls_scan_shape *shape, const rls_sequence *a, const rls_sequence *b, const float *h0_dev,
