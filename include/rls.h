@@ -322,7 +322,8 @@ int32_t rls_sample(const void *logits_dev, int32_t logits_type, int64_t rows, in
                    int64_t workspace_bytes, void *stream);
 
 /* A [batch][steps][channels] array: channels side by side, any strides (in elements) between steps and sequences.  Read-only
- * ones may repeat themselves (stride 0); written ones must not overlap themselves or anything else. */
+ * ones may repeat themselves (stride 0); written ones must not overlap themselves or anything else (RLS_ERR_SHAPE; views that lie between
+ * each other's rows are fine if they are as far apart, and may be turned down if not). */
 typedef struct {
     void *data_dev;
     int64_t batch_stride, step_stride;

@@ -56,6 +56,9 @@ int32_t rls_matrix_step(int32_t bf16, const void *a_dev, const void *b_dev, cons
  * it.  0 makes every tile do that whose first look finds something missing, for tests; a negative value restores the default. */
 int32_t rls_scan_wait_limit(int64_t ticks);
 
+/* Whether two arrays of a linear scan count as overlapping (1 or 0): what its calls turn down where one of the two is written. */
+int32_t rls_scan_overlap(const rls_scan_shape *shape, const rls_sequence *x, int32_t x_type, const rls_sequence *y, int32_t y_type);
+
 #ifdef __cplusplus
 }
 #endif

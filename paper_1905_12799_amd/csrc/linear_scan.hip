@@ -27,6 +27,7 @@
 // 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us; now 61 and 140, the floors 42 and 104.  The backward pass of
 // 8 x 4093 x 2048 in bf16 takes 153 us, 4.4 TB/s.  A launch that clears the items first is 5 us of it, with the gap after it 10.)
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "element_types.h"
@@ -1026,6 +1027,77 @@ int32_t check_sequence(const rls_scan_shape &shape, const rls_sequence *q, bool 
     return steps_inner || batch_inner ? RLS_OK : RLS_ERR_SHAPE;
 }
 
+// Where an array lies: rows of so many bytes, repeated at one or two distances.
+struct Place {
+    int64_t at, width;
+    struct { int64_t count, apart; } inner, outer;
+    int64_t end() const { return at + (inner.count - 1) * inner.apart + (outer.count - 1) * outer.apart + width; }
+};
+Place place_of(const void *data, int64_t bytes) { return Place{(int64_t)(uintptr_t)data, data ? bytes : 0, {1, 0}, {1, 0}}; }
+Place place_of(const rls_scan_shape &shape, const rls_sequence &q, int64_t element)
+{
+    Place r = place_of(q.data_dev, shape.steps > 0 ? shape.channels * element : 0);
+    r.inner = {shape.steps, q.step_stride * element};
+    r.outer = {shape.batch, q.batch_stride * element};
+    if (r.inner.apart > r.outer.apart) std::swap(r.inner, r.outer);
+    for (auto *d : {&r.inner, &r.outer}) {
+        if (r.width == 0 || d->apart == 0) d->count = 1;
+        // rows that touch are one
+        if (d->apart <= r.width && (d == &r.inner || r.inner.count == 1)) {
+            r.width += (d->count - 1) * d->apart;
+            d->count = 1;
+        }
+        if (d->count == 1) d->apart = 0;
+    }
+    return r;
+}
+
+// Whether two arrays have a byte in common.  Views of one buffer may lie between each other's rows: with the same distances that is found out
+// exactly; where they have more than two distances between them, arrays that reach into each other count as common.
+bool overlap(const Place &x, const Place &y)
+{
+    if (x.width == 0 || y.width == 0 || x.end() <= y.at || y.end() <= x.at) return false;
+    int64_t apart[4], n = 0;
+    for (const auto &d : {x.inner, x.outer, y.inner, y.outer})
+        if (d.count > 1) apart[n++] = d.apart;
+    std::sort(apart, apart + n);
+    n = std::unique(apart, apart + n) - apart;
+    if (n > 2) return true;
+    // y's rows less x's are i * near + j * far apart, with each of these between the two ends
+    auto ends = [&](int64_t of, int64_t *least, int64_t *most) {
+        *least = *most = 0;
+        for (const auto &d : {x.inner, x.outer})
+            if (d.count > 1 && d.apart == of) *least -= d.count - 1;
+        for (const auto &d : {y.inner, y.outer})
+            if (d.count > 1 && d.apart == of) *most += d.count - 1;
+    };
+    auto down = [](int64_t a, int64_t b) { return a / b - (a % b != 0 && (a < 0) != (b < 0)); };
+    const int64_t near = n > 0 ? apart[0] : 1, far = n > 1 ? apart[1] : 1;
+    int64_t i0 = 0, i1 = 0, j0 = 0, j1 = 0;
+    if (n > 0) ends(near, &i0, &i1);
+    if (n > 1) ends(far, &j0, &j1);
+    // a byte is common where they are less than x's width ahead, less than y's behind
+    const int64_t d = y.at - x.at, lo = -y.width + 1 - d, hi = x.width - 1 - d;
+    j0 = std::max(j0, down(lo - i1 * near + far - 1, far));
+    j1 = std::min(j1, down(hi - i0 * near, far));
+    if (j1 - j0 > 1000) return true;                // (windows of one array that overlap each other, many deep)
+    for (int64_t j = j0; j <= j1; ++j)
+        if (std::max(i0, down(lo - j * far + near - 1, near)) <= std::min(i1, down(hi - j * far, near))) return true;
+    return false;
+}
+
+// nothing that is written may lie in anything else; a state may take another one's place as a whole
+int32_t check_overlap(std::initializer_list<Place> written, std::initializer_list<Place> read)
+{
+    for (auto w = written.begin(); w != written.end(); ++w) {
+        for (const Place &r : read)
+            if (overlap(*w, r)) return RLS_ERR_SHAPE;
+        for (auto v = written.begin(); v != w; ++v)
+            if (overlap(*w, *v)) return RLS_ERR_SHAPE;
+    }
+    return RLS_OK;
+}
+
 int32_t plan_call(const rls_scan_shape &shape, bool unit_steps, void *workspace, int64_t bytes, ScanPlan *plan)
 {
     if (rls_linear_scan_workspace_bytes(shape.batch, shape.steps, shape.channels) > 0) {
@@ -1055,6 +1127,11 @@ int32_t rls_scan_wait_limit(int64_t ticks)
     return RLS_OK;
 }
 
+int32_t rls_scan_overlap(const rls_scan_shape *shape, const rls_sequence *x, int32_t x_type, const rls_sequence *y, int32_t y_type)
+{
+    return overlap(place_of(*shape, *x, type_bytes(x_type)), place_of(*shape, *y, type_bytes(y_type))) ? 1 : 0;
+}
+
 int64_t rls_linear_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels)
 {
     if (!sizes_fit(batch, steps, channels)) return RLS_ERR_INVALID_ARG;
@@ -1075,6 +1152,11 @@ int32_t rls_linear_scan(const rls_scan_shape *shape, const rls_sequence *a, cons
     const bool unit = a->step_stride == 1 && b->step_stride == 1 && h->step_stride == 1;
     ScanPlan plan;
     rc = plan_call(*shape, unit, workspace_dev, workspace_bytes, &plan);
+    if (rc != RLS_OK) return rc;
+    const int64_t wide = type_bytes(shape->type), gate = type_bytes(shape->gate_type), states = shape->batch * shape->channels * 4;
+    const Place none{}, start = place_of(h0_dev, states), last = place_of(h_last_dev, states), flags = place_of(reset_dev, shape->batch * shape->steps);
+    rc = check_overlap({place_of(*shape, *h, wide), last}, {place_of(*shape, *a, gate), place_of(*shape, *b, wide), flags});
+    if (rc == RLS_OK) rc = check_overlap({place_of(*shape, *h, wide), h_last_dev == h0_dev ? none : last}, {start});
     if (rc != RLS_OK) return rc;
     ScanArgs p{};
     p.batch = shape->batch; p.steps = shape->steps; p.channels = shape->channels; p.reverse = shape->reverse;
@@ -1098,6 +1180,12 @@ int32_t rls_linear_scan_backward(const rls_scan_shape *shape, const rls_sequence
     const bool unit = a->step_stride == 1 && h->step_stride == 1 && dh->step_stride == 1 && da->step_stride == 1 && db->step_stride == 1;
     ScanPlan plan;
     rc = plan_call(*shape, unit, workspace_dev, workspace_bytes, &plan);
+    if (rc != RLS_OK) return rc;
+    const int64_t wide = type_bytes(shape->type), gate = type_bytes(shape->gate_type), states = shape->batch * shape->channels * 4;
+    const Place none{}, start = place_of(h0_dev, states), last = place_of(dh_last_dev, states), first = place_of(dh0_dev, states),
+                flags = place_of(reset_dev, shape->batch * shape->steps), to_a = place_of(*shape, *da, gate), to_b = place_of(*shape, *db, wide);
+    rc = check_overlap({to_a, to_b, first}, {place_of(*shape, *a, gate), place_of(*shape, *h, wide), place_of(*shape, *dh, wide), start, flags});
+    if (rc == RLS_OK) rc = check_overlap({to_a, to_b, dh0_dev == dh_last_dev ? none : first}, {last});
     if (rc != RLS_OK) return rc;
     ScanArgs p{};
     p.batch = shape->batch; p.steps = shape->steps; p.channels = shape->channels; p.reverse = shape->reverse;
