@@ -155,9 +155,8 @@ def _stream() -> ctypes.c_void_p:
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _raw_stream(t: torch.Tensor) -> int:
-    """The current stream as a number (making a Stream object of it takes 3 us, a fifth of a short call)."""
-    device = t.device.index
+def _raw_stream(device: int) -> int:
+    """The current stream of the device that a call's tensors are on, as a number (making a Stream object of it takes 3 us, a fifth of a short call)."""
     if device != torch._C._cuda_getDevice():
         raise ValueError(f"the tensors are on device {device}, which is not the current one")
     return torch._C._cuda_getCurrentRawStream(device)
@@ -537,7 +536,7 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[to
     logprob = torch.empty(rows, dtype=torch.float32, device=device) if want_logprob else None
     ws, base, avail = _space(workspace, lambda: sample_workspace_bytes(rows, n), device)
     _check(lib().rls_sample(logits.data_ptr(), _TYPE_OF[logits.dtype], rows, n, logits.stride(0) if rows > 1 else n, *settings, to,
-                            logprob.data_ptr() if want_logprob else 0, base, avail, _raw_stream(logits)), "rls_sample")
+                            logprob.data_ptr() if want_logprob else 0, base, avail, _raw_stream(logits.get_device())), "rls_sample")
     return token, logprob
 
 
@@ -603,7 +602,7 @@ def linear_scan(a: torch.Tensor, b: torch.Tensor, h0: Optional[torch.Tensor] = N
     ws, base, avail = _space(workspace, lambda: linear_scan_workspace_bytes(B, T, C), b.device)
     held, at = _sequences(size, (a, a.dtype, "a"), (b, b.dtype, "b"), (h, b.dtype, "out"))
     _check(lib().rls_linear_scan(ctypes.byref(shape), at[0], at[1], _states(h0, size, "h0"), _resets(reset, size), at[2], _states(last, size, "last"),
-                                 base, avail, _raw_stream(b)), "rls_linear_scan")
+                                 base, avail, _raw_stream(b.get_device())), "rls_linear_scan")
     return h, last
 
 
@@ -620,7 +619,7 @@ def linear_scan_backward(a: torch.Tensor, h: torch.Tensor, dh: torch.Tensor, h0:
     ws, base, avail = _space(workspace, lambda: linear_scan_workspace_bytes(B, T, C), h.device)
     held, at = _sequences(size, (a, a.dtype, "a"), (h, h.dtype, "h"), (dh, h.dtype, "dh"), (da, a.dtype, "da"), (db, h.dtype, "db"))
     _check(lib().rls_linear_scan_backward(ctypes.byref(shape), at[0], at[1], at[2], _states(h0, size, "h0"), _resets(reset, size),
-                                          _states(dh_last, size, "dh_last"), at[3], at[4], dh0.data_ptr(), base, avail, _raw_stream(h)),
+                                          _states(dh_last, size, "dh_last"), at[3], at[4], dh0.data_ptr(), base, avail, _raw_stream(h.get_device())),
            "rls_linear_scan_backward")
     return da, db, dh0
 
@@ -630,7 +629,8 @@ class AdamW:
 
     state_bits 32 keeps m and v in fp32; 8 keeps m and sqrt(v) as torch.float8_e4m3fn codes (stored as uint8) with a power-of-two scale per
     256 elements, rounded at random from `seed`.  master=True keeps fp32 weights beside bf16 or fp16 parameters.  The moments start at zero;
-    exp_avg, exp_avg_sq, their scales and master, lists like params, take over existing ones (a resumed run: `step` steps already done)."""
+    exp_avg, exp_avg_sq, their scales and master, lists like params, take over existing ones (a resumed run: `step` steps already done).  The lists are
+    the optimizer's own: a tensor put into one of them, or another memory given to a tensor (p.data = ...), counts from the next step on."""
 
     def __init__(self, params: Sequence[torch.Tensor], state_bits: int = 32, master=None, seed: int = 0, step: int = 0, exp_avg=None,
                  exp_avg_sq=None, exp_avg_scale=None, exp_avg_sq_scale=None):
@@ -638,20 +638,66 @@ class AdamW:
         if self.state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
         for p in self.params:
-            if not p.is_cuda or p.dtype not in _TYPE_OF or not p.is_contiguous():
-                raise ValueError("params must be contiguous device tensors of fp32, bf16 or fp16")
+            self._check_param(p)
         held = torch.float32 if self.state_bits == 32 else torch.uint8
-        blocks = [((p.numel() + 255) // 256,) for p in self.params]
         shapes = [p.shape for p in self.params]
-        self.exp_avg = self._list(exp_avg, held, shapes, "exp_avg")
-        self.exp_avg_sq = self._list(exp_avg_sq, held, shapes, "exp_avg_sq")
+        self.exp_avg = self._list(exp_avg, held, shapes)
+        self.exp_avg_sq = self._list(exp_avg_sq, held, shapes)
         self.exp_avg_scale = self.exp_avg_sq_scale = None
         if self.state_bits == 8:
-            self.exp_avg_scale = self._list(exp_avg_scale, torch.float32, blocks, "exp_avg_scale")
-            self.exp_avg_sq_scale = self._list(exp_avg_sq_scale, torch.float32, blocks, "exp_avg_sq_scale")
+            blocks = [((p.numel() + 255) // 256,) for p in self.params]
+            self.exp_avg_scale = self._list(exp_avg_scale, torch.float32, blocks)
+            self.exp_avg_sq_scale = self._list(exp_avg_sq_scale, torch.float32, blocks)
         if master is True:
             master = [p.detach().float() for p in self.params]
-        self.master = self._list(master, torch.float32, shapes, "master") if master else None
+        self.master = list(master) if master else None
+        self._take()
+
+    def _list(self, given, dtype, shapes):
+        return [torch.zeros(k, dtype=dtype, device=p.device) for p, k in zip(self.params, shapes)] if given is None else list(given)
+
+    def _lists(self):
+        """Everything that a step reads and writes, gradients aside: lists with a tensor per parameter."""
+        return [x for x in (self.params, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale, self.exp_avg_sq_scale, self.master) if x is not None]
+
+    def _where(self):
+        at = torch.Tensor.data_ptr
+        places = [*map(at, self.params), *map(at, self.exp_avg), *map(at, self.exp_avg_sq)]
+        if self.state_bits == 8:
+            places += [*map(at, self.exp_avg_scale), *map(at, self.exp_avg_sq_scale)]
+        if self.master is not None:
+            places += map(at, self.master)
+        return places
+
+    @staticmethod
+    def _check_param(p):
+        if not p.is_cuda or p.dtype not in _TYPE_OF or not p.is_contiguous():
+            raise ValueError("params must be contiguous device tensors of fp32, bf16 or fp16")
+
+    def _take(self):
+        """Checks all tensors and takes their addresses (again, where a list has got another tensor or a tensor other memory)."""
+        self._addresses = None
+        held, wide = (torch.float32, 1) if self.state_bits == 32 else (torch.uint8, 256)
+        for name, given, dtype, block in (("exp_avg", self.exp_avg, held, 1), ("exp_avg_sq", self.exp_avg_sq, held, 1), ("master", self.master, torch.float32, 1),
+                                          ("exp_avg_scale", self.exp_avg_scale, torch.float32, wide), ("exp_avg_sq_scale", self.exp_avg_sq_scale, torch.float32, wide)):
+            if given is None:
+                continue
+            if len(given) != len(self.params):
+                raise ValueError(f"{name} needs a tensor per parameter")
+            for t, p in zip(given, self.params):
+                if _dev(t, dtype, name).numel() != (p.numel() + block - 1) // block:
+                    raise ValueError(f"{name} has a tensor of another size than its parameter's")
+        every = [t for x in self._lists() for t in x]
+        for p in self.params:
+            self._check_param(p)
+        self._device = self.params[0].get_device() if self.params else -1
+        if any(t.get_device() != self._device for t in every):
+            raise ValueError("an optimizer's tensors must be on one device")
+        # (an fp32 parameter's entry in master is not used, and may be the parameter itself)
+        used = [t for x in self._lists() for t, p in zip(x, self.params) if t.numel() > 0 and not (x is self.master and p.dtype == torch.float32)]
+        places = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in used)
+        if any(at + size > after for (at, size), (after, _) in zip(places, places[1:])):
+            raise ValueError("an optimizer's tensors must not overlap")
         self._tensors = (_AdamwTensor * max(1, len(self.params)))()
         self._each, self._forms = list(self._tensors)[:len(self.params)], [(p.shape, p.dtype) for p in self.params]
         for i, p in enumerate(self.params):
@@ -661,32 +707,30 @@ class AdamW:
             t.master_dev = self.master[i].data_ptr() if self.master and p.dtype != torch.float32 else None
             if self.state_bits == 8:
                 t.m_scale_dev, t.v_scale_dev = self.exp_avg_scale[i].data_ptr(), self.exp_avg_sq_scale[i].data_ptr()
-
-    def _list(self, given, dtype, shapes, name):
-        if given is None:
-            return [torch.zeros(k, dtype=dtype, device=p.device) for p, k in zip(self.params, shapes)]
-        given = list(given)
-        if len(given) != len(self.params):
-            raise ValueError(f"{name} needs a tensor per parameter")
-        for t, k in zip(given, shapes):
-            _dev(t, dtype, name)
-            if t.numel() != torch.Size(k).numel():
-                raise ValueError(f"{name} has a tensor of another size than its parameter's")
-        return given
+        # (the memory stays with these while its addresses are here, so that none of it can become another tensor's)
+        self._memory = [t.detach() for t in every]
+        self._addresses = self._where()
+        self._grad_types = [None] * len(self.params)
 
     def step(self, grads: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
              weight_decay: float = 0.01, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step with these gradients (fp32 or the parameter's type), times grad_scale (one fp32 on the device) where given."""
+        if self._where() != self._addresses:
+            self._take()
         if len(grads) != len(self.params):
             raise ValueError("step needs a gradient per parameter")
-        for t, (shape, dtype), g in zip(self._each, self._forms, grads):
-            if g.shape != shape or not g.is_cuda or (g.dtype != dtype and g.dtype != torch.float32) or not g.is_contiguous():
-                raise ValueError("a gradient must be a contiguous device tensor of its parameter's shape, in fp32 or the parameter's type")
-            t.grad_dev, t.grad_type = g.data_ptr(), _TYPE_OF[g.dtype]
+        device = self._device
+        for i, (t, (shape, dtype), g, known) in enumerate(zip(self._each, self._forms, grads, self._grad_types)):
+            kind = g.dtype
+            if g.shape != shape or g.get_device() != device or (kind is not dtype and kind is not torch.float32) or not g.is_contiguous():
+                raise ValueError("a gradient must be a contiguous tensor on its parameter's device, of its shape, in fp32 or the parameter's type")
+            t.grad_dev = g.data_ptr()
+            if kind is not known:
+                t.grad_type, self._grad_types[i] = _TYPE_OF[kind], kind
         if grad_scale is not None and _dev(grad_scale, torch.float32, "grad_scale").numel() != 1:
             raise ValueError("grad_scale must hold one number")
         options = _AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, self.step_count + 1, ctypes.c_uint64(self.seed).value, self.state_bits,
                                 None if grad_scale is None else grad_scale.data_ptr())
-        stream = _raw_stream(self.params[0]) if self.params else 0
+        stream = _raw_stream(device) if self.params else 0
         _check(lib().rls_adamw_step(self._tensors, len(self.params), ctypes.byref(options), stream), "rls_adamw_step")
         self.step_count += 1
