@@ -639,6 +639,8 @@ class AdamW:
             raise ValueError("state_bits must be 8 or 32")
         for p in self.params:
             self._check_param(p)
+        if self.state_bits == 8 and ((exp_avg is None) != (exp_avg_scale is None) or (exp_avg_sq is None) != (exp_avg_sq_scale is None)):
+            raise ValueError("moments in 8 bits need their scales, and scales their moments")
         held = torch.float32 if self.state_bits == 32 else torch.uint8
         shapes = [p.shape for p in self.params]
         self.exp_avg = self._list(exp_avg, held, shapes)
