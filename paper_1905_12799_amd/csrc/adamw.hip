@@ -132,9 +132,11 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(AdamArgs a)
     const G *const grad = static_cast<const G *>(t.grad);
     W *const weight = MASTER ? reinterpret_cast<W *>(t.master) : reinterpret_cast<W *>(param);
     S *const ms = static_cast<S *>(t.m), *const vs = static_cast<S *>(t.v);
-    // (the factor of the gradients goes into these, which are rounded once: applied to every gradient it would be two roundings more of v)
-    const double grad_scale = a.grad_scale ? (double)*a.grad_scale : 1.0;
-    const float in_m = (float)(a.one_less_beta1 * grad_scale), in_v = (float)(a.one_less_beta2 * grad_scale * grad_scale);
+    // The factor of the gradients goes into these, which are rounded once: applied to every gradient it would be two roundings more of v.  Its power of
+    // two is applied to the gradients, which is exact: the square of a factor of 1e-22, for gradients of 1e22, would be nothing.
+    int power = 0;
+    const double part = a.grad_scale ? (double)frexpf(*a.grad_scale, &power) : 1.0;
+    const float in_m = (float)(a.one_less_beta1 * part), in_v = (float)(a.one_less_beta2 * part * part);
 
     W w[kAdamTurns][4];
     G g[kAdamTurns][4];
@@ -182,7 +184,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(AdamArgs a)
         P rounded[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float ge = (float)g[i][e];
+            const float ge = ldexpf((float)g[i][e], power);
             m[e] = m[e] * a.beta1 + ge * in_m;
             v[e] = v[e] * a.beta2 + (ge * in_v) * ge;
             root[e] = sqrtf(v[e]);
