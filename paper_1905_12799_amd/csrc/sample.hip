@@ -855,8 +855,14 @@ __device__ inline Piece row_top(const LongArgs &q, int r)
 
 // whether all that top-k keeps goes through the list: its histogram needs no weights then
 __device__ inline bool k_by_list(const LongArgs &q, const RowRules &r) { return r.k < q.a.n && r.k <= kListedK; }
-// whether a row's cut has to be looked for (a single entry, its largest, is known from the maxima)
-__device__ inline bool cuts(const LongArgs &q, const RowRules &r, float top) { return top > -INFINITY && r.k != 1 && (r.k < q.a.n || r.p < 1.0f); }
+// Whether a row's one entry is its largest, which is known from the maxima.  (Not where temperature brings other entries to a distance of 0: the
+// one below the largest is at least 2^-25 of it, or the smallest number, away.)
+__device__ inline bool is_top(const RowRules &r, float top) { return (r.k == 1) & (fmaxf(fabsf(top) * 0x1p-25f, 0x1p-149f) * r.inv > 0.0f); }
+// whether a row's cut has to be looked for
+__device__ inline bool cuts(const LongArgs &q, const RowRules &r, float top)
+{
+    return top > -INFINITY && !is_top(r, top) && (r.k < q.a.n || r.p < 1.0f);
+}
 
 // `what` with a function from logits to distances: where nothing is infinite it has no case for that
 template <typename F>
@@ -1008,7 +1014,7 @@ __global__ void __launch_bounds__(kLongThreads) long_weight_kernel(LongArgs q)
     const int piece = blockIdx.x, r = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const RowRules rules = rules_of(q.a, q.row0 + r);
     const float top = row_top(q, r).top;
-    if (!(top > -INFINITY) || rules.k == 1) return;
+    if (!(top > -INFINITY) || is_top(rules, top)) return;
     const T *const x = static_cast<const T *>(q.a.logits) + (q.row0 + r) * q.a.ld;
     const int64_t segment = q.chunk / kLongWaves;
     const int64_t begin = min(q.a.n, piece * q.chunk + wave * segment), end = min(q.a.n, begin + segment);
@@ -1067,7 +1073,7 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
     const int64_t row = q.row0 + r;
     const RowRules rules = rules_of(q.a, row);
     const Piece p = row_top(q, r);
-    if (!(p.top > -INFINITY) || rules.k == 1) {
+    if (!(p.top > -INFINITY) || is_top(rules, p.top)) {
         if (threadIdx.x == 0) {
             if (p.top > -INFINITY) {
                 q.a.token[row] = (int32_t)p.at;
