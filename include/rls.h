@@ -309,7 +309,7 @@ int32_t rls_apply_actions(const int32_t *cfg_dev, const int8_t *action_dev, int6
  *   temperature_dev  [rows] fp32 or null (1); 0, less or NaN: the first entry of the order at temperature 1 (logprob 0)
  *   top_k_dev        [rows] int32 or null; less than 1: all
  *   top_p_dev        [rows] fp32 or null; 1, more or NaN: all
- *   min_p_dev        [rows] fp32 or null; 0, less or NaN: all
+ *   min_p_dev        [rows] fp32 or null; 0, less or NaN: all; more than 1 counts as 1 (entries with e_i = 1: the largest, and equal ones)
  *   token_dev        [rows] int32 (written);  logprob_dev  [rows] fp32 (written) or null
  *   workspace_dev    rls_sample_workspace_bytes(rows, n_choices) bytes, 256-byte aligned (may be 0 bytes, and null then)
  * 1 <= rows <= RLS_MAX_N, 1 <= n_choices <= RLS_MAX_CHOICES.

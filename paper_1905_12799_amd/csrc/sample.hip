@@ -40,7 +40,7 @@ struct SampleArgs {
 struct RowRules {
     float inv;                                          // 1 / temperature
     int64_t k;                                          // entries of top-k (n: all)
-    float p, least;                                     // of top-p (1: all), min-p (0: all)
+    float p, least;                                     // of top-p (1: all), min-p (0: all; 1 at most, which is what the largest have)
     double u;
 };
 __device__ inline RowRules rules_of(const SampleArgs &a, int64_t row)
@@ -55,7 +55,7 @@ __device__ inline RowRules rules_of(const SampleArgs &a, int64_t row)
     r.k = greedy ? 1 : (a.top_k && k >= 1 && k < a.n ? (int64_t)k : a.n);
     r.inv = a.temperature && !greedy ? fminf(1.0f / t, 3.4028235e38f) : 1.0f;
     r.p = a.top_p && p < 1.0f ? p : 1.0f;
-    r.least = a.min_p && m > 0.0f ? m : 0.0f;
+    r.least = a.min_p && m > 0.0f ? fminf(m, 1.0f) : 0.0f;
     r.u = u > 0.0f ? (double)u : 0.0;
     return r;
 }
