@@ -166,6 +166,11 @@ def _ptr(t: Optional[torch.Tensor]) -> ctypes.c_void_p:
     return ctypes.c_void_p(None if t is None else t.data_ptr())
 
 
+def _written(*tensors: torch.Tensor) -> None:
+    """Tells autograd that a call has changed a caller's tensors in place, as torch's own operations do."""
+    torch._C._increment_version([t for t in tensors if not t.is_inference()])
+
+
 def _check(rc: int, what: str) -> None:
     if rc != RLS_OK:
         raise RlsError(rc, what)
@@ -523,7 +528,7 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[to
            want_logprob: bool = True, out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """A draw per row of logits [rows, n_choices] (fp32, bf16 or fp16, rows contiguous) from uniform [rows]: (token int32, logprob fp32 or None).
 
-    temperature, top_p, min_p (fp32) and top_k (int32) have an entry per row; None leaves a rule out."""
+    temperature, top_p, min_p (fp32) and top_k (int32) have an entry per row; None leaves a rule out.  Nothing is differentiated through a draw."""
     if logits.dim() != 2 or not logits.is_cuda or logits.dtype not in _TYPE_OF or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be an fp32, bf16 or fp16 device matrix with unit stride along a row")
     rows, n = logits.shape
@@ -537,6 +542,8 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[to
     ws, base, avail = _space(workspace, lambda: sample_workspace_bytes(rows, n), device)
     _check(lib().rls_sample(logits.data_ptr(), _TYPE_OF[logits.dtype], rows, n, logits.stride(0) if rows > 1 else n, *settings, to,
                             logprob.data_ptr() if want_logprob else 0, base, avail, _raw_stream(logits.get_device())), "rls_sample")
+    if out is not None:
+        _written(out)
     return token, logprob
 
 
@@ -592,18 +599,47 @@ def linear_scan(a: torch.Tensor, b: torch.Tensor, h0: Optional[torch.Tensor] = N
     """h_t = a_t h_{t-1} + b_t over [batch, steps, channels]: (every state in b's type, the last one in fp32 [batch, channels]).
 
     a may be fp32 beside a b of fewer bits, and either may be an expanded view; reset [batch, steps] (bytes or bools) cuts the carry;
-    reverse runs from the last step to the first.  `last` may be h0 itself, for a state that is updated in place."""
+    reverse runs from the last step to the first.  `last` may be h0 itself, for a state that is updated in place.  Differentiable by a, b and h0."""
+    if torch.is_grad_enabled() and (a.requires_grad or b.requires_grad or (h0 is not None and h0.requires_grad)):
+        if out is not None or last is not None:
+            raise ValueError("out and last are for calls that nothing is differentiated by (torch.no_grad)")
+        return _Scan.apply(a, b, h0, reset, reverse, workspace)
     shape, size = _scan_shape(a, b, reverse), b.shape
     B, T, C = size
     # (empty_like takes 0.9 us, empty with a shape, a type and a device 1.9; the call for a single token takes 10)
     h = torch.empty_like(b, memory_format=torch.contiguous_format) if out is None else out
-    if last is None:
+    kept = last is not None
+    if not kept:
         last = torch.empty((B, C), dtype=torch.float32, device=b.device) if h0 is None else torch.empty_like(h0)
     ws, base, avail = _space(workspace, lambda: linear_scan_workspace_bytes(B, T, C), b.device)
     held, at = _sequences(size, (a, a.dtype, "a"), (b, b.dtype, "b"), (h, b.dtype, "out"))
     _check(lib().rls_linear_scan(ctypes.byref(shape), at[0], at[1], _states(h0, size, "h0"), _resets(reset, size), at[2], _states(last, size, "last"),
                                  base, avail, _raw_stream(b.get_device())), "rls_linear_scan")
+    if out is not None:
+        _written(h)
+    if kept:
+        _written(last)
     return h, last
+
+
+class _Scan(torch.autograd.Function):
+    """linear_scan as autograd sees it: both its results are differentiable."""
+
+    @staticmethod
+    def forward(ctx, a, b, h0, reset, reverse, workspace):
+        h, last = linear_scan(a, b, h0, reset, reverse, workspace)
+        ctx.save_for_backward(a, h, h0, reset)
+        ctx.reverse = reverse
+        ctx.set_materialize_grads(False)
+        return h, last
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh, dlast):
+        a, h, h0, reset = ctx.saved_tensors
+        dh = torch.zeros_like(h) if dh is None else dh.contiguous()
+        da, db, dh0 = linear_scan_backward(a, h, dh, h0, reset, None if dlast is None else dlast.contiguous(), ctx.reverse)
+        return da, db, None if h0 is None else dh0, None, None, None
 
 
 def linear_scan_backward(a: torch.Tensor, h: torch.Tensor, dh: torch.Tensor, h0: Optional[torch.Tensor] = None, reset: Optional[torch.Tensor] = None,
@@ -711,7 +747,8 @@ class AdamW:
                 t.m_scale_dev, t.v_scale_dev = self.exp_avg_scale[i].data_ptr(), self.exp_avg_sq_scale[i].data_ptr()
         # (the memory stays with these while its addresses are here, so that none of it can become another tensor's)
         self._memory = [t.detach() for t in every]
-        self._addresses = self._where()
+        self._counted = [p for p in self.params if not p.is_inference()]        # (see _written)
+        self._addresses, self._options = self._where(), _AdamwOptions()
         self._grad_types = [None] * len(self.params)
 
     def step(self, grads: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
@@ -731,8 +768,11 @@ class AdamW:
                 t.grad_type, self._grad_types[i] = _TYPE_OF[kind], kind
         if grad_scale is not None and _dev(grad_scale, torch.float32, "grad_scale").numel() != 1:
             raise ValueError("grad_scale must hold one number")
-        options = _AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, self.step_count + 1, ctypes.c_uint64(self.seed).value, self.state_bits,
-                                None if grad_scale is None else grad_scale.data_ptr())
+        o = self._options
+        o.lr, (o.beta1, o.beta2), o.eps, o.weight_decay = lr, betas, eps, weight_decay
+        o.step, o.seed, o.state_bits = self.step_count + 1, self.seed & 0xFFFFFFFFFFFFFFFF, self.state_bits
+        o.grad_scale_dev = None if grad_scale is None else grad_scale.data_ptr()
         stream = _raw_stream(device) if self.params else 0
-        _check(lib().rls_adamw_step(self._tensors, len(self.params), ctypes.byref(options), stream), "rls_adamw_step")
+        _check(lib().rls_adamw_step(self._tensors, len(self.params), ctypes.byref(o), stream), "rls_adamw_step")
+        torch._C._increment_version(self._counted)
         self.step_count += 1
