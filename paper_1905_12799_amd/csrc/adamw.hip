@@ -12,6 +12,7 @@
 
 #include "element_types.h"
 #include "rls_internal.h"
+#include "wave.h"
 
 namespace rls {
 
@@ -77,13 +78,6 @@ __device__ inline uint32_t encode(float x, float inv, uint32_t r, uint32_t least
     if (mag > 0.0f) code = max(code, (int)least);
     if (!(mag < INFINITY)) code = 127;
     return (uint32_t)code;
-}
-
-__device__ inline float wave_max(float x)
-{
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
-    return x;
 }
 
 template <typename T>

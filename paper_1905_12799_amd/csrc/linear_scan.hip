@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) scan_strip_kernel(ScanArgs p, 
 #pragma unroll
         for (int v = 0; v < V; ++v) sum += fabsf(x[v]);
         bool good = sum < INFINITY;
-        while (__builtin_expect(!good, 0)) {                                         // the state that the tile before has (it is running, as all are that published something)
+        while (__builtin_expect(!good, 0)) {                    // the state that the tile before has (it is running, as all are that published something)
             good = true;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) scan_strip_kernel(ScanArgs p, 
 #pragma unroll
             for (int v = 0; v < V; ++v) publish(items + k * row + v * lanes, item_of(of_tile.A[v], of_tile.H[v], of_tile.is_cut(v)));
         }
-        if (__builtin_expect(!look_back(past), 0)) {                                 // through all the tiles before, all of the workgroup together
+        if (__builtin_expect(!look_back(past), 0)) {            // through all the tiles before, all of the workgroup together
 #pragma unroll
             for (int v = 0; v < V; ++v) past[v] = c0 + v < C ? start[v] : 0.0f;
             for (int64_t j0 = (int64_t)group * L; j0 < i_begin; j0 += tile) {
@@ -526,8 +526,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) scan_strip_kernel(ScanArgs p, 
                 scan_wave(s);
                 float x[V], end[V];
                 const bool strange = scan_waves(s, unused, other);
-                if (strange)
-                    one_by_one(past, j0, x, end);
+                if (strange) one_by_one(past, j0, x, end);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const float then = other.of(v, past[v]);
@@ -721,7 +720,7 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
 #pragma unroll 4
             for (int l = first; l < 64; ++l) x = through(seen[w][l], x);
         }
-        while (__builtin_expect(!finite(x), 0)) {                        // the state that the tile before has (it is running, as all are that published something)
+        while (__builtin_expect(!finite(x), 0)) {   // the state that the tile before has (it is running, as all are that published something)
             const uint64_t item = look(items + k - 1);
             x = __uint_as_float((uint32_t)item);
             if (is_state(item)) break;
@@ -753,7 +752,7 @@ __global__ void __launch_bounds__(64 * kAlongWaves) scan_along_kernel(ScanArgs p
         __syncthreads();
         return chain;
     };
-    Steps<1, RESET> own[P], before, all;                   // per part: the wave's steps up to the lane's; the waves before; the tile
+    Steps<1, RESET> own[P], before, all;            // per part: the wave's steps up to the lane's; the waves before; the tile
     float past = 0.0f;                              // the state before the tile
     if (k == 0) {                                   // (before any barrier: the last state may be written over it, by another wave)
         const float *const from = q.n_tiles > 1 ? q.start : (BACK ? p.in : p.h0);

@@ -5,8 +5,8 @@
 // a cut is a place: what lies up to it is kept.  Weights are whole numbers, so their sums do not depend on who adds what.
 //
 // Reading the logits bounds it, 2 or 4 bytes for a maximum, an exponential and a sum.  What is done with a row goes by its length:
-// - up to kThreadRow entries a thread takes a row, in registers, places counted against each other;
-// - up to kGroupRow a workgroup of 64 to 1024 threads takes a row, read once into registers, a thread 4 to 32 entries in a row of
+// - up to kThreadRow entries a thread takes a row, in registers, places counted against each other; up to kLaneRow 16 lanes do, two to four entries each;
+// - up to kGroupRow a workgroup of 64 to 1024 threads takes a row, read once into registers, a thread 4 to 16 entries in a row of
 //   them.  A cut is found by a histogram over d (counts and weights in LDS) and, in the bin it lies in, by counting the places
 //   before each; where a bin holds more than fit the list in LDS, it is cut into bins of places, again and again.
 // - longer rows are cut into chunks, a workgroup each; a launch for each of the passes.
