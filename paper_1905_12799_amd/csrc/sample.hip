@@ -734,7 +734,8 @@ hipError_t launch_short_rows(const SampleArgs &a, hipStream_t s)
 constexpr int kLongThreads = 512;
 constexpr int kLongWaves = kLongThreads / 64;
 constexpr int kLongBins = 2048;
-constexpr int kLongList = 16384;
+constexpr int64_t kLongList = 16384;                    // entries of a row's list, or a 64th of the row where that is more: ordinary logits have a 500th in a bin
+inline int64_t list_of(int64_t n) { return std::max(kLongList, n / 64); }
 constexpr int64_t kListedK = 4096;                      // top-k of so many at most: all it keeps goes through the list, weights and top-p with it
 constexpr uint32_t kLdsList = 2048;                     // entries of it that the draw holds in LDS
 constexpr int kLongStage = 1024;                        // places a workgroup collects before it goes to the row's list one by one
@@ -759,12 +760,12 @@ struct RowBins {                                        // where a row's cuts li
 struct LongArgs {
     SampleArgs a;
     int64_t row0, chunk;
-    int32_t rows, pieces;
+    int32_t rows, pieces, list_size;
     Piece *piece;                                       // [rows][pieces]
     uint64_t *weight;                                   // [rows][pieces][kLongWaves]
     uint64_t *mass;                                     // [rows][kLongBins]
     uint32_t *count, *listed;                           // [rows][kLongBins], [rows]
-    uint64_t *list;                                     // [rows][kLongList]
+    uint64_t *list;                                     // [rows][list_size]
     RowBins *bins;                                      // [rows]
 };
 
@@ -1042,7 +1043,7 @@ __global__ void __launch_bounds__(kLongThreads) long_weight_kernel(LongArgs q)
                     if (at < kLongStage) stage[at] = place;
                     else {
                         const uint32_t to = atomicAdd(&q.listed[r], 1u);
-                        if (to < kLongList) q.list[(int64_t)r * kLongList + to] = place;
+                        if (to < (uint32_t)q.list_size) q.list[(int64_t)r * q.list_size + to] = place;
                     }
                 }
             });
@@ -1053,14 +1054,15 @@ __global__ void __launch_bounds__(kLongThreads) long_weight_kernel(LongArgs q)
             if (threadIdx.x == 0) base = atomicAdd(&q.listed[r], own);
             __syncthreads();
             for (uint32_t i = threadIdx.x; i < own; i += kLongThreads)
-                if (base + i < kLongList) q.list[(int64_t)r * kLongList + base + i] = stage[i];
+                if (base + i < (uint32_t)q.list_size) q.list[(int64_t)r * q.list_size + base + i] = stage[i];
         }
         w = wave_sum(w);
     }
     if (lane == 0) q.weight[((int64_t)r * q.pieces + piece) * kLongWaves + wave] = w;
 }
 
-// The cuts, from the list, or from the row itself where its bins hold more entries than the list; then the draw.
+// The cuts, from the list, or from the row itself where its bins hold more entries than the list (many equal ones; a workgroup goes through the
+// row then, some five times: 64 x 262144 equal logits with top-p 2.2 ms, 1 x 8388608 35 ms); then the draw.
 template <typename T>
 __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
 {
@@ -1099,9 +1101,9 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
     if (cuts(q, rules, p.top)) {
         const RowBins bins = q.bins[r];
         const uint32_t listed = q.listed[r];
-        const bool whole = listed <= kLongList;
+        const bool whole = listed <= (uint32_t)q.list_size;
         const bool near = listed <= kLdsList;
-        const uint64_t *const list = q.list + (int64_t)r * kLongList;
+        const uint64_t *const list = q.list + (int64_t)r * q.list_size;
         if (near)
             for (uint32_t i = threadIdx.x; i < listed; i += 1024) held[i] = list[i];        // (a thread reads its own ones)
         // those up to the cut, of one bin (or all)
@@ -1231,7 +1233,7 @@ LongLayout long_layout(int64_t rows, int64_t n)
     L.mass = take(L.rows * kLongBins * 8);
     L.count = take(L.rows * kLongBins * 4);
     L.listed = take(L.rows * 4);
-    L.list = take(L.rows * kLongList * 8);
+    L.list = take(L.rows * list_of(n) * 8);
     L.bins = take(L.rows * (int64_t)sizeof(RowBins));
     L.total = at;
     return L;
@@ -1248,6 +1250,7 @@ hipError_t launch_long_rows(const SampleArgs &a, char *ws, hipStream_t s)
         q.rows = (int32_t)std::min(L.rows, a.rows - row0);
         q.chunk = L.chunk;
         q.pieces = (int32_t)L.pieces;
+        q.list_size = (int32_t)list_of(a.n);
         q.piece = reinterpret_cast<Piece *>(ws + L.piece);
         q.weight = reinterpret_cast<uint64_t *>(ws + L.weight);
         q.mass = reinterpret_cast<uint64_t *>(ws + L.mass);
