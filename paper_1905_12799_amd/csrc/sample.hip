@@ -757,6 +757,10 @@ struct RowBins {                                        // where a row's cuts li
     uint64_t mass;                                      // of the row
     float scale;
 };
+struct InBins {                                         // of a segment: the entries in the bins of the row's cuts, the nearest and the furthest of them
+    uint32_t n;
+    float least, most;
+};
 struct LongArgs {
     SampleArgs a;
     int64_t row0, chunk;
@@ -765,6 +769,7 @@ struct LongArgs {
     uint64_t *weight;                                   // [rows][pieces][kLongWaves]
     uint64_t *mass;                                     // [rows][kLongBins]
     uint32_t *count, *listed;                           // [rows][kLongBins], [rows]
+    InBins *in_bins;                                    // [rows][pieces][kLongWaves]
     uint64_t *list;                                     // [rows][list_size]
     RowBins *bins;                                      // [rows]
 };
@@ -1033,21 +1038,32 @@ __global__ void __launch_bounds__(kLongThreads) long_weight_kernel(LongArgs q)
         if (threadIdx.x == 0) staged = 0;
         __syncthreads();
         const float near = q.bins[r].near, far = q.bins[r].far, k_near = q.bins[r].k_near, k_far = q.bins[r].k_far;
+        uint32_t in_bins = 0;
+        float least = INFINITY, most = 0.0f;
+        bool full = false;                              // the list (then nobody needs to know by how much)
         with_distances(top, rules.inv, [&](auto distance) {
             visit_span(x, begin, end, lane, 64, [&](float v, int64_t i) {
                 const float d = distance(v);
                 if (d < near) w += kept_weight(d, rules.least);
                 else if ((d < far) | ((d >= k_near) & (d < k_far))) {
                     const uint64_t place = (uint64_t)__float_as_uint(d) << 32 | (uint32_t)i;
+                    ++in_bins;
+                    least = fminf(least, d);
+                    most = fmaxf(most, d);
                     const uint32_t at = atomicAdd(&staged, 1u);
                     if (at < kLongStage) stage[at] = place;
-                    else {
+                    else if (!full) {
                         const uint32_t to = atomicAdd(&q.listed[r], 1u);
+                        full = to >= (uint32_t)q.list_size;
                         if (to < (uint32_t)q.list_size) q.list[(int64_t)r * q.list_size + to] = place;
                     }
                 }
             });
         });
+        in_bins = wave_reduce(in_bins, 0u, [](uint32_t a, uint32_t b) { return a + b; });
+        least = wave_min(least);
+        most = wave_max(most);
+        if (lane == 0) q.in_bins[((int64_t)r * q.pieces + piece) * kLongWaves + wave] = InBins{in_bins, least, most};
         __syncthreads();
         const uint32_t own = staged < kLongStage ? staged : kLongStage;
         if (own > 0) {                                  // (the same in every thread)
@@ -1061,8 +1077,9 @@ __global__ void __launch_bounds__(kLongThreads) long_weight_kernel(LongArgs q)
     if (lane == 0) q.weight[((int64_t)r * q.pieces + piece) * kLongWaves + wave] = w;
 }
 
-// The cuts, from the list, or from the row itself where its bins hold more entries than the list (many equal ones; a workgroup goes through the
-// row then, some five times: 64 x 262144 equal logits with top-p 2.2 ms, 1 x 8388608 35 ms); then the draw.
+// The cuts, from the list.  Where a row's bins hold more entries than the list and these are all equal, so many of them are kept, counted segment by
+// segment; where they are not (several values that lie close together, thousands of times each), a workgroup goes through the row, some five
+// times, 3 ms each for 8 million entries.  Then the draw.
 template <typename T>
 __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
 {
@@ -1097,10 +1114,86 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
         for (int u = 0; u < U; ++u)
             if (1024 * u + (int)threadIdx.x < segments) weight[1024 * u + threadIdx.x] = v[u];
     }
+    // a thread's part of a segment, in the order of the entries
+    constexpr int S = kMostSegments / 1024, E = kMostChunk / kLongWaves / 1024;
+    const int64_t part = (segment + 1023) / 1024;
+    auto keys_of = [&](int which, uint32_t (&key)[E]) {
+        const int64_t begin = which * segment, end = min(q.a.n, begin + segment), from = min(end, begin + part * threadIdx.x), to = min(end, from + part);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            const float v = logit_of(x[min(from + j, q.a.n - 1)]);
+            key[j] = from + j < to ? key_of(distance_from(p.top, v, rules.inv)) : kMaskedKey;
+        }
+        return from;
+    };
     uint64_t cut = ~0ull;
-    if (cuts(q, rules, p.top)) {
+    const uint32_t listed = q.listed[r];
+    const bool cut_it = cuts(q, rules, p.top);
+    bool equal = false;
+    uint32_t held_by[S], tied = 0;
+    uint64_t mine = 0;
+    if (cut_it && listed > (uint32_t)q.list_size) {
+        float least = INFINITY, most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const int at = (int)threadIdx.x * S + i;
+            const InBins in = at < segments ? q.in_bins[(int64_t)r * segments + at] : InBins{0, INFINITY, 0.0f};
+            held_by[i] = in.n;
+            mine += in.n;
+            least = fminf(least, in.least);
+            most = fmaxf(most, in.most);
+        }
+        Grp::range(s, most, least);
+        equal = least == most;
+        tied = __float_as_uint(most);
+    }
+    if (equal) {
         const RowBins bins = q.bins[r];
-        const uint32_t listed = q.listed[r];
+        __syncthreads();
+        uint64_t all;
+        uint64_t run = Grp::scan(s.waves, mine, &all);
+        // (they are of one bin: what lies before it is what lies before them)
+        const bool use_k = rules.k < q.a.n, by_list = k_by_list(q, rules);
+        const uint64_t each = weight_of_key(tied), before = by_list ? 0 : (use_k ? bins.k_mass_before : bins.p_mass_before);
+        uint64_t keep = use_k ? min(all, (uint64_t)rules.k - (by_list ? 0 : bins.k_before)) : all;
+        if (rules.p < 1.0f) {
+            const double limit = (double)rules.p * (double)(use_k ? before + keep * each : bins.mass);
+            uint64_t lo = 0;
+            while (lo < keep) {                         // the last one that begins below
+                const uint64_t mid = (lo + keep + 1) / 2;
+                if (begins_below(true, before + (mid - 1) * each, 0, limit)) lo = mid;
+                else keep = mid - 1;
+            }
+        }
+        const uint64_t drawn = kept_weight(distance_of(tied), rules.least);
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            const uint64_t inside = min((uint64_t)held_by[i], keep > run ? keep - run : 0);
+            if (inside > 0) {
+                weight[threadIdx.x * S + i] += drawn * inside;
+                if (run + inside == keep) {             // (one segment)
+                    found = (int)threadIdx.x * S + i;
+                    found_before = run;
+                }
+            }
+            run += held_by[i];
+        }
+        __syncthreads();
+        uint32_t key[E];
+        const int64_t from = keys_of(found, key);
+        uint64_t ones = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) ones += key[j] == tied ? 1 : 0;
+        run = found_before + Grp::scan(s.waves, ones, &all);
+        uint64_t mark = 0;
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            run += key[j] == tied ? 1 : 0;
+            mark = key[j] == tied && run == keep ? (uint64_t)tied << 32 | (uint32_t)(from + j) : mark;
+        }
+        cut = Grp::most(s, mark);
+    } else if (cut_it) {
+        const RowBins bins = q.bins[r];
         const bool whole = listed <= (uint32_t)q.list_size;
         const bool near = listed <= kLdsList;
         const uint64_t *const list = q.list + (int64_t)r * q.list_size;
@@ -1158,8 +1251,8 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
         });
     }
     __syncthreads();
-    constexpr int S = kMostSegments / 1024;
-    uint64_t mine = 0, total;
+    uint64_t total;
+    mine = 0;
 #pragma unroll
     for (int i = 0; i < S; ++i) mine += (int)threadIdx.x * S + i < segments ? weight[threadIdx.x * S + i] : 0;
     uint64_t run = Grp::scan(s.waves, mine, &total);
@@ -1176,16 +1269,8 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
         }
     }
     __syncthreads();
-    // the segment, a part per thread in the order of the entries
-    constexpr int E = kMostChunk / kLongWaves / 1024;
-    const int64_t begin = found * segment, end = min(q.a.n, begin + segment), part = (segment + 1023) / 1024;
-    const int64_t from = min(end, begin + part * threadIdx.x), to = min(end, from + part);
     uint32_t key[E];
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const float v = logit_of(x[min(from + j, q.a.n - 1)]);
-        key[j] = from + j < to ? key_of(distance_from(p.top, v, rules.inv)) : kMaskedKey;
-    }
+    const int64_t from = keys_of(found, key);
     auto drawn = [&](int j) -> uint64_t {
         return key[j] < kMaskedKey && ((uint64_t)key[j] << 32 | (uint32_t)(from + j)) <= cut ? kept_weight(distance_of(key[j]), rules.least) : 0;
     };
@@ -1218,7 +1303,7 @@ int64_t chunk_of(int64_t rows, int64_t n)
 
 struct LongLayout {
     int64_t rows, chunk, pieces;
-    int64_t piece, weight, mass, count, listed, list, bins, total;
+    int64_t piece, weight, mass, count, listed, in_bins, list, bins, total;
 };
 LongLayout long_layout(int64_t rows, int64_t n)
 {
@@ -1233,6 +1318,7 @@ LongLayout long_layout(int64_t rows, int64_t n)
     L.mass = take(L.rows * kLongBins * 8);
     L.count = take(L.rows * kLongBins * 4);
     L.listed = take(L.rows * 4);
+    L.in_bins = take(L.rows * L.pieces * kLongWaves * (int64_t)sizeof(InBins));
     L.list = take(L.rows * list_of(n) * 8);
     L.bins = take(L.rows * (int64_t)sizeof(RowBins));
     L.total = at;
@@ -1256,6 +1342,7 @@ hipError_t launch_long_rows(const SampleArgs &a, char *ws, hipStream_t s)
         q.mass = reinterpret_cast<uint64_t *>(ws + L.mass);
         q.count = reinterpret_cast<uint32_t *>(ws + L.count);
         q.listed = reinterpret_cast<uint32_t *>(ws + L.listed);
+        q.in_bins = reinterpret_cast<InBins *>(ws + L.in_bins);
         q.list = reinterpret_cast<uint64_t *>(ws + L.list);
         q.bins = reinterpret_cast<RowBins *>(ws + L.bins);
         const dim3 grid((unsigned)q.pieces, (unsigned)q.rows), each((unsigned)q.rows), threads(kLongThreads);
