@@ -300,7 +300,8 @@ int32_t rls_apply_actions(const int32_t *cfg_dev, const int8_t *action_dev, int6
  *   top-p:  of these the ones before which, in that order, the sum of w is less than p times the sum over all of them
  *   min-p:  of these the ones with e_i >= min_p
  *   token:  the first kept i (by index) up to which the kept w add up to more than uniform * (sum of the kept w)
- *   logprob: d_token - log(sum of the kept w), the log-probability of the draw among what was kept, in fp32
+ *   logprob: d_token - log(sum of the kept w), the log-probability of the draw among what was kept, in fp32 (of the rounded weights: a
+ *            weight is off by up to 2^-39 of the largest, so many small ones together move it against softmax's)
  * The first entry of the order is always kept.  Entries of -infinity (masked ones) and NaN are never drawn; a row without
  * any other gets token -1 and logprob -infinity.  Entries of +infinity share a draw among themselves.
  * Arguments
@@ -394,7 +395,7 @@ typedef struct {
     int32_t state_bits;        /* 32 or 8 */
     const float *grad_scale_dev;        /* one fp32 factor of all gradients (clipping, loss scaling), or null (1) */
 } rls_adamw_options;
-/* `tensors` is a host array, read before the call returns. */
+/* `tensors` is a host array, read before the call returns.  What a step updates must not overlap anything else that it reads or updates. */
 int32_t rls_adamw_step(const rls_adamw_tensor *tensors, int32_t n_tensors, const rls_adamw_options *options, void *stream);
 
 #ifdef __cplusplus

@@ -19,13 +19,14 @@
 // scan with look-back, Merrill and Garland 2016; they let compositions join as they come).  An item is one 64-bit word that is written
 // and read atomically and is all ones until then, so that no fence is needed (which would write the second-level cache back,
 // 100 us here).  A tile that has waited too long for another goes through all the tiles before it by itself, in the same way, so that no
-// order in which workgroups run can hold up a call.
+// order in which workgroups run can hold up a call.  (Composed by a launch of their own, chunks of time had their inputs read twice:
+// 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us; now 63 and 138, the floors 42 and 104.  The backward pass of
+// 8 x 4093 x 2048 in bf16 takes 154 us, 4.4 TB/s.  A launch that clears the items first is 5 us of it, with the gap after it 10.)
 //
 // Products of gates above 1, and what is added up under them, can pass the largest number where the states themselves do not (gates of 4
 // over a state of 0), or be no number.  A composition of that kind is not used: the tile's steps are taken one by one from the
-// state before it, thread after thread, and the tile publishes that a state will follow and nothing else.  (Composed by a launch of their own, chunks of time had their inputs read twice:
-// 64 x 262144 returns 138 us, 1 x 65521 x 1024 in bf16 246 us; now 61 and 140, the floors 42 and 104.  The backward pass of
-// 8 x 4093 x 2048 in bf16 takes 153 us, 4.4 TB/s.  A launch that clears the items first is 5 us of it, with the gap after it 10.)
+// state before it, thread after thread, and the tile publishes that a state will follow and nothing else.  (64 x 262144 with an infinity
+// every 300 steps and resets: 2.5 ms.)
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>

@@ -11,7 +11,7 @@
 //   before each; where a bin holds more than fit the list in LDS, it is cut into bins of places, again and again.
 // - longer rows are cut into chunks, a workgroup each; a launch for each of the passes.
 // What it takes, of that the reading of the logits at the rate of a large copy: 524288 x 3 10 us (2), 524288 x 20 52 (8), 8 x 2000 with
-// top-k and top-p 12, 2048 x 8000 44 (13), 64 x 128003 in bf16 with every rule 46 (3), 64 x 262144 with top-p 73 (13), 1 x 8388608 24 (7).
+// top-k and top-p 12, 2048 x 8000 44 (13), 64 x 128003 in bf16 with every rule 47 (3), 64 x 262144 with top-p 75 (13), 1 x 8388608 25 (7).
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -78,7 +78,7 @@ __device__ inline float distance_of(uint32_t key) { return __uint_as_float(key);
 
 // exp(-distance) = 2^(-distance log2 e), the logarithm in two pieces: an exponential of the hardware and eight operations.  (Without what a
 // general one does about results beyond the largest and below the smallest normal number: weights end at 2^-38, and beyond 100, at
-// infinity and where there is no number this is exp(-100), which is no weight.)
+// infinity and where there is no number this is exp(-100), which is no weight.  The steps are those of this target's expf, so that its weights are those of expf.)
 __device__ inline float exp_of(float x)
 {
     const float distance = fminf(x, 100.0f);
