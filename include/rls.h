@@ -350,7 +350,7 @@ typedef struct {
  * Gates may be anything: long sequences are cut into tiles that are composed, but where a product of gates, or what is added up under it, passes the
  * largest number the steps are taken one by one.  An input that is not finite makes every state from there on, up to the next reset, not
  * finite (infinite or NaN); after finite inputs whose states pass the largest number, later ones may be either.  A term smaller
- * than 2^-126 times the state that it comes from may be left out.
+ * than 2^-126 times the state that it comes from may be left out, also where later gates above 1 would bring it back.
  */
 int64_t rls_linear_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t channels);
 int32_t rls_linear_scan(const rls_scan_shape *shape, const rls_sequence *a, const rls_sequence *b, const float *h0_dev,

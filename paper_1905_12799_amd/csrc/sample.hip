@@ -1090,6 +1090,7 @@ __global__ void __launch_bounds__(1024) long_draw_kernel(LongArgs q)
     __shared__ uint64_t found_before;
     const int r = blockIdx.x;
     const int64_t row = q.row0 + r;
+    if (threadIdx.x == 0) { found = 0; found_before = 0; }      // (a place inside the row in any case)
     const RowRules rules = rules_of(q.a, row);
     const Piece p = row_top(q, r);
     if (!(p.top > -INFINITY) || is_top(rules, p.top)) {
