@@ -18,6 +18,8 @@
  *
  *   rls_sample          a draw per row of logits: temperature, top-k, top-p, min-p, from given uniform numbers
  *   rls_linear_scan     the gated linear recurrence h_t = a_t h_{t-1} + b_t, and its backward pass
+ *   rls_token_logprobs  log-probabilities of given entries of rows of logits, entropy, the best alternatives, and their gradient
+ *   rls_distill_loss    the divergence of rows of logits from a teacher's best entries, and its gradient
  *   rls_adamw_step      one AdamW step over all tensors of a model, moments in 32 or in 8 bits
  *
  * Conventions
@@ -321,6 +323,57 @@ int32_t rls_sample(const void *logits_dev, int32_t logits_type, int64_t rows, in
                    const float *uniform_dev, const float *temperature_dev, const int32_t *top_k_dev, const float *top_p_dev,
                    const float *min_p_dev, int32_t *token_dev, float *logprob_dev, void *workspace_dev,
                    int64_t workspace_bytes, void *stream);
+
+/*
+ * Log-probabilities of given entries, one per row of logits: of the actions that the search agent took (its policy loss), of the tokens of a
+ * sequence.  With x_max the row's largest logit and inv = min(1 / temperature, 2e38), in fp32:
+ *   d_i = (x_i - x_max) inv,  L = log(sum of exp(d_i)),  log p_i = d_i - L
+ *   logprob = log p_token;  entropy = L - (sum of exp(d_i) d_i) / (sum of exp(d_i)), in nats;  norm = (x_max, L), which the gradients start from
+ *   alternatives: the `top` first entries in the order of falling logits, equal ones by rising index, with their log p
+ * Entries of -infinity (masked ones) and NaN have probability 0, as for rls_sample, and are no alternatives; +infinity counts as the largest fp32
+ * number.  A row without any other: logprob -infinity, entropy 0, norm (-infinity, 0).  Alternatives beyond the entries that count are token -1
+ * with log p -infinity.  A token outside 0 .. n_choices - 1 (a padded position) gets logprob 0 and no gradient by it.
+ *   logits_dev       [rows][ld_logits] of logits_type, first n_choices columns used
+ *   token_dev        [rows] int32;  logprob_dev [rows] fp32 (written); both null: only the others are wanted
+ *   temperature_dev  [rows] fp32 or null (1); 0, less or NaN counts as 1 (the distribution that a greedy draw ignores)
+ *   entropy_dev      [rows] fp32 (written) or null;  norm_dev [rows][2] fp32 (written) or null
+ *   top              0 .. RLS_MAX_TOP;  top_logprob_dev, top_token_dev  [rows][top] fp32 and int32 (written), not looked at with top = 0
+ *   workspace_dev    rls_token_logprobs_workspace_bytes(rows, n_choices, top) bytes, 256-byte aligned (may be 0 bytes, and null then)
+ * 1 <= rows <= RLS_MAX_N, 1 <= n_choices <= RLS_MAX_CHOICES.  What is written must not lie in anything else (RLS_ERR_SHAPE).
+ */
+#define RLS_MAX_TOP 128
+int64_t rls_token_logprobs_workspace_bytes(int64_t rows, int64_t n_choices, int32_t top);
+int32_t rls_token_logprobs(const void *logits_dev, int32_t logits_type, int64_t rows, int64_t n_choices, int64_t ld_logits, const int32_t *token_dev,
+                           const float *temperature_dev, int32_t top, float *logprob_dev, float *entropy_dev, float *top_logprob_dev,
+                           int32_t *top_token_dev, float *norm_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+/*
+ * Gradient by the logits, from what the forward pass wrote (norm, and entropy where dentropy is given) and the gradients by logprob and entropy:
+ *   dx_i = inv (dlogprob ([i = token] - p_i) - dentropy p_i (log p_i + entropy)),  0 where p_i is 0 (but for the token itself)  and at masked entries
+ *   dlogprob_dev, dentropy_dev  [rows] fp32, either may be null (0)
+ *   dlogits_dev      [rows][ld_dlogits] of logits_type (written, first n_choices columns); logits_dev itself, with ld_dlogits = ld_logits, or apart
+ */
+int32_t rls_token_logprobs_backward(const void *logits_dev, int32_t logits_type, int64_t rows, int64_t n_choices, int64_t ld_logits,
+                                    const int32_t *token_dev, const float *temperature_dev, const float *norm_dev, const float *entropy_dev,
+                                    const float *dlogprob_dev, const float *dentropy_dev, void *dlogits_dev, int64_t ld_dlogits, void *stream);
+/*
+ * Learning from a teacher of which only its best entries are kept (what rls_token_logprobs lists): per row
+ *   p = the probabilities that the k given logits, or log-probabilities, have among themselves at the row's temperature
+ *   loss = sum of p_j (log p_j - log q_token_j), with q the probabilities of all of the row's own logits at that temperature
+ * A token outside 0 .. n_choices - 1, and a teacher's logit of -infinity or NaN, is no entry; a token may come more than once (its
+ * probabilities add up in the gradient).  A row without an entry has loss 0 and no gradient; one whose entry of probability above 0 is masked
+ * has loss +infinity.  The teacher is a constant: nothing is differentiated by it.
+ *   teacher_token_dev  [rows][k] int32;  teacher_logits_dev [rows][k] of teacher_type;  1 <= k <= RLS_MAX_TOP
+ *   loss_dev         [rows] fp32 (written);  norm_dev [rows][2] fp32 (written) or null, as above; the other arguments as above
+ */
+int64_t rls_distill_loss_workspace_bytes(int64_t rows, int64_t n_choices);
+int32_t rls_distill_loss(const void *logits_dev, int32_t logits_type, int64_t rows, int64_t n_choices, int64_t ld_logits, const int32_t *teacher_token_dev,
+                         const void *teacher_logits_dev, int32_t teacher_type, int32_t k, const float *temperature_dev, float *loss_dev, float *norm_dev,
+                         void *workspace_dev, int64_t workspace_bytes, void *stream);
+/* Gradient by the logits: dx_i = inv dloss (q_i - sum of p_j over the entries with token_j = i);  dloss_dev [rows] fp32, dlogits as above. */
+int32_t rls_distill_loss_backward(const void *logits_dev, int32_t logits_type, int64_t rows, int64_t n_choices, int64_t ld_logits,
+                                  const int32_t *teacher_token_dev, const void *teacher_logits_dev, int32_t teacher_type, int32_t k,
+                                  const float *temperature_dev, const float *norm_dev, const float *dloss_dev, void *dlogits_dev, int64_t ld_dlogits,
+                                  void *stream);
 
 /* A [batch][steps][channels] array: channels side by side, any strides (in elements) between steps and sequences.  Read-only
  * ones may repeat themselves (stride 0); written ones must not overlap themselves or anything else (RLS_ERR_SHAPE; views that lie between

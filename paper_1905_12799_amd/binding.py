@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -20,6 +20,7 @@ RLS_STATUS_NONFINITE = 1
 RLS_STATUS_RANGE = 2
 MAX_D, MAX_K, MAX_DEPTH = 32, 128, 12
 MAX_CHOICES = 1 << 24
+MAX_TOP = 128
 F32, BF16, F16 = 0, 1, 2
 _TYPE_OF = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 
@@ -115,6 +116,18 @@ def lib() -> ctypes.CDLL:
         L.rls_sample_workspace_bytes.argtypes = [i64, i64]
         L.rls_sample.restype = i32
         L.rls_sample.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.rls_token_logprobs_workspace_bytes.restype = i64
+        L.rls_token_logprobs_workspace_bytes.argtypes = [i64, i64, i32]
+        L.rls_token_logprobs.restype = i32
+        L.rls_token_logprobs.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.rls_token_logprobs_backward.restype = i32
+        L.rls_token_logprobs_backward.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.rls_distill_loss_workspace_bytes.restype = i64
+        L.rls_distill_loss_workspace_bytes.argtypes = [i64, i64]
+        L.rls_distill_loss.restype = i32
+        L.rls_distill_loss.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, i32, vp, vp, vp, vp, i64, vp]
+        L.rls_distill_loss_backward.restype = i32
+        L.rls_distill_loss_backward.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, i32, vp, vp, vp, vp, i64, vp]
         seq = vp                                         # addresses within one array: see _sequences
         L.rls_linear_scan_workspace_bytes.restype = i64
         L.rls_linear_scan_workspace_bytes.argtypes = [i64, i64, i64]
@@ -545,6 +558,176 @@ def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature: Optional[to
     if out is not None:
         _written(out)
     return token, logprob
+
+
+class LogProbs(NamedTuple):
+    """What token_logprobs returns, a row each: fp32, the tokens int32; None where it was not asked for."""
+    logprob: Optional[torch.Tensor]                      # [rows]
+    entropy: torch.Tensor                                # [rows]
+    top_logprob: Optional[torch.Tensor]                  # [rows, top]
+    top_token: Optional[torch.Tensor]                    # [rows, top]
+    norm: torch.Tensor                                   # [rows, 2]: the largest logit, and the logarithm of the sum of exponentials
+
+
+def token_logprobs_workspace_bytes(rows: int, n_choices: int, top: int = 0) -> int:
+    n = int(lib().rls_token_logprobs_workspace_bytes(rows, n_choices, top))
+    if n < 0:
+        raise RlsError(n, "rls_token_logprobs_workspace_bytes")
+    return n
+
+
+def _logits(t: torch.Tensor, name: str = "logits") -> Tuple[int, int, int, int, int]:
+    """(address, type, rows, columns, distance of the rows) of a matrix of logits."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in _TYPE_OF or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be an fp32, bf16 or fp16 device matrix with unit stride along a row")
+    rows, n = t.shape
+    return t.data_ptr(), _TYPE_OF[t.dtype], rows, n, t.stride(0) if rows > 1 else n
+
+
+def _rows_of(t: Optional[torch.Tensor], shape, dtype: torch.dtype, name: str) -> int:
+    """Address of a contiguous array of that shape (0 for None)."""
+    if t is None:
+        return 0
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    return _dev(t, dtype, name).data_ptr()
+
+
+def _gradient_of(logits: torch.Tensor, out: Optional[torch.Tensor]) -> Tuple[torch.Tensor, int, int]:
+    """Where the gradient by logits goes: the tensor, its address and the distance of its rows."""
+    if out is None:
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    elif out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must have the shape and the type of the logits")
+    at, _, _, _, ld = _logits(out, "out")
+    return out, at, ld
+
+
+def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], temperature: Optional[torch.Tensor] = None, top: int = 0,
+                   workspace: Optional[torch.Tensor] = None) -> LogProbs:
+    """Log-probability of tokens [rows] (int32; outside the row: 0, a padded position) under logits [rows, n_choices] (fp32, bf16 or fp16, rows
+    contiguous), the entropy of every row, and its `top` best entries with their log-probabilities (at most MAX_TOP; -1 where there are fewer).
+
+    temperature (fp32) has an entry per row.  tokens may be None.  logprob and entropy are differentiable by the logits."""
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return LogProbs(*_LogProbs.apply(logits, tokens, temperature, top, workspace))
+    at, kind, rows, n, ld = _logits(logits)
+    device = logits.device
+    token_at, temperature_at = _rows_of(tokens, (rows,), torch.int32, "tokens"), _rows_of(temperature, (rows,), torch.float32, "temperature")
+    ws, base, avail = _space(workspace, lambda: token_logprobs_workspace_bytes(rows, n, top), device)
+    entropy = torch.empty(rows, dtype=torch.float32, device=device)
+    logprob = None if tokens is None else torch.empty_like(entropy)
+    norm = torch.empty((rows, 2), dtype=torch.float32, device=device)
+    best = best_token = None
+    if top > 0:
+        best, best_token = torch.empty((rows, top), dtype=torch.float32, device=device), torch.empty((rows, top), dtype=torch.int32, device=device)
+    _check(lib().rls_token_logprobs(at, kind, rows, n, ld, token_at, temperature_at, top, 0 if tokens is None else logprob.data_ptr(), entropy.data_ptr(),
+                                    best.data_ptr() if top > 0 else 0, best_token.data_ptr() if top > 0 else 0, norm.data_ptr(), base, avail,
+                                    _raw_stream(logits.get_device())), "rls_token_logprobs")
+    return LogProbs(logprob, entropy, best, best_token, norm)
+
+
+class _LogProbs(torch.autograd.Function):
+    """token_logprobs as autograd sees it: logprob and entropy are differentiable, the alternatives and norm are not."""
+
+    @staticmethod
+    def forward(ctx, logits, tokens, temperature, top, workspace):
+        r = token_logprobs(logits, tokens, temperature, top, workspace)
+        ctx.save_for_backward(logits, tokens, temperature, r.norm, r.entropy)
+        ctx.mark_non_differentiable(*(t for t in (r.top_logprob, r.top_token, r.norm) if t is not None))
+        ctx.set_materialize_grads(False)
+        return tuple(r)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dlogprob, dentropy, *_):
+        logits, tokens, temperature, norm, entropy = ctx.saved_tensors
+        if dlogprob is None and dentropy is None:
+            return None, None, None, None, None
+        dlogprob, dentropy = (None if d is None else d.contiguous() for d in (dlogprob, dentropy))
+        return token_logprobs_backward(logits, tokens, norm, entropy, dlogprob, dentropy, temperature), None, None, None, None
+
+
+def token_logprobs_backward(logits: torch.Tensor, tokens: Optional[torch.Tensor], norm: torch.Tensor, entropy: Optional[torch.Tensor],
+                            dlogprob: Optional[torch.Tensor], dentropy: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient by the logits, in their type, from the norm and entropy that token_logprobs returned and the gradients by logprob and entropy
+    (either may be None).  `out` may be logits itself."""
+    at, kind, rows, n, ld = _logits(logits)
+    row = lambda t, dtype, name: _rows_of(t, (rows,), dtype, name)       # noqa: E731
+    dlogits, to, ld_to = _gradient_of(logits, out)
+    _check(lib().rls_token_logprobs_backward(at, kind, rows, n, ld, row(tokens, torch.int32, "tokens"), row(temperature, torch.float32, "temperature"),
+                                             _rows_of(norm, (rows, 2), torch.float32, "norm"), row(entropy, torch.float32, "entropy"),
+                                             row(dlogprob, torch.float32, "dlogprob"), row(dentropy, torch.float32, "dentropy"), to, ld_to,
+                                             _raw_stream(logits.get_device())), "rls_token_logprobs_backward")
+    if out is not None:
+        _written(out)
+    return dlogits
+
+
+def distill_loss_workspace_bytes(rows: int, n_choices: int) -> int:
+    n = int(lib().rls_distill_loss_workspace_bytes(rows, n_choices))
+    if n < 0:
+        raise RlsError(n, "rls_distill_loss_workspace_bytes")
+    return n
+
+
+def _teacher(tokens: torch.Tensor, logits: torch.Tensor, rows: int) -> Tuple[int, int, int, int]:
+    if logits.dim() != 2 or logits.shape[0] != rows or logits.dtype not in _TYPE_OF:
+        raise ValueError("teacher_logits must be [rows, k] in fp32, bf16 or fp16")
+    return (_rows_of(tokens, logits.shape, torch.int32, "teacher_tokens"), _dev(logits, logits.dtype, "teacher_logits").data_ptr(),
+            _TYPE_OF[logits.dtype], logits.shape[1])
+
+
+def distill_loss(logits: torch.Tensor, teacher_tokens: torch.Tensor, teacher_logits: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Divergence of every row of logits [rows, n_choices] from the distribution that the teacher's k best entries have among themselves: (loss fp32
+    [rows], norm fp32 [rows, 2] as token_logprobs returns it).
+
+    teacher_tokens int32 and teacher_logits (fp32, bf16 or fp16; logits or log-probabilities, such as token_logprobs' alternatives) are [rows, k],
+    k at most MAX_TOP; a token outside the row is no entry.  temperature (fp32) has an entry per row.  The loss is differentiable by the logits."""
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return _Distill.apply(logits, teacher_tokens, teacher_logits, temperature, workspace)
+    at, kind, rows, n, ld = _logits(logits)
+    token_at, teacher_at, teacher_kind, k = _teacher(teacher_tokens, teacher_logits, rows)
+    ws, base, avail = _space(workspace, lambda: distill_loss_workspace_bytes(rows, n), logits.device)
+    loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    norm = torch.empty((rows, 2), dtype=torch.float32, device=logits.device)
+    _check(lib().rls_distill_loss(at, kind, rows, n, ld, token_at, teacher_at, teacher_kind, k, _rows_of(temperature, (rows,), torch.float32, "temperature"),
+                                  loss.data_ptr(), norm.data_ptr(), base, avail, _raw_stream(logits.get_device())), "rls_distill_loss")
+    return loss, norm
+
+
+class _Distill(torch.autograd.Function):
+    """distill_loss as autograd sees it."""
+
+    @staticmethod
+    def forward(ctx, logits, teacher_tokens, teacher_logits, temperature, workspace):
+        loss, norm = distill_loss(logits, teacher_tokens, teacher_logits, temperature, workspace)
+        ctx.save_for_backward(logits, teacher_tokens, teacher_logits, temperature, norm)
+        ctx.mark_non_differentiable(norm)
+        return loss, norm
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss, _):
+        logits, teacher_tokens, teacher_logits, temperature, norm = ctx.saved_tensors
+        return distill_loss_backward(logits, teacher_tokens, teacher_logits, norm, dloss.contiguous(), temperature), None, None, None, None
+
+
+def distill_loss_backward(logits: torch.Tensor, teacher_tokens: torch.Tensor, teacher_logits: torch.Tensor, norm: torch.Tensor, dloss: torch.Tensor,
+                          temperature: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient by the logits, in their type, from the norm that distill_loss returned and the gradient dloss [rows].  `out` may be logits itself."""
+    at, kind, rows, n, ld = _logits(logits)
+    token_at, teacher_at, teacher_kind, k = _teacher(teacher_tokens, teacher_logits, rows)
+    dlogits, to, ld_to = _gradient_of(logits, out)
+    _check(lib().rls_distill_loss_backward(at, kind, rows, n, ld, token_at, teacher_at, teacher_kind, k,
+                                           _rows_of(temperature, (rows,), torch.float32, "temperature"), _rows_of(norm, (rows, 2), torch.float32, "norm"),
+                                           _rows_of(dloss, (rows,), torch.float32, "dloss"), to, ld_to, _raw_stream(logits.get_device())),
+           "rls_distill_loss_backward")
+    if out is not None:
+        _written(out)
+    return dlogits
 
 
 def linear_scan_workspace_bytes(batch: int, steps: int, channels: int) -> int:
