@@ -20,6 +20,7 @@
  *   rls_linear_scan     the gated linear recurrence h_t = a_t h_{t-1} + b_t, and its backward pass
  *   rls_token_logprobs  log-probabilities of given entries of rows of logits, entropy, the best alternatives, and their gradient
  *   rls_distill_loss    the divergence of rows of logits from a teacher's best entries, and its gradient
+ *   rls_gated_delta     the gated delta rule, a recurrence with a matrix per head for its state, and its backward pass
  *   rls_adamw_step      one AdamW step over all tensors of a model, moments in 32 or in 8 bits
  *
  * Conventions
@@ -419,6 +420,52 @@ int32_t rls_linear_scan(const rls_scan_shape *shape, const rls_sequence *a, cons
 int32_t rls_linear_scan_backward(const rls_scan_shape *shape, const rls_sequence *a, const rls_sequence *h, const rls_sequence *dh,
                                  const float *h0_dev, const uint8_t *reset_dev, const float *dh_last_dev, const rls_sequence *da,
                                  const rls_sequence *db, float *dh0_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
+
+/* A [batch][steps][heads][dim] array: dimensions side by side, any strides (in elements) between heads, steps and sequences.  Read-only ones may
+ * repeat themselves (stride 0); written ones must not overlap themselves or anything else (RLS_ERR_SHAPE). */
+typedef struct {
+    void *data_dev;
+    int64_t batch_stride, step_stride, head_stride;
+} rls_heads;
+
+typedef struct {
+    int64_t batch, steps;
+    int32_t heads;             /* of v, o, g, beta and the state */
+    int32_t key_heads;         /* of q and k; heads is a multiple, and head h reads key head h / (heads / key_heads) */
+    int32_t key_dim, value_dim;
+    int32_t type;              /* of q, k, v, o and their gradients: RLS_F32, RLS_BF16 or RLS_F16 */
+    float scale;               /* of the output */
+} rls_delta_shape;
+
+/*
+ * The gated delta rule: a recurrent layer beside rls_linear_scan whose state is a matrix S [key_dim][value_dim] per sequence and head.  Per step
+ *   S = exp(g_t) S;  y_t = v_t - S^T k_t;  S = S + beta_t k_t y_t^T;  o_t = scale S^T q_t,   all in fp32, o rounded to `type`
+ * It replaces what the state answers to a key by the step's value, in part (beta) and after forgetting (g).
+ *   g_dev       [batch][steps][heads] fp32, logarithms of the decay: 0 keeps everything, less than -87 (or -infinity) nothing
+ *   beta_dev    [batch][steps][heads] fp32
+ *   reset_dev   [batch][steps] bytes or null: where one is not 0 a sequence begins, and nothing is carried over from the step before
+ *   state_dev   [batch][heads][key_dim][value_dim] fp32, before the first step, or null (0)
+ *   o           (written);  last_dev as state_dev (written) or null, after the last step; it may be state_dev itself: a state kept in place
+ * steps = 0 leaves o alone and copies the state.  Keys of length 1 and beta in 0 .. 1 (2) keep the state in bounds; others are computed
+ * as they are.  Steps are taken in chunks whose decays are products: g above 0 may overflow within 64 steps where step by step it would not.
+ * Inputs or states that are not finite make what the same head computes in that call not finite, before and after them as well.
+ * 1 <= key_dim <= RLS_MAX_KEY_DIM, 1 <= value_dim <= RLS_MAX_VALUE_DIM, batch * heads <= 2^17, batch * steps <= 2^30.
+ */
+#define RLS_MAX_KEY_DIM 128
+#define RLS_MAX_VALUE_DIM 512
+int64_t rls_gated_delta_workspace_bytes(const rls_delta_shape *shape, int32_t backward);
+int32_t rls_gated_delta(const rls_delta_shape *shape, const rls_heads *q, const rls_heads *k, const rls_heads *v, const float *g_dev, const float *beta_dev,
+                        const float *state_dev, const uint8_t *reset_dev, const rls_heads *o, float *last_dev, void *workspace_dev, int64_t workspace_bytes,
+                        void *stream);
+/*
+ * Its backward pass, from the inputs (the states are computed again) and the gradients dout by o and dlast (null: 0) by the last state.
+ *   dq, dk, dv  (written) as q, k, v, summed over the heads that share a key head;  dg_dev, dbeta_dev (written) as g, beta: dg is 0 where nothing is carried
+ *   dstate_dev  (written) as state_dev, or null; may be dlast_dev's memory
+ */
+int32_t rls_gated_delta_backward(const rls_delta_shape *shape, const rls_heads *q, const rls_heads *k, const rls_heads *v, const float *g_dev,
+                                 const float *beta_dev, const float *state_dev, const uint8_t *reset_dev, const rls_heads *dout, const float *dlast_dev,
+                                 const rls_heads *dq, const rls_heads *dk, const rls_heads *dv, float *dg_dev, float *dbeta_dev, float *dstate_dev,
+                                 void *workspace_dev, int64_t workspace_bytes, void *stream);
 
 /*
  * One AdamW step (Table 2's optimizer, with decoupled weight decay) over any number of tensors.  Per element, in fp32:

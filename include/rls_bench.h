@@ -59,6 +59,10 @@ int32_t rls_scan_wait_limit(int64_t ticks);
 /* Whether two arrays of a linear scan count as overlapping (1 or 0): what its calls turn down where one of the two is written. */
 int32_t rls_scan_overlap(const rls_scan_shape *shape, const rls_sequence *x, int32_t x_type, const rls_sequence *y, int32_t y_type);
 
+/* Workspace that the chunks of one launch of a gated delta rule may take together before its sequences are cut into segments, a few launches
+ * each, for the calls of the host thread that sets it; 0: a chunk of every head at a time; a negative value restores the default.  For tests. */
+int32_t rls_delta_segment_bytes(int64_t bytes);
+
 #ifdef __cplusplus
 }
 #endif

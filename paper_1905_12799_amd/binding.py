@@ -50,6 +50,15 @@ class _ScanShape(ctypes.Structure):
                 ("gate_type", ctypes.c_int32), ("reverse", ctypes.c_int32)]
 
 
+class _DeltaShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("steps", ctypes.c_int64), ("heads", ctypes.c_int32), ("key_heads", ctypes.c_int32), ("key_dim", ctypes.c_int32),
+                ("value_dim", ctypes.c_int32), ("type", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data_dev", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("step_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 class _AdamwTensor(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int64), ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("param_dev", ctypes.c_void_p),
                 ("grad_dev", ctypes.c_void_p), ("master_dev", ctypes.c_void_p), ("m_dev", ctypes.c_void_p), ("v_dev", ctypes.c_void_p),
@@ -135,6 +144,12 @@ def lib() -> ctypes.CDLL:
         L.rls_linear_scan.argtypes = [ctypes.POINTER(_ScanShape), seq, seq, vp, vp, seq, vp, vp, i64, vp]
         L.rls_linear_scan_backward.restype = i32
         L.rls_linear_scan_backward.argtypes = [ctypes.POINTER(_ScanShape), seq, seq, seq, vp, vp, vp, seq, seq, vp, vp, i64, vp]
+        L.rls_gated_delta_workspace_bytes.restype = i64
+        L.rls_gated_delta_workspace_bytes.argtypes = [ctypes.POINTER(_DeltaShape), i32]
+        L.rls_gated_delta.restype = i32
+        L.rls_gated_delta.argtypes = [ctypes.POINTER(_DeltaShape), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.rls_gated_delta_backward.restype = i32
+        L.rls_gated_delta_backward.argtypes = [ctypes.POINTER(_DeltaShape), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
         L.rls_adamw_step.restype = i32
         L.rls_adamw_step.argtypes = [ctypes.POINTER(_AdamwTensor), i32, ctypes.POINTER(_AdamwOptions), vp]
         L.rls_profile_enable.restype = i32
@@ -841,6 +856,113 @@ def linear_scan_backward(a: torch.Tensor, h: torch.Tensor, dh: torch.Tensor, h0:
                                           _states(dh_last, size, "dh_last"), at[3], at[4], dh0.data_ptr(), base, avail, _raw_stream(h.get_device())),
            "rls_linear_scan_backward")
     return da, db, dh0
+
+
+def gated_delta_workspace_bytes(batch: int, steps: int, heads: int, key_heads: int, key_dim: int, value_dim: int, backward: bool = False) -> int:
+    shape = _DeltaShape(batch, steps, heads, key_heads, key_dim, value_dim, F32, 1.0)
+    n = int(lib().rls_gated_delta_workspace_bytes(ctypes.byref(shape), 1 if backward else 0))
+    if n < 0:
+        raise RlsError(n, "rls_gated_delta_workspace_bytes")
+    return n
+
+
+def _delta_shape(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: Optional[float]) -> _DeltaShape:
+    if q.dim() != 4 or v.dim() != 4 or q.shape != k.shape or q.shape[:2] != v.shape[:2] or q.dtype not in _TYPE_OF:
+        raise ValueError("q and k are [batch, steps, key_heads, key_dim], v is [batch, steps, heads, value_dim], all in fp32, bf16 or fp16")
+    B, T, key_heads, key_dim = q.shape
+    return _DeltaShape(B, T, v.shape[2], key_heads, key_dim, v.shape[3], _TYPE_OF[q.dtype], key_dim ** -0.5 if scale is None else scale)
+
+
+def _heads(dtype: torch.dtype, *named):
+    """rls_heads structs of (tensor, shape, name) side by side in one array, and their addresses; the array has to outlive the call."""
+    numbers = []
+    for t, shape, name in named:
+        if t.dtype != dtype or t.shape != shape or not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor of shape {tuple(shape)} and type {dtype}")
+        per_batch, per_step, per_head, one = t.stride()
+        if one != 1 and shape[3] > 1:
+            raise ValueError(f"{name} must have unit stride along its last dimension")
+        numbers += (t.data_ptr(), per_batch, per_step, per_head)
+    held = (ctypes.c_int64 * len(numbers))(*numbers)
+    base = ctypes.addressof(held)
+    return held, range(base, base + ctypes.sizeof(held), ctypes.sizeof(_Heads))
+
+
+def _delta_gates(v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor) -> Tuple[int, int]:
+    shape = v.shape[:3]
+    return _rows_of(g, shape, torch.float32, "g"), _rows_of(beta, shape, torch.float32, "beta")
+
+
+def gated_delta(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor, state: Optional[torch.Tensor] = None,
+                reset: Optional[torch.Tensor] = None, scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, last: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The gated delta rule over [batch, steps, heads, dim]: S = exp(g) S + beta k (v - exp(g) S^T k)^T, o = scale S^T q, with a matrix S [key_dim,
+    value_dim] per sequence and head: (o like v, the last state in fp32 [batch, heads, key_dim, value_dim]).
+
+    q and k may have fewer heads than v; g (logarithms of the decay) and beta are fp32 [batch, steps, heads]; reset [batch, steps] (bytes or bools) is set
+    where a sequence begins; scale is key_dim ** -0.5 unless given.  `last` may be state itself, for a state that is updated in place.  Differentiable
+    by q, k, v, g, beta and state."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, g, beta, state)):
+        if out is not None or last is not None:
+            raise ValueError("out and last are for calls that nothing is differentiated by (torch.no_grad)")
+        return _Delta.apply(q, k, v, g, beta, state, reset, scale, workspace)
+    shape = _delta_shape(q, k, v, scale)
+    size, states = v.shape, (v.shape[0], v.shape[2], q.shape[3], v.shape[3])
+    o = torch.empty_like(v, memory_format=torch.contiguous_format) if out is None else out
+    kept = last is not None
+    if not kept:
+        last = torch.empty(states, dtype=torch.float32, device=v.device) if state is None else torch.empty_like(state, memory_format=torch.contiguous_format)
+    ws, base, avail = _space(workspace, lambda: gated_delta_workspace_bytes(size[0], size[1], size[2], q.shape[2], q.shape[3], size[3]), v.device)
+    held, at = _heads(q.dtype, (q, q.shape, "q"), (k, q.shape, "k"), (v, size, "v"), (o, size, "out"))
+    g_at, beta_at = _delta_gates(v, g, beta)
+    _check(lib().rls_gated_delta(ctypes.byref(shape), at[0], at[1], at[2], g_at, beta_at, _rows_of(state, states, torch.float32, "state"), _resets(reset, size),
+                                 at[3], _rows_of(last, states, torch.float32, "last"), base, avail, _raw_stream(v.get_device())), "rls_gated_delta")
+    if out is not None:
+        _written(o)
+    if kept:
+        _written(last)
+    return o, last
+
+
+class _Delta(torch.autograd.Function):
+    """gated_delta as autograd sees it: both its results are differentiable."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, g, beta, state, reset, scale, workspace):
+        o, last = gated_delta(q, k, v, g, beta, state, reset, scale, workspace)
+        ctx.save_for_backward(q, k, v, g, beta, state, reset)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return o, last
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, do, dlast):
+        q, k, v, g, beta, state, reset = ctx.saved_tensors
+        do = torch.zeros_like(v, memory_format=torch.contiguous_format) if do is None else do
+        if do.stride(-1) != 1:
+            do = do.contiguous()
+        grads = gated_delta_backward(q, k, v, g, beta, do, state, reset, None if dlast is None else dlast.contiguous(), ctx.scale)
+        return (*grads[:5], None if state is None else grads[5], None, None, None)
+
+
+def gated_delta_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tensor, beta: torch.Tensor, do: torch.Tensor,
+                         state: Optional[torch.Tensor] = None, reset: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None,
+                         scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, ...]:
+    """Gradients of gated_delta from its inputs and the gradients by its results: (dq, dk, dv in their types, dg, dbeta and dstate in fp32).
+
+    Where an input was an expanded view, its gradient is that of every element: the sum along the expanded axes is the input's."""
+    shape = _delta_shape(q, k, v, scale)
+    size, states = v.shape, (v.shape[0], v.shape[2], q.shape[3], v.shape[3])
+    dq, dk, dv, dg, dbeta = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v, g, beta))
+    dstate = torch.empty(states, dtype=torch.float32, device=v.device)
+    ws, base, avail = _space(workspace, lambda: gated_delta_workspace_bytes(size[0], size[1], size[2], q.shape[2], q.shape[3], size[3], True), v.device)
+    held, at = _heads(q.dtype, (q, q.shape, "q"), (k, q.shape, "k"), (v, size, "v"), (do, size, "do"), (dq, q.shape, "dq"), (dk, q.shape, "dk"), (dv, size, "dv"))
+    g_at, beta_at = _delta_gates(v, g, beta)
+    _check(lib().rls_gated_delta_backward(ctypes.byref(shape), at[0], at[1], at[2], g_at, beta_at, _rows_of(state, states, torch.float32, "state"),
+                                          _resets(reset, size), at[3], _rows_of(dlast, states, torch.float32, "dlast"), at[4], at[5], at[6], dg.data_ptr(),
+                                          dbeta.data_ptr(), dstate.data_ptr(), base, avail, _raw_stream(v.get_device())), "rls_gated_delta_backward")
+    return dq, dk, dv, dg, dbeta, dstate
 
 
 class AdamW:

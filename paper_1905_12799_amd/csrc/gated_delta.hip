@@ -1,0 +1,1105 @@
+// The gated delta rule: a recurrence whose state is a matrix per head (rls.h gives the formulas), and its backward pass.
+//
+// Few steps are taken one by one, the state in registers: it is read and written once, which bounds it.
+//
+// Many are taken in chunks of 64.  With the sums of log-decays gamma inside a chunk, the state S0 before it, and over its steps i, j
+//   a_i = exp(gamma_i), D_ij = exp(gamma_i - gamma_j) for j <= i, c_j = D_63,j, G = D . (K K^T) below the diagonal, P = D . (Q K^T),
+// where what a reset lies between is 0, the differences y_i = v_i - (decayed state)^T k_i of all steps are one triangular system,
+//   (1 + G beta) Y = V - a . (K S0),  so with X = (1 + G beta)^-1   Y = X V - (X a K) S0,  S1 = a_63 S0 + (c beta K)^T Y,
+//   O = scale (a . (Q S0) + P (beta Y)).
+// X, X V and X a K are made for all chunks at once, then a chain of two products per chunk runs for 16 columns of the state at a time,
+// then all outputs at once.  The backward pass has the same shape, with a chain from the last chunk to the first:
+//   dY = X^T beta (scale P^T dO + c . (K dS1)),  dS0 = a_63 dS1 + scale (a Q)^T dO - (a K)^T dY.
+// All products are taken by the fp32 matrix instructions (16x16x4), whatever the inputs' type: the state is handed back in fp32 and what it
+// is made of must not be rounded to fewer bits on the way.  Their rate bounds the chunked forms.
+#include <algorithm>
+
+#include "element_types.h"
+#include "rls_internal.h"
+#include "wave.h"
+
+namespace rls {
+
+namespace {
+
+constexpr int kChunk = 64;
+constexpr int kEdge = kChunk + 4;                        // row of a chunk x chunk matrix in LDS (4 modulo 16: no bank is asked twice, by rows or by columns)
+constexpr float kNoCarry = -87.0f;                       // exp of less is below the smallest normal number
+
+using f4 = vec4<float>;
+
+struct Heads {
+    void *data;
+    int64_t batch, step, head;                           // distances in elements
+};
+struct DeltaArgs {
+    Heads q, k, v, o, dout, dq, dk, dv;
+    const float *g, *beta;                               // [batch][steps][heads]
+    const uint8_t *reset;                                // [batch][steps]
+    const float *state;                                  // before the first chunk of the launch, [batch * heads][dk][dv], or null
+    float *last;                                         // after the last one
+    float *dg, *dbeta;
+    int64_t batch, steps, chunk0;                        // the launch takes chunks chunk0 .. chunk0 + chunks - 1
+    int32_t heads, group, chunks;                        // group: heads that share a key head
+    int32_t key_dim, value_dim, columns;                 // columns: value_dim rounded up to 64
+    float scale;
+    // workspace, an entry per (head, chunk of the launch)
+    float *w, *y, *mt, *s, *x, *dy, *ds, *gq, *gk;       // [64][DK], [64][columns], [DK][64], [DK][columns], [64][64], [64][columns], [DK][columns], [64][DK] x 2
+    float *carry;                                        // a_63
+    int32_t keep;                                        // x is written
+    int32_t backward;                                    // direction of the chain
+};
+
+template <typename T>
+__device__ inline const T *at(const Heads &h, int64_t b, int64_t t, int64_t head)
+{
+    return static_cast<const T *>(h.data) + b * h.batch + t * h.step + head * h.head;
+}
+template <typename T>
+__device__ inline T *out_at(const Heads &h, int64_t b, int64_t t, int64_t head)
+{
+    return static_cast<T *>(h.data) + b * h.batch + t * h.step + head * h.head;
+}
+
+// ---- matrix instructions ----------------------------------------------------------------------------------------------
+// An operand of 16 x 16 x 16: lane l has four numbers along the axis that is summed over, from 4 (l / 16) on, of row (or column) l % 16.  A result
+// has the same form with its rows in the place of that axis, so it can be the next product's right operand as it is.
+
+__device__ inline int lane16() { return threadIdx.x & 15; }
+__device__ inline int lane4() { return (threadIdx.x & 63) >> 4 << 2; }
+
+__device__ inline f4 mm(f4 a, f4 b, f4 c)
+{
+#pragma unroll
+    for (int m = 0; m < 4; ++m) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[m], b[m], c, 0, 0, 0);
+    return c;
+}
+// the summed axis along the rows of memory
+__device__ inline f4 along(const float *p, int ld, int row, int k)
+{
+    return *reinterpret_cast<const f4 *>(p + (row + lane16()) * ld + k + lane4());
+}
+// and across them
+__device__ inline f4 across(const float *p, int ld, int k, int column)
+{
+    const float *const q = p + (k + lane4()) * ld + column + lane16();
+    return f4{q[0], q[ld], q[2 * ld], q[3 * ld]};
+}
+__device__ inline void put(float *p, int ld, int row, int column, f4 v)
+{
+    float *const q = p + (row + lane4()) * ld + column + lane16();
+#pragma unroll
+    for (int m = 0; m < 4; ++m) q[m * ld] = v[m];
+}
+__device__ inline f4 four(const float *p, int k) { return *reinterpret_cast<const f4 *>(p + k + lane4()); }
+
+// The tiles on and below the diagonal of a chunk x chunk matrix
+constexpr int kLower = 10;
+__device__ inline void lower_tile(int u, int &ti, int &tj)
+{
+    ti = u < 1 ? 0 : u < 3 ? 1 : u < 6 ? 2 : 3;
+    tj = u - ti * (ti + 1) / 2;
+}
+
+// ---- the gates of a chunk ----------------------------------------------------------------------------------------------
+
+struct alignas(16) Gates {
+    double gamma[kChunk];
+    float beta[kChunk], a[kChunk], c[kChunk];
+    int32_t part[kChunk];                                // resets up to here
+    uint8_t cut[kChunk];
+
+    // by the first wave; the others see it after a barrier
+    __device__ void load(const DeltaArgs &p, int64_t b, int64_t head, int64_t t0)
+    {
+        const int l = threadIdx.x;
+        if (l >= kChunk) return;
+        const int64_t t = t0 + l;
+        const bool in = t < p.steps;
+        const int64_t i = (b * p.steps + t) * p.heads + head;
+        const float g = in ? p.g[i] : 0.0f;
+        const bool no_carry = in && (g < kNoCarry || (p.reset && p.reset[b * p.steps + t] != 0));
+        beta[l] = in ? p.beta[i] : 0.0f;
+        cut[l] = no_carry;
+        double sum = no_carry ? 0.0 : (double)g;
+        for (int d = 1; d < kChunk; d <<= 1) {
+            const double before = __shfl_up(sum, d);
+            if (l >= d) sum += before;
+        }
+        const uint64_t cuts = __ballot(no_carry);
+        const int before = __popcll(cuts & (l == 63 ? ~0ull : (1ull << (l + 1)) - 1));
+        gamma[l] = sum;
+        part[l] = before;
+        a[l] = before == 0 ? expf((float)sum) : 0.0f;
+        const double end = __shfl(sum, 63);
+        c[l] = before == __popcll(cuts) ? expf((float)(end - sum)) : 0.0f;
+    }
+    __device__ float decay(int i, int j) const { return j <= i && part[i] == part[j] ? expf((float)(gamma[i] - gamma[j])) : 0.0f; }
+};
+
+// 64 rows of a head from step t0 on, `width` columns from `column` on, as fp32 in LDS; 0 behind the last step and the last column
+template <typename T>
+__device__ inline void load_rows(float *to, int ld, const DeltaArgs &p, const Heads &h, int64_t b, int64_t head, int64_t t0, int column, int width, int columns)
+{
+    constexpr int N = 16 / sizeof(T);
+    const int packs = width / N;
+    for (int u = threadIdx.x; u < kChunk * packs; u += blockDim.x) {
+        const int row = u / packs, at0 = u % packs * N, first = column + at0;
+        float x[N];
+        const bool in = t0 + row < p.steps;
+        const T *const from = at<T>(h, b, t0 + row, head) + first;
+        if (in && first + N <= columns) {
+            T raw[N];
+            __builtin_memcpy(raw, from, 16);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = (float)raw[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[i] = 0.0f;
+                if (in && first + i < columns) x[i] = (float)from[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<f4 *>(to + row * ld + at0 + i) = f4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+    }
+}
+// the same from 64 rows of the workspace
+__device__ inline void load_kept(float *to, int ld, const float *from, int ld_from, int column, int width)
+{
+    const int packs = width / 4;
+    for (int u = threadIdx.x; u < kChunk * packs; u += blockDim.x) {
+        const int row = u / packs, at0 = u % packs * 4;
+        *reinterpret_cast<f4 *>(to + row * ld + at0) = *reinterpret_cast<const f4 *>(from + (int64_t)row * ld_from + column + at0);
+    }
+}
+
+// ---- all chunks at once: X, X V, -(X a K), (c beta K)^T -----------------------------------------------------------------
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(DK * 4) delta_prepare_kernel(DeltaArgs p)
+{
+    constexpr int W = DK / 16, LD = DK + 4;              // waves: one for every 16 key dimensions
+    __shared__ Gates gates;
+    __shared__ __attribute__((aligned(16))) float k[kChunk * LD], x[kChunk * kEdge], n[kChunk * kEdge];
+    const int wave = threadIdx.x >> 6;
+    const int64_t unit = blockIdx.x, bh = unit / p.chunks, b = bh / p.heads, head = bh % p.heads, t0 = (p.chunk0 + unit % p.chunks) * kChunk;
+    gates.load(p, b, head, t0);
+    load_rows<T>(k, LD, p, p.k, b, head / p.group, t0, 0, DK, p.key_dim);
+    __syncthreads();
+    for (int u = wave; u < kLower; u += W) {
+        int ti, tj;
+        lower_tile(u, ti, tj);
+        f4 acc{};
+#pragma unroll
+        for (int kb = 0; kb < DK; kb += 16) acc = mm(along(k, LD, ti * 16, kb), along(k, LD, tj * 16, kb), acc);
+        const int j = tj * 16 + lane16();
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int i = ti * 16 + lane4() + m;
+            acc[m] = j < i ? acc[m] * gates.decay(i, j) * gates.beta[j] : 0.0f;
+        }
+        put(n, kEdge, ti * 16, tj * 16, acc);
+    }
+    __syncthreads();
+    // blocks on the diagonal: a lane solves for a column
+    for (int d = wave; d < 4; d += W) {
+        const int column = threadIdx.x & 63;
+        if (column >= 16) continue;
+        const float *const nd = n + d * 16 * kEdge + d * 16;
+        float col[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float sum = column == i ? 1.0f : 0.0f;
+#pragma unroll
+            for (int j = 0; j < i; ++j) sum = fmaf(-nd[i * kEdge + j], col[j], sum);
+            col[i] = sum;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[(d * 16 + i) * kEdge + d * 16 + column] = col[i];
+    }
+    __syncthreads();
+    // block (i, j) = -X_ii (sum over j <= l < i of N_il X_lj), one diagonal after the other
+    for (int apart = 1; apart < 4; ++apart) {
+        for (int j = wave; j + apart < 4; j += W) {
+            const int i = j + apart;
+            f4 sum{};
+            for (int l = j; l < i; ++l) sum = mm(along(n, kEdge, i * 16, l * 16), across(x, kEdge, l * 16, j * 16), sum);
+            put(x, kEdge, i * 16, j * 16, -mm(along(x, kEdge, i * 16, i * 16), sum, f4{}));
+        }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) p.carry[unit] = gates.a[kChunk - 1];
+    if (p.keep) {
+        for (int u = threadIdx.x; u < kChunk * kChunk; u += DK * 4) {
+            const int i = u / kChunk, j = u % kChunk;
+            p.x[unit * kChunk * kChunk + u] = j <= i ? x[i * kEdge + j] : 0.0f;
+        }
+    }
+    // a wave has 16 columns of K
+#pragma unroll
+    for (int ti = 0; ti < 4; ++ti) {
+        f4 acc{};
+        for (int kb = 0; kb <= ti; ++kb) acc = mm(along(x, kEdge, ti * 16, kb * 16) * four(gates.a, kb * 16), across(k, LD, kb * 16, wave * 16), acc);
+        put(p.w + unit * kChunk * DK, DK, ti * 16, wave * 16, -acc);
+    }
+    {
+        const int t = threadIdx.x & 63;
+        const float factor = gates.c[t] * gates.beta[t];
+        float *const mt = p.mt + unit * DK * kChunk + t;
+#pragma unroll
+        for (int d = 0; d < 16; ++d) mt[(wave * 16 + d) * kChunk] = factor * k[t * LD + wave * 16 + d];
+    }
+    for (int column = 0; column < p.columns; column += kChunk) {
+        __syncthreads();
+        load_rows<T>(n, kEdge, p, p.v, b, head, t0, column, kChunk, p.value_dim);
+        __syncthreads();
+        for (int u = wave; u < 16; u += W) {
+            const int ti = 3 - (u >> 2), tc = u & 3;
+            f4 acc{};
+            for (int kb = 0; kb <= ti; ++kb) acc = mm(along(x, kEdge, ti * 16, kb * 16), across(n, kEdge, kb * 16, tc * 16), acc);
+            put(p.y + unit * kChunk * p.columns, p.columns, ti * 16, column + tc * 16, acc);
+        }
+    }
+}
+
+// ---- the chain over chunks, 16 columns of the state by a workgroup -------------------------------------------------------
+// y += w S;  S' = carry S (+ ds) + mt y.  S before every chunk goes to s (backward: to ds, in the place of what it has read there).
+
+template <int DK>
+struct ChainStep {                                       // what a wave needs of a chunk
+    static constexpr int TS = DK / 16 >= 4 ? DK / 64 : 1;
+    f4 w[DK / 16], mt[TS][4], y, ds[TS];
+    float carry;
+};
+
+template <int DK>
+__global__ void __launch_bounds__(256) delta_chain_kernel(DeltaArgs p)
+{
+    constexpr int TS = ChainStep<DK>::TS, LD = 20;
+    __shared__ float s_l[DK * LD], y_l[kChunk * LD];
+    const int wave = threadIdx.x >> 6, slices = p.columns / 16;
+    // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
+    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
+    const int column = (int)(place % slices) * 16, j = column + lane16();
+    if (bh >= p.batch * p.heads) return;
+    const bool mine = wave * TS * 16 < DK;
+    const int rows = wave * TS * 16;                     // of the state
+    float *const ys = p.backward ? p.dy : p.y, *const ss = p.backward ? p.ds : p.s;
+    f4 state[TS];
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int row = rows + i * 16 + lane4() + m;
+            state[i][m] = p.state && mine && row < p.key_dim && j < p.value_dim ? p.state[(bh * p.key_dim + row) * p.value_dim + j] : 0.0f;
+        }
+    const auto load = [&](int n) {
+        const int64_t unit = bh * p.chunks + (p.backward ? p.chunks - 1 - n : n);
+        ChainStep<DK> c;
+        const float *const w = p.w + unit * kChunk * DK;
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) c.w[kb] = along(w, DK, wave * 16, kb * 16);
+        c.y = across(ys + unit * kChunk * p.columns, p.columns, wave * 16, column);
+        c.carry = p.carry[unit];
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < TS; ++i) {
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) c.mt[i][kb] = along(p.mt + unit * DK * kChunk, kChunk, rows + i * 16, kb * 16);
+                c.ds[i] = p.backward ? across(p.ds + unit * DK * p.columns, p.columns, rows + i * 16, column) : f4{};
+            }
+        }
+        return c;
+    };
+    ChainStep<DK> c = load(0);
+    for (int n = 0; n < p.chunks; ++n) {
+        const int64_t unit = bh * p.chunks + (p.backward ? p.chunks - 1 - n : n);
+        const ChainStep<DK> next = load(min(n + 1, p.chunks - 1));
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < TS; ++i) {
+                put(s_l, LD, rows + i * 16, 0, state[i]);
+                if (ss) put(ss + unit * DK * p.columns, p.columns, rows + i * 16, column, state[i]);
+            }
+        }
+        __syncthreads();
+        f4 y = c.y;
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) y = mm(c.w[kb], across(s_l, LD, kb * 16, 0), y);
+        put(y_l, LD, wave * 16, 0, y);
+        put(ys + unit * kChunk * p.columns, p.columns, wave * 16, column, y);
+        __syncthreads();
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < TS; ++i) {
+                f4 acc = state[i] * c.carry + c.ds[i];
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) acc = mm(c.mt[i][kb], across(y_l, LD, kb * 16, 0), acc);
+                state[i] = acc;
+            }
+        }
+        c = next;
+    }
+    if (!p.last || !mine || j >= p.value_dim) return;
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int row = rows + i * 16 + lane4() + m;
+            if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[i][m];
+        }
+}
+
+// ---- all outputs at once --------------------------------------------------------------------------------------------------
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(256) delta_output_kernel(DeltaArgs p)
+{
+    constexpr int LD = DK + 4, KSize = kChunk * (LD > kEdge ? LD : kEdge);
+    __shared__ Gates gates;
+    __shared__ __attribute__((aligned(16))) float q[kChunk * LD], k[KSize];        // k: then P beta
+    const int wave = threadIdx.x >> 6;
+    const int64_t unit = blockIdx.x, bh = unit / p.chunks, b = bh / p.heads, head = bh % p.heads, t0 = (p.chunk0 + unit % p.chunks) * kChunk;
+    gates.load(p, b, head, t0);
+    load_rows<T>(q, LD, p, p.q, b, head / p.group, t0, 0, DK, p.key_dim);
+    load_rows<T>(k, LD, p, p.k, b, head / p.group, t0, 0, DK, p.key_dim);
+    __syncthreads();
+    f4 pt[3];
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+        const int u = wave + 4 * e;
+        pt[e] = f4{};
+        if (u >= kLower) continue;
+        int ti, tj;
+        lower_tile(u, ti, tj);
+#pragma unroll
+        for (int kb = 0; kb < DK; kb += 16) pt[e] = mm(along(q, LD, ti * 16, kb), along(k, LD, tj * 16, kb), pt[e]);
+        const int j = tj * 16 + lane16();
+#pragma unroll
+        for (int m = 0; m < 4; ++m) pt[e][m] *= gates.decay(ti * 16 + lane4() + m, j) * gates.beta[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+        const int u = wave + 4 * e;
+        if (u >= kLower) continue;
+        int ti, tj;
+        lower_tile(u, ti, tj);
+        put(k, kEdge, ti * 16, tj * 16, pt[e]);
+    }
+    __syncthreads();
+    const float *const s = p.s + unit * DK * p.columns, *const y = p.y + unit * kChunk * p.columns;
+    for (int column = wave * 16; column < p.columns; column += 64) {
+        f4 acc[4] = {};
+#pragma unroll
+        for (int kb = 0; kb < DK; kb += 16) {
+            const f4 right = across(s, p.columns, kb, column);
+#pragma unroll
+            for (int ti = 0; ti < 4; ++ti) acc[ti] = mm(along(q, LD, ti * 16, kb), right, acc[ti]);
+        }
+#pragma unroll
+        for (int ti = 0; ti < 4; ++ti) acc[ti] *= four(gates.a, ti * 16);
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const f4 right = across(y, p.columns, kb * 16, column);
+#pragma unroll
+            for (int ti = kb; ti < 4; ++ti) acc[ti] = mm(along(k, kEdge, ti * 16, kb * 16), right, acc[ti]);
+        }
+        const int j = column + lane16();
+        if (j >= p.value_dim) continue;
+#pragma unroll
+        for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const int64_t t = t0 + ti * 16 + lane4() + m;
+                if (t < p.steps) out_at<T>(p.o, b, t, head)[j] = (T)(p.scale * acc[ti][m]);
+            }
+    }
+}
+
+// ---- backward: what the chain needs ------------------------------------------------------------------------------------------
+// w = X^T (beta c K), mt = -(a K)^T, dy = X^T (beta scale P^T dO), ds = scale (a Q)^T dO
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(DK * 4) delta_back_prepare_kernel(DeltaArgs p)
+{
+    constexpr int W = DK / 16, LD = DK + 4, Most = (kLower + W - 1) / W;
+    __shared__ Gates gates;
+    __shared__ __attribute__((aligned(16))) float q[kChunk * LD], k[kChunk * LD], x[kChunk * kEdge], r[kChunk * kEdge], d[kChunk * kEdge];
+    __shared__ __attribute__((aligned(16))) float by_p[kChunk], by_k[kChunk], by_q[kChunk];
+    const int wave = threadIdx.x >> 6;
+    const int64_t unit = blockIdx.x, bh = unit / p.chunks, b = bh / p.heads, head = bh % p.heads, t0 = (p.chunk0 + unit % p.chunks) * kChunk;
+    gates.load(p, b, head, t0);
+    load_rows<T>(q, LD, p, p.q, b, head / p.group, t0, 0, DK, p.key_dim);
+    load_rows<T>(k, LD, p, p.k, b, head / p.group, t0, 0, DK, p.key_dim);
+    load_kept(x, kEdge, p.x + unit * kChunk * kChunk, kChunk, 0, kChunk);
+    __syncthreads();
+    if (threadIdx.x < kChunk) {
+        const int t = threadIdx.x;
+        by_p[t] = gates.beta[t] * p.scale;
+        by_k[t] = gates.beta[t] * gates.c[t];
+        by_q[t] = gates.a[t] * p.scale;
+    }
+    for (int u = wave; u < kLower; u += W) {
+        int ti, tj;
+        lower_tile(u, ti, tj);
+        f4 acc{};
+#pragma unroll
+        for (int kb = 0; kb < DK; kb += 16) acc = mm(along(q, LD, ti * 16, kb), along(k, LD, tj * 16, kb), acc);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) acc[m] *= gates.decay(ti * 16 + lane4() + m, tj * 16 + lane16());
+        put(r, kEdge, ti * 16, tj * 16, acc);
+    }
+    __syncthreads();
+    // R = X^T (beta scale) P^T, on and above the diagonal: tile (tj, ti) of the lower tile (ti, tj)
+    f4 rt[Most];
+#pragma unroll
+    for (int e = 0; e < Most; ++e) {
+        const int u = wave + W * e;
+        rt[e] = f4{};
+        if (u >= kLower) continue;
+        int ti, tj;
+        lower_tile(u, ti, tj);
+        for (int kb = tj; kb <= ti; ++kb) rt[e] = mm(across(x, kEdge, kb * 16, tj * 16) * four(by_p, kb * 16), along(r, kEdge, ti * 16, kb * 16), rt[e]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < Most; ++e) {
+        const int u = wave + W * e;
+        if (u >= kLower) continue;
+        int ti, tj;
+        lower_tile(u, ti, tj);
+        put(r, kEdge, tj * 16, ti * 16, rt[e]);
+    }
+#pragma unroll
+    for (int ti = 0; ti < 4; ++ti) {
+        f4 acc{};
+        for (int kb = ti; kb < 4; ++kb) acc = mm(across(x, kEdge, kb * 16, ti * 16) * four(by_k, kb * 16), across(k, LD, kb * 16, wave * 16), acc);
+        put(p.w + unit * kChunk * DK, DK, ti * 16, wave * 16, acc);
+    }
+    {
+        const int t = threadIdx.x & 63;
+        const float factor = -gates.a[t];
+        float *const mt = p.mt + unit * DK * kChunk + t;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mt[(wave * 16 + i) * kChunk] = factor * k[t * LD + wave * 16 + i];
+    }
+    for (int column = 0; column < p.columns; column += kChunk) {
+        __syncthreads();
+        load_rows<T>(d, kEdge, p, p.dout, b, head, t0, column, kChunk, p.value_dim);
+        __syncthreads();
+        for (int u = wave; u < 16; u += W) {
+            const int ti = u >> 2, tc = u & 3;
+            f4 acc{};
+            for (int kb = ti; kb < 4; ++kb) acc = mm(along(r, kEdge, ti * 16, kb * 16), across(d, kEdge, kb * 16, tc * 16), acc);
+            put(p.dy + unit * kChunk * p.columns, p.columns, ti * 16, column + tc * 16, acc);
+        }
+        f4 acc[4] = {};
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const f4 left = across(q, LD, kb * 16, wave * 16) * four(by_q, kb * 16);
+#pragma unroll
+            for (int tc = 0; tc < 4; ++tc) acc[tc] = mm(left, across(d, kEdge, kb * 16, tc * 16), acc[tc]);
+        }
+#pragma unroll
+        for (int tc = 0; tc < 4; ++tc) put(p.ds + unit * DK * p.columns, p.columns, wave * 16, column + tc * 16, acc[tc]);
+    }
+}
+
+// ---- backward: all gradients at once -------------------------------------------------------------------------------------------
+
+__device__ inline float row_sum(float x)
+{
+    return row_reduce(x, [](float a, float b) { return a + b; });
+}
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(DK * 4) delta_back_output_kernel(DeltaArgs p)
+{
+    constexpr int W = DK / 16, LD = DK + 4, Most = (kLower + W - 1) / W;
+    __shared__ Gates gates;
+    __shared__ __attribute__((aligned(16))) float q[kChunk * LD], k[kChunk * LD], d[kChunk * kEdge], e_[kChunk * kEdge], y[kChunk * kEdge];
+    __shared__ float by_row[4][kChunk], by_column[4][kChunk], by_itself[kChunk]; // of the chunk x chunk matrix, by tile; its diagonal, which no decay is in
+    __shared__ float by_state[W][kChunk], kept[W][kChunk], dots[W];              // by wave
+    const int wave = threadIdx.x >> 6;
+    const int64_t unit = blockIdx.x, bh = unit / p.chunks, b = bh / p.heads, head = bh % p.heads, t0 = (p.chunk0 + unit % p.chunks) * kChunk;
+    gates.load(p, b, head, t0);
+    load_rows<T>(q, LD, p, p.q, b, head / p.group, t0, 0, DK, p.key_dim);
+    load_rows<T>(k, LD, p, p.k, b, head / p.group, t0, 0, DK, p.key_dim);
+    f4 o_state[4] = {}, y_state[4] = {}, carried[4] = {}, from_o[Most] = {}, from_y[Most] = {};
+    float dot = 0.0f;
+    const float *const s = p.s + unit * DK * p.columns, *const ds = p.ds + unit * DK * p.columns;
+    for (int column = 0; column < p.columns; column += kChunk) {
+        __syncthreads();
+        load_rows<T>(d, kEdge, p, p.dout, b, head, t0, column, kChunk, p.value_dim);
+        load_kept(e_, kEdge, p.dy + unit * kChunk * p.columns, p.columns, column, kChunk);
+        load_kept(y, kEdge, p.y + unit * kChunk * p.columns, p.columns, column, kChunk);
+        __syncthreads();
+        for (int u = threadIdx.x; u < kChunk * kChunk; u += DK * 4) {            // dv is dy
+            const int row = u / kChunk, j = u % kChunk;
+            if (t0 + row < p.steps && column + j < p.value_dim) out_at<T>(p.dv, b, t0 + row, head)[column + j] = (T)e_[row * kEdge + j];
+        }
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+            const f4 before = along(s, p.columns, wave * 16, column + kb * 16), after = along(ds, p.columns, wave * 16, column + kb * 16);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) dot = fmaf(before[m], after[m], dot);
+#pragma unroll
+            for (int ti = 0; ti < 4; ++ti) {
+                o_state[ti] = mm(along(d, kEdge, ti * 16, kb * 16), before, o_state[ti]);
+                y_state[ti] = mm(along(e_, kEdge, ti * 16, kb * 16), before, y_state[ti]);
+                carried[ti] = mm(along(y, kEdge, ti * 16, kb * 16), after, carried[ti]);
+            }
+#pragma unroll
+            for (int e = 0; e < Most; ++e) {
+                const int u = wave + W * e;
+                if (u >= kLower) continue;
+                int ti, tj;
+                lower_tile(u, ti, tj);
+                const f4 right = along(y, kEdge, tj * 16, kb * 16);
+                from_o[e] = mm(along(d, kEdge, ti * 16, kb * 16), right, from_o[e]);
+                from_y[e] = mm(along(e_, kEdge, ti * 16, kb * 16), right, from_y[e]);
+            }
+        }
+    }
+    __syncthreads();
+    // d: the gradient by Q K^T, e_: by K K^T
+#pragma unroll
+    for (int e = 0; e < Most; ++e) {
+        const int u = wave + W * e;
+        if (u >= kLower) continue;
+        int ti, tj;
+        lower_tile(u, ti, tj);
+        f4 qk{}, kk{};
+#pragma unroll
+        for (int kb = 0; kb < DK; kb += 16) {
+            const f4 right = along(k, LD, tj * 16, kb);
+            qk = mm(along(q, LD, ti * 16, kb), right, qk);
+            kk = mm(along(k, LD, ti * 16, kb), right, kk);
+        }
+        const int j = tj * 16 + lane16();
+        const float beta = gates.beta[j];
+        float column_sum = 0.0f;
+        f4 by_qk, by_kk;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int i = ti * 16 + lane4() + m;
+            const float decay = gates.decay(i, j);
+            const float o = p.scale * from_o[e][m] * decay, f = i > j ? from_y[e][m] * decay : 0.0f, by_decay = o * qk[m] - f * kk[m];
+            by_qk[m] = o * beta;
+            by_kk[m] = -f * beta;
+            if (i == j) by_itself[i] = by_decay;
+            column_sum += i == j ? 0.0f : by_decay;
+            const float sum = row_sum(i == j ? 0.0f : by_decay * beta);
+            if (lane16() == 0) by_row[tj][i] = sum;
+        }
+        column_sum += __shfl_xor(column_sum, 16);
+        column_sum += __shfl_xor(column_sum, 32);
+        if (lane4() == 0) by_column[ti][j] = column_sum;
+        put(d, kEdge, ti * 16, tj * 16, by_qk);
+        put(e_, kEdge, ti * 16, tj * 16, by_kk);
+    }
+#pragma unroll
+    for (int ti = 0; ti < 4; ++ti) {
+        const f4 a = four(gates.a, ti * 16), c = four(gates.c, ti * 16);
+        o_state[ti] *= a * p.scale;
+        y_state[ti] *= a;
+        carried[ti] *= c;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int i = ti * 16 + lane4() + m;
+            const float qi = q[i * LD + wave * 16 + lane16()], ki = k[i * LD + wave * 16 + lane16()];
+            const float state_sum = row_sum(qi * o_state[ti][m] - ki * y_state[ti][m]), kept_sum = row_sum(ki * carried[ti][m]);
+            if (lane16() == 0) by_state[wave][i] = state_sum, kept[wave][i] = kept_sum;
+        }
+    }
+    dot = wave_reduce(dot, 0.0f, [](float x, float z) { return x + z; });
+    if ((threadIdx.x & 63) == 0) dots[wave] = dot;
+    __syncthreads();
+    const int col = wave * 16 + lane16();
+#pragma unroll
+    for (int ti = 0; ti < 4; ++ti) {
+        f4 dq = o_state[ti], dk = carried[ti] * four(gates.beta, ti * 16) - y_state[ti];
+        for (int kb = 0; kb <= ti; ++kb) {
+            const f4 right = across(k, LD, kb * 16, wave * 16);
+            dq = mm(along(d, kEdge, ti * 16, kb * 16), right, dq);
+            dk = mm(along(e_, kEdge, ti * 16, kb * 16), right, dk);
+        }
+        for (int kb = ti; kb < 4; ++kb) {
+            dk = mm(across(d, kEdge, kb * 16, ti * 16), across(q, LD, kb * 16, wave * 16), dk);
+            dk = mm(across(e_, kEdge, kb * 16, ti * 16), across(k, LD, kb * 16, wave * 16), dk);
+        }
+        if (p.group > 1) {                               // added up over the heads that share the keys by another launch
+            put(p.gq + unit * kChunk * DK, DK, ti * 16, wave * 16, dq);
+            put(p.gk + unit * kChunk * DK, DK, ti * 16, wave * 16, dk);
+        } else if (col < p.key_dim) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const int64_t t = t0 + ti * 16 + lane4() + m;
+                if (t >= p.steps) continue;
+                out_at<T>(p.dq, b, t, head)[col] = (T)dq[m];
+                out_at<T>(p.dk, b, t, head)[col] = (T)dk[m];
+            }
+        }
+    }
+    if (wave == 0) {
+        const int i = threadIdx.x, tile = i >> 4;
+        const float beta = gates.beta[i];
+        float held = 0.0f, slope = 0.0f, all = 0.0f;
+        for (int w = 0; w < W; ++w) held += kept[w][i], slope += by_state[w][i], all += dots[w];
+        float column = 0.0f;
+        for (int ti = tile; ti < 4; ++ti) column += by_column[ti][i];
+        for (int tj = 0; tj <= tile; ++tj) slope += by_row[tj][i];
+        const float dbeta = held + column + by_itself[i], on = beta * held;      // on: of what goes on behind the chunk
+        double sum = (double)slope - (double)(beta * column) - (double)on, carried_on = on;
+        for (int step = 32; step > 0; step >>= 1) carried_on += __shfl_xor(carried_on, step);
+        if (i == kChunk - 1) sum += carried_on + (double)gates.a[kChunk - 1] * all;
+        for (int step = 1; step < kChunk; step <<= 1) {
+            const double later = __shfl_down(sum, step);
+            if (i + step < kChunk) sum += later;
+        }
+        if (t0 + i < p.steps) {
+            const int64_t to = (b * p.steps + t0 + i) * p.heads + head;
+            p.dg[to] = gates.cut[i] ? 0.0f : (float)sum;
+            p.dbeta[to] = dbeta;
+        }
+    }
+}
+
+// the gradients by queries and keys that heads share: the sum over the heads, in their order
+template <typename T>
+__global__ void __launch_bounds__(256) delta_group_kernel(DeltaArgs p, int dk)
+{
+    const int64_t key_heads = p.heads / p.group, unit = blockIdx.x, n = unit % p.chunks, bk = unit / p.chunks, b = bk / key_heads, key = bk % key_heads;
+    const int64_t t0 = (p.chunk0 + n) * kChunk;
+    for (int u = threadIdx.x; u < kChunk * dk; u += 256) {
+        const int row = u / dk, col = u % dk;
+        if (t0 + row >= p.steps || col >= p.key_dim) continue;
+        float dq = 0.0f, dkey = 0.0f;
+        for (int h = 0; h < p.group; ++h) {
+            const int64_t from = ((b * p.heads + key * p.group + h) * p.chunks + n) * kChunk * dk + u;
+            dq += p.gq[from];
+            dkey += p.gk[from];
+        }
+        out_at<T>(p.dq, b, t0 + row, key)[col] = (T)dq;
+        out_at<T>(p.dk, b, t0 + row, key)[col] = (T)dkey;
+    }
+}
+
+// ---- a few steps, one by one --------------------------------------------------------------------------------------------------
+// A workgroup has 64 columns of a head's state in registers: 16 groups of lanes, every 16th row each, a lane four columns.  S^T k and S^T q are
+// summed together, so a step has one barrier: o = e^g S^T q + (k . q) beta y.
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(256) delta_step_kernel(DeltaArgs p)
+{
+    constexpr int R = DK / 16;
+    __shared__ f4 sums[2][2][4][16];                     // [step parity][S^T k, S^T q][wave][columns]
+    __shared__ float kq_part[2][4];
+    const int tiles = p.columns / 64, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, group = threadIdx.x >> 4;
+    const int64_t bh = blockIdx.x / tiles, b = bh / p.heads, head = bh % p.heads;
+    const int j = blockIdx.x % tiles * 64 + (lane & 15) * 4;
+    const bool whole = j + 4 <= p.value_dim;
+    f4 s[R];
+    const int64_t base = bh * p.key_dim * p.value_dim + j;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int row = group + 16 * i;
+        s[i] = f4{};
+        if (!p.state || row >= p.key_dim) continue;
+        const float *const from = p.state + base + (int64_t)row * p.value_dim;
+        if (whole) __builtin_memcpy(&s[i], from, 16);
+        else
+            for (int m = 0; m < 4; ++m)
+                if (j + m < p.value_dim) s[i][m] = from[m];
+    }
+    for (int64_t t = 0; t < p.steps; ++t) {
+        const T *const kt = at<T>(p.k, b, t, head / p.group), *const qt = at<T>(p.q, b, t, head / p.group), *const vt = at<T>(p.v, b, t, head) + j;
+        const int64_t gate = (b * p.steps + t) * p.heads + head;
+        const float g = p.g[gate], beta = p.beta[gate];
+        const bool cut = g < kNoCarry || (p.reset && p.reset[b * p.steps + t] != 0);
+        const float carry = cut ? 0.0f : expf(g);
+        float k[R], q[R];
+        f4 v{};
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int row = group + 16 * i;
+            k[i] = row < p.key_dim ? (float)kt[row] : 0.0f;
+            q[i] = row < p.key_dim ? (float)qt[row] : 0.0f;
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+            if (j + m < p.value_dim) v[m] = (float)vt[m];
+        if (cut)
+#pragma unroll
+            for (int i = 0; i < R; ++i) s[i] = f4{};
+        f4 sk{}, sq{};
+        float kq = 0.0f;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m) sk[m] = fmaf(s[i][m], k[i], sk[m]), sq[m] = fmaf(s[i][m], q[i], sq[m]);
+            kq = fmaf(k[i], q[i], kq);
+        }
+        for (int d = 16; d < 64; d <<= 1) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m) sk[m] += __shfl_xor(sk[m], d), sq[m] += __shfl_xor(sq[m], d);
+            kq += __shfl_xor(kq, d);
+        }
+        const int turn = t & 1;
+        if (lane < 16) sums[turn][0][wave][lane] = sk, sums[turn][1][wave][lane] = sq;
+        if (lane == 0) kq_part[turn][wave] = kq;
+        __syncthreads();
+        sk = sq = f4{};
+        kq = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) sk += sums[turn][0][w][lane & 15], sq += sums[turn][1][w][lane & 15], kq += kq_part[turn][w];
+        const f4 u = beta * (v - carry * sk);
+#pragma unroll
+        for (int i = 0; i < R; ++i) s[i] = s[i] * carry + k[i] * u;
+        if (threadIdx.x < 16) {
+            const f4 o = p.scale * (carry * sq + kq * u);
+            T *const to = out_at<T>(p.o, b, t, head) + j;
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+                if (j + m < p.value_dim) to[m] = (T)o[m];
+        }
+    }
+    if (!p.last) return;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int row = group + 16 * i;
+        if (row >= p.key_dim) continue;
+        float *const to = p.last + base + (int64_t)row * p.value_dim;
+        if (whole) __builtin_memcpy(to, &s[i], 16);
+        else
+            for (int m = 0; m < 4; ++m)
+                if (j + m < p.value_dim) to[m] = s[i][m];
+    }
+}
+
+// ---- launches -------------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kFewSteps = 8;
+constexpr int64_t kSegmentBytes = 256ll << 20;           // workspace of the chunks that a launch takes: what the last-level cache holds
+thread_local int64_t g_segment_bytes = kSegmentBytes;
+
+int padded_key(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
+
+struct DeltaPlan {
+    int64_t chunks, segment, segments, units;            // chunks of a sequence, of a segment; units: (head, chunk) of a segment
+    int dk, columns;
+    int64_t w, y, mt, s, x, dy, ds, gq, gk, carry, bounds, way, total;       // places in the workspace; way: the gradient by the state between segments
+};
+DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
+{
+    DeltaPlan P{};
+    P.dk = padded_key(h.key_dim);
+    P.columns = (int)align_up(h.value_dim, 64);
+    P.chunks = (h.steps + kChunk - 1) / kChunk;
+    if (P.chunks == 0 || (!backward && h.steps <= kFewSteps)) return P;
+    const int64_t bh = h.batch * h.heads, side = kChunk * (int64_t)P.dk, rows = kChunk * (int64_t)P.columns, state = (int64_t)P.dk * P.columns;
+    const bool shared = h.heads != h.key_heads;
+    const int64_t each = 4 * (2 * side + rows + state + (backward ? rows + state + kChunk * kChunk + (shared ? 2 * side : 0) : 0));
+    const int64_t most = std::max<int64_t>(1, g_segment_bytes / each / bh);
+    P.segments = (P.chunks + most - 1) / most;
+    P.segment = (P.chunks + P.segments - 1) / P.segments;
+    P.segments = (P.chunks + P.segment - 1) / P.segment;
+    P.units = bh * P.segment;
+    int64_t at = 0;
+    const auto take = [&](int64_t floats) { const int64_t here = at; at += align_up(floats * 4, 256); return here; };
+    P.w = take(P.units * side);
+    P.mt = take(P.units * side);
+    P.y = take(P.units * rows);
+    P.s = take(P.units * state);
+    P.carry = take(P.units);
+    if (backward) {
+        P.x = take(P.units * kChunk * kChunk);
+        P.dy = take(P.units * rows);
+        P.ds = take(P.units * state);
+        if (shared) P.gq = take(P.units * side), P.gk = take(P.units * side);
+        if (P.segments > 1) {
+            P.bounds = take((P.segments - 1) * bh * h.key_dim * h.value_dim);
+            P.way = take(2 * bh * h.key_dim * h.value_dim);
+        }
+    } else if (P.segments > 1) {
+        P.way = take(2 * bh * h.key_dim * h.value_dim);
+    }
+    P.total = at;
+    return P;
+}
+
+void set_workspace(DeltaArgs &p, const DeltaPlan &P, char *ws)
+{
+    const auto to = [&](int64_t place) { return reinterpret_cast<float *>(ws + place); };
+    p.w = to(P.w); p.mt = to(P.mt); p.y = to(P.y); p.s = to(P.s); p.carry = to(P.carry);
+    p.x = to(P.x); p.dy = to(P.dy); p.ds = to(P.ds); p.gq = to(P.gq); p.gk = to(P.gk);
+    p.columns = P.columns;
+}
+
+template <typename T, int DK>
+struct DeltaLaunch {
+    static void prepare(const DeltaArgs &p, hipStream_t s)
+    {
+        hipLaunchKernelGGL((delta_prepare_kernel<T, DK>), dim3((unsigned)(p.batch * p.heads * p.chunks)), dim3(DK * 4), 0, s, p);
+    }
+    static void chain(const DeltaArgs &p, hipStream_t s)
+    {
+        const int64_t grid = (p.batch * p.heads + 7) / 8 * 8 * (p.columns / 16);
+        hipLaunchKernelGGL((delta_chain_kernel<DK>), dim3((unsigned)grid), dim3(256), 0, s, p);
+    }
+    static hipError_t forward(DeltaArgs p, const DeltaPlan &P, float *way, hipStream_t s)
+    {
+        if (p.steps <= kFewSteps) {
+            p.columns = P.columns;
+            hipLaunchKernelGGL((delta_step_kernel<T, DK>), dim3((unsigned)(p.batch * p.heads * (p.columns / 64))), dim3(256), 0, s, p);
+            return hipGetLastError();
+        }
+        const int64_t state = p.batch * p.heads * p.key_dim * p.value_dim;
+        float *const last = p.last;
+        for (int64_t seg = 0; seg < P.segments; ++seg) {
+            p.chunk0 = seg * P.segment;
+            p.chunks = (int32_t)std::min(P.segment, P.chunks - p.chunk0);
+            p.last = seg + 1 < P.segments ? way + (seg & 1) * state : last;
+            prepare(p, s);
+            chain(p, s);
+            hipLaunchKernelGGL((delta_output_kernel<T, DK>), dim3((unsigned)(p.batch * p.heads * p.chunks)), dim3(256), 0, s, p);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            p.state = p.last;
+        }
+        return hipSuccess;
+    }
+    // The states before the segments first (nothing to do with one segment), then the segments from the last to the first
+    static hipError_t backward(DeltaArgs p, const DeltaPlan &P, const float *dlast, float *dstate, float *bounds, float *way, hipStream_t s)
+    {
+        const int64_t state = p.batch * p.heads * p.key_dim * p.value_dim;
+        const float *const first = p.state;
+        float *const keep_s = p.s;
+        for (int64_t seg = 0; seg + 1 < P.segments; ++seg) {
+            p.chunk0 = seg * P.segment;
+            p.chunks = (int32_t)P.segment;
+            p.state = seg == 0 ? first : bounds + (seg - 1) * state;
+            p.last = bounds + seg * state;
+            p.s = nullptr;
+            prepare(p, s);
+            chain(p, s);
+        }
+        p.s = keep_s;
+        for (int64_t seg = P.segments - 1; seg >= 0; --seg) {
+            p.chunk0 = seg * P.segment;
+            p.chunks = (int32_t)std::min(P.segment, P.chunks - p.chunk0);
+            p.state = seg == 0 ? first : bounds + (seg - 1) * state;
+            p.last = nullptr;
+            p.keep = 1;
+            prepare(p, s);
+            chain(p, s);
+            const dim3 grid((unsigned)(p.batch * p.heads * p.chunks));
+            hipLaunchKernelGGL((delta_back_prepare_kernel<T, DK>), grid, dim3(DK * 4), 0, s, p);
+            DeltaArgs back = p;
+            back.backward = 1;
+            back.state = dlast;
+            back.last = seg > 0 ? way + (seg & 1) * state : dstate;
+            chain(back, s);
+            dlast = back.last;
+            hipLaunchKernelGGL((delta_back_output_kernel<T, DK>), grid, dim3(DK * 4), 0, s, p);
+            if (p.group > 1)
+                hipLaunchKernelGGL(delta_group_kernel<T>, dim3((unsigned)(p.batch * (p.heads / p.group) * p.chunks)), dim3(256), 0, s, p, DK);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
+};
+
+template <typename T, typename F>
+hipError_t by_key_dim(int dk, F f)
+{
+    return dk == 32 ? f(DeltaLaunch<T, 32>{}) : dk == 64 ? f(DeltaLaunch<T, 64>{}) : f(DeltaLaunch<T, 128>{});
+}
+template <typename F>
+hipError_t by_shape(const rls_delta_shape &h, const DeltaPlan &P, F f)
+{
+    return h.type == RLS_F32 ? by_key_dim<float>(P.dk, f) : h.type == RLS_BF16 ? by_key_dim<__bf16>(P.dk, f) : by_key_dim<_Float16>(P.dk, f);
+}
+
+int32_t check_delta(const rls_delta_shape *h)
+{
+    if (!h) return RLS_ERR_NULL;
+    if (h->batch < 1 || h->steps < 0 || h->heads < 1 || h->key_heads < 1 || h->key_dim < 1 || h->value_dim < 1 || !is_type(h->type)) return RLS_ERR_INVALID_ARG;
+    if (h->key_dim > RLS_MAX_KEY_DIM || h->value_dim > RLS_MAX_VALUE_DIM || h->steps > RLS_MAX_N || h->batch > (1 << 17) ||
+        h->batch * h->heads > (1 << 17) || h->batch * h->steps > (1 << 30))
+        return RLS_ERR_INVALID_ARG;
+    return h->heads % h->key_heads != 0 ? RLS_ERR_SHAPE : RLS_OK;
+}
+
+// an array of heads: bytes from its first to its last element, and whether it stays clear of itself
+struct Reach {
+    uintptr_t from = 0, to = 0;
+    bool meets(const Reach &o) const { return from < o.to && o.from < to; }
+};
+Reach reach(const void *p, int64_t bytes) { return {(uintptr_t)p, p ? (uintptr_t)p + (uintptr_t)bytes : (uintptr_t)p}; }
+int32_t check_heads(const rls_delta_shape &h, const rls_heads *x, int32_t heads, int32_t dim, bool written, Reach *r)
+{
+    if (!x) return RLS_ERR_NULL;
+    if (h.steps > 0 && !x->data_dev) return RLS_ERR_NULL;
+    if (x->batch_stride < 0 || x->step_stride < 0 || x->head_stride < 0) return RLS_ERR_SHAPE;
+    if (h.steps == 0) return RLS_OK;
+    struct { int64_t apart, count; } d[3] = {{x->batch_stride, h.batch}, {x->step_stride, h.steps}, {x->head_stride, heads}};
+    int64_t last = dim;
+    for (const auto &e : d) {
+        if (e.count == 1) continue;
+        if (e.apart > (1ll << 40) / (e.count - 1)) return RLS_ERR_SHAPE;        // (no memory reaches that far)
+        last += (e.count - 1) * e.apart;
+    }
+    *r = reach(x->data_dev, last * type_bytes(h.type));
+    if (!written) return RLS_OK;
+    std::sort(d, d + 3, [](const auto &p, const auto &q) { return p.apart < q.apart; });
+    int64_t width = dim;
+    for (const auto &e : d) {
+        if (e.count == 1) continue;
+        if (e.apart < width) return RLS_ERR_SHAPE;
+        width = e.apart * (e.count - 1) + width;
+    }
+    return RLS_OK;
+}
+Heads heads_of(const rls_heads *x) { return {x->data_dev, x->batch_stride, x->step_stride, x->head_stride}; }
+
+int32_t apart(std::initializer_list<Reach> written, std::initializer_list<Reach> read)
+{
+    for (auto w = written.begin(); w != written.end(); ++w) {
+        for (const Reach &r : read)
+            if (w->meets(r)) return RLS_ERR_SHAPE;
+        for (auto v = written.begin(); v != w; ++v)
+            if (w->meets(*v)) return RLS_ERR_SHAPE;
+    }
+    return RLS_OK;
+}
+
+DeltaArgs args_of(const rls_delta_shape &h, const rls_heads *q, const rls_heads *k, const rls_heads *v, const float *g, const float *beta, const uint8_t *reset)
+{
+    DeltaArgs p{};
+    p.q = heads_of(q); p.k = heads_of(k); p.v = heads_of(v);
+    p.g = g; p.beta = beta; p.reset = reset;
+    p.batch = h.batch; p.steps = h.steps; p.heads = h.heads; p.group = h.heads / h.key_heads;
+    p.key_dim = h.key_dim; p.value_dim = h.value_dim; p.scale = h.scale;
+    return p;
+}
+
+int32_t check_workspace(int64_t need, const void *ws, int64_t bytes)
+{
+    return need > 0 && (!ws || (uintptr_t)ws % 256 != 0 || bytes < need) ? RLS_ERR_WORKSPACE : RLS_OK;
+}
+
+__global__ void __launch_bounds__(256) delta_copy_kernel(const float *from, float *to, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = from ? from[i] : 0.0f;
+}
+hipError_t copy_state(const float *from, float *to, int64_t n, hipStream_t s)
+{
+    if (to && to != from) hipLaunchKernelGGL(delta_copy_kernel, dim3((unsigned)std::min<int64_t>(4096, (n + 255) / 256)), dim3(256), 0, s, from, to, n);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+}  // namespace rls
+
+using namespace rls;
+
+extern "C" {
+
+int32_t rls_delta_segment_bytes(int64_t bytes)
+{
+    g_segment_bytes = bytes < 0 ? kSegmentBytes : bytes;
+    return RLS_OK;
+}
+
+int64_t rls_gated_delta_workspace_bytes(const rls_delta_shape *shape, int32_t backward)
+{
+    const int32_t rc = check_delta(shape);
+    return rc != RLS_OK ? rc : plan_delta(*shape, backward != 0).total;
+}
+
+int32_t rls_gated_delta(const rls_delta_shape *shape, const rls_heads *q, const rls_heads *k, const rls_heads *v, const float *g_dev, const float *beta_dev,
+                        const float *state_dev, const uint8_t *reset_dev, const rls_heads *o, float *last_dev, void *workspace_dev, int64_t workspace_bytes,
+                        void *stream)
+{
+    int32_t rc = check_delta(shape);
+    if (rc != RLS_OK) return rc;
+    const rls_delta_shape &h = *shape;
+    if (h.steps > 0 && (!g_dev || !beta_dev)) return RLS_ERR_NULL;
+    Reach rq, rk, rv, ro;
+    rc = check_heads(h, q, h.key_heads, h.key_dim, false, &rq);
+    if (rc == RLS_OK) rc = check_heads(h, k, h.key_heads, h.key_dim, false, &rk);
+    if (rc == RLS_OK) rc = check_heads(h, v, h.heads, h.value_dim, false, &rv);
+    if (rc == RLS_OK) rc = check_heads(h, o, h.heads, h.value_dim, true, &ro);
+    if (rc != RLS_OK) return rc;
+    const DeltaPlan P = plan_delta(h, false);
+    rc = check_workspace(P.total, workspace_dev, workspace_bytes);
+    if (rc != RLS_OK) return rc;
+    const int64_t gates = h.batch * h.steps * h.heads * 4, state = h.batch * h.heads * (int64_t)h.key_dim * h.value_dim;
+    const Reach rs = reach(state_dev, state * 4), rl = reach(last_dev, state * 4), rw = reach(workspace_dev, P.total);
+    rc = apart({ro, rl, rw}, {rq, rk, rv, reach(g_dev, gates), reach(beta_dev, gates), reach(reset_dev, h.batch * h.steps)});
+    if (rc == RLS_OK) rc = apart({ro, last_dev == state_dev ? Reach{} : rl, rw}, {rs});
+    if (rc != RLS_OK) return rc;
+    const hipStream_t s = (hipStream_t)stream;
+    if (h.steps == 0) {
+        RLS_HIP_TRY(copy_state(state_dev, last_dev, state, s));
+        return RLS_OK;
+    }
+    DeltaArgs p = args_of(h, q, k, v, g_dev, beta_dev, reset_dev);
+    p.o = heads_of(o);
+    p.state = state_dev;
+    p.last = last_dev;
+    set_workspace(p, P, static_cast<char *>(workspace_dev));
+    float *const way = reinterpret_cast<float *>(static_cast<char *>(workspace_dev) + P.way);
+    RLS_HIP_TRY(by_shape(h, P, [&](auto launch) { return launch.forward(p, P, way, s); }));
+    return RLS_OK;
+}
+
+int32_t rls_gated_delta_backward(const rls_delta_shape *shape, const rls_heads *q, const rls_heads *k, const rls_heads *v, const float *g_dev,
+                                 const float *beta_dev, const float *state_dev, const uint8_t *reset_dev, const rls_heads *dout, const float *dlast_dev,
+                                 const rls_heads *dq, const rls_heads *dk, const rls_heads *dv, float *dg_dev, float *dbeta_dev, float *dstate_dev,
+                                 void *workspace_dev, int64_t workspace_bytes, void *stream)
+{
+    int32_t rc = check_delta(shape);
+    if (rc != RLS_OK) return rc;
+    const rls_delta_shape &h = *shape;
+    if (h.steps > 0 && (!g_dev || !beta_dev || !dg_dev || !dbeta_dev)) return RLS_ERR_NULL;
+    Reach rq, rk, rv, ro, tq, tk, tv;
+    rc = check_heads(h, q, h.key_heads, h.key_dim, false, &rq);
+    if (rc == RLS_OK) rc = check_heads(h, k, h.key_heads, h.key_dim, false, &rk);
+    if (rc == RLS_OK) rc = check_heads(h, v, h.heads, h.value_dim, false, &rv);
+    if (rc == RLS_OK) rc = check_heads(h, dout, h.heads, h.value_dim, false, &ro);
+    if (rc == RLS_OK) rc = check_heads(h, dq, h.key_heads, h.key_dim, true, &tq);
+    if (rc == RLS_OK) rc = check_heads(h, dk, h.key_heads, h.key_dim, true, &tk);
+    if (rc == RLS_OK) rc = check_heads(h, dv, h.heads, h.value_dim, true, &tv);
+    if (rc != RLS_OK) return rc;
+    const DeltaPlan P = plan_delta(h, true);
+    rc = check_workspace(P.total, workspace_dev, workspace_bytes);
+    if (rc != RLS_OK) return rc;
+    const int64_t gates = h.batch * h.steps * h.heads * 4, state = h.batch * h.heads * (int64_t)h.key_dim * h.value_dim;
+    const Reach rl = reach(dlast_dev, state * 4), ts = reach(dstate_dev, state * 4), tg = reach(dg_dev, gates), tb = reach(dbeta_dev, gates),
+                rw = reach(workspace_dev, P.total);
+    rc = apart({tq, tk, tv, tg, tb, ts, rw},
+               {rq, rk, rv, ro, reach(g_dev, gates), reach(beta_dev, gates), reach(reset_dev, h.batch * h.steps), reach(state_dev, state * 4)});
+    if (rc == RLS_OK) rc = apart({tq, tk, tv, tg, tb, dstate_dev == dlast_dev ? Reach{} : ts, rw}, {rl});
+    if (rc != RLS_OK) return rc;
+    const hipStream_t s = (hipStream_t)stream;
+    if (h.steps == 0) {
+        RLS_HIP_TRY(copy_state(dlast_dev, dstate_dev, state, s));
+        return RLS_OK;
+    }
+    DeltaArgs p = args_of(h, q, k, v, g_dev, beta_dev, reset_dev);
+    p.dout = heads_of(dout); p.dq = heads_of(dq); p.dk = heads_of(dk); p.dv = heads_of(dv);
+    p.dg = dg_dev; p.dbeta = dbeta_dev; p.state = state_dev;
+    char *const ws = static_cast<char *>(workspace_dev);
+    set_workspace(p, P, ws);
+    float *const bounds = reinterpret_cast<float *>(ws + P.bounds), *const way = reinterpret_cast<float *>(ws + P.way);
+    RLS_HIP_TRY(by_shape(h, P, [&](auto launch) { return launch.backward(p, P, dlast_dev, dstate_dev, bounds, way, s); }));
+    return RLS_OK;
+}
+
+}  // extern "C"

@@ -856,7 +856,7 @@ int32_t check_rows(const void *logits, int32_t type, int64_t rows, int64_t n, in
 {
     if (!logits) return RLS_ERR_NULL;
     if (rows < 1 || rows > RLS_MAX_N || n < 1 || n > RLS_MAX_CHOICES || !is_type(type)) return RLS_ERR_INVALID_ARG;
-    return ld < n ? RLS_ERR_SHAPE : RLS_OK;
+    return ld < n || ld > (1LL << 40) / rows ? RLS_ERR_SHAPE : RLS_OK;      // (no memory reaches that far)
 }
 
 // bytes from..to of an array
@@ -901,7 +901,7 @@ hipError_t backward(int32_t type, const GradArgs &g, hipStream_t s)
 int32_t check_gradients(const RowArgs &a, int64_t element, const void *out, int64_t ld_out, std::initializer_list<Span> read)
 {
     if (!out) return RLS_ERR_NULL;
-    if (ld_out < a.n) return RLS_ERR_SHAPE;
+    if (ld_out < a.n || ld_out > (1LL << 40) / a.rows) return RLS_ERR_SHAPE;
     const Span to = matrix(out, a.rows, a.n, ld_out, element), from = matrix(a.logits, a.rows, a.n, a.ld, element);
     if (to.meets(from) && !(out == a.logits && (ld_out == a.ld || a.rows == 1))) return RLS_ERR_SHAPE;
     return check_apart({to}, read);
