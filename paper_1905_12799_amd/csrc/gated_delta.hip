@@ -10,9 +10,12 @@
 // X, X V and X a K are made for all chunks at once, then a chain of two products per chunk runs for 16 columns of the state at a time,
 // then all outputs at once.  The backward pass has the same shape, with a chain from the last chunk to the first:
 //   dY = X^T beta (scale P^T dO + c . (K dS1)),  dS0 = a_63 dS1 + scale (a Q)^T dO - (a K)^T dY.
-// All products are taken by the fp32 matrix instructions (16x16x4), whatever the inputs' type: the state is handed back in fp32 and what it
-// is made of must not be rounded to fewer bits on the way.  Their rate bounds the chunked forms.
+// The state is handed back in fp32, and what it is made of must not be rounded to fewer bits on the way.  So a matrix instruction of 16-bit operands takes an
+// fp32 number as the sum of three bf16 numbers (24 bits, what is left out is 2^-27 of it), an fp16 input as two and a bf16 input as it is, and of the products
+// of two such sums those that count in fp32: three for a bf16 input with an fp32 operand, six for two of fp32, at 1/16 of an fp32 instruction's time each.
+// Small and awkward products (the inverse) are left to the fp32 instructions.
 #include <algorithm>
+#include <type_traits>
 
 #include "element_types.h"
 #include "rls_internal.h"
@@ -46,8 +49,10 @@ struct DeltaArgs {
     // workspace, an entry per (head, chunk of the launch)
     float *w, *y, *mt, *s, *x, *dy, *ds, *gq, *gk;       // [64][DK], [64][columns], [DK][64], [DK][columns], [64][64], [64][columns], [DK][columns], [64][DK] x 2
     float *carry;                                        // a_63
-    int32_t keep;                                        // x is written
-    int32_t backward;                                    // direction of the chain
+    float *gates;                                        // [2][64]: a, c beta
+    // planes, in the order in which the chain's lanes hold them: of X and scale P beta; per (key head, chunk) of K, Q and K^T
+    __bf16 *xp, *pp, *kp, *qp, *kt;
+    int32_t keep;                                        // x (and, by the chain, s and y) are written
 };
 
 template <typename T>
@@ -92,6 +97,96 @@ __device__ inline void put(float *p, int ld, int row, int column, f4 v)
     for (int m = 0; m < 4; ++m) q[m * ld] = v[m];
 }
 __device__ inline f4 four(const float *p, int k) { return *reinterpret_cast<const f4 *>(p + k + lane4()); }
+
+// ---- numbers as sums of bf16 numbers -----------------------------------------------------------------------------------
+// An operand of 16 x 16 x 32: lane l has eight numbers along the axis that is summed over, from 8 (l / 16) on, of row (or column) l % 16.
+
+using b8 = vec8<__bf16>;
+using b4 = vec4<__bf16>;
+
+template <typename T>
+constexpr int kPlanes = sizeof(T) == 4 ? 3 : std::is_same<T, __bf16>::value ? 1 : 2;
+
+template <int N, typename B, typename F>
+__device__ inline void split(F x, B (&to)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        to[i] = __builtin_convertvector(x, B);
+        x -= __builtin_convertvector(to[i], F);
+    }
+}
+template <typename T>
+struct Raw {                                             // eight inputs as they come
+    T x[8];
+};
+template <typename T, int N>
+__device__ inline void planes_of(const Raw<T> &r, b8 (&to)[N])
+{
+    vec8<float> x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)r.x[i];
+    split(x, to);
+}
+template <>
+__device__ inline void planes_of<__bf16, 1>(const Raw<__bf16> &r, b8 (&to)[1])
+{
+    __builtin_memcpy(&to[0], r.x, 16);
+}
+// eight inputs of a row from column d on, 0 where there are none
+template <typename T>
+__device__ inline Raw<T> load_raw(const T *row, bool in, int d, int columns)
+{
+    Raw<T> r;
+    if (in && d + 8 <= columns) {
+        __builtin_memcpy(r.x, row + d, 8 * sizeof(T));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.x[i] = in && d + i < columns ? row[d + i] : (T)0.0f;
+    }
+    return r;
+}
+template <int NA, int NB>
+__device__ inline f4 mmp(const b8 (&a)[NA], const b8 (&b)[NB], f4 c)
+{
+#pragma unroll
+    for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                if (i + j == sum) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
+    return c;
+}
+// Memory in the order of the lanes: a block of 64 x 8 numbers for every 16 rows, 32 of the summed axis and plane.  Where number k (a multiple of 8) of a
+// row begins, with `blocks` blocks along the summed axis and N planes
+template <int N>
+__device__ inline int place_in(int row, int k, int blocks, int plane)
+{
+    return (((row >> 4) * blocks + (k >> 5)) * N + plane) * 512 + ((row & 15) + ((k & 31) >> 3) * 16) * 8;
+}
+template <int N>
+__device__ inline void load_block(b8 (&to)[N], const __bf16 *p, int block)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) to[i] = *reinterpret_cast<const b8 *>(p + (block * N + i) * 512 + (threadIdx.x & 63) * 8);
+}
+__device__ inline int lane8() { return (threadIdx.x & 63) >> 4 << 3; }
+// from planes in memory, rows ld apart and planes `plane` apart
+template <int N>
+__device__ inline void load_planes(b8 (&to)[N], const __bf16 *p, int plane, int ld, int row, int k)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) to[i] = *reinterpret_cast<const b8 *>(p + i * plane + (row + lane16()) * ld + k + lane8());
+}
+// a result (four rows of a column) into planes whose rows are the columns: the next product's right operand
+__device__ inline void put_planes(__bf16 *p, int plane, int ld, int row, f4 v)
+{
+    b4 to[3];
+    split(v, to);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) *reinterpret_cast<b4 *>(p + i * plane + lane16() * ld + row + lane4()) = to[i];
+}
 
 // The tiles on and below the diagonal of a chunk x chunk matrix
 constexpr int kLower = 10;
@@ -174,39 +269,77 @@ __device__ inline void load_kept(float *to, int ld, const float *from, int ld_fr
     }
 }
 
-// ---- all chunks at once: X, X V, -(X a K), (c beta K)^T -----------------------------------------------------------------
+// ---- all chunks at once: X, P and K^T -------------------------------------------------------------------------------------
 
 template <typename T, int DK>
-__global__ void __launch_bounds__(DK * 4) delta_prepare_kernel(DeltaArgs p)
+__global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
 {
-    constexpr int W = DK / 16, LD = DK + 4;              // waves: one for every 16 key dimensions
+    constexpr int NI = kPlanes<T>, LD = DK + 8, Plane = kChunk * LD;
     __shared__ Gates gates;
-    __shared__ __attribute__((aligned(16))) float k[kChunk * LD], x[kChunk * kEdge], n[kChunk * kEdge];
+    __shared__ __attribute__((aligned(16))) __bf16 k[NI * Plane], q[NI * Plane];
+    __shared__ __attribute__((aligned(16))) float x[kChunk * kEdge], n[kChunk * kEdge];       // n: G beta below the diagonal; scale P beta, turned, from it on
     const int wave = threadIdx.x >> 6;
-    const int64_t unit = blockIdx.x, bh = unit / p.chunks, b = bh / p.heads, head = bh % p.heads, t0 = (p.chunk0 + unit % p.chunks) * kChunk;
+    const int64_t unit = blockIdx.x, bh = unit / p.chunks, chunk = unit % p.chunks, b = bh / p.heads, head = bh % p.heads, key = head / p.group;
+    const int64_t t0 = (p.chunk0 + chunk) * kChunk, inputs = ((b * (p.heads / p.group) + key) * p.chunks + chunk) * NI * kChunk * DK;
+    const bool first = head % p.group == 0;              // of the heads that share the keys: it writes their planes
     gates.load(p, b, head, t0);
-    load_rows<T>(k, LD, p, p.k, b, head / p.group, t0, 0, DK, p.key_dim);
+    for (int u = threadIdx.x; u < kChunk * DK / 8; u += 256) {
+        const int row = u / (DK / 8), d = u % (DK / 8) * 8;
+        const bool in = t0 + row < p.steps;
+        b8 pk[NI], pq[NI];
+        planes_of(load_raw(at<T>(p.k, b, t0 + row, key), in, d, p.key_dim), pk);
+        planes_of(load_raw(at<T>(p.q, b, t0 + row, key), in, d, p.key_dim), pq);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            *reinterpret_cast<b8 *>(k + i * Plane + row * LD + d) = pk[i];
+            *reinterpret_cast<b8 *>(q + i * Plane + row * LD + d) = pq[i];
+            if (first) {
+                *reinterpret_cast<b8 *>(p.kp + inputs + place_in<NI>(row, d, DK / 32, i)) = pk[i];
+                *reinterpret_cast<b8 *>(p.qp + inputs + place_in<NI>(row, d, DK / 32, i)) = pq[i];
+            }
+        }
+    }
     __syncthreads();
-    for (int u = wave; u < kLower; u += W) {
+    for (int u = wave; u < kLower; u += 4) {
         int ti, tj;
         lower_tile(u, ti, tj);
-        f4 acc{};
+        f4 kk{}, qk{};
 #pragma unroll
-        for (int kb = 0; kb < DK; kb += 16) acc = mm(along(k, LD, ti * 16, kb), along(k, LD, tj * 16, kb), acc);
+        for (int kb = 0; kb < DK; kb += 32) {
+            b8 left[NI], right[NI];
+            load_planes(right, k, Plane, LD, tj * 16, kb);
+            load_planes(left, k, Plane, LD, ti * 16, kb);
+            kk = mmp(left, right, kk);
+            load_planes(left, q, Plane, LD, ti * 16, kb);
+            qk = mmp(left, right, qk);
+        }
         const int j = tj * 16 + lane16();
+        const float beta = gates.beta[j];
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const int i = ti * 16 + lane4() + m;
-            acc[m] = j < i ? acc[m] * gates.decay(i, j) * gates.beta[j] : 0.0f;
+            const float decay = gates.decay(i, j) * beta;
+            if (j < i) n[i * kEdge + j] = kk[m] * decay;
+            if (j <= i) n[j * kEdge + i] = qk[m] * decay * p.scale;
         }
-        put(n, kEdge, ti * 16, tj * 16, acc);
+    }
+    if (first) {
+        for (int u = threadIdx.x; u < DK * 8; u += 256) {
+            const int d = u % DK, t = u / DK * 8;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                b8 v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = k[i * Plane + (t + e) * LD + d];
+                *reinterpret_cast<b8 *>(p.kt + inputs + place_in<NI>(d, t, 2, i)) = v;
+            }
+        }
     }
     __syncthreads();
     // blocks on the diagonal: a lane solves for a column
-    for (int d = wave; d < 4; d += W) {
+    if ((threadIdx.x & 63) < 16) {
         const int column = threadIdx.x & 63;
-        if (column >= 16) continue;
-        const float *const nd = n + d * 16 * kEdge + d * 16;
+        const float *const nd = n + wave * 16 * kEdge + wave * 16;
         float col[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -216,13 +349,13 @@ __global__ void __launch_bounds__(DK * 4) delta_prepare_kernel(DeltaArgs p)
             col[i] = sum;
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[(d * 16 + i) * kEdge + d * 16 + column] = col[i];
+        for (int i = 0; i < 16; ++i) x[(wave * 16 + i) * kEdge + wave * 16 + column] = col[i];
     }
     __syncthreads();
     // block (i, j) = -X_ii (sum over j <= l < i of N_il X_lj), one diagonal after the other
     for (int apart = 1; apart < 4; ++apart) {
-        for (int j = wave; j + apart < 4; j += W) {
-            const int i = j + apart;
+        if (wave + apart < 4) {
+            const int j = wave, i = j + apart;
             f4 sum{};
             for (int l = j; l < i; ++l) sum = mm(along(n, kEdge, i * 16, l * 16), across(x, kEdge, l * 16, j * 16), sum);
             put(x, kEdge, i * 16, j * 16, -mm(along(x, kEdge, i * 16, i * 16), sum, f4{}));
@@ -230,191 +363,155 @@ __global__ void __launch_bounds__(DK * 4) delta_prepare_kernel(DeltaArgs p)
         __syncthreads();
     }
     if (threadIdx.x == 0) p.carry[unit] = gates.a[kChunk - 1];
-    if (p.keep) {
-        for (int u = threadIdx.x; u < kChunk * kChunk; u += DK * 4) {
-            const int i = u / kChunk, j = u % kChunk;
-            p.x[unit * kChunk * kChunk + u] = j <= i ? x[i * kEdge + j] : 0.0f;
-        }
+    if (threadIdx.x < kChunk) {
+        float *const to = p.gates + unit * 2 * kChunk + threadIdx.x;
+        to[0] = gates.a[threadIdx.x];
+        to[kChunk] = gates.c[threadIdx.x] * gates.beta[threadIdx.x];
     }
-    // a wave has 16 columns of K
+    for (int u = threadIdx.x; u < kChunk * 8; u += 256) {
+        const int i = u / 8, j = u % 8 * 8;
+        vec8<float> vx, vp;
 #pragma unroll
-    for (int ti = 0; ti < 4; ++ti) {
-        f4 acc{};
-        for (int kb = 0; kb <= ti; ++kb) acc = mm(along(x, kEdge, ti * 16, kb * 16) * four(gates.a, kb * 16), across(k, LD, kb * 16, wave * 16), acc);
-        put(p.w + unit * kChunk * DK, DK, ti * 16, wave * 16, -acc);
-    }
-    {
-        const int t = threadIdx.x & 63;
-        const float factor = gates.c[t] * gates.beta[t];
-        float *const mt = p.mt + unit * DK * kChunk + t;
-#pragma unroll
-        for (int d = 0; d < 16; ++d) mt[(wave * 16 + d) * kChunk] = factor * k[t * LD + wave * 16 + d];
-    }
-    for (int column = 0; column < p.columns; column += kChunk) {
-        __syncthreads();
-        load_rows<T>(n, kEdge, p, p.v, b, head, t0, column, kChunk, p.value_dim);
-        __syncthreads();
-        for (int u = wave; u < 16; u += W) {
-            const int ti = 3 - (u >> 2), tc = u & 3;
-            f4 acc{};
-            for (int kb = 0; kb <= ti; ++kb) acc = mm(along(x, kEdge, ti * 16, kb * 16), across(n, kEdge, kb * 16, tc * 16), acc);
-            put(p.y + unit * kChunk * p.columns, p.columns, ti * 16, column + tc * 16, acc);
+        for (int e = 0; e < 8; ++e) {
+            vx[e] = j + e <= i ? x[i * kEdge + j + e] : 0.0f;
+            vp[e] = j + e <= i ? n[(j + e) * kEdge + i] : 0.0f;
         }
+        b8 px[3], pp[3];
+        split(vx, px);
+        split(vp, pp);
+#pragma unroll
+        for (int plane = 0; plane < 3; ++plane) {
+            const int64_t to = unit * 3 * kChunk * kChunk + place_in<3>(i, j, 2, plane);
+            *reinterpret_cast<b8 *>(p.xp + to) = px[plane];
+            *reinterpret_cast<b8 *>(p.pp + to) = pp[plane];
+        }
+        if (p.keep) __builtin_memcpy(p.x + (unit * kChunk + i) * kChunk + j, &vx, 32);
     }
 }
 
-// ---- the chain over chunks, 16 columns of the state by a workgroup -------------------------------------------------------
-// y += w S;  S' = carry S (+ ds) + mt y.  S before every chunk goes to s (backward: to ds, in the place of what it has read there).
+// ---- the chain over chunks, 16 columns of the state by a workgroup --------------------------------------------------------
+// Eight waves, 16 of the chunk's steps for two of them.  The first four: R = V - a (K S), Y = X R.  The other four, beside them: o = scale a (Q S)
+// + scale P beta Y.  Then all of them: S = carry S + K^T (c beta Y), 16 rows of it each.  Three barriers a chunk; what a chunk needs of memory is
+// read while the one before it is worked on.
 
-template <int DK>
-struct ChainStep {                                       // what a wave needs of a chunk
-    static constexpr int TS = DK / 16 >= 4 ? DK / 64 : 1;
-    f4 w[DK / 16], mt[TS][4], y, ds[TS];
-    float carry;
-};
-
-template <int DK>
-__global__ void __launch_bounds__(256) delta_chain_kernel(DeltaArgs p)
+// Steps behind the last one are worked on with the last one's v: beta is 0 there, and what they give is not written.
+template <typename T, int DK, bool KEEP>
+__global__ void __launch_bounds__(512) delta_chain_kernel(DeltaArgs p)
 {
-    constexpr int TS = ChainStep<DK>::TS, LD = 20;
-    __shared__ float s_l[DK * LD], y_l[kChunk * LD];
-    const int wave = threadIdx.x >> 6, slices = p.columns / 16;
+    constexpr int NI = kPlanes<T>, LD = DK + 8, SPlane = 16 * LD, CL = kChunk + 8, CPlane = 16 * CL, Square = kChunk * kChunk;
+    __shared__ __attribute__((aligned(16))) __bf16 st[3 * SPlane], rt[3 * CPlane], yt[3 * CPlane], ut[3 * CPlane];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile = wave & 3, slices = p.columns / 16;
+    const bool answers = wave >= 4, mine = wave < DK / 16, low = tile >= 2;      // low: rows whose sums reach over the second half of the steps
     // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
     const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
-    const int column = (int)(place % slices) * 16, j = column + lane16();
     if (bh >= p.batch * p.heads) return;
-    const bool mine = wave * TS * 16 < DK;
-    const int rows = wave * TS * 16;                     // of the state
-    float *const ys = p.backward ? p.dy : p.y, *const ss = p.backward ? p.ds : p.s;
-    f4 state[TS];
+    const int64_t b = bh / p.heads, head = bh % p.heads, key = head / p.group, kbh = b * (p.heads / p.group) + key;
+    const int column = (int)(place % slices) * 16, j = column + lane16(), read = min(j, p.value_dim - 1);
+    f4 state{};
 #pragma unroll
-    for (int i = 0; i < TS; ++i)
+    for (int m = 0; m < 4; ++m) {
+        const int row = wave * 16 + lane4() + m;
+        if (p.state && mine && row < p.key_dim && j < p.value_dim) state[m] = p.state[(bh * p.key_dim + row) * p.value_dim + j];
+    }
+    // where a wave's part of a chunk begins; the next chunk's follows behind it
+    const __bf16 *rows_at = (answers ? p.qp : p.kp) + kbh * p.chunks * NI * kChunk * DK + tile * (DK / 32) * NI * 512;
+    const __bf16 *left_at = (answers ? p.pp : p.xp) + bh * p.chunks * 3 * Square + tile * 2 * 3 * 512;
+    const __bf16 *kt_at = p.kt + kbh * p.chunks * NI * kChunk * DK + (mine ? wave : 0) * 2 * NI * 512;
+    const float *gates_at = p.gates + bh * p.chunks * 2 * kChunk + tile * 16;
+    const T *const v_at = at<T>(p.v, b, 0, head);
+    b8 rows[DK / 32][NI], left[2][3], kt[2][NI];
+    T v[4];
+    f4 a, cbeta;
+    float carry;
+    const auto load_rows_of = [&](int n) {
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const int row = rows + i * 16 + lane4() + m;
-            state[i][m] = p.state && mine && row < p.key_dim && j < p.value_dim ? p.state[(bh * p.key_dim + row) * p.value_dim + j] : 0.0f;
+        for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at + (int64_t)n * NI * kChunk * DK, kb);
+        a = four(gates_at + (int64_t)n * 2 * kChunk, 0);
+        if (!answers) {
+            const int64_t t = (p.chunk0 + n) * kChunk + tile * 16 + lane4();
+#pragma unroll
+            for (int m = 0; m < 4; ++m) v[m] = v_at[min(t + m, p.steps - 1) * p.v.step + read];
         }
-    const auto load = [&](int n) {
-        const int64_t unit = bh * p.chunks + (p.backward ? p.chunks - 1 - n : n);
-        ChainStep<DK> c;
-        const float *const w = p.w + unit * kChunk * DK;
-#pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) c.w[kb] = along(w, DK, wave * 16, kb * 16);
-        c.y = across(ys + unit * kChunk * p.columns, p.columns, wave * 16, column);
-        c.carry = p.carry[unit];
-        if (mine) {
-#pragma unroll
-            for (int i = 0; i < TS; ++i) {
-#pragma unroll
-                for (int kb = 0; kb < 4; ++kb) c.mt[i][kb] = along(p.mt + unit * DK * kChunk, kChunk, rows + i * 16, kb * 16);
-                c.ds[i] = p.backward ? across(p.ds + unit * DK * p.columns, p.columns, rows + i * 16, column) : f4{};
-            }
-        }
-        return c;
     };
-    ChainStep<DK> c = load(0);
+    const auto load_left_of = [&](int n) {
+        load_block(left[0], left_at + (int64_t)n * 3 * Square, 0);
+        if (low) load_block(left[1], left_at + (int64_t)n * 3 * Square, 1);
+        if (!answers) cbeta = four(gates_at + (int64_t)n * 2 * kChunk + kChunk, 0);
+    };
+    const auto load_kt_of = [&](int n) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) load_block(kt[kb], kt_at + (int64_t)n * NI * kChunk * DK, kb);
+        carry = p.carry[bh * p.chunks + n];
+    };
+    load_rows_of(0);
+    load_left_of(0);
+    load_kt_of(0);
     for (int n = 0; n < p.chunks; ++n) {
-        const int64_t unit = bh * p.chunks + (p.backward ? p.chunks - 1 - n : n);
-        const ChainStep<DK> next = load(min(n + 1, p.chunks - 1));
+        const int64_t unit = bh * p.chunks + n;
+        const int after = min(n + 1, p.chunks - 1);
         if (mine) {
-#pragma unroll
-            for (int i = 0; i < TS; ++i) {
-                put(s_l, LD, rows + i * 16, 0, state[i]);
-                if (ss) put(ss + unit * DK * p.columns, p.columns, rows + i * 16, column, state[i]);
-            }
+            put_planes(st, SPlane, LD, wave * 16, state);
+            if (KEEP) put(p.s + unit * DK * p.columns, p.columns, wave * 16, column, state);
         }
         __syncthreads();
-        f4 y = c.y;
+        f4 by_state{};
 #pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) y = mm(c.w[kb], across(s_l, LD, kb * 16, 0), y);
-        put(y_l, LD, wave * 16, 0, y);
-        put(ys + unit * kChunk * p.columns, p.columns, wave * 16, column, y);
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            b8 s[3];
+            load_planes(s, st, SPlane, LD, 0, kb * 32);
+            by_state = mmp(rows[kb], s, by_state);
+        }
+        by_state *= a;
+        if (!answers) {
+            const f4 x{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+            put_planes(rt, CPlane, CL, tile * 16, x - by_state);
+        }
+        load_rows_of(after);
+        __syncthreads();
+        if (!answers) {
+            b8 r[3];
+            load_planes(r, rt, CPlane, CL, 0, 0);
+            f4 y = mmp(left[0], r, f4{});
+            if (low) {
+                load_planes(r, rt, CPlane, CL, 0, 32);
+                y = mmp(left[1], r, y);
+            }
+            put_planes(yt, CPlane, CL, tile * 16, y);
+            put_planes(ut, CPlane, CL, tile * 16, y * cbeta);
+            if (KEEP) put(p.y + unit * kChunk * p.columns, p.columns, tile * 16, column, y);
+            load_left_of(after);
+        }
         __syncthreads();
         if (mine) {
+            state *= carry;
 #pragma unroll
-            for (int i = 0; i < TS; ++i) {
-                f4 acc = state[i] * c.carry + c.ds[i];
-#pragma unroll
-                for (int kb = 0; kb < 4; ++kb) acc = mm(c.mt[i][kb], across(y_l, LD, kb * 16, 0), acc);
-                state[i] = acc;
+            for (int kb = 0; kb < 2; ++kb) {
+                b8 u[3];
+                load_planes(u, ut, CPlane, CL, 0, kb * 32);
+                state = mmp(kt[kb], u, state);
             }
+            load_kt_of(after);
         }
-        c = next;
+        if (!KEEP && answers) {
+            b8 y[3];
+            load_planes(y, yt, CPlane, CL, 0, 0);
+            f4 o = mmp(left[0], y, by_state * p.scale);
+            if (low) {
+                load_planes(y, yt, CPlane, CL, 0, 32);
+                o = mmp(left[1], y, o);
+            }
+            load_left_of(after);
+            const int64_t t = (p.chunk0 + n) * kChunk + tile * 16 + lane4();
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+                if (t + m < p.steps && j < p.value_dim) out_at<T>(p.o, b, t + m, head)[j] = (T)o[m];
+        }
     }
     if (!p.last || !mine || j >= p.value_dim) return;
 #pragma unroll
-    for (int i = 0; i < TS; ++i)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const int row = rows + i * 16 + lane4() + m;
-            if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[i][m];
-        }
-}
-
-// ---- all outputs at once --------------------------------------------------------------------------------------------------
-
-template <typename T, int DK>
-__global__ void __launch_bounds__(256) delta_output_kernel(DeltaArgs p)
-{
-    constexpr int LD = DK + 4, KSize = kChunk * (LD > kEdge ? LD : kEdge);
-    __shared__ Gates gates;
-    __shared__ __attribute__((aligned(16))) float q[kChunk * LD], k[KSize];        // k: then P beta
-    const int wave = threadIdx.x >> 6;
-    const int64_t unit = blockIdx.x, bh = unit / p.chunks, b = bh / p.heads, head = bh % p.heads, t0 = (p.chunk0 + unit % p.chunks) * kChunk;
-    gates.load(p, b, head, t0);
-    load_rows<T>(q, LD, p, p.q, b, head / p.group, t0, 0, DK, p.key_dim);
-    load_rows<T>(k, LD, p, p.k, b, head / p.group, t0, 0, DK, p.key_dim);
-    __syncthreads();
-    f4 pt[3];
-#pragma unroll
-    for (int e = 0; e < 3; ++e) {
-        const int u = wave + 4 * e;
-        pt[e] = f4{};
-        if (u >= kLower) continue;
-        int ti, tj;
-        lower_tile(u, ti, tj);
-#pragma unroll
-        for (int kb = 0; kb < DK; kb += 16) pt[e] = mm(along(q, LD, ti * 16, kb), along(k, LD, tj * 16, kb), pt[e]);
-        const int j = tj * 16 + lane16();
-#pragma unroll
-        for (int m = 0; m < 4; ++m) pt[e][m] *= gates.decay(ti * 16 + lane4() + m, j) * gates.beta[j];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 3; ++e) {
-        const int u = wave + 4 * e;
-        if (u >= kLower) continue;
-        int ti, tj;
-        lower_tile(u, ti, tj);
-        put(k, kEdge, ti * 16, tj * 16, pt[e]);
-    }
-    __syncthreads();
-    const float *const s = p.s + unit * DK * p.columns, *const y = p.y + unit * kChunk * p.columns;
-    for (int column = wave * 16; column < p.columns; column += 64) {
-        f4 acc[4] = {};
-#pragma unroll
-        for (int kb = 0; kb < DK; kb += 16) {
-            const f4 right = across(s, p.columns, kb, column);
-#pragma unroll
-            for (int ti = 0; ti < 4; ++ti) acc[ti] = mm(along(q, LD, ti * 16, kb), right, acc[ti]);
-        }
-#pragma unroll
-        for (int ti = 0; ti < 4; ++ti) acc[ti] *= four(gates.a, ti * 16);
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            const f4 right = across(y, p.columns, kb * 16, column);
-#pragma unroll
-            for (int ti = kb; ti < 4; ++ti) acc[ti] = mm(along(k, kEdge, ti * 16, kb * 16), right, acc[ti]);
-        }
-        const int j = column + lane16();
-        if (j >= p.value_dim) continue;
-#pragma unroll
-        for (int ti = 0; ti < 4; ++ti)
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int64_t t = t0 + ti * 16 + lane4() + m;
-                if (t < p.steps) out_at<T>(p.o, b, t, head)[j] = (T)(p.scale * acc[ti][m]);
-            }
+    for (int m = 0; m < 4; ++m) {
+        const int row = wave * 16 + lane4() + m;
+        if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[m];
     }
 }
 
@@ -505,6 +602,94 @@ __global__ void __launch_bounds__(DK * 4) delta_back_prepare_kernel(DeltaArgs p)
 #pragma unroll
         for (int tc = 0; tc < 4; ++tc) put(p.ds + unit * DK * p.columns, p.columns, wave * 16, column + tc * 16, acc[tc]);
     }
+}
+
+// ---- backward: the chain from the last chunk to the first ----------------------------------------------------------------
+// dy += w dS;  dS' = carry dS + ds + mt dy.  dS of every chunk goes to ds, in the place of what was read there.
+
+template <int DK>
+struct BackStep {                                       // what a wave needs of a chunk
+    static constexpr int TS = DK / 16 >= 4 ? DK / 64 : 1;
+    f4 w[DK / 16], mt[TS][4], y, ds[TS];
+    float carry;
+};
+
+template <int DK>
+__global__ void __launch_bounds__(256) delta_back_chain_kernel(DeltaArgs p)
+{
+    constexpr int TS = BackStep<DK>::TS, LD = 20;
+    __shared__ float s_l[DK * LD], y_l[kChunk * LD];
+    const int wave = threadIdx.x >> 6, slices = p.columns / 16;
+    // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
+    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
+    const int column = (int)(place % slices) * 16, j = column + lane16();
+    if (bh >= p.batch * p.heads) return;
+    const bool mine = wave * TS * 16 < DK;
+    const int rows = wave * TS * 16;                     // of the state
+    float *const ys = p.dy, *const ss = p.ds;
+    f4 state[TS];
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int row = rows + i * 16 + lane4() + m;
+            state[i][m] = p.state && mine && row < p.key_dim && j < p.value_dim ? p.state[(bh * p.key_dim + row) * p.value_dim + j] : 0.0f;
+        }
+    const auto load = [&](int n) {
+        const int64_t unit = bh * p.chunks + p.chunks - 1 - n;
+        BackStep<DK> c;
+        const float *const w = p.w + unit * kChunk * DK;
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) c.w[kb] = along(w, DK, wave * 16, kb * 16);
+        c.y = across(ys + unit * kChunk * p.columns, p.columns, wave * 16, column);
+        c.carry = p.carry[unit];
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < TS; ++i) {
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) c.mt[i][kb] = along(p.mt + unit * DK * kChunk, kChunk, rows + i * 16, kb * 16);
+                c.ds[i] = across(p.ds + unit * DK * p.columns, p.columns, rows + i * 16, column);
+            }
+        }
+        return c;
+    };
+    BackStep<DK> c = load(0);
+    for (int n = 0; n < p.chunks; ++n) {
+        const int64_t unit = bh * p.chunks + p.chunks - 1 - n;
+        const BackStep<DK> next = load(min(n + 1, p.chunks - 1));
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < TS; ++i) {
+                put(s_l, LD, rows + i * 16, 0, state[i]);
+                put(ss + unit * DK * p.columns, p.columns, rows + i * 16, column, state[i]);
+            }
+        }
+        __syncthreads();
+        f4 y = c.y;
+#pragma unroll
+        for (int kb = 0; kb < DK / 16; ++kb) y = mm(c.w[kb], across(s_l, LD, kb * 16, 0), y);
+        put(y_l, LD, wave * 16, 0, y);
+        put(ys + unit * kChunk * p.columns, p.columns, wave * 16, column, y);
+        __syncthreads();
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < TS; ++i) {
+                f4 acc = state[i] * c.carry + c.ds[i];
+#pragma unroll
+                for (int kb = 0; kb < 4; ++kb) acc = mm(c.mt[i][kb], across(y_l, LD, kb * 16, 0), acc);
+                state[i] = acc;
+            }
+        }
+        c = next;
+    }
+    if (!p.last || !mine || j >= p.value_dim) return;
+#pragma unroll
+    for (int i = 0; i < TS; ++i)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const int row = rows + i * 16 + lane4() + m;
+            if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[i][m];
+        }
 }
 
 // ---- backward: all gradients at once -------------------------------------------------------------------------------------------
@@ -790,7 +975,7 @@ int padded_key(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
 struct DeltaPlan {
     int64_t chunks, segment, segments, units;            // chunks of a sequence, of a segment; units: (head, chunk) of a segment
     int dk, columns;
-    int64_t w, y, mt, s, x, dy, ds, gq, gk, carry, bounds, way, total;       // places in the workspace; way: the gradient by the state between segments
+    int64_t w, y, mt, s, x, dy, ds, gq, gk, carry, gates, xp, pp, kp, qp, kt, bounds, way, total;       // places in the workspace; way: the gradient by the state between segments
 };
 DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
 {
@@ -801,7 +986,8 @@ DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
     if (P.chunks == 0 || (!backward && h.steps <= kFewSteps)) return P;
     const int64_t bh = h.batch * h.heads, side = kChunk * (int64_t)P.dk, rows = kChunk * (int64_t)P.columns, state = (int64_t)P.dk * P.columns;
     const bool shared = h.heads != h.key_heads;
-    const int64_t each = 4 * (2 * side + rows + state + (backward ? rows + state + kChunk * kChunk + (shared ? 2 * side : 0) : 0));
+    const int64_t planes = 3, square = kChunk * kChunk;          // (as for fp32: the workspace does not go by the type)
+    const int64_t each = 2 * (6 * square + 3 * planes * side) + (backward ? 4 * (2 * side + 2 * rows + 2 * state + square + (shared ? 2 * side : 0)) : 0);
     const int64_t most = std::max<int64_t>(1, g_segment_bytes / each / bh);
     P.segments = (P.chunks + most - 1) / most;
     P.segment = (P.chunks + P.segments - 1) / P.segments;
@@ -809,13 +995,20 @@ DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
     P.units = bh * P.segment;
     int64_t at = 0;
     const auto take = [&](int64_t floats) { const int64_t here = at; at += align_up(floats * 4, 256); return here; };
-    P.w = take(P.units * side);
-    P.mt = take(P.units * side);
-    P.y = take(P.units * rows);
-    P.s = take(P.units * state);
     P.carry = take(P.units);
+    P.gates = take(P.units * 2 * kChunk);
+    P.xp = take(P.units * 3 * square / 2);
+    P.pp = take(P.units * 3 * square / 2);
+    const int64_t inputs = P.units / (h.heads / h.key_heads) * planes * side / 2;
+    P.kp = take(inputs);
+    P.qp = take(inputs);
+    P.kt = take(inputs);
     if (backward) {
-        P.x = take(P.units * kChunk * kChunk);
+        P.w = take(P.units * side);
+        P.mt = take(P.units * side);
+        P.y = take(P.units * rows);
+        P.s = take(P.units * state);
+        P.x = take(P.units * square);
         P.dy = take(P.units * rows);
         P.ds = take(P.units * state);
         if (shared) P.gq = take(P.units * side), P.gk = take(P.units * side);
@@ -834,6 +1027,9 @@ void set_workspace(DeltaArgs &p, const DeltaPlan &P, char *ws)
 {
     const auto to = [&](int64_t place) { return reinterpret_cast<float *>(ws + place); };
     p.w = to(P.w); p.mt = to(P.mt); p.y = to(P.y); p.s = to(P.s); p.carry = to(P.carry);
+    p.gates = to(P.gates);
+    const auto planes = [&](int64_t place) { return reinterpret_cast<__bf16 *>(ws + place); };
+    p.xp = planes(P.xp); p.pp = planes(P.pp); p.kp = planes(P.kp); p.qp = planes(P.qp); p.kt = planes(P.kt);
     p.x = to(P.x); p.dy = to(P.dy); p.ds = to(P.ds); p.gq = to(P.gq); p.gk = to(P.gk);
     p.columns = P.columns;
 }
@@ -842,12 +1038,13 @@ template <typename T, int DK>
 struct DeltaLaunch {
     static void prepare(const DeltaArgs &p, hipStream_t s)
     {
-        hipLaunchKernelGGL((delta_prepare_kernel<T, DK>), dim3((unsigned)(p.batch * p.heads * p.chunks)), dim3(DK * 4), 0, s, p);
+        hipLaunchKernelGGL((delta_prepare_kernel<T, DK>), dim3((unsigned)(p.batch * p.heads * p.chunks)), dim3(256), 0, s, p);
     }
-    static void chain(const DeltaArgs &p, hipStream_t s)
+    static unsigned slices(const DeltaArgs &p) { return (unsigned)((p.batch * p.heads + 7) / 8 * 8 * (p.columns / 16)); }
+    static void chain(const DeltaArgs &p, bool keep, hipStream_t s)
     {
-        const int64_t grid = (p.batch * p.heads + 7) / 8 * 8 * (p.columns / 16);
-        hipLaunchKernelGGL((delta_chain_kernel<DK>), dim3((unsigned)grid), dim3(256), 0, s, p);
+        auto *const kernel = keep ? delta_chain_kernel<T, DK, true> : delta_chain_kernel<T, DK, false>;
+        hipLaunchKernelGGL(kernel, dim3(slices(p)), dim3(512), 0, s, p);
     }
     static hipError_t forward(DeltaArgs p, const DeltaPlan &P, float *way, hipStream_t s)
     {
@@ -863,8 +1060,7 @@ struct DeltaLaunch {
             p.chunks = (int32_t)std::min(P.segment, P.chunks - p.chunk0);
             p.last = seg + 1 < P.segments ? way + (seg & 1) * state : last;
             prepare(p, s);
-            chain(p, s);
-            hipLaunchKernelGGL((delta_output_kernel<T, DK>), dim3((unsigned)(p.batch * p.heads * p.chunks)), dim3(256), 0, s, p);
+            chain(p, false, s);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             p.state = p.last;
@@ -876,17 +1072,14 @@ struct DeltaLaunch {
     {
         const int64_t state = p.batch * p.heads * p.key_dim * p.value_dim;
         const float *const first = p.state;
-        float *const keep_s = p.s;
         for (int64_t seg = 0; seg + 1 < P.segments; ++seg) {
             p.chunk0 = seg * P.segment;
             p.chunks = (int32_t)P.segment;
             p.state = seg == 0 ? first : bounds + (seg - 1) * state;
             p.last = bounds + seg * state;
-            p.s = nullptr;
             prepare(p, s);
-            chain(p, s);
+            chain(p, true, s);
         }
-        p.s = keep_s;
         for (int64_t seg = P.segments - 1; seg >= 0; --seg) {
             p.chunk0 = seg * P.segment;
             p.chunks = (int32_t)std::min(P.segment, P.chunks - p.chunk0);
@@ -894,14 +1087,13 @@ struct DeltaLaunch {
             p.last = nullptr;
             p.keep = 1;
             prepare(p, s);
-            chain(p, s);
+            chain(p, true, s);
             const dim3 grid((unsigned)(p.batch * p.heads * p.chunks));
             hipLaunchKernelGGL((delta_back_prepare_kernel<T, DK>), grid, dim3(DK * 4), 0, s, p);
             DeltaArgs back = p;
-            back.backward = 1;
             back.state = dlast;
             back.last = seg > 0 ? way + (seg & 1) * state : dstate;
-            chain(back, s);
+            hipLaunchKernelGGL((delta_back_chain_kernel<DK>), dim3(slices(p)), dim3(256), 0, s, back);
             dlast = back.last;
             hipLaunchKernelGGL((delta_back_output_kernel<T, DK>), grid, dim3(DK * 4), 0, s, p);
             if (p.group > 1)
