@@ -50,6 +50,7 @@ struct DeltaArgs {
     float *w, *y, *mt, *s, *x, *dy, *ds, *gq, *gk;       // [64][DK], [64][columns], [DK][64], [DK][columns], [64][64], [64][columns], [DK][columns], [64][DK] x 2
     float *carry;                                        // a_63
     float *gates;                                        // [2][64]: a, c beta
+    float *spare;                                        // 64 numbers that nothing reads
     // planes, in the order in which the chain's lanes hold them: of X and scale P beta; per (key head, chunk) of K, Q and K^T
     __bf16 *xp, *pp, *kp, *qp, *kt;
     int32_t keep;                                        // x (and, by the chain, s and y) are written
@@ -179,13 +180,15 @@ __device__ inline void load_planes(b8 (&to)[N], const __bf16 *p, int plane, int 
 #pragma unroll
     for (int i = 0; i < N; ++i) to[i] = *reinterpret_cast<const b8 *>(p + i * plane + (row + lane16()) * ld + k + lane8());
 }
-// a result (four rows of a column) into planes whose rows are the columns: the next product's right operand
-__device__ inline void put_planes(__bf16 *p, int plane, int ld, int row, f4 v)
+// a result (four rows, from `row` on, of 16 columns) as the next product's right operand, which sums over the rows: blocks in the order of the lanes, so that no
+// bank is asked twice
+__device__ inline void put_block(__bf16 *p, int row, f4 v)
 {
     b4 to[3];
     split(v, to);
+    const int k = row + lane4();
 #pragma unroll
-    for (int i = 0; i < 3; ++i) *reinterpret_cast<b4 *>(p + i * plane + lane16() * ld + row + lane4()) = to[i];
+    for (int i = 0; i < 3; ++i) *reinterpret_cast<b4 *>(p + place_in<3>(lane16(), k, 1, i) + (k & 4)) = to[i];
 }
 
 // The tiles on and below the diagonal of a chunk x chunk matrix
@@ -394,19 +397,28 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
 // + scale P beta Y.  Then all of them: S = carry S + K^T (c beta Y), 16 rows of it each.  Three barriers a chunk; what a chunk needs of memory is
 // read while the one before it is worked on.
 
+// Every wave of a kind has the same loads and stores in the same order, none of them behind a branch, so that it waits for a load by how many came after it
+// and for nothing else: what has no place to go is stored to a spare one.  (Behind branches a chunk took 2.4 us in place of 1.0.)
 // Steps behind the last one are worked on with the last one's v: beta is 0 there, and what they give is not written.
-template <typename T, int DK, bool KEEP>
-__global__ void __launch_bounds__(512) delta_chain_kernel(DeltaArgs p)
+template <int DK>
+struct alignas(16) ChainShared {
+    __bf16 s[3 * 16 * DK], r[3 * 16 * kChunk], y[3 * 16 * kChunk], u[3 * 16 * kChunk];
+};
+__device__ inline void all_waves()
 {
-    constexpr int NI = kPlanes<T>, LD = DK + 8, SPlane = 16 * LD, CL = kChunk + 8, CPlane = 16 * CL, Square = kChunk * kChunk;
-    __shared__ __attribute__((aligned(16))) __bf16 st[3 * SPlane], rt[3 * CPlane], yt[3 * CPlane], ut[3 * CPlane];
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile = wave & 3, slices = p.columns / 16;
-    const bool answers = wave >= 4, mine = wave < DK / 16, low = tile >= 2;      // low: rows whose sums reach over the second half of the steps
-    // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
-    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
-    if (bh >= p.batch * p.heads) return;
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+template <typename T, int DK, bool KEEP, bool ANSWERS>
+__device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_t bh, int slice)
+{
+    constexpr int NI = kPlanes<T>, Square = kChunk * kChunk, Inputs = NI * kChunk * DK;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile = wave & 3;
+    const bool mine = wave < DK / 16;                    // it has 16 rows of the state
     const int64_t b = bh / p.heads, head = bh % p.heads, key = head / p.group, kbh = b * (p.heads / p.group) + key;
-    const int column = (int)(place % slices) * 16, j = column + lane16(), read = min(j, p.value_dim - 1);
+    const int column = slice * 16, j = column + lane16();
     f4 state{};
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
@@ -414,98 +426,110 @@ __global__ void __launch_bounds__(512) delta_chain_kernel(DeltaArgs p)
         if (p.state && mine && row < p.key_dim && j < p.value_dim) state[m] = p.state[(bh * p.key_dim + row) * p.value_dim + j];
     }
     // where a wave's part of a chunk begins; the next chunk's follows behind it
-    const __bf16 *rows_at = (answers ? p.qp : p.kp) + kbh * p.chunks * NI * kChunk * DK + tile * (DK / 32) * NI * 512;
-    const __bf16 *left_at = (answers ? p.pp : p.xp) + bh * p.chunks * 3 * Square + tile * 2 * 3 * 512;
-    const __bf16 *kt_at = p.kt + kbh * p.chunks * NI * kChunk * DK + (mine ? wave : 0) * 2 * NI * 512;
-    const float *gates_at = p.gates + bh * p.chunks * 2 * kChunk + tile * 16;
-    const T *const v_at = at<T>(p.v, b, 0, head);
+    const __bf16 *rows_at = (ANSWERS ? p.qp : p.kp) + kbh * p.chunks * Inputs + tile * (DK / 32) * NI * 512;
+    const __bf16 *left_at = (ANSWERS ? p.pp : p.xp) + bh * p.chunks * 3 * Square + tile * 2 * 3 * 512;
+    const __bf16 *kt_at = p.kt + kbh * p.chunks * Inputs + (mine ? wave : 0) * 2 * NI * 512;
+    const float *a_at = p.gates + bh * p.chunks * 2 * kChunk + tile * 16, *cbeta_at = a_at + kChunk, *carry_at = p.carry + bh * p.chunks;
+    const int64_t t0 = p.chunk0 * kChunk + tile * 16 + lane4();
+    const T *const v_at = at<T>(p.v, b, 0, head) + min(j, p.value_dim - 1);
+    T *const spare = reinterpret_cast<T *>(p.spare) + (threadIdx.x & 63);
     b8 rows[DK / 32][NI], left[2][3], kt[2][NI];
     T v[4];
-    f4 a, cbeta;
+    f4 a, cbeta{};
     float carry;
+    // a chunk's loads in three groups, each right after the last use of what it takes the place of
     const auto load_rows_of = [&](int n) {
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at + (int64_t)n * NI * kChunk * DK, kb);
-        a = four(gates_at + (int64_t)n * 2 * kChunk, 0);
-        if (!answers) {
-            const int64_t t = (p.chunk0 + n) * kChunk + tile * 16 + lane4();
+        for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at, kb);
+        a = four(a_at, 0);
+        if (!ANSWERS) {
+            const int64_t t = t0 + (int64_t)n * kChunk;
 #pragma unroll
-            for (int m = 0; m < 4; ++m) v[m] = v_at[min(t + m, p.steps - 1) * p.v.step + read];
+            for (int m = 0; m < 4; ++m) v[m] = v_at[min(t + m, p.steps - 1) * p.v.step];
         }
     };
-    const auto load_left_of = [&](int n) {
-        load_block(left[0], left_at + (int64_t)n * 3 * Square, 0);
-        if (low) load_block(left[1], left_at + (int64_t)n * 3 * Square, 1);
-        if (!answers) cbeta = four(gates_at + (int64_t)n * 2 * kChunk + kChunk, 0);
+    const auto load_left_of = [&]() {
+        load_block(left[0], left_at, 0);
+        load_block(left[1], left_at, 1);
+        if (!ANSWERS) cbeta = four(cbeta_at, 0);
     };
-    const auto load_kt_of = [&](int n) {
+    const auto load_kt_of = [&]() {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) load_block(kt[kb], kt_at + (int64_t)n * NI * kChunk * DK, kb);
-        carry = p.carry[bh * p.chunks + n];
+        for (int kb = 0; kb < 2; ++kb) load_block(kt[kb], kt_at, kb);
+        carry = *carry_at;
     };
     load_rows_of(0);
-    load_left_of(0);
-    load_kt_of(0);
+    load_left_of();
+    load_kt_of();
     for (int n = 0; n < p.chunks; ++n) {
         const int64_t unit = bh * p.chunks + n;
-        const int after = min(n + 1, p.chunks - 1);
+        const bool more = n + 1 < p.chunks;              // (behind the last chunk the loads are of the last one again)
+        if (more) {
+            rows_at += Inputs;
+            kt_at += Inputs;
+            left_at += 3 * Square;
+            a_at += 2 * kChunk;
+            cbeta_at += 2 * kChunk;
+            ++carry_at;
+        }
         if (mine) {
-            put_planes(st, SPlane, LD, wave * 16, state);
+            put_block(sh.s, wave * 16, state);
             if (KEEP) put(p.s + unit * DK * p.columns, p.columns, wave * 16, column, state);
         }
-        __syncthreads();
-        f4 by_state{};
+        all_waves();
+        // K S, and beside the next product Q S
+        const auto rows_by_state = [&] {
+            // (all operands are asked for before the first product: one after the other, each would wait for LDS by itself)
+            b8 s[DK / 32][3];
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) {
-            b8 s[3];
-            load_planes(s, st, SPlane, LD, 0, kb * 32);
-            by_state = mmp(rows[kb], s, by_state);
-        }
-        by_state *= a;
-        if (!answers) {
+            for (int kb = 0; kb < DK / 32; ++kb) load_block(s[kb], sh.s, kb);
+            __builtin_amdgcn_sched_barrier(0);
+            f4 sum{}, other{};
+#pragma unroll
+            for (int kb = 0; kb < DK / 32; ++kb) (kb & 1 ? other : sum) = mmp(rows[kb], s[kb], kb & 1 ? other : sum);
+            return (sum + other) * a;
+        };
+        f4 by_query{};
+        if (!ANSWERS) {
             const f4 x{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-            put_planes(rt, CPlane, CL, tile * 16, x - by_state);
+            put_block(sh.r, tile * 16, x - rows_by_state());
+            load_rows_of(more ? n + 1 : n);
         }
-        load_rows_of(after);
-        __syncthreads();
-        if (!answers) {
-            b8 r[3];
-            load_planes(r, rt, CPlane, CL, 0, 0);
-            f4 y = mmp(left[0], r, f4{});
-            if (low) {
-                load_planes(r, rt, CPlane, CL, 0, 32);
-                y = mmp(left[1], r, y);
-            }
-            put_planes(yt, CPlane, CL, tile * 16, y);
-            put_planes(ut, CPlane, CL, tile * 16, y * cbeta);
+        all_waves();
+        if (ANSWERS) {
+            by_query = rows_by_state();
+            load_rows_of(more ? n + 1 : n);
+        } else {
+            b8 r[2][3];
+            load_block(r[0], sh.r, 0);
+            load_block(r[1], sh.r, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            f4 y = mmp(left[0], r[0], f4{});
+            if (tile >= 2) y += mmp(left[1], r[1], f4{});
+            put_block(sh.y, tile * 16, y);
+            put_block(sh.u, tile * 16, y * cbeta);
             if (KEEP) put(p.y + unit * kChunk * p.columns, p.columns, tile * 16, column, y);
-            load_left_of(after);
+            load_left_of();
         }
-        __syncthreads();
-        if (mine) {
-            state *= carry;
+        all_waves();
+        b8 u[2][3], y[2][3];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                b8 u[3];
-                load_planes(u, ut, CPlane, CL, 0, kb * 32);
-                state = mmp(kt[kb], u, state);
-            }
-            load_kt_of(after);
+        for (int kb = 0; kb < 2; ++kb) load_block(u[kb], sh.u, kb);
+        if (!KEEP && ANSWERS) {
+            load_block(y[0], sh.y, 0);
+            load_block(y[1], sh.y, 1);
         }
-        if (!KEEP && answers) {
-            b8 y[3];
-            load_planes(y, yt, CPlane, CL, 0, 0);
-            f4 o = mmp(left[0], y, by_state * p.scale);
-            if (low) {
-                load_planes(y, yt, CPlane, CL, 0, 32);
-                o = mmp(left[1], y, o);
-            }
-            load_left_of(after);
-            const int64_t t = (p.chunk0 + n) * kChunk + tile * 16 + lane4();
+        __builtin_amdgcn_sched_barrier(0);
+        state = mmp(kt[0], u[0], state * carry) + mmp(kt[1], u[1], f4{});
+        if (!KEEP && ANSWERS) {
+            f4 o = mmp(left[0], y[0], by_query * p.scale);
+            if (tile >= 2) o += mmp(left[1], y[1], f4{});
+            const int64_t t = t0 + (int64_t)n * kChunk;
 #pragma unroll
-            for (int m = 0; m < 4; ++m)
-                if (t + m < p.steps && j < p.value_dim) out_at<T>(p.o, b, t + m, head)[j] = (T)o[m];
+            for (int m = 0; m < 4; ++m) *(t + m < p.steps && j < p.value_dim ? out_at<T>(p.o, b, t + m, head) + j : spare) = (T)o[m];
         }
+        if (ANSWERS) load_left_of();
+        load_kt_of();
     }
     if (!p.last || !mine || j >= p.value_dim) return;
 #pragma unroll
@@ -513,6 +537,18 @@ __global__ void __launch_bounds__(512) delta_chain_kernel(DeltaArgs p)
         const int row = wave * 16 + lane4() + m;
         if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[m];
     }
+}
+
+template <typename T, int DK, bool KEEP>
+__global__ void __launch_bounds__(512, 2) delta_chain_kernel(DeltaArgs p)
+{
+    __shared__ ChainShared<DK> sh;
+    // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
+    const int slices = p.columns / 16;
+    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
+    if (bh >= p.batch * p.heads) return;
+    if (threadIdx.x < 256) run_chain<T, DK, KEEP, false>(p, sh, bh, (int)(place % slices));
+    else run_chain<T, DK, KEEP, true>(p, sh, bh, (int)(place % slices));
 }
 
 // ---- backward: what the chain needs ------------------------------------------------------------------------------------------
@@ -975,7 +1011,7 @@ int padded_key(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
 struct DeltaPlan {
     int64_t chunks, segment, segments, units;            // chunks of a sequence, of a segment; units: (head, chunk) of a segment
     int dk, columns;
-    int64_t w, y, mt, s, x, dy, ds, gq, gk, carry, gates, xp, pp, kp, qp, kt, bounds, way, total;       // places in the workspace; way: the gradient by the state between segments
+    int64_t w, y, mt, s, x, dy, ds, gq, gk, carry, gates, spare, xp, pp, kp, qp, kt, bounds, way, total;       // places in the workspace; way: the gradient by the state between segments
 };
 DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
 {
@@ -997,6 +1033,7 @@ DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
     const auto take = [&](int64_t floats) { const int64_t here = at; at += align_up(floats * 4, 256); return here; };
     P.carry = take(P.units);
     P.gates = take(P.units * 2 * kChunk);
+    P.spare = take(64);
     P.xp = take(P.units * 3 * square / 2);
     P.pp = take(P.units * 3 * square / 2);
     const int64_t inputs = P.units / (h.heads / h.key_heads) * planes * side / 2;
@@ -1027,7 +1064,7 @@ void set_workspace(DeltaArgs &p, const DeltaPlan &P, char *ws)
 {
     const auto to = [&](int64_t place) { return reinterpret_cast<float *>(ws + place); };
     p.w = to(P.w); p.mt = to(P.mt); p.y = to(P.y); p.s = to(P.s); p.carry = to(P.carry);
-    p.gates = to(P.gates);
+    p.gates = to(P.gates); p.spare = to(P.spare);
     const auto planes = [&](int64_t place) { return reinterpret_cast<__bf16 *>(ws + place); };
     p.xp = planes(P.xp); p.pp = planes(P.pp); p.kp = planes(P.kp); p.qp = planes(P.qp); p.kt = planes(P.kt);
     p.x = to(P.x); p.dy = to(P.dy); p.ds = to(P.ds); p.gq = to(P.gq); p.gk = to(P.gk);
