@@ -47,13 +47,14 @@ struct DeltaArgs {
     int32_t key_dim, value_dim, columns;                 // columns: value_dim rounded up to 64
     float scale;
     // workspace, an entry per (head, chunk of the launch)
-    float *w, *y, *mt, *s, *x, *dy, *ds, *gq, *gk;       // [64][DK], [64][columns], [DK][64], [DK][columns], [64][64], [64][columns], [DK][columns], [64][DK] x 2
+    float *y, *s, *dy, *ds, *gq, *gk;                    // [64][columns], [DK][columns], the same two, [64][DK] x 2
     float *carry;                                        // a_63
     float *gates;                                        // [2][64]: a, c beta
     float *spare;                                        // 64 numbers that nothing reads
-    // planes, in the order in which the chain's lanes hold them: of X and scale P beta; per (key head, chunk) of K, Q and K^T
-    __bf16 *xp, *pp, *kp, *qp, *kt;
-    int32_t keep;                                        // x (and, by the chain, s and y) are written
+    // planes, in the order in which the chain's lanes hold them: of X and scale P beta (backward: turned, and X^T beside X); per (key head, chunk) of
+    // K, Q, K^T (and Q^T)
+    __bf16 *xp, *pp, *xt, *kp, *qp, *kt, *qt;
+    int32_t keep;                                        // for the backward pass
 };
 
 template <typename T>
@@ -182,13 +183,14 @@ __device__ inline void load_planes(b8 (&to)[N], const __bf16 *p, int plane, int 
 }
 // a result (four rows, from `row` on, of 16 columns) as the next product's right operand, which sums over the rows: blocks in the order of the lanes, so that no
 // bank is asked twice
+template <int N = 3>
 __device__ inline void put_block(__bf16 *p, int row, f4 v)
 {
-    b4 to[3];
+    b4 to[N];
     split(v, to);
     const int k = row + lane4();
 #pragma unroll
-    for (int i = 0; i < 3; ++i) *reinterpret_cast<b4 *>(p + place_in<3>(lane16(), k, 1, i) + (k & 4)) = to[i];
+    for (int i = 0; i < N; ++i) *reinterpret_cast<b4 *>(p + place_in<N>(lane16(), k, 1, i) + (k & 4)) = to[i];
 }
 
 // The tiles on and below the diagonal of a chunk x chunk matrix
@@ -234,43 +236,6 @@ struct alignas(16) Gates {
     }
     __device__ float decay(int i, int j) const { return j <= i && part[i] == part[j] ? expf((float)(gamma[i] - gamma[j])) : 0.0f; }
 };
-
-// 64 rows of a head from step t0 on, `width` columns from `column` on, as fp32 in LDS; 0 behind the last step and the last column
-template <typename T>
-__device__ inline void load_rows(float *to, int ld, const DeltaArgs &p, const Heads &h, int64_t b, int64_t head, int64_t t0, int column, int width, int columns)
-{
-    constexpr int N = 16 / sizeof(T);
-    const int packs = width / N;
-    for (int u = threadIdx.x; u < kChunk * packs; u += blockDim.x) {
-        const int row = u / packs, at0 = u % packs * N, first = column + at0;
-        float x[N];
-        const bool in = t0 + row < p.steps;
-        const T *const from = at<T>(h, b, t0 + row, head) + first;
-        if (in && first + N <= columns) {
-            T raw[N];
-            __builtin_memcpy(raw, from, 16);
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = (float)raw[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                x[i] = 0.0f;
-                if (in && first + i < columns) x[i] = (float)from[i];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < N; i += 4) *reinterpret_cast<f4 *>(to + row * ld + at0 + i) = f4{x[i], x[i + 1], x[i + 2], x[i + 3]};
-    }
-}
-// the same from 64 rows of the workspace
-__device__ inline void load_kept(float *to, int ld, const float *from, int ld_from, int column, int width)
-{
-    const int packs = width / 4;
-    for (int u = threadIdx.x; u < kChunk * packs; u += blockDim.x) {
-        const int row = u / packs, at0 = u % packs * 4;
-        *reinterpret_cast<f4 *>(to + row * ld + at0) = *reinterpret_cast<const f4 *>(from + (int64_t)row * ld_from + column + at0);
-    }
-}
 
 // ---- all chunks at once: X, P and K^T -------------------------------------------------------------------------------------
 
@@ -335,6 +300,10 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = k[i * Plane + (t + e) * LD + d];
                 *reinterpret_cast<b8 *>(p.kt + inputs + place_in<NI>(d, t, 2, i)) = v;
+                if (!p.keep) continue;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = q[i * Plane + (t + e) * LD + d];
+                *reinterpret_cast<b8 *>(p.qt + inputs + place_in<NI>(d, t, 2, i)) = v;
             }
         }
     }
@@ -373,22 +342,28 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
     }
     for (int u = threadIdx.x; u < kChunk * 8; u += 256) {
         const int i = u / 8, j = u % 8 * 8;
-        vec8<float> vx, vp;
+        vec8<float> vx, vp, vt;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             vx[e] = j + e <= i ? x[i * kEdge + j + e] : 0.0f;
-            vp[e] = j + e <= i ? n[(j + e) * kEdge + i] : 0.0f;
+            if (p.keep) {
+                vp[e] = j + e >= i ? n[i * kEdge + j + e] : 0.0f;
+                vt[e] = j + e >= i ? x[(j + e) * kEdge + i] : 0.0f;
+            } else {
+                vp[e] = j + e <= i ? n[(j + e) * kEdge + i] : 0.0f;
+            }
         }
-        b8 px[3], pp[3];
+        b8 px[3], pp[3], pt[3];
         split(vx, px);
         split(vp, pp);
+        if (p.keep) split(vt, pt);
 #pragma unroll
         for (int plane = 0; plane < 3; ++plane) {
             const int64_t to = unit * 3 * kChunk * kChunk + place_in<3>(i, j, 2, plane);
             *reinterpret_cast<b8 *>(p.xp + to) = px[plane];
             *reinterpret_cast<b8 *>(p.pp + to) = pp[plane];
+            if (p.keep) *reinterpret_cast<b8 *>(p.xt + to) = pt[plane];
         }
-        if (p.keep) __builtin_memcpy(p.x + (unit * kChunk + i) * kChunk + j, &vx, 32);
     }
 }
 
@@ -398,7 +373,8 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
 // read while the one before it is worked on.
 
 // Every wave of a kind has the same loads and stores in the same order, none of them behind a branch, so that it waits for a load by how many came after it
-// and for nothing else: what has no place to go is stored to a spare one.  (Behind branches a chunk took 2.4 us in place of 1.0.)
+// and for nothing else: what has no place to go is stored to a spare one.  Products with a block of zeros are taken too, for the same reason and because
+// the compiler leaves out the wait states between a matrix instruction and what reads its result behind a branch to an earlier block.
 // Steps behind the last one are worked on with the last one's v: beta is 0 there, and what they give is not written.
 template <int DK>
 struct alignas(16) ChainShared {
@@ -504,8 +480,7 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
             load_block(r[0], sh.r, 0);
             load_block(r[1], sh.r, 1);
             __builtin_amdgcn_sched_barrier(0);
-            f4 y = mmp(left[0], r[0], f4{});
-            if (tile >= 2) y += mmp(left[1], r[1], f4{});
+            const f4 y = mmp(left[0], r[0], f4{}) + mmp(left[1], r[1], f4{});
             put_block(sh.y, tile * 16, y);
             put_block(sh.u, tile * 16, y * cbeta);
             if (KEEP) put(p.y + unit * kChunk * p.columns, p.columns, tile * 16, column, y);
@@ -522,8 +497,7 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
         __builtin_amdgcn_sched_barrier(0);
         state = mmp(kt[0], u[0], state * carry) + mmp(kt[1], u[1], f4{});
         if (!KEEP && ANSWERS) {
-            f4 o = mmp(left[0], y[0], by_query * p.scale);
-            if (tile >= 2) o += mmp(left[1], y[1], f4{});
+            const f4 o = mmp(left[0], y[0], by_query * p.scale) + mmp(left[1], y[1], f4{});
             const int64_t t = t0 + (int64_t)n * kChunk;
 #pragma unroll
             for (int m = 0; m < 4; ++m) *(t + m < p.steps && j < p.value_dim ? out_at<T>(p.o, b, t + m, head) + j : spare) = (T)o[m];
@@ -551,226 +525,258 @@ __global__ void __launch_bounds__(512, 2) delta_chain_kernel(DeltaArgs p)
     else run_chain<T, DK, KEEP, true>(p, sh, bh, (int)(place % slices));
 }
 
-// ---- backward: what the chain needs ------------------------------------------------------------------------------------------
-// w = X^T (beta c K), mt = -(a K)^T, dy = X^T (beta scale P^T dO), ds = scale (a Q)^T dO
+// ---- backward: the chain from the last chunk to the first ----------------------------------------------------------------
+// Z = c beta (K dS) + (scale P beta)^T dO and dY = X^T Z by the first four waves, then by all of them dS = carry dS + Q^T (scale a dO) - K^T (a dY).
+// dS behind every chunk goes to ds, dY to dy.  Loads and stores as in the forward chain.
 
 template <typename T, int DK>
-__global__ void __launch_bounds__(DK * 4) delta_back_prepare_kernel(DeltaArgs p)
-{
-    constexpr int W = DK / 16, LD = DK + 4, Most = (kLower + W - 1) / W;
-    __shared__ Gates gates;
-    __shared__ __attribute__((aligned(16))) float q[kChunk * LD], k[kChunk * LD], x[kChunk * kEdge], r[kChunk * kEdge], d[kChunk * kEdge];
-    __shared__ __attribute__((aligned(16))) float by_p[kChunk], by_k[kChunk], by_q[kChunk];
-    const int wave = threadIdx.x >> 6;
-    const int64_t unit = blockIdx.x, bh = unit / p.chunks, b = bh / p.heads, head = bh % p.heads, t0 = (p.chunk0 + unit % p.chunks) * kChunk;
-    gates.load(p, b, head, t0);
-    load_rows<T>(q, LD, p, p.q, b, head / p.group, t0, 0, DK, p.key_dim);
-    load_rows<T>(k, LD, p, p.k, b, head / p.group, t0, 0, DK, p.key_dim);
-    load_kept(x, kEdge, p.x + unit * kChunk * kChunk, kChunk, 0, kChunk);
-    __syncthreads();
-    if (threadIdx.x < kChunk) {
-        const int t = threadIdx.x;
-        by_p[t] = gates.beta[t] * p.scale;
-        by_k[t] = gates.beta[t] * gates.c[t];
-        by_q[t] = gates.a[t] * p.scale;
-    }
-    for (int u = wave; u < kLower; u += W) {
-        int ti, tj;
-        lower_tile(u, ti, tj);
-        f4 acc{};
-#pragma unroll
-        for (int kb = 0; kb < DK; kb += 16) acc = mm(along(q, LD, ti * 16, kb), along(k, LD, tj * 16, kb), acc);
-#pragma unroll
-        for (int m = 0; m < 4; ++m) acc[m] *= gates.decay(ti * 16 + lane4() + m, tj * 16 + lane16());
-        put(r, kEdge, ti * 16, tj * 16, acc);
-    }
-    __syncthreads();
-    // R = X^T (beta scale) P^T, on and above the diagonal: tile (tj, ti) of the lower tile (ti, tj)
-    f4 rt[Most];
-#pragma unroll
-    for (int e = 0; e < Most; ++e) {
-        const int u = wave + W * e;
-        rt[e] = f4{};
-        if (u >= kLower) continue;
-        int ti, tj;
-        lower_tile(u, ti, tj);
-        for (int kb = tj; kb <= ti; ++kb) rt[e] = mm(across(x, kEdge, kb * 16, tj * 16) * four(by_p, kb * 16), along(r, kEdge, ti * 16, kb * 16), rt[e]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < Most; ++e) {
-        const int u = wave + W * e;
-        if (u >= kLower) continue;
-        int ti, tj;
-        lower_tile(u, ti, tj);
-        put(r, kEdge, tj * 16, ti * 16, rt[e]);
-    }
-#pragma unroll
-    for (int ti = 0; ti < 4; ++ti) {
-        f4 acc{};
-        for (int kb = ti; kb < 4; ++kb) acc = mm(across(x, kEdge, kb * 16, ti * 16) * four(by_k, kb * 16), across(k, LD, kb * 16, wave * 16), acc);
-        put(p.w + unit * kChunk * DK, DK, ti * 16, wave * 16, acc);
-    }
-    {
-        const int t = threadIdx.x & 63;
-        const float factor = -gates.a[t];
-        float *const mt = p.mt + unit * DK * kChunk + t;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mt[(wave * 16 + i) * kChunk] = factor * k[t * LD + wave * 16 + i];
-    }
-    for (int column = 0; column < p.columns; column += kChunk) {
-        __syncthreads();
-        load_rows<T>(d, kEdge, p, p.dout, b, head, t0, column, kChunk, p.value_dim);
-        __syncthreads();
-        for (int u = wave; u < 16; u += W) {
-            const int ti = u >> 2, tc = u & 3;
-            f4 acc{};
-            for (int kb = ti; kb < 4; ++kb) acc = mm(along(r, kEdge, ti * 16, kb * 16), across(d, kEdge, kb * 16, tc * 16), acc);
-            put(p.dy + unit * kChunk * p.columns, p.columns, ti * 16, column + tc * 16, acc);
-        }
-        f4 acc[4] = {};
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            const f4 left = across(q, LD, kb * 16, wave * 16) * four(by_q, kb * 16);
-#pragma unroll
-            for (int tc = 0; tc < 4; ++tc) acc[tc] = mm(left, across(d, kEdge, kb * 16, tc * 16), acc[tc]);
-        }
-#pragma unroll
-        for (int tc = 0; tc < 4; ++tc) put(p.ds + unit * DK * p.columns, p.columns, wave * 16, column + tc * 16, acc[tc]);
-    }
-}
-
-// ---- backward: the chain from the last chunk to the first ----------------------------------------------------------------
-// dy += w dS;  dS' = carry dS + ds + mt dy.  dS of every chunk goes to ds, in the place of what was read there.
-
-template <int DK>
-struct BackStep {                                       // what a wave needs of a chunk
-    static constexpr int TS = DK / 16 >= 4 ? DK / 64 : 1;
-    f4 w[DK / 16], mt[TS][4], y, ds[TS];
-    float carry;
+struct alignas(16) BackShared {
+    // (q is read to a chunk's end, so the next chunk's has a place of its own)
+    __bf16 s[3 * 16 * DK], o[kPlanes<T> * 16 * kChunk], q[2][3 * 16 * kChunk], z[3 * 16 * kChunk], u[3 * 16 * kChunk];
 };
 
-template <int DK>
-__global__ void __launch_bounds__(256) delta_back_chain_kernel(DeltaArgs p)
+template <typename T, int DK, bool FEEDS>
+__device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh, int64_t bh, int slice)
 {
-    constexpr int TS = BackStep<DK>::TS, LD = 20;
-    __shared__ float s_l[DK * LD], y_l[kChunk * LD];
-    const int wave = threadIdx.x >> 6, slices = p.columns / 16;
-    // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
-    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
-    const int column = (int)(place % slices) * 16, j = column + lane16();
-    if (bh >= p.batch * p.heads) return;
-    const bool mine = wave * TS * 16 < DK;
-    const int rows = wave * TS * 16;                     // of the state
-    float *const ys = p.dy, *const ss = p.ds;
-    f4 state[TS];
+    constexpr int NI = kPlanes<T>, Square = kChunk * kChunk, Inputs = NI * kChunk * DK;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile = wave & 3;
+    const bool mine = wave < DK / 16;
+    const int64_t b = bh / p.heads, head = bh % p.heads, key = head / p.group, kbh = b * (p.heads / p.group) + key, end = p.chunks - 1;
+    const int column = slice * 16, j = column + lane16();
+    f4 state{};
 #pragma unroll
-    for (int i = 0; i < TS; ++i)
+    for (int m = 0; m < 4; ++m) {
+        const int row = wave * 16 + lane4() + m;
+        if (p.state && mine && row < p.key_dim && j < p.value_dim) state[m] = p.state[(bh * p.key_dim + row) * p.value_dim + j];
+    }
+    const __bf16 *rows_at = p.kp + (kbh * p.chunks + end) * Inputs + tile * (DK / 32) * NI * 512;
+    const __bf16 *pt_at = p.pp + (bh * p.chunks + end) * 3 * Square + tile * 2 * 3 * 512, *xt_at = p.xt + (bh * p.chunks + end) * 3 * Square + tile * 2 * 3 * 512;
+    const int64_t turned = (kbh * p.chunks + end) * Inputs + (mine ? wave : 0) * 2 * NI * 512;
+    const __bf16 *kt_at = p.kt + turned, *qt_at = p.qt + turned;
+    const float *a_at = p.gates + (bh * p.chunks + end) * 2 * kChunk + tile * 16, *cbeta_at = a_at + kChunk, *carry_at = p.carry + bh * p.chunks + end;
+    const int64_t t0 = p.chunk0 * kChunk + tile * 16 + lane4();
+    const T *const d_at = at<T>(p.dout, b, 0, head) + min(j, p.value_dim - 1);
+    b8 rows[DK / 32][NI], pt[2][3], xt[2][3], kt[2][NI], qt[2][NI];
+    T d[4];
+    f4 a, cbeta;
+    float carry;
+    const auto load_first = [&](int n) {
+        if (FEEDS) {
+            const int64_t t = t0 + (int64_t)n * kChunk;
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const int row = rows + i * 16 + lane4() + m;
-            state[i][m] = p.state && mine && row < p.key_dim && j < p.value_dim ? p.state[(bh * p.key_dim + row) * p.value_dim + j] : 0.0f;
+            for (int m = 0; m < 4; ++m) d[m] = d_at[min(t + m, p.steps - 1) * p.dout.step];
+            a = four(a_at, 0);
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at, kb);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) load_block(pt[kb], pt_at, kb);
+            cbeta = four(cbeta_at, 0);
         }
-    const auto load = [&](int n) {
-        const int64_t unit = bh * p.chunks + p.chunks - 1 - n;
-        BackStep<DK> c;
-        const float *const w = p.w + unit * kChunk * DK;
-#pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) c.w[kb] = along(w, DK, wave * 16, kb * 16);
-        c.y = across(ys + unit * kChunk * p.columns, p.columns, wave * 16, column);
-        c.carry = p.carry[unit];
-        if (mine) {
-#pragma unroll
-            for (int i = 0; i < TS; ++i) {
-#pragma unroll
-                for (int kb = 0; kb < 4; ++kb) c.mt[i][kb] = along(p.mt + unit * DK * kChunk, kChunk, rows + i * 16, kb * 16);
-                c.ds[i] = across(p.ds + unit * DK * p.columns, p.columns, rows + i * 16, column);
-            }
-        }
-        return c;
     };
-    BackStep<DK> c = load(0);
-    for (int n = 0; n < p.chunks; ++n) {
-        const int64_t unit = bh * p.chunks + p.chunks - 1 - n;
-        const BackStep<DK> next = load(min(n + 1, p.chunks - 1));
-        if (mine) {
+    const auto load_second = [&]() {
 #pragma unroll
-            for (int i = 0; i < TS; ++i) {
-                put(s_l, LD, rows + i * 16, 0, state[i]);
-                put(ss + unit * DK * p.columns, p.columns, rows + i * 16, column, state[i]);
-            }
+        for (int kb = 0; kb < 2; ++kb) load_block(xt[kb], xt_at, kb);
+        a = four(a_at, 0);
+    };
+    const auto load_third = [&]() {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            load_block(kt[kb], kt_at, kb);
+            load_block(qt[kb], qt_at, kb);
         }
-        __syncthreads();
-        f4 y = c.y;
-#pragma unroll
-        for (int kb = 0; kb < DK / 16; ++kb) y = mm(c.w[kb], across(s_l, LD, kb * 16, 0), y);
-        put(y_l, LD, wave * 16, 0, y);
-        put(ys + unit * kChunk * p.columns, p.columns, wave * 16, column, y);
-        __syncthreads();
-        if (mine) {
-#pragma unroll
-            for (int i = 0; i < TS; ++i) {
-                f4 acc = state[i] * c.carry + c.ds[i];
-#pragma unroll
-                for (int kb = 0; kb < 4; ++kb) acc = mm(c.mt[i][kb], across(y_l, LD, kb * 16, 0), acc);
-                state[i] = acc;
-            }
+        carry = *carry_at;
+    };
+    load_first((int)end);
+    if (!FEEDS) load_second();
+    load_third();
+    for (int n = (int)end; n >= 0; --n) {
+        const int64_t unit = bh * p.chunks + n;
+        if (n > 0) {
+            rows_at -= Inputs;
+            kt_at -= Inputs;
+            qt_at -= Inputs;
+            pt_at -= 3 * Square;
+            xt_at -= 3 * Square;
+            a_at -= 2 * kChunk;
+            cbeta_at -= 2 * kChunk;
+            --carry_at;
         }
-        c = next;
+        const int before = n > 0 ? n - 1 : 0;
+        if (mine) {
+            put_block(sh.s, wave * 16, state);
+            put(p.ds + unit * DK * p.columns, p.columns, wave * 16, column, state);
+        }
+        if (FEEDS) {
+            f4 x;
+#pragma unroll
+            for (int m = 0; m < 4; ++m) x[m] = j < p.value_dim ? (float)d[m] : 0.0f;
+            put_block<NI>(sh.o, tile * 16, x);
+            put_block(sh.q[n & 1], tile * 16, x * a * p.scale);
+            load_first(before);
+        }
+        all_waves();
+        const auto by_queries = [&] {
+            b8 x[2][3];
+            load_block(x[0], sh.q[n & 1], 0);
+            load_block(x[1], sh.q[n & 1], 1);
+            __builtin_amdgcn_sched_barrier(0);
+            state = mmp(qt[0], x[0], state * carry) + mmp(qt[1], x[1], f4{});
+        };
+        if (FEEDS) {
+            by_queries();
+        } else {
+            b8 s[DK / 32][3], o[2][NI];
+#pragma unroll
+            for (int kb = 0; kb < DK / 32; ++kb) load_block(s[kb], sh.s, kb);
+            load_block(o[0], sh.o, 0);
+            load_block(o[1], sh.o, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            f4 sum{}, other{};
+#pragma unroll
+            for (int kb = 0; kb < DK / 32; ++kb) (kb & 1 ? other : sum) = mmp(rows[kb], s[kb], kb & 1 ? other : sum);
+            const f4 z = mmp(pt[0], o[0], f4{}) + mmp(pt[1], o[1], f4{});
+            put_block(sh.z, tile * 16, z + (sum + other) * cbeta);
+            load_first(before);
+        }
+        all_waves();
+        if (!FEEDS) {
+            b8 z[2][3];
+            load_block(z[0], sh.z, 0);
+            load_block(z[1], sh.z, 1);
+            __builtin_amdgcn_sched_barrier(0);
+            const f4 y = mmp(xt[0], z[0], f4{}) + mmp(xt[1], z[1], f4{});
+            put_block(sh.u, tile * 16, -y * a);
+            put(p.dy + unit * kChunk * p.columns, p.columns, tile * 16, column, y);
+            load_second();
+        }
+        all_waves();
+        if (!FEEDS) by_queries();
+        b8 u[2][3];
+        load_block(u[0], sh.u, 0);
+        load_block(u[1], sh.u, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        state = mmp(kt[0], u[0], state) + mmp(kt[1], u[1], f4{});
+        load_third();
     }
     if (!p.last || !mine || j >= p.value_dim) return;
 #pragma unroll
-    for (int i = 0; i < TS; ++i)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const int row = rows + i * 16 + lane4() + m;
-            if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[i][m];
-        }
+    for (int m = 0; m < 4; ++m) {
+        const int row = wave * 16 + lane4() + m;
+        if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[m];
+    }
+}
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(512, 2) delta_back_chain_kernel(DeltaArgs p)
+{
+    __shared__ BackShared<T, DK> sh;
+    const int slices = p.columns / 16;
+    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
+    if (bh >= p.batch * p.heads) return;
+    if (threadIdx.x < 256) run_back_chain<T, DK, false>(p, sh, bh, (int)(place % slices));
+    else run_back_chain<T, DK, true>(p, sh, bh, (int)(place % slices));
 }
 
 // ---- backward: all gradients at once -------------------------------------------------------------------------------------------
+// Over the value dimensions, 64 at a time: dO S^T, dY S^T, Y dS^T (16 key dimensions by a wave) and dO Y^T, dY Y^T; then with the gradients by Q K^T and
+// K K^T the products over the chunk's steps.
 
 __device__ inline float row_sum(float x)
 {
     return row_reduce(x, [](float a, float b) { return a + b; });
 }
 
-template <typename T, int DK>
-__global__ void __launch_bounds__(DK * 4) delta_back_output_kernel(DeltaArgs p)
+template <int NI>
+union BackOutputShared {
+    struct {
+        __bf16 o[NI * kChunk * kChunk], dy[3 * kChunk * kChunk], y[3 * kChunk * kChunk];
+    } in;
+    struct {
+        __bf16 qk[3 * kChunk * kChunk], qk_turned[3 * kChunk * kChunk], kk[3 * kChunk * kChunk], kk_turned[3 * kChunk * kChunk];
+    } by;
+};
+
+// a tile on or below the diagonal as the left operand that sums over its columns, and (turned) over its rows
+__device__ inline void put_tile(__bf16 *p, __bf16 *turned, int ti, int tj, f4 v)
 {
-    constexpr int W = DK / 16, LD = DK + 4, Most = (kLower + W - 1) / W;
+    b4 to[3];
+    split(v, to);
+    const int i = ti * 16 + lane4(), j = tj * 16 + lane16();
+#pragma unroll
+    for (int plane = 0; plane < 3; ++plane) {
+        *reinterpret_cast<b4 *>(turned + place_in<3>(j, i, 2, plane) + (i & 4)) = to[plane];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) p[place_in<3>(i + m, j, 2, plane) + (j & 7)] = to[plane][m];
+    }
+}
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(DK * 4, DK == 128 ? 2 : 1) delta_back_output_kernel(DeltaArgs p)
+{
+    constexpr int NI = kPlanes<T>, W = DK / 16, Most = (kLower + W - 1) / W;
     __shared__ Gates gates;
-    __shared__ __attribute__((aligned(16))) float q[kChunk * LD], k[kChunk * LD], d[kChunk * kEdge], e_[kChunk * kEdge], y[kChunk * kEdge];
+    __shared__ __attribute__((aligned(16))) BackOutputShared<NI> sh;
     __shared__ float by_row[4][kChunk], by_column[4][kChunk], by_itself[kChunk]; // of the chunk x chunk matrix, by tile; its diagonal, which no decay is in
     __shared__ float by_state[W][kChunk], kept[W][kChunk], dots[W];              // by wave
-    const int wave = threadIdx.x >> 6;
-    const int64_t unit = blockIdx.x, bh = unit / p.chunks, b = bh / p.heads, head = bh % p.heads, t0 = (p.chunk0 + unit % p.chunks) * kChunk;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t unit = blockIdx.x, bh = unit / p.chunks, chunk = unit % p.chunks, b = bh / p.heads, head = bh % p.heads, key = head / p.group;
+    const int64_t t0 = (p.chunk0 + chunk) * kChunk, inputs = ((b * (p.heads / p.group) + key) * p.chunks + chunk) * NI * kChunk * DK;
     gates.load(p, b, head, t0);
-    load_rows<T>(q, LD, p, p.q, b, head / p.group, t0, 0, DK, p.key_dim);
-    load_rows<T>(k, LD, p, p.k, b, head / p.group, t0, 0, DK, p.key_dim);
     f4 o_state[4] = {}, y_state[4] = {}, carried[4] = {}, from_o[Most] = {}, from_y[Most] = {};
     float dot = 0.0f;
-    const float *const s = p.s + unit * DK * p.columns, *const ds = p.ds + unit * DK * p.columns;
+    const float *const s = p.s + unit * DK * p.columns + (wave * 16 + lane16()) * p.columns, *const ds = p.ds + unit * DK * p.columns + (wave * 16 + lane16()) * p.columns;
     for (int column = 0; column < p.columns; column += kChunk) {
         __syncthreads();
-        load_rows<T>(d, kEdge, p, p.dout, b, head, t0, column, kChunk, p.value_dim);
-        load_kept(e_, kEdge, p.dy + unit * kChunk * p.columns, p.columns, column, kChunk);
-        load_kept(y, kEdge, p.y + unit * kChunk * p.columns, p.columns, column, kChunk);
-        __syncthreads();
-        for (int u = threadIdx.x; u < kChunk * kChunk; u += DK * 4) {            // dv is dy
-            const int row = u / kChunk, j = u % kChunk;
-            if (t0 + row < p.steps && column + j < p.value_dim) out_at<T>(p.dv, b, t0 + row, head)[column + j] = (T)e_[row * kEdge + j];
+        for (int u = threadIdx.x; u < kChunk * 8; u += DK * 4) {
+            const int row = u / 8, j = u % 8 * 8;
+            const bool in = t0 + row < p.steps;
+            b8 po[NI], pd[3], py[3];
+            planes_of(load_raw(at<T>(p.dout, b, t0 + row, head), in, column + j, p.value_dim), po);
+            vec8<float> dy, y;
+            const int64_t from = (unit * kChunk + row) * p.columns + column + j;
+            __builtin_memcpy(&dy, p.dy + from, 32);
+            __builtin_memcpy(&y, p.y + from, 32);
+            if (in) {                                    // dv is dy
+                T *const to = out_at<T>(p.dv, b, t0 + row, head) + column + j;
+                T v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (T)dy[e];
+                if (column + j + 8 <= p.value_dim) __builtin_memcpy(to, v, sizeof(v));
+                else
+                    for (int e = 0; e < 8; ++e)
+                        if (column + j + e < p.value_dim) to[e] = v[e];
+            }
+            split(dy, pd);
+            split(y, py);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) *reinterpret_cast<b8 *>(sh.in.o + place_in<NI>(row, j, 2, i)) = po[i];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                *reinterpret_cast<b8 *>(sh.in.dy + place_in<3>(row, j, 2, i)) = pd[i];
+                *reinterpret_cast<b8 *>(sh.in.y + place_in<3>(row, j, 2, i)) = py[i];
+            }
         }
+        __syncthreads();
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-            const f4 before = along(s, p.columns, wave * 16, column + kb * 16), after = along(ds, p.columns, wave * 16, column + kb * 16);
+        for (int kb = 0; kb < 2; ++kb) {
+            vec8<float> before, after;
+            __builtin_memcpy(&before, s + column + kb * 32 + lane8(), 32);
+            __builtin_memcpy(&after, ds + column + kb * 32 + lane8(), 32);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) dot = fmaf(before[m], after[m], dot);
+            for (int m = 0; m < 8; ++m) dot = fmaf(before[m], after[m], dot);
+            b8 ps[3], pd[3];
+            split(before, ps);
+            split(after, pd);
 #pragma unroll
             for (int ti = 0; ti < 4; ++ti) {
-                o_state[ti] = mm(along(d, kEdge, ti * 16, kb * 16), before, o_state[ti]);
-                y_state[ti] = mm(along(e_, kEdge, ti * 16, kb * 16), before, y_state[ti]);
-                carried[ti] = mm(along(y, kEdge, ti * 16, kb * 16), after, carried[ti]);
+                b8 o[NI], dy[3], y[3];
+                load_block(o, sh.in.o, ti * 2 + kb);
+                load_block(dy, sh.in.dy, ti * 2 + kb);
+                load_block(y, sh.in.y, ti * 2 + kb);
+                o_state[ti] = mmp(o, ps, o_state[ti]);
+                y_state[ti] = mmp(dy, ps, y_state[ti]);
+                carried[ti] = mmp(y, pd, carried[ti]);
             }
 #pragma unroll
             for (int e = 0; e < Most; ++e) {
@@ -778,14 +784,16 @@ __global__ void __launch_bounds__(DK * 4) delta_back_output_kernel(DeltaArgs p)
                 if (u >= kLower) continue;
                 int ti, tj;
                 lower_tile(u, ti, tj);
-                const f4 right = along(y, kEdge, tj * 16, kb * 16);
-                from_o[e] = mm(along(d, kEdge, ti * 16, kb * 16), right, from_o[e]);
-                from_y[e] = mm(along(e_, kEdge, ti * 16, kb * 16), right, from_y[e]);
+                b8 o[NI], dy[3], y[3];
+                load_block(y, sh.in.y, tj * 2 + kb);
+                load_block(o, sh.in.o, ti * 2 + kb);
+                load_block(dy, sh.in.dy, ti * 2 + kb);
+                from_o[e] = mmp(o, y, from_o[e]);
+                from_y[e] = mmp(dy, y, from_y[e]);
             }
         }
     }
     __syncthreads();
-    // d: the gradient by Q K^T, e_: by K K^T
 #pragma unroll
     for (int e = 0; e < Most; ++e) {
         const int u = wave + W * e;
@@ -794,10 +802,13 @@ __global__ void __launch_bounds__(DK * 4) delta_back_output_kernel(DeltaArgs p)
         lower_tile(u, ti, tj);
         f4 qk{}, kk{};
 #pragma unroll
-        for (int kb = 0; kb < DK; kb += 16) {
-            const f4 right = along(k, LD, tj * 16, kb);
-            qk = mm(along(q, LD, ti * 16, kb), right, qk);
-            kk = mm(along(k, LD, ti * 16, kb), right, kk);
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            b8 left[NI], right[NI];
+            load_block(right, p.kp + inputs, tj * (DK / 32) + kb);
+            load_block(left, p.qp + inputs, ti * (DK / 32) + kb);
+            qk = mmp(left, right, qk);
+            load_block(left, p.kp + inputs, ti * (DK / 32) + kb);
+            kk = mmp(left, right, kk);
         }
         const int j = tj * 16 + lane16();
         const float beta = gates.beta[j];
@@ -818,9 +829,17 @@ __global__ void __launch_bounds__(DK * 4) delta_back_output_kernel(DeltaArgs p)
         column_sum += __shfl_xor(column_sum, 16);
         column_sum += __shfl_xor(column_sum, 32);
         if (lane4() == 0) by_column[ti][j] = column_sum;
-        put(d, kEdge, ti * 16, tj * 16, by_qk);
-        put(e_, kEdge, ti * 16, tj * 16, by_kk);
+        put_tile(sh.by.qk, sh.by.qk_turned, ti, tj, by_qk);
+        put_tile(sh.by.kk, sh.by.kk_turned, ti, tj, by_kk);
+        if (ti == tj) {                                  // what a block of 32 has above the diagonal
+            const int other = ti ^ 1;
+            if (other > ti) {
+                put_tile(sh.by.qk, sh.by.qk_turned, ti, other, f4{});
+                put_tile(sh.by.kk, sh.by.kk_turned, ti, other, f4{});
+            }
+        }
     }
+    const int col = wave * 16 + lane16(), read = min(col, p.key_dim - 1);
 #pragma unroll
     for (int ti = 0; ti < 4; ++ti) {
         const f4 a = four(gates.a, ti * 16), c = four(gates.c, ti * 16);
@@ -830,26 +849,40 @@ __global__ void __launch_bounds__(DK * 4) delta_back_output_kernel(DeltaArgs p)
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const int i = ti * 16 + lane4() + m;
-            const float qi = q[i * LD + wave * 16 + lane16()], ki = k[i * LD + wave * 16 + lane16()];
+            const int64_t t = min(t0 + i, p.steps - 1);
+            // (behind the last step and key dimension the other factors are 0)
+            const float qi = (float)at<T>(p.q, b, t, key)[read], ki = (float)at<T>(p.k, b, t, key)[read];
             const float state_sum = row_sum(qi * o_state[ti][m] - ki * y_state[ti][m]), kept_sum = row_sum(ki * carried[ti][m]);
             if (lane16() == 0) by_state[wave][i] = state_sum, kept[wave][i] = kept_sum;
         }
     }
     dot = wave_reduce(dot, 0.0f, [](float x, float z) { return x + z; });
     if ((threadIdx.x & 63) == 0) dots[wave] = dot;
+    b8 kt[2][NI], qt[2][NI];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        load_block(kt[kb], p.kt + inputs, wave * 2 + kb);
+        load_block(qt[kb], p.qt + inputs, wave * 2 + kb);
+    }
     __syncthreads();
-    const int col = wave * 16 + lane16();
 #pragma unroll
     for (int ti = 0; ti < 4; ++ti) {
         f4 dq = o_state[ti], dk = carried[ti] * four(gates.beta, ti * 16) - y_state[ti];
-        for (int kb = 0; kb <= ti; ++kb) {
-            const f4 right = across(k, LD, kb * 16, wave * 16);
-            dq = mm(along(d, kEdge, ti * 16, kb * 16), right, dq);
-            dk = mm(along(e_, kEdge, ti * 16, kb * 16), right, dk);
-        }
-        for (int kb = ti; kb < 4; ++kb) {
-            dk = mm(across(d, kEdge, kb * 16, ti * 16), across(q, LD, kb * 16, wave * 16), dk);
-            dk = mm(across(e_, kEdge, kb * 16, ti * 16), across(k, LD, kb * 16, wave * 16), dk);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            b8 x[3];
+            if (kb <= ti / 2) {
+                load_block(x, sh.by.qk, ti * 2 + kb);
+                dq = mmp(x, kt[kb], dq);
+                load_block(x, sh.by.kk, ti * 2 + kb);
+                dk = mmp(x, kt[kb], dk);
+            }
+            if (kb >= ti / 2) {
+                load_block(x, sh.by.qk_turned, ti * 2 + kb);
+                dk = mmp(x, qt[kb], dk);
+                load_block(x, sh.by.kk_turned, ti * 2 + kb);
+                dk = mmp(x, kt[kb], dk);
+            }
         }
         if (p.group > 1) {                               // added up over the heads that share the keys by another launch
             put(p.gq + unit * kChunk * DK, DK, ti * 16, wave * 16, dq);
@@ -1003,15 +1036,17 @@ __global__ void __launch_bounds__(256) delta_step_kernel(DeltaArgs p)
 // ---- launches -------------------------------------------------------------------------------------------------------------------
 
 constexpr int64_t kFewSteps = 8;
-constexpr int64_t kSegmentBytes = 256ll << 20;           // workspace of the chunks that a launch takes: what the last-level cache holds
-thread_local int64_t g_segment_bytes = kSegmentBytes;
+// Workspace of the chunks that a launch takes.  Forward: what the last-level cache holds, nearly (8191 steps x 32 heads in 128, 256, 512, 1024 MB: 460, 372, 366,
+// 409 us).  Backward: more, as the states before every segment but the first cost a forward pass without outputs.
+constexpr int64_t kSegmentBytes = 384ll << 20, kBackSegmentBytes = 2ll << 30;
+thread_local int64_t g_segment_bytes = -1;
 
 int padded_key(int dk) { return dk <= 32 ? 32 : dk <= 64 ? 64 : 128; }
 
 struct DeltaPlan {
     int64_t chunks, segment, segments, units;            // chunks of a sequence, of a segment; units: (head, chunk) of a segment
     int dk, columns;
-    int64_t w, y, mt, s, x, dy, ds, gq, gk, carry, gates, spare, xp, pp, kp, qp, kt, bounds, way, total;       // places in the workspace; way: the gradient by the state between segments
+    int64_t y, s, dy, ds, gq, gk, carry, gates, spare, xp, pp, xt, kp, qp, kt, qt, bounds, way, total;       // places in the workspace; way: the gradient by the state between segments
 };
 DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
 {
@@ -1023,8 +1058,8 @@ DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
     const int64_t bh = h.batch * h.heads, side = kChunk * (int64_t)P.dk, rows = kChunk * (int64_t)P.columns, state = (int64_t)P.dk * P.columns;
     const bool shared = h.heads != h.key_heads;
     const int64_t planes = 3, square = kChunk * kChunk;          // (as for fp32: the workspace does not go by the type)
-    const int64_t each = 2 * (6 * square + 3 * planes * side) + (backward ? 4 * (2 * side + 2 * rows + 2 * state + square + (shared ? 2 * side : 0)) : 0);
-    const int64_t most = std::max<int64_t>(1, g_segment_bytes / each / bh);
+    const int64_t each = 2 * (6 * square + 3 * planes * side) + (backward ? 2 * (3 * square + planes * side) + 4 * (2 * rows + 2 * state + (shared ? 2 * side : 0)) : 0);
+    const int64_t limit = g_segment_bytes >= 0 ? g_segment_bytes : backward ? kBackSegmentBytes : kSegmentBytes, most = std::max<int64_t>(1, limit / each / bh);
     P.segments = (P.chunks + most - 1) / most;
     P.segment = (P.chunks + P.segments - 1) / P.segments;
     P.segments = (P.chunks + P.segment - 1) / P.segment;
@@ -1041,11 +1076,10 @@ DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
     P.qp = take(inputs);
     P.kt = take(inputs);
     if (backward) {
-        P.w = take(P.units * side);
-        P.mt = take(P.units * side);
+        P.xt = take(P.units * 3 * square / 2);
+        P.qt = take(inputs);
         P.y = take(P.units * rows);
         P.s = take(P.units * state);
-        P.x = take(P.units * square);
         P.dy = take(P.units * rows);
         P.ds = take(P.units * state);
         if (shared) P.gq = take(P.units * side), P.gk = take(P.units * side);
@@ -1063,11 +1097,11 @@ DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
 void set_workspace(DeltaArgs &p, const DeltaPlan &P, char *ws)
 {
     const auto to = [&](int64_t place) { return reinterpret_cast<float *>(ws + place); };
-    p.w = to(P.w); p.mt = to(P.mt); p.y = to(P.y); p.s = to(P.s); p.carry = to(P.carry);
-    p.gates = to(P.gates); p.spare = to(P.spare);
+    p.y = to(P.y); p.s = to(P.s); p.dy = to(P.dy); p.ds = to(P.ds); p.gq = to(P.gq); p.gk = to(P.gk);
+    p.carry = to(P.carry); p.gates = to(P.gates); p.spare = to(P.spare);
     const auto planes = [&](int64_t place) { return reinterpret_cast<__bf16 *>(ws + place); };
-    p.xp = planes(P.xp); p.pp = planes(P.pp); p.kp = planes(P.kp); p.qp = planes(P.qp); p.kt = planes(P.kt);
-    p.x = to(P.x); p.dy = to(P.dy); p.ds = to(P.ds); p.gq = to(P.gq); p.gk = to(P.gk);
+    p.xp = planes(P.xp); p.pp = planes(P.pp); p.xt = planes(P.xt);
+    p.kp = planes(P.kp); p.qp = planes(P.qp); p.kt = planes(P.kt); p.qt = planes(P.qt);
     p.columns = P.columns;
 }
 
@@ -1109,6 +1143,7 @@ struct DeltaLaunch {
     {
         const int64_t state = p.batch * p.heads * p.key_dim * p.value_dim;
         const float *const first = p.state;
+        p.keep = 1;
         for (int64_t seg = 0; seg + 1 < P.segments; ++seg) {
             p.chunk0 = seg * P.segment;
             p.chunks = (int32_t)P.segment;
@@ -1122,15 +1157,13 @@ struct DeltaLaunch {
             p.chunks = (int32_t)std::min(P.segment, P.chunks - p.chunk0);
             p.state = seg == 0 ? first : bounds + (seg - 1) * state;
             p.last = nullptr;
-            p.keep = 1;
             prepare(p, s);
             chain(p, true, s);
             const dim3 grid((unsigned)(p.batch * p.heads * p.chunks));
-            hipLaunchKernelGGL((delta_back_prepare_kernel<T, DK>), grid, dim3(DK * 4), 0, s, p);
             DeltaArgs back = p;
             back.state = dlast;
             back.last = seg > 0 ? way + (seg & 1) * state : dstate;
-            hipLaunchKernelGGL((delta_back_chain_kernel<DK>), dim3(slices(p)), dim3(256), 0, s, back);
+            hipLaunchKernelGGL((delta_back_chain_kernel<T, DK>), dim3(slices(p)), dim3(512), 0, s, back);
             dlast = back.last;
             hipLaunchKernelGGL((delta_back_output_kernel<T, DK>), grid, dim3(DK * 4), 0, s, p);
             if (p.group > 1)
@@ -1241,7 +1274,7 @@ extern "C" {
 
 int32_t rls_delta_segment_bytes(int64_t bytes)
 {
-    g_segment_bytes = bytes < 0 ? kSegmentBytes : bytes;
+    g_segment_bytes = bytes < 0 ? -1 : bytes;
     return RLS_OK;
 }
 
