@@ -679,8 +679,9 @@ __global__ void __launch_bounds__(512, 2) delta_back_chain_kernel(DeltaArgs p)
 }
 
 // ---- backward: all gradients at once -------------------------------------------------------------------------------------------
-// Over the value dimensions, 64 at a time: dO S^T, dY S^T, Y dS^T (16 key dimensions by a wave) and dO Y^T, dY Y^T; then with the gradients by Q K^T and
-// K K^T the products over the chunk's steps.
+// Over the value dimensions, 64 at a time: dO S^T, dY S^T, Y dS^T (16 key dimensions by a wave) and dO Y^T, dY Y^T; then with the gradient by Q K^T, and after
+// it with the one by K K^T, the products over the chunk's steps.  LDS and registers for two workgroups on a compute unit: it waits for memory and barriers
+// two thirds of the time (one workgroup: 320 us for 4 x 2048 steps x 16 heads of 128 x 128).
 
 __device__ inline float row_sum(float x)
 {
@@ -693,7 +694,7 @@ union BackOutputShared {
         __bf16 o[NI * kChunk * kChunk], dy[3 * kChunk * kChunk], y[3 * kChunk * kChunk];
     } in;
     struct {
-        __bf16 qk[3 * kChunk * kChunk], qk_turned[3 * kChunk * kChunk], kk[3 * kChunk * kChunk], kk_turned[3 * kChunk * kChunk];
+        __bf16 rows[3 * kChunk * kChunk], turned[3 * kChunk * kChunk];           // the gradient by Q K^T, then the one by K K^T
     } by;
 };
 
@@ -712,7 +713,7 @@ __device__ inline void put_tile(__bf16 *p, __bf16 *turned, int ti, int tj, f4 v)
 }
 
 template <typename T, int DK>
-__global__ void __launch_bounds__(DK * 4, DK == 128 ? 2 : 1) delta_back_output_kernel(DeltaArgs p)
+__global__ void __launch_bounds__(DK * 4, DK == 128 ? 4 : DK == 64 ? 2 : 1) delta_back_output_kernel(DeltaArgs p)
 {
     constexpr int NI = kPlanes<T>, W = DK / 16, Most = (kLower + W - 1) / W;
     __shared__ Gates gates;
@@ -725,7 +726,8 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 2 : 1) delta_back_output_k
     gates.load(p, b, head, t0);
     f4 o_state[4] = {}, y_state[4] = {}, carried[4] = {}, from_o[Most] = {}, from_y[Most] = {};
     float dot = 0.0f;
-    const float *const s = p.s + unit * DK * p.columns + (wave * 16 + lane16()) * p.columns, *const ds = p.ds + unit * DK * p.columns + (wave * 16 + lane16()) * p.columns;
+    const float *const s = p.s + unit * DK * p.columns, *const ds = p.ds + unit * DK * p.columns;
+    const int row_at = (wave * 16 + lane16()) * p.columns + lane8();
     for (int column = 0; column < p.columns; column += kChunk) {
         __syncthreads();
         for (int u = threadIdx.x; u < kChunk * 8; u += DK * 4) {
@@ -758,25 +760,27 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 2 : 1) delta_back_output_k
             }
         }
         __syncthreads();
-#pragma unroll
+#pragma unroll 1
         for (int kb = 0; kb < 2; ++kb) {
             vec8<float> before, after;
-            __builtin_memcpy(&before, s + column + kb * 32 + lane8(), 32);
-            __builtin_memcpy(&after, ds + column + kb * 32 + lane8(), 32);
+            __builtin_memcpy(&before, s + (row_at + column + kb * 32), 32);
+            __builtin_memcpy(&after, ds + (row_at + column + kb * 32), 32);
 #pragma unroll
             for (int m = 0; m < 8; ++m) dot = fmaf(before[m], after[m], dot);
-            b8 ps[3], pd[3];
-            split(before, ps);
-            split(after, pd);
+            b8 right[3], left[3], o[NI];
+            split(before, right);
 #pragma unroll
             for (int ti = 0; ti < 4; ++ti) {
-                b8 o[NI], dy[3], y[3];
                 load_block(o, sh.in.o, ti * 2 + kb);
-                load_block(dy, sh.in.dy, ti * 2 + kb);
-                load_block(y, sh.in.y, ti * 2 + kb);
-                o_state[ti] = mmp(o, ps, o_state[ti]);
-                y_state[ti] = mmp(dy, ps, y_state[ti]);
-                carried[ti] = mmp(y, pd, carried[ti]);
+                load_block(left, sh.in.dy, ti * 2 + kb);
+                o_state[ti] = mmp(o, right, o_state[ti]);
+                y_state[ti] = mmp(left, right, y_state[ti]);
+            }
+            split(after, right);
+#pragma unroll
+            for (int ti = 0; ti < 4; ++ti) {
+                load_block(left, sh.in.y, ti * 2 + kb);
+                carried[ti] = mmp(left, right, carried[ti]);
             }
 #pragma unroll
             for (int e = 0; e < Most; ++e) {
@@ -784,12 +788,11 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 2 : 1) delta_back_output_k
                 if (u >= kLower) continue;
                 int ti, tj;
                 lower_tile(u, ti, tj);
-                b8 o[NI], dy[3], y[3];
-                load_block(y, sh.in.y, tj * 2 + kb);
+                load_block(right, sh.in.y, tj * 2 + kb);
                 load_block(o, sh.in.o, ti * 2 + kb);
-                load_block(dy, sh.in.dy, ti * 2 + kb);
-                from_o[e] = mmp(o, y, from_o[e]);
-                from_y[e] = mmp(dy, y, from_y[e]);
+                load_block(left, sh.in.dy, ti * 2 + kb);
+                from_o[e] = mmp(o, right, from_o[e]);
+                from_y[e] = mmp(left, right, from_y[e]);
             }
         }
     }
@@ -801,7 +804,7 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 2 : 1) delta_back_output_k
         int ti, tj;
         lower_tile(u, ti, tj);
         f4 qk{}, kk{};
-#pragma unroll
+#pragma unroll 1
         for (int kb = 0; kb < DK / 32; ++kb) {
             b8 left[NI], right[NI];
             load_block(right, p.kp + inputs, tj * (DK / 32) + kb);
@@ -813,14 +816,14 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 2 : 1) delta_back_output_k
         const int j = tj * 16 + lane16();
         const float beta = gates.beta[j];
         float column_sum = 0.0f;
-        f4 by_qk, by_kk;
+        f4 by_qk;
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const int i = ti * 16 + lane4() + m;
             const float decay = gates.decay(i, j);
             const float o = p.scale * from_o[e][m] * decay, f = i > j ? from_y[e][m] * decay : 0.0f, by_decay = o * qk[m] - f * kk[m];
             by_qk[m] = o * beta;
-            by_kk[m] = -f * beta;
+            from_y[e][m] = -f * beta;
             if (i == j) by_itself[i] = by_decay;
             column_sum += i == j ? 0.0f : by_decay;
             const float sum = row_sum(i == j ? 0.0f : by_decay * beta);
@@ -829,61 +832,81 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 2 : 1) delta_back_output_k
         column_sum += __shfl_xor(column_sum, 16);
         column_sum += __shfl_xor(column_sum, 32);
         if (lane4() == 0) by_column[ti][j] = column_sum;
-        put_tile(sh.by.qk, sh.by.qk_turned, ti, tj, by_qk);
-        put_tile(sh.by.kk, sh.by.kk_turned, ti, tj, by_kk);
-        if (ti == tj) {                                  // what a block of 32 has above the diagonal
-            const int other = ti ^ 1;
-            if (other > ti) {
-                put_tile(sh.by.qk, sh.by.qk_turned, ti, other, f4{});
-                put_tile(sh.by.kk, sh.by.kk_turned, ti, other, f4{});
-            }
-        }
+        put_tile(sh.by.rows, sh.by.turned, ti, tj, by_qk);
+        // what a block of 32 has above the diagonal
+        if (ti == tj && (ti & 1) == 0) put_tile(sh.by.rows, sh.by.turned, ti, ti + 1, f4{});
     }
-    const int col = wave * 16 + lane16(), read = min(col, p.key_dim - 1);
+    const int col = wave * 16 + lane16();
 #pragma unroll
     for (int ti = 0; ti < 4; ++ti) {
         const f4 a = four(gates.a, ti * 16), c = four(gates.c, ti * 16);
         o_state[ti] *= a * p.scale;
         y_state[ti] *= a;
         carried[ti] *= c;
+        // four steps of q and k
+        f4 q{}, k{};
+        const int64_t from = inputs + place_in<NI>(col, ti * 16 + lane4(), 2, 0) + (lane4() & 4);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            q += __builtin_convertvector(*reinterpret_cast<const b4 *>(p.qt + from + i * 512), f4);
+            k += __builtin_convertvector(*reinterpret_cast<const b4 *>(p.kt + from + i * 512), f4);
+        }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const int i = ti * 16 + lane4() + m;
-            const int64_t t = min(t0 + i, p.steps - 1);
-            // (behind the last step and key dimension the other factors are 0)
-            const float qi = (float)at<T>(p.q, b, t, key)[read], ki = (float)at<T>(p.k, b, t, key)[read];
-            const float state_sum = row_sum(qi * o_state[ti][m] - ki * y_state[ti][m]), kept_sum = row_sum(ki * carried[ti][m]);
+            const float state_sum = row_sum(q[m] * o_state[ti][m] - k[m] * y_state[ti][m]), kept_sum = row_sum(k[m] * carried[ti][m]);
             if (lane16() == 0) by_state[wave][i] = state_sum, kept[wave][i] = kept_sum;
         }
+        carried[ti] = carried[ti] * four(gates.beta, ti * 16) - y_state[ti];
     }
     dot = wave_reduce(dot, 0.0f, [](float x, float z) { return x + z; });
     if ((threadIdx.x & 63) == 0) dots[wave] = dot;
+    __syncthreads();
     b8 kt[2][NI], qt[2][NI];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
         load_block(kt[kb], p.kt + inputs, wave * 2 + kb);
         load_block(qt[kb], p.qt + inputs, wave * 2 + kb);
     }
-    __syncthreads();
 #pragma unroll
-    for (int ti = 0; ti < 4; ++ti) {
-        f4 dq = o_state[ti], dk = carried[ti] * four(gates.beta, ti * 16) - y_state[ti];
+    for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             b8 x[3];
             if (kb <= ti / 2) {
-                load_block(x, sh.by.qk, ti * 2 + kb);
-                dq = mmp(x, kt[kb], dq);
-                load_block(x, sh.by.kk, ti * 2 + kb);
-                dk = mmp(x, kt[kb], dk);
+                load_block(x, sh.by.rows, ti * 2 + kb);
+                o_state[ti] = mmp(x, kt[kb], o_state[ti]);
             }
             if (kb >= ti / 2) {
-                load_block(x, sh.by.qk_turned, ti * 2 + kb);
-                dk = mmp(x, qt[kb], dk);
-                load_block(x, sh.by.kk_turned, ti * 2 + kb);
-                dk = mmp(x, kt[kb], dk);
+                load_block(x, sh.by.turned, ti * 2 + kb);
+                carried[ti] = mmp(x, qt[kb], carried[ti]);
             }
         }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < Most; ++e) {
+        const int u = wave + W * e;
+        if (u >= kLower) continue;
+        int ti, tj;
+        lower_tile(u, ti, tj);
+        put_tile(sh.by.rows, sh.by.turned, ti, tj, from_y[e]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ti = 0; ti < 4; ++ti) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            b8 x[3];
+            if (kb <= ti / 2) {
+                load_block(x, sh.by.rows, ti * 2 + kb);
+                carried[ti] = mmp(x, kt[kb], carried[ti]);
+            }
+            if (kb >= ti / 2) {
+                load_block(x, sh.by.turned, ti * 2 + kb);
+                carried[ti] = mmp(x, kt[kb], carried[ti]);
+            }
+        }
+        const f4 dq = o_state[ti], dk = carried[ti];
         if (p.group > 1) {                               // added up over the heads that share the keys by another launch
             put(p.gq + unit * kChunk * DK, DK, ti * 16, wave * 16, dq);
             put(p.gk + unit * kChunk * DK, DK, ti * 16, wave * 16, dk);
