@@ -244,15 +244,21 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
 {
     constexpr int NI = kPlanes<T>, LD = DK + 8, Plane = kChunk * LD;
     __shared__ Gates gates;
-    __shared__ __attribute__((aligned(16))) __bf16 k[NI * Plane], q[NI * Plane];
-    __shared__ __attribute__((aligned(16))) float x[kChunk * kEdge], n[kChunk * kEdge];       // n: G beta below the diagonal; scale P beta, turned, from it on
+    constexpr int XBytes = kChunk * kEdge * 4, QBytes = NI * Plane * 2;
+    __shared__ __attribute__((aligned(16))) __bf16 k[NI * Plane];
+    __shared__ __attribute__((aligned(16))) char qx[QBytes > XBytes ? QBytes : XBytes];
+    __bf16 *const q = reinterpret_cast<__bf16 *>(qx);
+    float *const x = reinterpret_cast<float *>(qx);      // X comes when q has been used
+    __shared__ __attribute__((aligned(16))) float n[kChunk * kEdge];             // G beta below the diagonal; scale P beta, turned, from it on
     const int wave = threadIdx.x >> 6;
     const int64_t unit = blockIdx.x, bh = unit / p.chunks, chunk = unit % p.chunks, b = bh / p.heads, head = bh % p.heads, key = head / p.group;
     const int64_t t0 = (p.chunk0 + chunk) * kChunk, inputs = ((b * (p.heads / p.group) + key) * p.chunks + chunk) * NI * kChunk * DK;
     const bool first = head % p.group == 0;              // of the heads that share the keys: it writes their planes
     gates.load(p, b, head, t0);
-    for (int u = threadIdx.x; u < kChunk * DK / 8; u += 256) {
-        const int row = u / (DK / 8), d = u % (DK / 8) * 8;
+    // (a wave reads what makes one block, so that it writes a kilobyte in a row)
+    const int in_block = threadIdx.x & 15, along_block = (threadIdx.x & 63) >> 4 << 3;
+    for (int u = wave; u < 4 * (DK / 32); u += 4) {
+        const int row = u / (DK / 32) * 16 + in_block, d = u % (DK / 32) * 32 + along_block;
         const bool in = t0 + row < p.steps;
         b8 pk[NI], pq[NI];
         planes_of(load_raw(at<T>(p.k, b, t0 + row, key), in, d, p.key_dim), pk);
@@ -292,8 +298,8 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
         }
     }
     if (first) {
-        for (int u = threadIdx.x; u < DK * 8; u += 256) {
-            const int d = u % DK, t = u / DK * 8;
+        for (int u = wave; u < DK / 16 * 2; u += 4) {
+            const int d = u / 2 * 16 + in_block, t = u % 2 * 32 + along_block;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 b8 v;
@@ -340,8 +346,8 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
         to[0] = gates.a[threadIdx.x];
         to[kChunk] = gates.c[threadIdx.x] * gates.beta[threadIdx.x];
     }
-    for (int u = threadIdx.x; u < kChunk * 8; u += 256) {
-        const int i = u / 8, j = u % 8 * 8;
+    for (int u = wave; u < 8; u += 4) {
+        const int i = u / 2 * 16 + in_block, j = u % 2 * 32 + along_block;
         vec8<float> vx, vp, vt;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -371,6 +377,24 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
 // Eight waves, 16 of the chunk's steps for two of them.  The first four: R = V - a (K S), Y = X R.  The other four, beside them: o = scale a (Q S)
 // + scale P beta Y.  Then all of them: S = carry S + K^T (c beta Y), 16 rows of it each.  Three barriers a chunk; what a chunk needs of memory is
 // read while the one before it is worked on.
+
+// rows (operands of 32 numbers of the summed axis each) times planes in LDS, which are asked for two blocks ahead of their products
+template <int NI, int BLOCKS>
+__device__ inline f4 rows_by(const b8 (&rows)[BLOCKS][NI], const __bf16 *planes)
+{
+    b8 s[2][3];
+    load_block(s[0], planes, 0);
+    if (BLOCKS > 1) load_block(s[1], planes, 1);
+    __builtin_amdgcn_sched_barrier(0);
+    f4 sum{}, other{};
+#pragma unroll
+    for (int kb = 0; kb < BLOCKS; ++kb) {
+        (kb & 1 ? other : sum) = mmp(rows[kb], s[kb & 1], kb & 1 ? other : sum);
+        if (kb + 2 < BLOCKS) load_block(s[kb & 1], planes, kb + 2);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    return sum + other;
+}
 
 // Every wave of a kind has the same loads and stores in the same order, none of them behind a branch, so that it waits for a load by how many came after it
 // and for nothing else: what has no place to go is stored to a spare one.  Products with a block of zeros are taken too, for the same reason and because
@@ -414,7 +438,9 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
     f4 a, cbeta{};
     float carry;
     // a chunk's loads in three groups, each right after the last use of what it takes the place of
+    constexpr bool kIdle = KEEP && ANSWERS;              // for the backward pass nothing is answered
     const auto load_rows_of = [&](int n) {
+        if (kIdle) return;
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at, kb);
         a = four(a_at, 0);
@@ -425,6 +451,7 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
         }
     };
     const auto load_left_of = [&]() {
+        if (kIdle) return;
         load_block(left[0], left_at, 0);
         load_block(left[1], left_at, 1);
         if (!ANSWERS) cbeta = four(cbeta_at, 0);
@@ -453,27 +480,16 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
             if (KEEP) put(p.s + unit * DK * p.columns, p.columns, wave * 16, column, state);
         }
         all_waves();
-        // K S, and beside the next product Q S
-        const auto rows_by_state = [&] {
-            // (all operands are asked for before the first product: one after the other, each would wait for LDS by itself)
-            b8 s[DK / 32][3];
-#pragma unroll
-            for (int kb = 0; kb < DK / 32; ++kb) load_block(s[kb], sh.s, kb);
-            __builtin_amdgcn_sched_barrier(0);
-            f4 sum{}, other{};
-#pragma unroll
-            for (int kb = 0; kb < DK / 32; ++kb) (kb & 1 ? other : sum) = mmp(rows[kb], s[kb], kb & 1 ? other : sum);
-            return (sum + other) * a;
-        };
         f4 by_query{};
         if (!ANSWERS) {
             const f4 x{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
-            put_block(sh.r, tile * 16, x - rows_by_state());
+            put_block(sh.r, tile * 16, x - rows_by(rows, sh.s) * a);
             load_rows_of(more ? n + 1 : n);
         }
         all_waves();
-        if (ANSWERS) {
-            by_query = rows_by_state();
+        if (kIdle) {
+        } else if (ANSWERS) {
+            by_query = rows_by(rows, sh.s) * a;
             load_rows_of(more ? n + 1 : n);
         } else {
             b8 r[2][3];
@@ -514,7 +530,7 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
 }
 
 template <typename T, int DK, bool KEEP>
-__global__ void __launch_bounds__(512, 2) delta_chain_kernel(DeltaArgs p)
+__global__ void __launch_bounds__(512, kPlanes<T> == 1 && (KEEP || DK < 128) ? 4 : 2) delta_chain_kernel(DeltaArgs p)
 {
     __shared__ ChainShared<DK> sh;
     // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
@@ -526,13 +542,15 @@ __global__ void __launch_bounds__(512, 2) delta_chain_kernel(DeltaArgs p)
 }
 
 // ---- backward: the chain from the last chunk to the first ----------------------------------------------------------------
-// Z = c beta (K dS) + (scale P beta)^T dO and dY = X^T Z by the first four waves, then by all of them dS = carry dS + Q^T (scale a dO) - K^T (a dY).
-// dS behind every chunk goes to ds, dY to dy.  Loads and stores as in the forward chain.
+// Z = c beta (K dS) + E and dY = X^T Z by the first four waves, then by all of them dS = carry dS + Q^T (scale a dO) - K^T (a dY).  The other four are a
+// chunk ahead with what depends on dO alone: E = (scale P beta)^T dO, and scale a dO.  dS behind every chunk goes to ds, dY to dy.  Loads and stores as in
+// the forward chain.
 
 template <typename T, int DK>
 struct alignas(16) BackShared {
     // (q is read to a chunk's end, so the next chunk's has a place of its own)
     __bf16 s[3 * 16 * DK], o[kPlanes<T> * 16 * kChunk], q[2][3 * 16 * kChunk], z[3 * 16 * kChunk], u[3 * 16 * kChunk];
+    f4 e[4][64];
 };
 
 template <typename T, int DK, bool FEEDS>
@@ -550,36 +568,33 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
         if (p.state && mine && row < p.key_dim && j < p.value_dim) state[m] = p.state[(bh * p.key_dim + row) * p.value_dim + j];
     }
     const __bf16 *rows_at = p.kp + (kbh * p.chunks + end) * Inputs + tile * (DK / 32) * NI * 512;
-    const __bf16 *pt_at = p.pp + (bh * p.chunks + end) * 3 * Square + tile * 2 * 3 * 512, *xt_at = p.xt + (bh * p.chunks + end) * 3 * Square + tile * 2 * 3 * 512;
+    const __bf16 *square_at = (FEEDS ? p.pp : p.xt) + (bh * p.chunks + end) * 3 * Square + tile * 2 * 3 * 512;
     const int64_t turned = (kbh * p.chunks + end) * Inputs + (mine ? wave : 0) * 2 * NI * 512;
     const __bf16 *kt_at = p.kt + turned, *qt_at = p.qt + turned;
     const float *a_at = p.gates + (bh * p.chunks + end) * 2 * kChunk + tile * 16, *cbeta_at = a_at + kChunk, *carry_at = p.carry + bh * p.chunks + end;
     const int64_t t0 = p.chunk0 * kChunk + tile * 16 + lane4();
     const T *const d_at = at<T>(p.dout, b, 0, head) + min(j, p.value_dim - 1);
-    b8 rows[DK / 32][NI], pt[2][3], xt[2][3], kt[2][NI], qt[2][NI];
+    b8 rows[DK / 32][NI], square[2][3], kt[2][NI], qt[2][NI];                  // square: of X^T, or of P turned
     T d[4];
-    f4 a, cbeta;
+    f4 a, cbeta{};
     float carry;
-    const auto load_first = [&](int n) {
-        if (FEEDS) {
-            const int64_t t = t0 + (int64_t)n * kChunk;
+    const auto load_rows_of = [&]() {
 #pragma unroll
-            for (int m = 0; m < 4; ++m) d[m] = d_at[min(t + m, p.steps - 1) * p.dout.step];
-            a = four(a_at, 0);
-        } else {
-#pragma unroll
-            for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at, kb);
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) load_block(pt[kb], pt_at, kb);
-            cbeta = four(cbeta_at, 0);
-        }
+        for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at, kb);
+        cbeta = four(cbeta_at, 0);
     };
-    const auto load_second = [&]() {
+    const auto load_d_of = [&](int64_t n) {
+        const int64_t t = t0 + n * kChunk;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) load_block(xt[kb], xt_at, kb);
+        for (int m = 0; m < 4; ++m) d[m] = d_at[min(t + m, p.steps - 1) * p.dout.step];
         a = four(a_at, 0);
     };
-    const auto load_third = [&]() {
+    const auto load_square_of = [&]() {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) load_block(square[kb], square_at, kb);
+        if (!FEEDS) a = four(a_at, 0);
+    };
+    const auto load_turned_of = [&]() {
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             load_block(kt[kb], kt_at, kb);
@@ -587,33 +602,54 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
         }
         carry = *carry_at;
     };
-    load_first((int)end);
-    if (!FEEDS) load_second();
-    load_third();
+    // what a chunk's dO gives, into LDS; then the loads of the chunk before it (of chunk `next`, which is the first one again at the end)
+    const auto feed = [&](int of) {
+        f4 x;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) x[m] = j < p.value_dim ? (float)d[m] : 0.0f;
+        put_block<NI>(sh.o, tile * 16, x);
+        put_block(sh.q[of & 1], tile * 16, x * a * p.scale);
+    };
+    const auto feed_square = [&]() {
+        b8 o[2][NI];
+        load_block(o[0], sh.o, 0);
+        load_block(o[1], sh.o, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        sh.e[tile][threadIdx.x & 63] = mmp(square[0], o[0], f4{}) + mmp(square[1], o[1], f4{});
+    };
+    const auto back = [&](bool more) {                   // the pointers of what is a chunk ahead
+        if (!more) return;
+        square_at -= 3 * Square;
+        a_at -= 2 * kChunk;
+    };
+    if (FEEDS) {
+        load_d_of(end);
+        load_square_of();
+        back(end > 0);
+        feed((int)end);
+        load_d_of(max(end - 1, (int64_t)0));
+        all_waves();
+        feed_square();
+        load_square_of();
+    } else {
+        load_rows_of();
+        load_square_of();
+        all_waves();
+    }
+    load_turned_of();
     for (int n = (int)end; n >= 0; --n) {
         const int64_t unit = bh * p.chunks + n;
         if (n > 0) {
             rows_at -= Inputs;
             kt_at -= Inputs;
             qt_at -= Inputs;
-            pt_at -= 3 * Square;
-            xt_at -= 3 * Square;
-            a_at -= 2 * kChunk;
             cbeta_at -= 2 * kChunk;
             --carry_at;
         }
-        const int before = n > 0 ? n - 1 : 0;
+        back(FEEDS ? n > 1 : n > 0);
         if (mine) {
             put_block(sh.s, wave * 16, state);
             put(p.ds + unit * DK * p.columns, p.columns, wave * 16, column, state);
-        }
-        if (FEEDS) {
-            f4 x;
-#pragma unroll
-            for (int m = 0; m < 4; ++m) x[m] = j < p.value_dim ? (float)d[m] : 0.0f;
-            put_block<NI>(sh.o, tile * 16, x);
-            put_block(sh.q[n & 1], tile * 16, x * a * p.scale);
-            load_first(before);
         }
         all_waves();
         const auto by_queries = [&] {
@@ -625,30 +661,26 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
         };
         if (FEEDS) {
             by_queries();
+            feed(n - 1);                                 // (behind the first chunk: once more, for nobody)
+            load_d_of(max(n - 2, 0));
         } else {
-            b8 s[DK / 32][3], o[2][NI];
-#pragma unroll
-            for (int kb = 0; kb < DK / 32; ++kb) load_block(s[kb], sh.s, kb);
-            load_block(o[0], sh.o, 0);
-            load_block(o[1], sh.o, 1);
-            __builtin_amdgcn_sched_barrier(0);
-            f4 sum{}, other{};
-#pragma unroll
-            for (int kb = 0; kb < DK / 32; ++kb) (kb & 1 ? other : sum) = mmp(rows[kb], s[kb], kb & 1 ? other : sum);
-            const f4 z = mmp(pt[0], o[0], f4{}) + mmp(pt[1], o[1], f4{});
-            put_block(sh.z, tile * 16, z + (sum + other) * cbeta);
-            load_first(before);
+            const f4 z = sh.e[tile][threadIdx.x & 63];
+            put_block(sh.z, tile * 16, z + rows_by(rows, sh.s) * cbeta);
+            load_rows_of();
         }
         all_waves();
-        if (!FEEDS) {
+        if (FEEDS) {
+            feed_square();
+            load_square_of();
+        } else {
             b8 z[2][3];
             load_block(z[0], sh.z, 0);
             load_block(z[1], sh.z, 1);
             __builtin_amdgcn_sched_barrier(0);
-            const f4 y = mmp(xt[0], z[0], f4{}) + mmp(xt[1], z[1], f4{});
+            const f4 y = mmp(square[0], z[0], f4{}) + mmp(square[1], z[1], f4{});
             put_block(sh.u, tile * 16, -y * a);
             put(p.dy + unit * kChunk * p.columns, p.columns, tile * 16, column, y);
-            load_second();
+            load_square_of();
         }
         all_waves();
         if (!FEEDS) by_queries();
@@ -657,7 +689,7 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
         load_block(u[1], sh.u, 1);
         __builtin_amdgcn_sched_barrier(0);
         state = mmp(kt[0], u[0], state) + mmp(kt[1], u[1], f4{});
-        load_third();
+        load_turned_of();
     }
     if (!p.last || !mine || j >= p.value_dim) return;
 #pragma unroll
@@ -668,7 +700,7 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
 }
 
 template <typename T, int DK>
-__global__ void __launch_bounds__(512, 2) delta_back_chain_kernel(DeltaArgs p)
+__global__ void __launch_bounds__(512, kPlanes<T> == 1 ? 4 : 2) delta_back_chain_kernel(DeltaArgs p)
 {
     __shared__ BackShared<T, DK> sh;
     const int slices = p.columns / 16;
