@@ -173,6 +173,22 @@ __device__ inline void load_block(b8 (&to)[N], const __bf16 *p, int block)
 #pragma unroll
     for (int i = 0; i < N; ++i) to[i] = *reinterpret_cast<const b8 *>(p + (block * N + i) * 512 + (threadIdx.x & 63) * 8);
 }
+// two chains of products, none waits for more than half of the others
+template <int NA, int NB>
+__device__ inline void mmp(const b8 (&a)[NA], const b8 (&b)[NB], f4 &even, f4 &odd)
+{
+    int n = 0;
+#pragma unroll
+    for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                if (i + j == sum) {
+                    f4 &c = n++ & 1 ? odd : even;
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], c, 0, 0, 0);
+                }
+}
 __device__ inline int lane8() { return (threadIdx.x & 63) >> 4 << 3; }
 // from planes in memory, rows ld apart and planes `plane` apart
 template <int N>
@@ -204,7 +220,7 @@ __device__ inline void lower_tile(int u, int &ti, int &tj)
 // ---- the gates of a chunk ----------------------------------------------------------------------------------------------
 
 struct alignas(16) Gates {
-    double gamma[kChunk];
+    double gamma[kChunk];                                // times log2(e)
     float beta[kChunk], a[kChunk], c[kChunk];
     int32_t part[kChunk];                                // resets up to here
     uint8_t cut[kChunk];
@@ -214,27 +230,23 @@ struct alignas(16) Gates {
     {
         const int l = threadIdx.x;
         if (l >= kChunk) return;
-        const int64_t t = t0 + l;
-        const bool in = t < p.steps;
-        const int64_t i = (b * p.steps + t) * p.heads + head;
-        const float g = in ? p.g[i] : 0.0f;
-        const bool no_carry = in && (g < kNoCarry || (p.reset && p.reset[b * p.steps + t] != 0));
-        beta[l] = in ? p.beta[i] : 0.0f;
+        const int64_t t = min(t0 + l, p.steps - 1), i = (b * p.steps + t) * p.heads + head;
+        const bool in = t0 + l < p.steps;
+        const float g = p.g[i], given = p.beta[i];
+        const uint8_t reset = p.reset ? p.reset[b * p.steps + t] : 0;
+        const bool no_carry = in && (g < kNoCarry || reset != 0);
+        beta[l] = in ? given : 0.0f;
         cut[l] = no_carry;
-        double sum = no_carry ? 0.0 : (double)g;
-        for (int d = 1; d < kChunk; d <<= 1) {
-            const double before = __shfl_up(sum, d);
-            if (l >= d) sum += before;
-        }
+        const double sum = wave_scan(!in || no_carry ? 0.0 : (double)g * 1.4426950408889634, 0.0, [](double x, double y) { return x + y; });
         const uint64_t cuts = __ballot(no_carry);
         const int before = __popcll(cuts & (l == 63 ? ~0ull : (1ull << (l + 1)) - 1));
         gamma[l] = sum;
         part[l] = before;
-        a[l] = before == 0 ? expf((float)sum) : 0.0f;
-        const double end = __shfl(sum, 63);
-        c[l] = before == __popcll(cuts) ? expf((float)(end - sum)) : 0.0f;
+        a[l] = before == 0 ? __builtin_amdgcn_exp2f((float)sum) : 0.0f;
+        const double end = last_lane(sum);
+        c[l] = before == __popcll(cuts) ? __builtin_amdgcn_exp2f((float)(end - sum)) : 0.0f;
     }
-    __device__ float decay(int i, int j) const { return j <= i && part[i] == part[j] ? expf((float)(gamma[i] - gamma[j])) : 0.0f; }
+    __device__ float decay(int i, int j) const { return j <= i && part[i] == part[j] ? __builtin_amdgcn_exp2f((float)(gamma[i] - gamma[j])) : 0.0f; }
 };
 
 // ---- all chunks at once: X, P and K^T -------------------------------------------------------------------------------------
@@ -254,15 +266,23 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
     const int64_t unit = blockIdx.x, bh = unit / p.chunks, chunk = unit % p.chunks, b = bh / p.heads, head = bh % p.heads, key = head / p.group;
     const int64_t t0 = (p.chunk0 + chunk) * kChunk, inputs = ((b * (p.heads / p.group) + key) * p.chunks + chunk) * NI * kChunk * DK;
     const bool first = head % p.group == 0;              // of the heads that share the keys: it writes their planes
-    gates.load(p, b, head, t0);
     // (a wave reads what makes one block, so that it writes a kilobyte in a row)
     const int in_block = threadIdx.x & 15, along_block = (threadIdx.x & 63) >> 4 << 3;
-    for (int u = wave; u < 4 * (DK / 32); u += 4) {
-        const int row = u / (DK / 32) * 16 + in_block, d = u % (DK / 32) * 32 + along_block;
+    Raw<T> raw_k[DK / 32], raw_q[DK / 32];               // (all asked for before the first is used)
+#pragma unroll
+    for (int e = 0; e < DK / 32; ++e) {
+        const int u = wave + 4 * e, row = u / (DK / 32) * 16 + in_block, d = u % (DK / 32) * 32 + along_block;
         const bool in = t0 + row < p.steps;
+        raw_k[e] = load_raw(at<T>(p.k, b, t0 + row, key), in, d, p.key_dim);
+        raw_q[e] = load_raw(at<T>(p.q, b, t0 + row, key), in, d, p.key_dim);
+    }
+    gates.load(p, b, head, t0);
+#pragma unroll
+    for (int e = 0; e < DK / 32; ++e) {
+        const int u = wave + 4 * e, row = u / (DK / 32) * 16 + in_block, d = u % (DK / 32) * 32 + along_block;
         b8 pk[NI], pq[NI];
-        planes_of(load_raw(at<T>(p.k, b, t0 + row, key), in, d, p.key_dim), pk);
-        planes_of(load_raw(at<T>(p.q, b, t0 + row, key), in, d, p.key_dim), pq);
+        planes_of(raw_k[e], pk);
+        planes_of(raw_q[e], pq);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             *reinterpret_cast<b8 *>(k + i * Plane + row * LD + d) = pk[i];
@@ -375,8 +395,9 @@ __global__ void __launch_bounds__(256) delta_prepare_kernel(DeltaArgs p)
 
 // ---- the chain over chunks, 16 columns of the state by a workgroup --------------------------------------------------------
 // Eight waves, 16 of the chunk's steps for two of them.  The first four: R = V - a (K S), Y = X R.  The other four, beside them: o = scale a (Q S)
-// + scale P beta Y.  Then all of them: S = carry S + K^T (c beta Y), 16 rows of it each.  Three barriers a chunk; what a chunk needs of memory is
-// read while the one before it is worked on.
+// + scale P beta Y, a chunk's last product beside the next chunk's first, and what can be done ahead (V) or later (Y's planes) for the first four.
+// Then all of them: S = carry S + K^T (c beta Y), 16 rows of it each.  Three barriers a chunk; what a chunk needs of memory is read while the one before
+// it is worked on.  The first four's path bounds it: splits of numbers, LDS and the latency of some 30 matrix instructions.
 
 // rows (operands of 32 numbers of the summed axis each) times planes in LDS, which are asked for two blocks ahead of their products
 template <int NI, int BLOCKS>
@@ -386,14 +407,14 @@ __device__ inline f4 rows_by(const b8 (&rows)[BLOCKS][NI], const __bf16 *planes)
     load_block(s[0], planes, 0);
     if (BLOCKS > 1) load_block(s[1], planes, 1);
     __builtin_amdgcn_sched_barrier(0);
-    f4 sum{}, other{};
+    f4 c[4] = {};
 #pragma unroll
     for (int kb = 0; kb < BLOCKS; ++kb) {
-        (kb & 1 ? other : sum) = mmp(rows[kb], s[kb & 1], kb & 1 ? other : sum);
+        mmp(rows[kb], s[kb & 1], c[kb & 1 ? 2 : 0], c[kb & 1 ? 3 : 1]);
         if (kb + 2 < BLOCKS) load_block(s[kb & 1], planes, kb + 2);
         __builtin_amdgcn_sched_barrier(0);
     }
-    return sum + other;
+    return (c[0] + c[1]) + (c[2] + c[3]);
 }
 
 // Every wave of a kind has the same loads and stores in the same order, none of them behind a branch, so that it waits for a load by how many came after it
@@ -403,6 +424,18 @@ __device__ inline f4 rows_by(const b8 (&rows)[BLOCKS][NI], const __bf16 *planes)
 template <int DK>
 struct alignas(16) ChainShared {
     __bf16 s[3 * 16 * DK], r[3 * 16 * kChunk], y[3 * 16 * kChunk], u[3 * 16 * kChunk];
+    f4 v[4][64], y32[4][64];                             // as lanes hold them
+};
+// Four rows of a chunk (from `row` on) of an array of heads: how far they are from the chunk's first row.  A chunk's last rows may lie behind the last step;
+// they are read as the last step's.
+struct Rows {
+    int64_t apart[4];
+    __device__ void set(int row, int64_t step, int64_t steps)                    // steps: from the chunk's first row on
+    {
+        const int most = (int)min<int64_t>(kChunk, steps) - 1;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) apart[m] = min(row + m, most) * step;
+    }
 };
 __device__ inline void all_waves()
 {
@@ -430,28 +463,22 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
     const __bf16 *left_at = (ANSWERS ? p.pp : p.xp) + bh * p.chunks * 3 * Square + tile * 2 * 3 * 512;
     const __bf16 *kt_at = p.kt + kbh * p.chunks * Inputs + (mine ? wave : 0) * 2 * NI * 512;
     const float *a_at = p.gates + bh * p.chunks * 2 * kChunk + tile * 16, *cbeta_at = a_at + kChunk, *carry_at = p.carry + bh * p.chunks;
-    const int64_t t0 = p.chunk0 * kChunk + tile * 16 + lane4();
-    const T *const v_at = at<T>(p.v, b, 0, head) + min(j, p.value_dim - 1);
-    T *const spare = reinterpret_cast<T *>(p.spare) + (threadIdx.x & 63);
+    const int row = tile * 16 + lane4(), steps_left = (int)min<int64_t>(p.steps - p.chunk0 * kChunk, (int64_t)p.chunks * kChunk);   // of this launch
+    const T *v_at = at<T>(p.v, b, p.chunk0 * kChunk, head) + min(j, p.value_dim - 1);
+    T *o_at = KEEP ? nullptr : out_at<T>(p.o, b, p.chunk0 * kChunk + row, head) + j, *const spare = reinterpret_cast<T *>(p.spare) + (threadIdx.x & 63);
+    Rows v_rows;
+    constexpr bool kQueries = ANSWERS && !KEEP;          // for the backward pass nothing is answered
     b8 rows[DK / 32][NI], left[2][3], kt[2][NI];
     T v[4];
-    f4 a, cbeta{};
+    f4 a, cbeta{}, by_query{};
     float carry;
-    // a chunk's loads in three groups, each right after the last use of what it takes the place of
-    constexpr bool kIdle = KEEP && ANSWERS;              // for the backward pass nothing is answered
-    const auto load_rows_of = [&](int n) {
-        if (kIdle) return;
+    // a chunk's loads in groups, each right after the last use of what it takes the place of
+    const auto load_rows_of = [&]() {
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at, kb);
         a = four(a_at, 0);
-        if (!ANSWERS) {
-            const int64_t t = t0 + (int64_t)n * kChunk;
-#pragma unroll
-            for (int m = 0; m < 4; ++m) v[m] = v_at[min(t + m, p.steps - 1) * p.v.step];
-        }
     };
     const auto load_left_of = [&]() {
-        if (kIdle) return;
         load_block(left[0], left_at, 0);
         load_block(left[1], left_at, 1);
         if (!ANSWERS) cbeta = four(cbeta_at, 0);
@@ -461,65 +488,100 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
         for (int kb = 0; kb < 2; ++kb) load_block(kt[kb], kt_at, kb);
         carry = *carry_at;
     };
-    load_rows_of(0);
-    load_left_of();
+    // (chunk after chunk)
+    const auto load_v_of = [&](int n) {
+        if (n == 0 || n == p.chunks - 1) v_rows.set(row, p.v.step, steps_left - n * kChunk);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) v[m] = v_at[v_rows.apart[m]];
+        if (n + 1 < p.chunks) v_at += kChunk * p.v.step;
+    };
+    const auto put_v = [&]() { sh.v[tile][threadIdx.x & 63] = f4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]}; };
+    // + scale P beta Y, of chunk n
+    const auto answer = [&](int n) {
+        b8 y[2][3];
+        load_block(y[0], sh.y, 0);
+        load_block(y[1], sh.y, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const f4 o = mmp(left[0], y[0], by_query * p.scale) + mmp(left[1], y[1], f4{});
+        const int rows_in = j < p.value_dim ? steps_left - n * kChunk - row : 0;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) *(m < rows_in ? o_at + m * p.o.step : spare) = (T)o[m];
+        o_at += kChunk * p.o.step;
+    };
+    if (!ANSWERS) __builtin_amdgcn_s_setprio(3);         // the others wait for them
+    if (!ANSWERS || kQueries) {
+        load_rows_of();
+        load_left_of();
+    }
+    if (ANSWERS) {
+        load_v_of(0);
+        put_v();
+        load_v_of(min(1, p.chunks - 1));
+    }
     load_kt_of();
     for (int n = 0; n < p.chunks; ++n) {
         const int64_t unit = bh * p.chunks + n;
-        const bool more = n + 1 < p.chunks;              // (behind the last chunk the loads are of the last one again)
-        if (more) {
+        if (n + 1 < p.chunks) {                          // (behind the last chunk the loads are of the last one again)
             rows_at += Inputs;
             kt_at += Inputs;
-            left_at += 3 * Square;
             a_at += 2 * kChunk;
             cbeta_at += 2 * kChunk;
             ++carry_at;
         }
+        if (ANSWERS ? n > 0 : n + 1 < p.chunks) left_at += 3 * Square;         // (P is needed a chunk later)
         if (mine) {
             put_block(sh.s, wave * 16, state);
             if (KEEP) put(p.s + unit * DK * p.columns, p.columns, wave * 16, column, state);
         }
         all_waves();
-        f4 by_query{};
         if (!ANSWERS) {
-            const f4 x{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+            const f4 x = sh.v[tile][threadIdx.x & 63];
             put_block(sh.r, tile * 16, x - rows_by(rows, sh.s) * a);
-            load_rows_of(more ? n + 1 : n);
+            load_rows_of();
+        } else if (kQueries && n > 0) {
+            answer(n - 1);
+            load_left_of();
         }
         all_waves();
-        if (kIdle) {
-        } else if (ANSWERS) {
-            by_query = rows_by(rows, sh.s) * a;
-            load_rows_of(more ? n + 1 : n);
-        } else {
+        if (!ANSWERS) {
             b8 r[2][3];
             load_block(r[0], sh.r, 0);
             load_block(r[1], sh.r, 1);
             __builtin_amdgcn_sched_barrier(0);
-            const f4 y = mmp(left[0], r[0], f4{}) + mmp(left[1], r[1], f4{});
-            put_block(sh.y, tile * 16, y);
+            f4 c[4] = {};
+            mmp(left[0], r[0], c[0], c[1]);
+            mmp(left[1], r[1], c[2], c[3]);
+            const f4 y = (c[0] + c[1]) + (c[2] + c[3]);
             put_block(sh.u, tile * 16, y * cbeta);
             if (KEEP) put(p.y + unit * kChunk * p.columns, p.columns, tile * 16, column, y);
+            else sh.y32[tile][threadIdx.x & 63] = y;
             load_left_of();
+        } else {
+            put_v();
+            load_v_of(min(n + 2, p.chunks - 1));
+            if (kQueries) {
+                by_query = rows_by(rows, sh.s) * a;
+                load_rows_of();
+            }
         }
         all_waves();
-        b8 u[2][3], y[2][3];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) load_block(u[kb], sh.u, kb);
-        if (!KEEP && ANSWERS) {
-            load_block(y[0], sh.y, 0);
-            load_block(y[1], sh.y, 1);
-        }
+        b8 u[2][3];
+        load_block(u[0], sh.u, 0);
+        load_block(u[1], sh.u, 1);
         __builtin_amdgcn_sched_barrier(0);
-        state = mmp(kt[0], u[0], state * carry) + mmp(kt[1], u[1], f4{});
-        if (!KEEP && ANSWERS) {
-            const f4 o = mmp(left[0], y[0], by_query * p.scale) + mmp(left[1], y[1], f4{});
-            const int64_t t = t0 + (int64_t)n * kChunk;
-#pragma unroll
-            for (int m = 0; m < 4; ++m) *(t + m < p.steps && j < p.value_dim ? out_at<T>(p.o, b, t + m, head) + j : spare) = (T)o[m];
-        }
-        if (ANSWERS) load_left_of();
+        f4 c[4] = {state * carry, f4{}, f4{}, f4{}};
+        mmp(kt[0], u[0], c[0], c[1]);
+        mmp(kt[1], u[1], c[2], c[3]);
+        state = (c[0] + c[1]) + (c[2] + c[3]);
+        if (kQueries) put_block(sh.y, tile * 16, sh.y32[tile][threadIdx.x & 63]);
         load_kt_of();
+    }
+    if (kQueries) {
+        // (the four of them by themselves: each reads what all of them have put)
+        all_waves();
+        answer(p.chunks - 1);
+    } else {
+        all_waves();
     }
     if (!p.last || !mine || j >= p.value_dim) return;
 #pragma unroll
@@ -572,8 +634,9 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
     const int64_t turned = (kbh * p.chunks + end) * Inputs + (mine ? wave : 0) * 2 * NI * 512;
     const __bf16 *kt_at = p.kt + turned, *qt_at = p.qt + turned;
     const float *a_at = p.gates + (bh * p.chunks + end) * 2 * kChunk + tile * 16, *cbeta_at = a_at + kChunk, *carry_at = p.carry + bh * p.chunks + end;
-    const int64_t t0 = p.chunk0 * kChunk + tile * 16 + lane4();
-    const T *const d_at = at<T>(p.dout, b, 0, head) + min(j, p.value_dim - 1);
+    const int row = tile * 16 + lane4(), steps_left = (int)min<int64_t>(p.steps - p.chunk0 * kChunk, (int64_t)p.chunks * kChunk);
+    const T *d_at = at<T>(p.dout, b, (p.chunk0 + end) * kChunk, head) + min(j, p.value_dim - 1);
+    Rows d_rows;
     b8 rows[DK / 32][NI], square[2][3], kt[2][NI], qt[2][NI];                  // square: of X^T, or of P turned
     T d[4];
     f4 a, cbeta{};
@@ -583,10 +646,12 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
         for (int kb = 0; kb < DK / 32; ++kb) load_block(rows[kb], rows_at, kb);
         cbeta = four(cbeta_at, 0);
     };
-    const auto load_d_of = [&](int64_t n) {
-        const int64_t t = t0 + n * kChunk;
+    // (chunk after chunk, the last one first)
+    const auto load_d_of = [&](int n) {
+        if (n >= end - 1) d_rows.set(row, p.dout.step, steps_left - n * kChunk);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) d[m] = d_at[min(t + m, p.steps - 1) * p.dout.step];
+        for (int m = 0; m < 4; ++m) d[m] = d_at[d_rows.apart[m]];
+        if (n > 0) d_at -= kChunk * p.dout.step;
         a = four(a_at, 0);
     };
     const auto load_square_of = [&]() {
@@ -622,12 +687,13 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
         square_at -= 3 * Square;
         a_at -= 2 * kChunk;
     };
+    if (!FEEDS) __builtin_amdgcn_s_setprio(3);           // the others wait for them
     if (FEEDS) {
-        load_d_of(end);
+        load_d_of((int)end);
         load_square_of();
         back(end > 0);
         feed((int)end);
-        load_d_of(max(end - 1, (int64_t)0));
+        load_d_of(max((int)end - 1, 0));
         all_waves();
         feed_square();
         load_square_of();
@@ -677,7 +743,10 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
             load_block(z[0], sh.z, 0);
             load_block(z[1], sh.z, 1);
             __builtin_amdgcn_sched_barrier(0);
-            const f4 y = mmp(square[0], z[0], f4{}) + mmp(square[1], z[1], f4{});
+            f4 c[4] = {};
+            mmp(square[0], z[0], c[0], c[1]);
+            mmp(square[1], z[1], c[2], c[3]);
+            const f4 y = (c[0] + c[1]) + (c[2] + c[3]);
             put_block(sh.u, tile * 16, -y * a);
             put(p.dy + unit * kChunk * p.columns, p.columns, tile * 16, column, y);
             load_square_of();

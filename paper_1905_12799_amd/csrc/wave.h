@@ -24,6 +24,11 @@ __device__ inline uint64_t lane_move(uint64_t old, uint64_t x)
     const uint32_t lo = lane_move<CTRL, ROWS>((uint32_t)old, (uint32_t)x), hi = lane_move<CTRL, ROWS>((uint32_t)(old >> 32), (uint32_t)(x >> 32));
     return (uint64_t)hi << 32 | lo;
 }
+template <int CTRL, int ROWS>
+__device__ inline double lane_move(double old, double x)
+{
+    return __longlong_as_double((long long)lane_move<CTRL, ROWS>((uint64_t)__double_as_longlong(old), (uint64_t)__double_as_longlong(x)));
+}
 
 // join of a lane's value with those of all lanes before it; join(earlier, later) is associative, `none` changes nothing
 template <typename T, typename F>
@@ -40,6 +45,8 @@ __device__ inline T wave_scan(T x, T none, F join)
 __device__ inline uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
 __device__ inline float last_lane(float x) { return __uint_as_float(last_lane(__float_as_uint(x))); }
 __device__ inline uint64_t last_lane(uint64_t x) { return (uint64_t)last_lane((uint32_t)(x >> 32)) << 32 | last_lane((uint32_t)x); }
+
+__device__ inline double last_lane(double x) { return __longlong_as_double((long long)last_lane((uint64_t)__double_as_longlong(x))); }
 
 // The same over rows of 16 lanes, each by itself: a scan, and a join that all lanes of the row get
 template <typename T, typename F>
