@@ -193,6 +193,22 @@ struct Team {
         for (int w = 0; w < kWaves; ++w) x = slots[w] > x ? slots[w] : x;
         return x;
     }
+    // A place that at least `least` of the places, one a thread, are at or above: the lowest of what every wave finds by taking off its largest so many times.
+    // 0 where a wave has fewer.
+    static __device__ uint64_t low_threshold(uint32_t least, uint64_t x, uint64_t *slots)
+    {
+        uint64_t last = 0;
+        for (uint32_t i = 0; i < (least + kWaves - 1) / kWaves; ++i) {
+            last = wave_reduce(x, (uint64_t)0, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+            if (x == last) x = 0;
+        }
+        if (NT == 64) return last;
+        sync();
+        if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = last;
+        sync();
+        for (int w = 0; w < kWaves; ++w) last = slots[w] < last ? slots[w] : last;
+        return last;
+    }
     // A place that at least `least` and at most `most` of the places are at or above, of which at_or_above(p) counts the wave's; 1 if there are
     // fewer than `least`.  hi: an upper bound of all places.  The range is halved, 64 times at most.
     template <typename F>
@@ -231,8 +247,8 @@ struct Team {
 };
 __device__ inline uint32_t wave_count(bool x) { return (uint32_t)__popcll(__ballot(x)); }
 
-// The entries [begin, end) of a row, packs one thread after the other; f(index, pack) for whole packs, g(index, x) for what is left
-template <typename T, int NT, typename F, typename G>
+// The entries [begin, end) of a row, packs one thread after the other, so many read ahead; f(index, pack) for whole packs, g(index, x) for what is left
+template <typename T, int NT, int AHEAD, typename F, typename G>
 __device__ inline void for_entries(const T *x, int64_t begin, int64_t end, F f, G g)
 {
     constexpr int N = Pack<T>::N;
@@ -240,13 +256,16 @@ __device__ inline void for_entries(const T *x, int64_t begin, int64_t end, F f, 
     const int64_t packs = (end - begin) / N, rest = begin + packs * N;
     const T *const p = x + begin;
     int64_t i = t;
-    for (; i + 3 * NT < packs; i += 4 * NT) {
-        Pack<T> v[4];
+    if (AHEAD > 1) {
+        for (; i + (AHEAD - 1) * NT < packs; i += AHEAD * NT) {
+            Pack<T> v[AHEAD];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = load_pack(p + (i + j * NT) * N);
+            for (int j = 0; j < AHEAD; ++j) v[j] = load_pack(p + (i + j * NT) * N);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) f(begin + (i + j * NT) * N, v[j]);
+            for (int j = 0; j < AHEAD; ++j) f(begin + (i + j * NT) * N, v[j]);
+        }
     }
+#pragma unroll 1
     for (; i < packs; i += NT) f(begin + i * N, load_pack(p + i * N));
     for (int64_t j = rest + t; j < end; j += NT) g(j, x[j]);
 }
@@ -265,7 +284,7 @@ __device__ inline Seen read_row(const T *x, int64_t begin, int64_t end, float c,
         }
         s.add(v, c);
     };
-    for_entries<T, NT>(x, begin, end, [&](int64_t j, const Pack<T> &p) {
+    for_entries<T, NT, 4>(x, begin, end, [&](int64_t j, const Pack<T> &p) {
         constexpr int N = Pack<T>::N;
         float v[N], top = s.top;
 #pragma unroll
@@ -313,12 +332,16 @@ __device__ inline void best_of_list(uint64_t *list, uint64_t *few, uint32_t n, u
         n = s.listed < (uint32_t)kRanked ? s.listed : (uint32_t)kRanked;
         from = few;
     }
-    for (uint32_t i = t; i < n; i += NT) {
-        const uint64_t mine = from[i];
+    // so many lanes count what is before an entry
+    const uint32_t lanes = n * 8 <= NT ? 8 : n * 4 <= NT ? 4 : n * 2 <= NT ? 2 : 1;
+    for (uint32_t first = 0; first < n; first += NT / lanes) {
+        const uint32_t i = first + t / lanes;
+        const uint64_t mine = i < n ? from[i] : 0;
         uint32_t before = 0;
 #pragma unroll 4
-        for (uint32_t j = 0; j < n; ++j) before += from[j] > mine;
-        if (before < top) put(before, mine);
+        for (uint32_t j = t & (lanes - 1); j < n; j += lanes) before += from[j] > mine;
+        for (uint32_t d = 1; d < lanes; d <<= 1) before += __shfl_xor(before, d);
+        if (i < n && (t & (lanes - 1)) == 0 && before < top) put(before, mine);
     }
 }
 
@@ -340,33 +363,50 @@ __device__ inline void best_of_row(const T *x, int64_t begin, int64_t end, uint3
             }
         };
         if (mine)
-            for_entries<T, NT>(x, begin, end, [&](int64_t j, const Pack<T> &p) {
+            for_entries<T, NT, 1>(x, begin, end, [&](int64_t j, const Pack<T> &p) {
                 float most = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < Pack<T>::N; ++i) most = fmaxf(most, logit_of(p.x[i]));
-                if (!(most < logit_at(least)))           // (a threshold below every number's is none)
+                if (most < logit_at(least)) return;      // (a threshold below every number's is none)
+                uint32_t found = 0;
 #pragma unroll
-                    for (int i = 0; i < Pack<T>::N; ++i) one(j + i, p.x[i]);
+                for (int i = 0; i < Pack<T>::N; ++i) found += place_of(logit_of(p.x[i]), (uint32_t)(j + i)) >= least;
+                if (found == 0) return;
+                uint32_t at = atomicAdd(&s.listed, found);
+#pragma unroll
+                for (int i = 0; i < Pack<T>::N; ++i) {
+                    const uint64_t place = place_of(logit_of(p.x[i]), (uint32_t)(j + i));
+                    if (place >= least && at < (uint32_t)kListed) list[at] = place;
+                    at += place >= least;
+                }
             }, one);
         Tm::sync();
         return s.listed;
     };
-    const uint64_t hi = Tm::max_place(best, slots);
-    uint64_t least = 1;
-    if (end - begin > kListed || NT > 64)                // (a wave lists its whole row)
-        least = Tm::threshold(top, 2 * top, hi, [&](uint64_t p) { return wave_count(best >= p); }, s);
-    uint32_t n = list_from(least, best >= least);
-    if (n > (uint32_t)kListed) {
-        // many large logits with few threads: the row is counted again and again, until no more are left than asked for
+    uint64_t least = 1, hi = 0;
+    if (NT > 64) {                                       // (a wave lists its whole row)
+        // (a few rounds in every wave and one barrier; halving the range of places takes some 20 of both)
+        least = top <= 8 * Tm::kWaves ? Tm::low_threshold(top, best, slots) : 0;
+        if (least == 0) {
+            hi = Tm::max_place(best, slots);
+            least = Tm::threshold(top, 2 * top, hi, [&](uint64_t p) { return wave_count(best >= p); }, s);
+        }
+    }
+    uint32_t n;
+#pragma unroll 1
+    for (bool mine = best >= least;; mine = true) {
+        n = list_from(least, mine);
+        if (n <= (uint32_t)kListed) break;
+        // many large logits with few threads: the row is counted again and again, until the list holds them
+        if (hi == 0) hi = Tm::max_place(best, slots);
         least = Tm::threshold(top, kListed, hi, [&](uint64_t p) {
             uint32_t c = 0;
-            for_entries<T, NT>(x, begin, end, [&](int64_t j, const Pack<T> &v) {
+            for_entries<T, NT, 1>(x, begin, end, [&](int64_t j, const Pack<T> &v) {
+#pragma unroll 1
                 for (int i = 0; i < Pack<T>::N; ++i) c += place_of(logit_of(v.x[i]), (uint32_t)(j + i)) >= p;
             }, [&](int64_t j, T raw) { c += place_of(logit_of(raw), (uint32_t)j) >= p; });
             return (uint32_t)wave_sum((uint64_t)c);
         }, s);
-        n = list_from(least, true);
-        n = n < (uint32_t)kListed ? n : (uint32_t)kListed;
     }
     best_of_list<NT>(list, few, n, top, s, slots, put);
 }
@@ -547,7 +587,7 @@ __global__ void __launch_bounds__(kPieceThreads) logprobs_piece_kernel(RowArgs a
     }
 }
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 1024;
 
 template <typename T, bool TOP, bool TEACHER>
 __global__ void __launch_bounds__(kJoinThreads) logprobs_join_kernel(RowArgs a)
@@ -728,7 +768,7 @@ __global__ void __launch_bounds__(NT == 64 ? 256 : NT) logprobs_grad_kernel(Grad
     } else {
         s = slope_of(g, row);
     }
-    for_entries<T, NT>(x, begin, end, [&](int64_t j, const Pack<T> &p) {
+    for_entries<T, NT, 4>(x, begin, end, [&](int64_t j, const Pack<T> &p) {
         Pack<T> d;
 #pragma unroll
         for (int i = 0; i < N; ++i) d.x[i] = (T)slope_at(s, logit_of(p.x[i]));
@@ -763,7 +803,7 @@ Cut cut_of(int64_t rows, int64_t n, int32_t top)
     Cut c{n, 1, 0, 0};
     if (n <= 16384 || rows >= 512) return c;
     int64_t pieces = std::min<int64_t>((1024 + rows - 1) / rows, n / 8192);
-    if (top > 0) pieces = std::min<int64_t>(pieces, kListed / top);
+    if (top > 0) pieces = std::min<int64_t>(pieces, std::max<int64_t>(4, kRanked / top));         // (the join counts their lists at once)
     if (pieces <= 1) return c;
     c.piece = align_up((n + pieces - 1) / pieces, 64);
     c.pieces = (int32_t)((n + c.piece - 1) / c.piece);
