@@ -44,7 +44,7 @@ struct DeltaArgs {
     float *dg, *dbeta;
     int64_t batch, steps, chunk0;                        // the launch takes chunks chunk0 .. chunk0 + chunks - 1
     int32_t heads, group, chunks;                        // group: heads that share a key head
-    int32_t key_dim, value_dim, columns;                 // columns: value_dim rounded up to 64
+    int32_t key_dim, value_dim, columns, slices;         // columns: value_dim rounded up to 64; slices: of 16 columns, that a chain goes through
     float scale;
     // workspace, an entry per (head, chunk of the launch)
     float *y, *s, *dy, *ds, *gq, *gk;                    // [64][columns], [DK][columns], the same two, [64][DK] x 2
@@ -596,11 +596,10 @@ __global__ void __launch_bounds__(512, kPlanes<T> == 1 && (KEEP || DK < 128) ? 4
 {
     __shared__ ChainShared<DK> sh;
     // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
-    const int slices = p.columns / 16;
-    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
+    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / p.slices * 8 + die;
     if (bh >= p.batch * p.heads) return;
-    if (threadIdx.x < 256) run_chain<T, DK, KEEP, false>(p, sh, bh, (int)(place % slices));
-    else run_chain<T, DK, KEEP, true>(p, sh, bh, (int)(place % slices));
+    if (threadIdx.x < 256) run_chain<T, DK, KEEP, false>(p, sh, bh, (int)(place % p.slices));
+    else run_chain<T, DK, KEEP, true>(p, sh, bh, (int)(place % p.slices));
 }
 
 // ---- backward: the chain from the last chunk to the first ----------------------------------------------------------------
@@ -772,11 +771,10 @@ template <typename T, int DK>
 __global__ void __launch_bounds__(512, kPlanes<T> == 1 ? 4 : 2) delta_back_chain_kernel(DeltaArgs p)
 {
     __shared__ BackShared<T, DK> sh;
-    const int slices = p.columns / 16;
-    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / slices * 8 + die;
+    const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / p.slices * 8 + die;
     if (bh >= p.batch * p.heads) return;
-    if (threadIdx.x < 256) run_back_chain<T, DK, false>(p, sh, bh, (int)(place % slices));
-    else run_back_chain<T, DK, true>(p, sh, bh, (int)(place % slices));
+    if (threadIdx.x < 256) run_back_chain<T, DK, false>(p, sh, bh, (int)(place % p.slices));
+    else run_back_chain<T, DK, true>(p, sh, bh, (int)(place % p.slices));
 }
 
 // ---- backward: all gradients at once -------------------------------------------------------------------------------------------
@@ -814,7 +812,7 @@ __device__ inline void put_tile(__bf16 *p, __bf16 *turned, int ti, int tj, f4 v)
 }
 
 template <typename T, int DK>
-__global__ void __launch_bounds__(DK * 4, DK == 128 ? 4 : DK == 64 ? 2 : 1) delta_back_output_kernel(DeltaArgs p)
+__global__ void __launch_bounds__(DK * 4, DK == 128 ? (kPlanes<T> == 3 ? 2 : 4) : DK == 64 ? 2 : 1) delta_back_output_kernel(DeltaArgs p)
 {
     constexpr int NI = kPlanes<T>, W = DK / 16, Most = (kLower + W - 1) / W;
     __shared__ Gates gates;
@@ -897,6 +895,18 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 4 : DK == 64 ? 2 : 1) delt
             }
         }
     }
+    // q and k of four steps times 16 in this wave's key dimensions (all asked for at once, long before they are used)
+    const int col = wave * 16 + lane16();
+    b4 qs[4][NI], ks[4][NI];
+#pragma unroll
+    for (int ti = 0; ti < 4; ++ti) {
+        const int64_t from = inputs + place_in<NI>(col, ti * 16 + lane4(), 2, 0) + (lane4() & 4);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            qs[ti][i] = *reinterpret_cast<const b4 *>(p.qt + from + i * 512);
+            ks[ti][i] = *reinterpret_cast<const b4 *>(p.kt + from + i * 512);
+        }
+    }
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < Most; ++e) {
@@ -905,7 +915,7 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 4 : DK == 64 ? 2 : 1) delt
         int ti, tj;
         lower_tile(u, ti, tj);
         f4 qk{}, kk{};
-#pragma unroll 1
+#pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) {
             b8 left[NI], right[NI];
             load_block(right, p.kp + inputs, tj * (DK / 32) + kb);
@@ -937,20 +947,17 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? 4 : DK == 64 ? 2 : 1) delt
         // what a block of 32 has above the diagonal
         if (ti == tj && (ti & 1) == 0) put_tile(sh.by.rows, sh.by.turned, ti, ti + 1, f4{});
     }
-    const int col = wave * 16 + lane16();
 #pragma unroll
     for (int ti = 0; ti < 4; ++ti) {
         const f4 a = four(gates.a, ti * 16), c = four(gates.c, ti * 16);
         o_state[ti] *= a * p.scale;
         y_state[ti] *= a;
         carried[ti] *= c;
-        // four steps of q and k
         f4 q{}, k{};
-        const int64_t from = inputs + place_in<NI>(col, ti * 16 + lane4(), 2, 0) + (lane4() & 4);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-            q += __builtin_convertvector(*reinterpret_cast<const b4 *>(p.qt + from + i * 512), f4);
-            k += __builtin_convertvector(*reinterpret_cast<const b4 *>(p.kt + from + i * 512), f4);
+            q += __builtin_convertvector(qs[ti][i], f4);
+            k += __builtin_convertvector(ks[ti][i], f4);
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
@@ -1159,7 +1166,9 @@ __global__ void __launch_bounds__(256) delta_step_kernel(DeltaArgs p)
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
 
-constexpr int64_t kFewSteps = 8;
+// Up to so many steps are taken one by one.  (A step adds 1.5 to 2 us, 2.6 us with 256 heads of 128 x 128 and 18 us with 2048, which the chunks take in 17 us for
+// 32 heads, 51 for 256 and 400 for 2048.)
+int64_t few_steps(int64_t batch, int64_t heads) { return batch * heads >= 256 ? 16 : 6; }
 // Workspace of the chunks that a launch takes.  Forward: what the last-level cache holds, nearly (8191 steps x 32 heads in 128, 256, 512, 1024 MB: 460, 372, 366,
 // 409 us).  Backward: more, as the states before every segment but the first cost a forward pass without outputs.
 constexpr int64_t kSegmentBytes = 384ll << 20, kBackSegmentBytes = 2ll << 30;
@@ -1178,7 +1187,7 @@ DeltaPlan plan_delta(const rls_delta_shape &h, bool backward)
     P.dk = padded_key(h.key_dim);
     P.columns = (int)align_up(h.value_dim, 64);
     P.chunks = (h.steps + kChunk - 1) / kChunk;
-    if (P.chunks == 0 || (!backward && h.steps <= kFewSteps)) return P;
+    if (P.chunks == 0 || (!backward && h.steps <= few_steps(h.batch, h.heads))) return P;
     const int64_t bh = h.batch * h.heads, side = kChunk * (int64_t)P.dk, rows = kChunk * (int64_t)P.columns, state = (int64_t)P.dk * P.columns;
     const bool shared = h.heads != h.key_heads;
     const int64_t planes = 3, square = kChunk * kChunk;          // (as for fp32: the workspace does not go by the type)
@@ -1235,7 +1244,7 @@ struct DeltaLaunch {
     {
         hipLaunchKernelGGL((delta_prepare_kernel<T, DK>), dim3((unsigned)(p.batch * p.heads * p.chunks)), dim3(256), 0, s, p);
     }
-    static unsigned slices(const DeltaArgs &p) { return (unsigned)((p.batch * p.heads + 7) / 8 * 8 * (p.columns / 16)); }
+    static unsigned slices(const DeltaArgs &p) { return (unsigned)((p.batch * p.heads + 7) / 8 * 8 * p.slices); }
     static void chain(const DeltaArgs &p, bool keep, hipStream_t s)
     {
         auto *const kernel = keep ? delta_chain_kernel<T, DK, true> : delta_chain_kernel<T, DK, false>;
@@ -1243,13 +1252,14 @@ struct DeltaLaunch {
     }
     static hipError_t forward(DeltaArgs p, const DeltaPlan &P, float *way, hipStream_t s)
     {
-        if (p.steps <= kFewSteps) {
+        if (p.steps <= few_steps(p.batch, p.heads)) {
             p.columns = P.columns;
             hipLaunchKernelGGL((delta_step_kernel<T, DK>), dim3((unsigned)(p.batch * p.heads * (p.columns / 64))), dim3(256), 0, s, p);
             return hipGetLastError();
         }
         const int64_t state = p.batch * p.heads * p.key_dim * p.value_dim;
         float *const last = p.last;
+        p.slices = (p.value_dim + 15) / 16;
         for (int64_t seg = 0; seg < P.segments; ++seg) {
             p.chunk0 = seg * P.segment;
             p.chunks = (int32_t)std::min(P.segment, P.chunks - p.chunk0);
@@ -1268,6 +1278,7 @@ struct DeltaLaunch {
         const int64_t state = p.batch * p.heads * p.key_dim * p.value_dim;
         const float *const first = p.state;
         p.keep = 1;
+        p.slices = p.columns / 16;                       // (what is kept is read up to the last of the columns)
         for (int64_t seg = 0; seg + 1 < P.segments; ++seg) {
             p.chunk0 = seg * P.segment;
             p.chunks = (int32_t)P.segment;

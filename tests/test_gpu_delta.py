@@ -68,7 +68,7 @@ def close(got, want, T, K, twice, what, terms=0.0):
 
 
 SHAPES = [(1, 1, 1, 1, 1, 1), (2, 1, 4, 2, 128, 128), (3, 5, 3, 1, 17, 130), (2, 8, 2, 2, 33, 5), (1, 9, 2, 1, 64, 64), (2, 37, 4, 4, 64, 64), (1, 63, 1, 1, 16, 16),
-          (1, 64, 2, 1, 32, 100), (2, 65, 2, 2, 128, 128), (1, 128, 1, 1, 100, 33), (3, 130, 6, 2, 40, 72), (2, 300, 3, 3, 65, 200), (1, 700, 4, 1, 128, 64), (9, 70, 1, 1, 20, 512)]
+          (1, 64, 2, 1, 32, 100), (2, 65, 2, 2, 128, 128), (1, 128, 1, 1, 100, 33), (3, 130, 6, 2, 40, 72), (2, 300, 3, 3, 65, 200), (1, 700, 4, 1, 128, 64), (9, 70, 1, 1, 20, 512), (64, 12, 4, 2, 16, 24), (65, 16, 4, 4, 24, 70)]
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
