@@ -885,11 +885,11 @@ hipError_t launch_backward(GradArgs g, hipStream_t s)
         auto *const kernel = a.teacher ? logprobs_grad_kernel<T, 64, true> : logprobs_grad_kernel<T, 64, false>;
         return by_rows(a, kMostRows, [&](int64_t rows) { hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, g); });
     }
-    // pieces of at most 16384 entries; of fewer, down to 2048, where there are few rows
-    g.piece = std::min<int64_t>(16384, std::max<int64_t>(2048, align_up((a.rows * a.n + 2047) / 2048, 64)));
+    // pieces of at most 8192 entries; of fewer, down to 2048, where there are few rows (8192 x 32001 in bf16: 218 us with 16384, 211 with 8192)
+    g.piece = std::min<int64_t>(8192, std::max<int64_t>(2048, align_up((a.rows * a.n + 2047) / 2048, 64)));
     g.pieces = (int32_t)((a.n + g.piece - 1) / g.piece);
     auto *const kernel = a.teacher ? logprobs_grad_kernel<T, 256, true> : logprobs_grad_kernel<T, 256, false>;
-    return by_rows(a, kMostRows / 1024, [&](int64_t rows) { hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * g.pieces)), dim3(256), 0, s, g); });
+    return by_rows(a, std::max<int64_t>(1, (1 << 23) / g.pieces), [&](int64_t rows) { hipLaunchKernelGGL(kernel, dim3((unsigned)(rows * g.pieces)), dim3(256), 0, s, g); });
 }
 
 int32_t check_rows(const void *logits, int32_t type, int64_t rows, int64_t n, int64_t ld)

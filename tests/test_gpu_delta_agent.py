@@ -80,7 +80,7 @@ def test_gradients(example, steps):
               example.policy_loss(exact, batch64, advantage.double(), returns.double(), plain_layer, plain_logprobs)),
              (example.teaching_loss(agent, xs, tokens, scores), example.teaching_loss(exact, xs.double(), tokens, scores, plain_layer, plain_distill))]
     for mine, plain in pairs:
-        assert abs(float(mine) - float(plain)) <= 2.0 ** -14 * (1 + abs(float(plain)))
+        assert abs(float(mine.detach()) - float(plain.detach())) <= 2.0 ** -14 * (1 + abs(float(plain.detach())))
         got = torch.autograd.grad(mine, agent.params, allow_unused=True)
         want = torch.autograd.grad(plain, exact.params, allow_unused=True)
         for i, (x, y) in enumerate(zip(got, want)):
