@@ -406,3 +406,24 @@ def test_past_32_bits(rls):
     g = rls.token_logprobs_backward(x, tokens, r.norm, r.entropy, torch.ones(rows + 100, device="cuda"), out=x)
     w = few.norm.clone()
     assert float(g[-1, n - 1]) > 0.9 and g[0, 0] < 0 and bool(w.isfinite().all())
+
+
+@pytest.mark.parametrize("n", [3, 18])
+def test_many_rows(rls, n):
+    """More rows than a launch takes: the first and the last ones against the same rows by themselves."""
+    rows = (1 << 21) + 9
+    x = torch.randn(rows, n, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda")
+    tokens = torch.arange(rows, dtype=torch.int32, device="cuda") % n
+    r = rls.token_logprobs(x, tokens, top=2)
+    by = torch.ones(rows, device="cuda")
+    g = rls.token_logprobs_backward(x, tokens, r.norm, r.entropy, by, by)
+    k, s = tokens[:, None].contiguous(), by[:, None].contiguous()
+    loss, norm = rls.distill_loss(x, k, s)
+    d = rls.distill_loss_backward(x, k, s, norm, by)
+    for part in (slice(0, 50), slice((1 << 21) - 20, rows)):
+        px, pt = x[part].clone(), tokens[part].clone()
+        q = rls.token_logprobs(px, pt, top=2)
+        assert all(torch.equal(a[part], b) for a, b in zip(r, q))
+        assert torch.equal(g[part], rls.token_logprobs_backward(px, pt, q.norm, q.entropy, by[part].clone(), by[part].clone()))
+        pl, pn = rls.distill_loss(px, k[part].clone(), s[part].clone())
+        assert torch.equal(loss[part], pl) and torch.equal(d[part], rls.distill_loss_backward(px, k[part].clone(), s[part].clone(), pn, by[part].clone()))
