@@ -12,7 +12,7 @@
 //
 // Reading the logits bounds the forward pass, reading and writing them the backward one: 4096 x 50021 in bf16 forward 89 us (4.6 TB/s), 8192 x 32001 in bf16
 // backward 211 (5.0 TB/s, what a large copy reaches), 2048 x 128003 with 64 entries of a teacher 216 (4.9).  Where there is little to read it is dependent steps:
-// 524288 x 3 in fp32 5 us forward and 6 backward, 64 x 128003 in bf16 with 20 alternatives 18 and 8 (7 and 4 without).
+// 524288 x 3 in fp32 5 us forward and 6 backward, 524288 x 20 33 and 45, 64 x 128003 in bf16 with 20 alternatives 18 and 8 (7 and 4 without).
 #include <algorithm>
 
 #include "element_types.h"
@@ -27,7 +27,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr float kLeast = -200.0f;                        // of d2: 2^-200 is 0
 constexpr float kLargest = 3.4028234663852886e38f;
 constexpr int kThreadRow = 16;                           // entries that a thread takes by itself
-constexpr int kWaveRow = 1024;                           // a wave
+constexpr int kWaveRow = 1024;                           // a wave, or 16 lanes
 constexpr int kListed = 4096;                            // places that a workgroup's list holds
 constexpr int kRanked = 256;                             // of them that are counted against each other at once
 
@@ -130,6 +130,23 @@ __device__ inline Seen wave_join(Seen v, float c)
     v.sum = wave_reduce(v.sum, 0.0f, plus);
     v.sum2 = wave_reduce(v.sum2, 0.0f, plus);
     return v;
+}
+
+// over the lanes that take a row together, 16 or all 64 of a wave; the same in each of them
+template <int L, typename T, typename F>
+__device__ inline T lanes_reduce(T x, T none, F join)
+{
+    return L == 16 ? row_reduce(x, join) : wave_reduce(x, none, join);
+}
+template <int L>
+__device__ inline float lanes_max(float x)
+{
+    return lanes_reduce<L>(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int L>
+__device__ inline float lanes_sum(float x)
+{
+    return lanes_reduce<L>(x, 0.0f, [](float a, float b) { return a + b; });
 }
 
 // NT threads that take a row together: a wave by itself, or a workgroup
@@ -445,40 +462,51 @@ __device__ inline float teacher_at(const RowArgs &a, int64_t i)
                     : a.teacher_type == RLS_BF16 ? (float)static_cast<const __bf16 *>(a.teacher)[i] : (float)static_cast<const _Float16 *>(a.teacher)[i];
     return x > kLargest ? kLargest : x;
 }
-// A wave's view of the teacher of a row: two entries a lane, entries that do not count are at -infinity
+// What the lanes that take a row have of its teacher: 128 entries among them; entries that do not count are at -infinity
+template <int L>
 struct Teacher {
-    float x[2];
-    int32_t token[2];
+    static constexpr int E = RLS_MAX_TOP / L;
+    float x[E];
+    int32_t token[E];
     float top, sum;
-};
-__device__ inline Teacher teacher_of(const RowArgs &a, int64_t row, float c)
-{
-    const int lane = threadIdx.x & 63;
-    Teacher t;
+
+    __device__ void load(const RowArgs &a, int64_t row, float c)
+    {
+        const int lane = threadIdx.x & (L - 1);
+        top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const int j = lane + 64 * e;
-        t.token[e] = j < a.k ? a.token[row * a.k + j] : -1;
-        const float x = j < a.k ? teacher_at(a, row * a.k + j) : -INFINITY;
-        t.x[e] = t.token[e] >= 0 && t.token[e] < a.n && x > -INFINITY ? x : -INFINITY;
+        for (int e = 0; e < E; ++e) {
+            x[e] = -INFINITY;
+            token[e] = -1;
+            const int j = lane + L * e;
+            if (L * e < a.k && j < a.k) {
+                token[e] = a.token[row * a.k + j];
+                const float v = teacher_at(a, row * a.k + j);
+                if (token[e] >= 0 && token[e] < a.n && v > -INFINITY) x[e] = v;
+            }
+            top = fmaxf(top, x[e]);
+        }
+        top = lanes_max<L>(top);
+        sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum += power_of(distance2(x[e], top, c));
+        sum = lanes_sum<L>(sum);
     }
-    t.top = wave_max(fmaxf(t.x[0], t.x[1]));
-    t.sum = wave_reduce(power_of(distance2(t.x[0], t.top, c)) + power_of(distance2(t.x[1], t.top, c)), 0.0f, [](float p, float q) { return p + q; });
-    return t;
-}
-// The loss of a row, by a wave
-template <typename T>
-__device__ inline void put_loss(const RowArgs &a, int64_t row, const T *x, const Seen &v, float inv, float log, const Teacher &t)
+    __device__ float share(int e, float c) const { return sum > 0.0f ? power_of(distance2(x[e], top, c)) / sum : 0.0f; }
+};
+// The loss of a row
+template <int L, typename T>
+__device__ inline void put_loss(const RowArgs &a, int64_t row, bool live, const T *x, const Seen &v, float inv, float log, const Teacher<L> &t)
 {
     const float log_teacher = t.sum > 0.0f ? logf(t.sum) : 0.0f;
     float loss = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const float p = t.sum > 0.0f ? power_of(distance2(t.x[e], t.top, inv * kLog2e)) / t.sum : 0.0f;
+    for (int e = 0; e < Teacher<L>::E; ++e) {
+        const float p = t.share(e, inv * kLog2e);
         if (p > 0.0f) loss = fmaf(p, ((t.x[e] - t.top) * inv - log_teacher) - v.logprob(logit_of(x[t.token[e]]), inv, log), loss);
     }
-    loss = wave_reduce(loss, 0.0f, [](float p, float q) { return p + q; });
-    if ((threadIdx.x & 63) == 0) {
+    loss = lanes_sum<L>(loss);
+    if ((threadIdx.x & (L - 1)) == 0 && live) {
         a.logprob[row] = loss;
         if (a.norm) a.norm[2 * row] = v.top, a.norm[2 * row + 1] = log;
     }
@@ -522,6 +550,77 @@ __global__ void __launch_bounds__(256) logprobs_thread_kernel(RowArgs a)
     }
 }
 
+// ---- rows that 16 lanes take, or a wave, in registers: P packs a lane ---------------------------------------------------
+// Alternatives are taken off one after the other: the best of the lanes' best places, whose lane then looks for its next.
+
+constexpr int kTakenOff = 16;                            // alternatives; more go through a list
+
+template <typename T, int L, int P, bool TOP, bool TEACHER>
+__global__ void __launch_bounds__(256) logprobs_lanes_kernel(RowArgs a)
+{
+    constexpr int N = Pack<T>::N;
+    const int lane = threadIdx.x & (L - 1), n = (int)a.n;
+    const int64_t at = a.row0 + (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L, row = min(at, a.rows - 1);
+    const bool live = at < a.rows;                       // (the others go along with the last row)
+    const T *const x = static_cast<const T *>(a.logits) + row * a.ld;
+    const float inv = inverse_of(a.temperature, row), c = inv * kLog2e;
+    Teacher<L> teacher;
+    if (TEACHER) teacher.load(a, row, c);
+    float v[P][N];
+    Seen s;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int first = (i * L + lane) * N;
+        if (first + N <= n) {
+            const Pack<T> raw = load_pack(x + first);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[i][e] = logit_of(raw.x[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[i][e] = first + e < n ? logit_of(x[first + e]) : -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) s.top = fmaxf(s.top, v[i][e]);
+    }
+    s.top = lanes_max<L>(s.top);
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int e = 0; e < N; ++e) s.add(v[i][e], c);
+    s.sum = lanes_sum<L>(s.sum);
+    s.sum2 = lanes_sum<L>(s.sum2);
+    const float log = s.log_sum();
+    if (TEACHER) {
+        put_loss<L>(a, row, live, x, s, inv, log, teacher);
+        return;
+    }
+    if (lane == 0 && live) put_row(a, row, x, s, inv, log);
+    if (!TOP) return;
+    const auto best_below = [&](uint64_t limit) {
+        uint64_t best = 0;
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const uint64_t place = place_of(v[i][e], (uint32_t)((i * L + lane) * N + e));
+                if (place < limit && place > best) best = place;
+            }
+        return best;
+    };
+    uint64_t mine = best_below(~0ull);
+#pragma unroll 1
+    for (int rank = 0; rank < a.top; ++rank) {
+        const uint64_t best = lanes_reduce<L>(mine, (uint64_t)0, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
+        if (best == 0 ? lane == 0 : mine == best) {
+            if (live) {
+                a.top_logprob[row * a.top + rank] = best == 0 ? -INFINITY : s.logprob(logit_at(best), inv, log);
+                a.top_token[row * a.top + rank] = best == 0 ? -1 : (int32_t)index_at(best);
+            }
+            mine = best_below(best);
+        }
+    }
+}
+
 // ---- rows that a wave or a workgroup takes ---------------------------------------------------------------------------
 
 template <int NT, bool TOP>
@@ -541,13 +640,13 @@ __global__ void __launch_bounds__(NT == 64 ? 256 : NT) logprobs_row_kernel(RowAr
     if (row >= a.rows) return;                           // (whole waves, whole workgroups)
     const T *const x = static_cast<const T *>(a.logits) + row * a.ld;
     const float inv = inverse_of(a.temperature, row), c = inv * kLog2e;
-    Teacher teacher;
-    if (TEACHER && (NT == 64 || threadIdx.x < 64)) teacher = teacher_of(a, row, c);
+    Teacher<64> teacher;
+    if (TEACHER && (NT == 64 || threadIdx.x < 64)) teacher.load(a, row, c);
     uint64_t best = 0;
     const Seen v = Tm::join(read_row<T, NT, TOP>(x, 0, a.n, c, &best), c, s.team);
     const float log = v.log_sum();
     if (TEACHER) {
-        if (NT == 64 || threadIdx.x < 64) put_loss(a, row, x, v, inv, log, teacher);
+        if (NT == 64 || threadIdx.x < 64) put_loss<64>(a, row, true, x, v, inv, log, teacher);
         return;
     }
     if (Tm::tid() == 0) put_row(a, row, x, v, inv, log);
@@ -599,8 +698,8 @@ __global__ void __launch_bounds__(kJoinThreads) logprobs_join_kernel(RowArgs a)
     const int64_t row = blockIdx.x;
     const T *const x = static_cast<const T *>(a.logits) + row * a.ld;
     const float inv = inverse_of(a.temperature, row), c = inv * kLog2e;
-    Teacher teacher;
-    if (TEACHER && threadIdx.x < 64) teacher = teacher_of(a, row, c);
+    Teacher<64> teacher;
+    if (TEACHER && threadIdx.x < 64) teacher.load(a, row, c);
     Seen mine;
     for (int i = threadIdx.x; i < a.pieces; i += kJoinThreads) {
         const float *const part = a.part + (row * a.pieces + i) * 4;
@@ -617,7 +716,7 @@ __global__ void __launch_bounds__(kJoinThreads) logprobs_join_kernel(RowArgs a)
     const Seen v = Tm::join(mine, c, s.team);
     const float log = v.log_sum();
     if (TEACHER) {
-        if (threadIdx.x < 64) put_loss(a, row, x, v, inv, log, teacher);
+        if (threadIdx.x < 64) put_loss<64>(a, row, true, x, v, inv, log, teacher);
         return;
     }
     if (threadIdx.x == 0) put_row(a, row, x, v, inv, log);
@@ -704,39 +803,47 @@ __global__ void __launch_bounds__(256) logprobs_grad_thread_kernel(GradArgs g)
     }
 }
 
-// A piece of a row by a team; TEACHER: the teacher's entries are written after the others
-template <typename T, int NT, bool TEACHER>
-__global__ void __launch_bounds__(NT == 64 ? 256 : NT) logprobs_grad_kernel(GradArgs g)
+// A piece of a row by a workgroup (L = 256), or a whole row by 16 lanes or a wave; TEACHER: the teacher's entries are written after the others
+template <typename T, int L, bool TEACHER>
+__global__ void __launch_bounds__(256) logprobs_grad_kernel(GradArgs g)
 {
-    using Tm = Team<NT>;
-    constexpr int N = Pack<T>::N;
-    __shared__ float share[TEACHER ? 128 * (NT == 64 ? 4 : 1) : 1];
-    __shared__ int32_t where[TEACHER ? 128 * (NT == 64 ? 4 : 1) : 1];
-    __shared__ bool taught[NT == 64 ? 4 : 1];
+    constexpr int N = Pack<T>::N, R = 256 / L, W = L < 64 ? L : 64, E = RLS_MAX_TOP / W;
+    __shared__ float share[TEACHER ? R : 1][RLS_MAX_TOP];
+    __shared__ int32_t where[TEACHER ? R : 1][RLS_MAX_TOP];
+    __shared__ bool taught[R];
+    const auto sync = [] {
+        if (L == 256) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
     const RowArgs &a = g.row;
-    const int64_t unit = NT == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-    const int64_t row = a.row0 + unit / g.pieces, begin = unit % g.pieces * g.piece, end = min(a.n, begin + g.piece);
-    if (row >= a.rows) return;
+    const int lane = threadIdx.x & (L - 1), team = L == 256 ? 0 : threadIdx.x / L;      // (a workgroup's row is known to be one)
+    const int64_t unit = (int64_t)blockIdx.x * R + team, at = a.row0 + unit / g.pieces, row = min(at, a.rows - 1);
+    const int64_t begin = unit % g.pieces * g.piece, end = at < a.rows ? min(a.n, begin + g.piece) : begin;        // (nothing of the rows behind the last)
     const T *const x = static_cast<const T *>(a.logits) + row * a.ld;
     T *const out = static_cast<T *>(g.out) + row * g.ld_out;
     Slope s;
-    float late[2] = {0.0f, 0.0f};                        // what two entries of the teacher that lie in this piece get
-    int32_t late_at[2] = {-1, -1};
+    float late[E];                                       // what entries of the teacher that lie in this piece get
+    int32_t late_at[E];
     if (TEACHER) {
         const float inv = inverse_of(a.temperature, row);
-        const int team = NT == 64 ? threadIdx.x >> 6 : 0, base = team * 128;
-        if (NT == 64 || threadIdx.x < 64) {
-            const Teacher t = teacher_of(a, row, inv * kLog2e);
-            const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int e = 0; e < E; ++e) late_at[e] = -1;
+        Teacher<W> t;
+        if (lane < W) {
+            t.load(a, row, inv * kLog2e);
             if (lane == 0) taught[team] = t.sum > 0.0f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float p = t.sum > 0.0f ? power_of(distance2(t.x[e], t.top, inv * kLog2e)) / t.sum : 0.0f;
-                share[base + lane + 64 * e] = p;
-                where[base + lane + 64 * e] = p > 0.0f ? t.token[e] : -1;
+            for (int e = 0; e < E; ++e) {
+                const float p = t.share(e, inv * kLog2e);
+                share[team][lane + W * e] = p;
+                where[team][lane + W * e] = p > 0.0f ? t.token[e] : -1;
             }
         }
-        Tm::sync();
+        sync();
         s.top = a.norm[2 * row];
         s.c = inv * kLog2e;
         s.log2_sum = a.norm[2 * row + 1] * kLog2e;
@@ -745,32 +852,32 @@ __global__ void __launch_bounds__(NT == 64 ? 256 : NT) logprobs_grad_kernel(Grad
         s.at_token = taught[team] ? -inv * g.by_logprob[row] : 0.0f;
         s.each = s.at_token;
         // an entry of the teacher: its first place in the list writes it, with what all its places have
-        if (NT == 64 || threadIdx.x < 64) {
+        if (lane < W) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int mine = (threadIdx.x & 63) + 64 * e;
-                const int32_t at = where[base + mine];
-                if (at < begin || at >= end) continue;
+            for (int e = 0; e < E; ++e) {
+                const int mine = lane + W * e;
+                const int32_t to = where[team][mine];
+                if (W * e >= a.k || to < begin || to >= end) continue;
                 float p = 0.0f;
                 bool first = true;
                 for (int j = 0; j < a.k; ++j) {
-                    const bool same = where[base + j] == at;
+                    const bool same = where[team][j] == to;
                     if (same && j < mine) first = false;
-                    p += same ? share[base + j] : 0.0f;
+                    p += same ? share[team][j] : 0.0f;
                 }
-                const float v = logit_of(x[at]);
+                const float v = logit_of(x[to]);
                 if (first && v > -INFINITY) {
                     const float l2 = distance2(v, s.top, s.c) - s.log2_sum;
                     late[e] = -s.each * (power_of(l2) - p);
-                    late_at[e] = at;
+                    late_at[e] = to;
                 }
             }
         }
-        Tm::sync();                                      // the logits may lie where the gradients go
+        sync();                                          // the logits may lie where the gradients go
     } else {
         s = slope_of(g, row);
     }
-    for_entries<T, NT, 4>(x, begin, end, [&](int64_t j, const Pack<T> &p) {
+    const auto pack = [&](int64_t j, const Pack<T> &p) {
         Pack<T> d;
 #pragma unroll
         for (int i = 0; i < N; ++i) d.x[i] = (T)slope_at(s, logit_of(p.x[i]));
@@ -780,15 +887,34 @@ __global__ void __launch_bounds__(NT == 64 ? 256 : NT) logprobs_grad_kernel(Grad
                 if (s.token == j + i) d.x[i] = (T)slope_at_token(s, p.x[i], slope_at(s, logit_of(p.x[i])));
         }
         store_pack(out + j, d);
-    }, [&](int64_t j, T raw) {
+    };
+    const auto one = [&](int64_t j, T raw) {
         float d = slope_at(s, logit_of(raw));
         if (!TEACHER && s.token == j) d = slope_at_token(s, raw, d);
         out[j] = (T)d;
-    });
+    };
+    const int64_t packs = (end - begin) / N;
+    if (L == 256) {
+        int64_t i = lane;
+        for (; i + 3 * L < packs; i += 4 * L) {
+            Pack<T> v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = load_pack(x + begin + (i + j * L) * N);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) pack(begin + (i + j * L) * N, v[j]);
+        }
+#pragma unroll 1
+        for (; i < packs; i += L) pack(begin + i * N, load_pack(x + begin + i * N));
+    } else {
+#pragma unroll 1
+        for (int i = lane; i < packs; i += L) pack(begin + i * N, load_pack(x + begin + i * N));
+    }
+    for (int64_t j = begin + packs * N + lane; j < end; j += L) one(j, x[j]);
     if (TEACHER) {
-        Tm::sync();                                      // (what was stored before the barrier comes before what is stored behind it)
-        if (late_at[0] >= 0) out[late_at[0]] = (T)late[0];
-        if (late_at[1] >= 0) out[late_at[1]] = (T)late[1];
+        sync();                                          // (what was stored before the barrier comes before what is stored behind it)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (late_at[e] >= 0) out[late_at[e]] = (T)late[e];
     }
 }
 
@@ -839,10 +965,22 @@ constexpr int64_t kMostRows = 1 << 21;
 template <typename T, int NT>
 hipError_t launch_rows(RowArgs a, hipStream_t s)
 {
-    auto *const kernel = a.teacher ? logprobs_row_kernel<T, NT, false, true>
-                         : a.top > 0 ? logprobs_row_kernel<T, NT, true, false> : logprobs_row_kernel<T, NT, false, false>;
+    void (*kernel)(RowArgs) = logprobs_row_kernel<T, NT, true, false>;
+    if constexpr (NT > 64) {                             // (rows of a wave come here for their alternatives only)
+        if (a.top == 0) kernel = a.teacher ? logprobs_row_kernel<T, NT, false, true> : logprobs_row_kernel<T, NT, false, false>;
+    }
     return by_rows(a, kMostRows, [&](int64_t rows) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)(NT == 64 ? (rows + 3) / 4 : rows)), dim3(NT == 64 ? 256 : NT), 0, s, a);
+    });
+}
+
+template <typename T, int L, int P>
+hipError_t launch_lanes(RowArgs a, hipStream_t s)
+{
+    auto *const kernel = a.teacher ? logprobs_lanes_kernel<T, L, P, false, true>
+                         : a.top > 0 ? logprobs_lanes_kernel<T, L, P, true, false> : logprobs_lanes_kernel<T, L, P, false, false>;
+    return by_rows(a, kMostRows, [&](int64_t rows) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 256 / L - 1) / (256 / L))), dim3(256), 0, s, a);
     });
 }
 
@@ -853,6 +991,14 @@ hipError_t launch_forward(RowArgs a, char *ws, hipStream_t s)
         auto *const kernel = a.n <= 4 ? logprobs_thread_kernel<T, 4> : a.n <= 8 ? logprobs_thread_kernel<T, 8> : logprobs_thread_kernel<T, 16>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((a.rows + 255) / 256)), dim3(256), 0, s, a);
         return hipGetLastError();
+    }
+    // 16 lanes for rows of up to 256 entries (524288 x 20 in fp32 with a wave a row: 128 us, with 3 alternatives 602)
+    if (a.n <= kWaveRow && a.top <= kTakenOff) {
+        constexpr int N = Pack<T>::N;
+        if (a.n <= 16 * N) return launch_lanes<T, 16, 1>(a, s);
+        if (a.n <= 256) return launch_lanes<T, 16, 256 / (16 * N)>(a, s);
+        if (a.n <= 64 * N) return launch_lanes<T, 64, 1>(a, s);
+        return launch_lanes<T, 64, kWaveRow / (64 * N)>(a, s);
     }
     const Cut c = cut_of(a.rows, a.n, a.top);
     if (c.pieces == 1) {
@@ -881,11 +1027,15 @@ hipError_t launch_backward(GradArgs g, hipStream_t s)
         hipLaunchKernelGGL(kernel, dim3((unsigned)((a.rows + 255) / 256)), dim3(256), 0, s, g);
         return hipGetLastError();
     }
-    if (a.n <= kWaveRow) {
+    if (a.n <= kWaveRow) {                               // 16 lanes a row up to 256 entries, else a wave (524288 x 20 in bf16 with a wave a row: 448 us)
+        const int lanes = a.n <= 256 ? 16 : 64;
         g.piece = kWaveRow;
         g.pieces = 1;
-        auto *const kernel = a.teacher ? logprobs_grad_kernel<T, 64, true> : logprobs_grad_kernel<T, 64, false>;
-        return by_rows(a, kMostRows, [&](int64_t rows) { hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, g); });
+        auto *const kernel = lanes == 16 ? (a.teacher ? logprobs_grad_kernel<T, 16, true> : logprobs_grad_kernel<T, 16, false>)
+                             : (a.teacher ? logprobs_grad_kernel<T, 64, true> : logprobs_grad_kernel<T, 64, false>);
+        return by_rows(a, kMostRows, [&](int64_t rows) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 256 / lanes - 1) / (256 / lanes))), dim3(256), 0, s, g);
+        });
     }
     // pieces of at most 8192 entries; of fewer, down to 2048, where there are few rows (8192 x 32001 in bf16: 218 us with 16384, 211 with 8192)
     g.piece = std::min<int64_t>(8192, std::max<int64_t>(2048, align_up((a.rows * a.n + 2047) / 2048, 64)));
