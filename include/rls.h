@@ -422,7 +422,7 @@ int32_t rls_linear_scan_backward(const rls_scan_shape *shape, const rls_sequence
                                  const rls_sequence *db, float *dh0_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);
 
 /* A [batch][steps][heads][dim] array: dimensions side by side, any strides (in elements) between heads, steps and sequences.  Read-only ones may
- * repeat themselves (stride 0); written ones must not overlap themselves or anything else (RLS_ERR_SHAPE). */
+ * repeat themselves (stride 0); written ones must not overlap themselves or anything else (RLS_ERR_SHAPE; arrays that reach into each other count as overlapping). */
 typedef struct {
     void *data_dev;
     int64_t batch_stride, step_stride, head_stride;

@@ -5,18 +5,19 @@
 // Many are taken in chunks of 64.  With the sums of log-decays gamma inside a chunk, the state S0 before it, and over its steps i, j
 //   a_i = exp(gamma_i), D_ij = exp(gamma_i - gamma_j) for j <= i, c_j = D_63,j, G = D . (K K^T) below the diagonal, P = D . (Q K^T),
 // where what a reset lies between is 0, the differences y_i = v_i - (decayed state)^T k_i of all steps are one triangular system,
-//   (1 + G beta) Y = V - a . (K S0),  so with X = (1 + G beta)^-1   Y = X V - (X a K) S0,  S1 = a_63 S0 + (c beta K)^T Y,
+//   (1 + G beta) Y = V - a . (K S0),  so with X = (1 + G beta)^-1   Y = X (V - a . (K S0)),  S1 = a_63 S0 + (c beta K)^T Y,
 //   O = scale (a . (Q S0) + P (beta Y)).
-// X, X V and X a K are made for all chunks at once, then a chain of two products per chunk runs for 16 columns of the state at a time,
-// then all outputs at once.  The backward pass has the same shape, with a chain from the last chunk to the first:
-//   dY = X^T beta (scale P^T dO + c . (K dS1)),  dS0 = a_63 dS1 + scale (a Q)^T dO - (a K)^T dY.
+// X and P are made for all chunks at once; then a chain of these products per chunk runs for 16 columns of the state at a time, with the outputs in it.
+// The backward pass keeps S0 and Y of every chunk, has a chain from the last chunk to the first,
+//   dY = X^T beta (scale P^T dO + c . (K dS1)),  dS0 = a_63 dS1 + scale (a Q)^T dO - (a K)^T dY,
+// and then takes all other gradients at once.
 // The state is handed back in fp32, and what it is made of must not be rounded to fewer bits on the way.  So a matrix instruction of 16-bit operands takes an
 // fp32 number as the sum of three bf16 numbers (24 bits, what is left out is 2^-27 of it), an fp16 input as two and a bf16 input as it is, and of the products
 // of two such sums those that count in fp32: three for a bf16 input with an fp32 operand, six for two of fp32, at 1/16 of an fp32 instruction's time each.
 // Small and awkward products (the inverse) are left to the fp32 instructions.
-// What it takes, heads of 128 x 128 in bf16: a token of 64 x 32 heads 59 us (4.6 TB/s of state); 8191 steps of 32 heads 358, of that 113 to prepare the chunks and
-// 262 in the chain, 2.0 a chunk (all of it with fp32 instructions and outputs apart: 1349); gradients of 4 x 2048 steps of 16 heads 595: 73, 149, 186 in the
-// chain back, 193 for all gradients (1288).
+// What it takes, heads of 128 x 128 in bf16: a token of 64 x 32 heads 59 us (4.6 TB/s of state); 8191 steps of 32 heads 361, of that 114 to prepare the chunks and
+// 270 in the chain, 2.1 a chunk (all of it with fp32 instructions and outputs apart: 1349); gradients of 4 x 2048 steps of 16 heads 591: 72, 149, 187 in the
+// chain back, 189 for all gradients (1288).  (Launches by themselves, as a profiler has them, add up to more than a pass among others.)
 #include <algorithm>
 #include <type_traits>
 
