@@ -274,3 +274,46 @@ def test_graph_and_streams(rls):
                 results.append([both(x, None) for _ in range(3)][-1])
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for r, w in zip(results, want) for x, y in zip(r, w))
+
+
+@pytest.mark.parametrize("T", [4, 100])
+def test_sequences_past_32_bits(rls, T):
+    """Sequences whose rows begin more than 2^31 elements after each other's."""
+    H, K = 2, 64
+    d = inputs(2, T, H, H, K, K, "bf16", 5)
+    far = torch.empty((1 << 31) + 3 * T * H * K, dtype=torch.bfloat16, device="cuda")
+    views = {n: far[i * T * H * K:].as_strided((2, T, H, K), (1 << 31, H * K, K, 1)) for i, n in enumerate("qkv")}
+    for n, x in views.items():
+        x.copy_(d[n])
+    o, last = rls.gated_delta(**{**d, **views})
+    want, end = rls.gated_delta(**d)
+    assert torch.equal(o, want) and torch.equal(last, end)
+    rest = d["g"], d["beta"], o, d["state"], None, last
+    for x, y in zip(rls.gated_delta_backward(*views.values(), *rest), rls.gated_delta_backward(d["q"], d["k"], d["v"], *rest)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("T", [2, 70, 300])
+def test_the_states_gradient_in_place(rls, short_segments, T):
+    """Through the C ABI: dstate written where dlast was, with one segment and with several; without dlast or dstate at all."""
+    B, H, K, V = 2, 2, 32, 48
+    d = inputs(B, T, H, 1, K, V, "f32", 9, True)
+    do, dlast = torch.randn(B, T, H, V, device="cuda"), torch.randn(B, H, K, V, device="cuda")
+    args = [d[n] for n in ("q", "k", "v", "g", "beta")]
+    want = rls.gated_delta_backward(*args, do, d["state"], d["reset"], dlast)
+    none = rls.gated_delta_backward(*args, do, d["state"], d["reset"])
+    for segment in (-1, 0):
+        short_segments(segment)
+        shape = rls._DeltaShape(B, T, H, 1, K, V, 0, K ** -0.5)
+        ws = torch.empty(rls.gated_delta_workspace_bytes(B, T, H, 1, K, V, True) + 256, dtype=torch.uint8, device="cuda")
+        base = ws.data_ptr() + -ws.data_ptr() % 256
+        for by, to, expected in ((dlast.clone(), "same", want), (None, None, none)):
+            out = [torch.empty_like(x) for x in want[:5]]
+            held, at = rls._heads(torch.float32, *((x, x.shape, "x") for x in (d["q"], d["k"], d["v"], do, out[0], out[1], out[2])))
+            rc = rls.lib().rls_gated_delta_backward(ctypes.byref(shape), at[0], at[1], at[2], d["g"].data_ptr(), d["beta"].data_ptr(), d["state"].data_ptr(),
+                                                    d["reset"].data_ptr(), at[3], 0 if by is None else by.data_ptr(), at[4], at[5], at[6], out[3].data_ptr(),
+                                                    out[4].data_ptr(), by.data_ptr() if to else 0, base, ws.numel() - 256,
+                                                    torch.cuda.current_stream().cuda_stream)
+            assert rc == 0
+            assert all(torch.equal(x, y) for x, y in zip(out, expected))
+            assert by is None or torch.equal(by, want[5])
