@@ -19,6 +19,11 @@ def sources():
     return [os.path.join(CSRC, s) for s in SOURCES]
 
 
+def compile_flags():
+    return ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=off", "-mllvm", "-amdgpu-mfma-vgpr-form",
+            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+
+
 def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
@@ -31,8 +36,7 @@ def is_stale() -> bool:
 def build_library(verbose: bool = False) -> str:
     """Compile every kernel file for gfx950, side by side, and link the shared library. Always compiles."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    flags = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=off", "-mllvm", "-amdgpu-mfma-vgpr-form",
-             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    flags = compile_flags()
     # the Lloyd kernels of the larger padded numbers of features are objects of their own (they take longest and go first)
     lloyd = os.path.join(CSRC, "kmeans_lloyd.hip")
     units = [(lloyd, ["-DRLS_LLOYD_DPAD=32"]), (lloyd, ["-DRLS_LLOYD_DPAD=16"]), (lloyd, [])] + [(s, []) for s in sources() if s != lloyd]

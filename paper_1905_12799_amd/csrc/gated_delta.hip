@@ -423,7 +423,8 @@ __device__ inline f4 rows_by(const b8 (&rows)[BLOCKS][NI], const __bf16 *planes)
 
 // Every wave of a kind has the same loads and stores in the same order, none of them behind a branch, so that it waits for a load by how many came after it
 // and for nothing else: what has no place to go is stored to a spare one.  Products with a block of zeros are taken too, for the same reason and because
-// the compiler leaves out the wait states between a matrix instruction and what reads its result behind a branch to an earlier block.
+// the compiler has left out the wait states between a matrix instruction and what read its result behind a branch to an earlier block (a test looks for that
+// along every path of the listings).
 // Steps behind the last one are worked on with the last one's v: beta is 0 there, and what they give is not written.
 template <int DK>
 struct alignas(16) ChainShared {
