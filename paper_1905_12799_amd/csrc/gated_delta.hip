@@ -1047,9 +1047,10 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? (kPlanes<T> == 3 ? 2 : 4) 
         double sum = (double)slope - (double)(beta * column) - (double)on, carried_on = on;
         for (int step = 32; step > 0; step >>= 1) carried_on += __shfl_xor(carried_on, step);
         if (i == kChunk - 1) sum += carried_on + (double)gates.a[kChunk - 1] * all;
+        // the steps from here to the next cut (all behind a cut add up to 0, which their roundings would not)
         for (int step = 1; step < kChunk; step <<= 1) {
             const double later = __shfl_down(sum, step);
-            if (i + step < kChunk) sum += later;
+            if (i + step < kChunk && gates.part[i + step] == gates.part[i]) sum += later;
         }
         if (t0 + i < p.steps) {
             const int64_t to = (b * p.steps + t0 + i) * p.heads + head;
