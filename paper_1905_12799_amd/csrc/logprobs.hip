@@ -747,9 +747,10 @@ struct GradArgs {
     int32_t pieces;
 };
 
-// dx = (token's entry: at_token) - p (each + by_log log p)
+// dx = inv ((token's entry: at_token) - p (each + by_log log p)).  inv comes last: what it is multiplied with may be the small difference of large numbers, and
+// 0 where inv is as large as it gets
 struct Slope {
-    float top, c, log2_sum, at_token, each, by_log;
+    float top, c, inv, log2_sum, at_token, each, by_log;
     int32_t token;
 };
 __device__ inline Slope slope_of(const GradArgs &g, int64_t row)
@@ -759,16 +760,17 @@ __device__ inline Slope slope_of(const GradArgs &g, int64_t row)
     Slope s;
     s.top = a.norm[2 * row];
     s.c = inv * kLog2e;
+    s.inv = inv;
     s.log2_sum = a.norm[2 * row + 1] * kLog2e;
     s.token = a.token ? a.token[row] : -1;
     const bool given = s.token >= 0 && s.token < a.n && g.by_logprob;
-    s.at_token = given ? inv * g.by_logprob[row] : 0.0f;
-    s.by_log = g.by_entropy ? inv * g.by_entropy[row] : 0.0f;
+    s.at_token = given ? g.by_logprob[row] : 0.0f;
+    s.by_log = g.by_entropy ? g.by_entropy[row] : 0.0f;
     s.each = s.at_token + (g.by_entropy ? s.by_log * a.entropy[row] : 0.0f);
     if (!given) s.token = -1;
     return s;
 }
-// (an entry whose probability is 0 has no part in the entropy, and its gradient is 0 whatever the factors are)
+// without inv (an entry whose probability is 0 has no part in the entropy, and its gradient is 0 whatever the factors are)
 __device__ inline float slope_at(const Slope &s, float x)
 {
     const float l2 = distance2(x, s.top, s.c) - s.log2_sum, p = power_of(l2);
@@ -799,7 +801,7 @@ __global__ void __launch_bounds__(256) logprobs_grad_thread_kernel(GradArgs g)
         if (i >= n) continue;
         float d = slope_at(s, logit_of(l[i]));
         if (i == s.token) d = slope_at_token(s, l[i], d);
-        out[i] = (T)d;
+        out[i] = (T)(d * s.inv);
     }
 }
 
@@ -846,10 +848,11 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(GradArgs g)
         sync();
         s.top = a.norm[2 * row];
         s.c = inv * kLog2e;
+        s.inv = inv;
         s.log2_sum = a.norm[2 * row + 1] * kLog2e;
         s.by_log = 0.0f;
         s.token = -1;
-        s.at_token = taught[team] ? -inv * g.by_logprob[row] : 0.0f;
+        s.at_token = taught[team] ? -g.by_logprob[row] : 0.0f;
         s.each = s.at_token;
         // an entry of the teacher: its first place in the list writes it, with what all its places have
         if (lane < W) {
@@ -868,7 +871,7 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(GradArgs g)
                 const float v = logit_of(x[to]);
                 if (first && v > -INFINITY) {
                     const float l2 = distance2(v, s.top, s.c) - s.log2_sum;
-                    late[e] = -s.each * (power_of(l2) - p);
+                    late[e] = -s.each * (power_of(l2) - p) * s.inv;
                     late_at[e] = to;
                 }
             }
@@ -880,18 +883,18 @@ __global__ void __launch_bounds__(256) logprobs_grad_kernel(GradArgs g)
     const auto pack = [&](int64_t j, const Pack<T> &p) {
         Pack<T> d;
 #pragma unroll
-        for (int i = 0; i < N; ++i) d.x[i] = (T)slope_at(s, logit_of(p.x[i]));
+        for (int i = 0; i < N; ++i) d.x[i] = (T)(slope_at(s, logit_of(p.x[i])) * s.inv);
         if (!TEACHER && s.token >= j && s.token < j + N) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (s.token == j + i) d.x[i] = (T)slope_at_token(s, p.x[i], slope_at(s, logit_of(p.x[i])));
+                if (s.token == j + i) d.x[i] = (T)(slope_at_token(s, p.x[i], slope_at(s, logit_of(p.x[i]))) * s.inv);
         }
         store_pack(out + j, d);
     };
     const auto one = [&](int64_t j, T raw) {
         float d = slope_at(s, logit_of(raw));
         if (!TEACHER && s.token == j) d = slope_at_token(s, raw, d);
-        out[j] = (T)d;
+        out[j] = (T)(d * s.inv);
     };
     const int64_t packs = (end - begin) / N;
     if (L == 256) {
