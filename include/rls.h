@@ -447,8 +447,9 @@ typedef struct {
  *   state_dev   [batch][heads][key_dim][value_dim] fp32, before the first step, or null (0)
  *   o           (written);  last_dev as state_dev (written) or null, after the last step; it may be state_dev itself: a state kept in place
  * steps = 0 leaves o alone and copies the state.  Keys of length 1 and beta in 0 .. 1 (2) keep the state in bounds; others are computed
- * as they are.  Steps are taken in chunks whose decays are products: g above 0 may overflow within 64 steps where step by step it would not.
- * Inputs or states that are not finite make what the same head computes in that call not finite, before and after them as well.
+ * as they are.  What is not finite, an input or a state, makes not finite what follows from it step by step in its head, from there on up to the next
+ * reset or gate that keeps nothing, and nothing else.  Steps are taken in chunks; a head whose state is not finite at the end of one of a call's
+ * launches has that launch's steps taken one by one instead (some 1 to 4 us each), also where it was a product over a chunk that passed the largest number.
  * 1 <= key_dim <= RLS_MAX_KEY_DIM, 1 <= value_dim <= RLS_MAX_VALUE_DIM, batch * heads <= 2^17, batch * steps <= 2^30.
  */
 #define RLS_MAX_KEY_DIM 128
@@ -461,6 +462,9 @@ int32_t rls_gated_delta(const rls_delta_shape *shape, const rls_heads *q, const 
  * Its backward pass, from the inputs (the states are computed again) and the gradients dout by o and dlast (null: 0) by the last state.
  *   dq, dk, dv  (written) as q, k, v, summed over the heads that share a key head;  dg_dev, dbeta_dev (written) as g, beta: dg is 0 where nothing is carried
  *   dstate_dev  (written) as state_dev, or null; may be dlast_dev's memory
+ * What is not finite, a gradient or anything it meets in the recurrence, may make the gradients of its head between the resets or gates that keep nothing on both
+ * sides of it not finite (with a key or query, those of all heads that share it), and no others; so may decays whose product over up to 64 steps passes the
+ * largest number.
  */
 int32_t rls_gated_delta_backward(const rls_delta_shape *shape, const rls_heads *q, const rls_heads *k, const rls_heads *v, const float *g_dev,
                                  const float *beta_dev, const float *state_dev, const uint8_t *reset_dev, const rls_heads *dout, const float *dlast_dev,

@@ -901,7 +901,7 @@ def gated_delta(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, g: torch.Tens
 
     q and k may have fewer heads than v; g (logarithms of the decay) and beta are fp32 [batch, steps, heads]; reset [batch, steps] (bytes or bools) is set
     where a sequence begins; scale is key_dim ** -0.5 unless given.  `last` may be state itself, for a state that is updated in place.  Differentiable
-    by q, k, v, g, beta and state."""
+    by q, k, v, g, beta and state.  Numbers that are not finite reach what follows in their head up to the next reset, as in linear_scan, and nothing else."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (q, k, v, g, beta, state)):
         if out is not None or last is not None:
             raise ValueError("out and last are for calls that nothing is differentiated by (torch.no_grad)")

@@ -61,6 +61,15 @@ struct DeltaArgs {
     int32_t keep;                                        // for the backward pass
 };
 
+// A kernel's arguments read anew, for code behind its loops that hardly any call reaches: none of them is kept in a register until then
+__device__ inline const DeltaArgs &arguments_again()
+{
+    auto *const held = __builtin_amdgcn_kernarg_segment_ptr();
+    uint64_t at = (uint64_t)held;
+    asm volatile("" : "+s"(at));
+    return *(const DeltaArgs *)at;
+}
+
 template <typename T>
 __device__ inline const T *at(const Heads &h, int64_t b, int64_t t, int64_t head)
 {
@@ -249,6 +258,19 @@ struct alignas(16) Gates {
         a[l] = before == 0 ? __builtin_amdgcn_exp2f((float)sum) : 0.0f;
         const double end = last_lane(sum);
         c[l] = before == __popcll(cuts) ? __builtin_amdgcn_exp2f((float)(end - sum)) : 0.0f;
+    }
+    // The sums anew, each from a cut on, for gates that are not finite: those do not go away by being subtracted
+    __device__ void sum_within_cuts(const DeltaArgs &p, int64_t gate, int l, bool in)
+    {
+        double sum = in && !cut[l] ? (double)p.g[gate] * 1.4426950408889634 : 0.0;
+        for (int step = 1; step < kChunk; step <<= 1) {
+            const double before = __shfl_up(sum, step);
+            if (l >= step && part[l - step] == part[l]) sum += before;
+        }
+        const double end = __shfl(sum, kChunk - 1);
+        gamma[l] = sum;
+        a[l] = part[l] == 0 ? __builtin_amdgcn_exp2f((float)sum) : 0.0f;
+        c[l] = part[l] == part[kChunk - 1] ? __builtin_amdgcn_exp2f((float)(end - sum)) : 0.0f;
     }
     __device__ float decay(int i, int j) const { return j <= i && part[i] == part[j] ? __builtin_amdgcn_exp2f((float)(gamma[i] - gamma[j])) : 0.0f; }
 };
@@ -449,8 +471,25 @@ __device__ inline void all_waves()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+__device__ inline bool not_finite(f4 state)
+{
+    bool bad = false;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) bad |= !(fabsf(state[m]) < INFINITY);
+    return bad;
+}
+// 16 rows and columns of the state at the end, column j by this lane
+__device__ inline void put_state(const DeltaArgs &p, int64_t bh, int row, int j, f4 state)
+{
+    if (!p.last || j >= p.value_dim) return;
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+        if (row + lane4() + m < p.key_dim) p.last[(bh * p.key_dim + row + lane4() + m) * p.value_dim + j] = state[m];
+}
+
+// Returns the state at the end, 16 rows of a wave
 template <typename T, int DK, bool KEEP, bool ANSWERS>
-__device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_t bh, int slice)
+__device__ inline f4 run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_t bh, int slice)
 {
     constexpr int NI = kPlanes<T>, Square = kChunk * kChunk, Inputs = NI * kChunk * DK;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile = wave & 3;
@@ -583,30 +622,108 @@ __device__ inline void run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_
         if (kQueries) put_block(sh.y, tile * 16, sh.y32[tile][threadIdx.x & 63]);
         load_kt_of();
     }
-    if (kQueries) {
-        // (the four of them by themselves: each reads what all of them have put)
-        all_waves();
-        answer(p.chunks - 1);
-    } else {
-        all_waves();
-    }
-    if (!p.last || !mine || j >= p.value_dim) return;
+    all_waves();
+    if (kQueries) answer(p.chunks - 1);                  // (the four of them by themselves: each reads what all of them have put)
+    return state;
+}
+
+// What a chain multiplies by 0 - the state before a reset, steps on the other side of one - does not go away if it is infinite or no number.  Once in the state
+// it stays there to the chain's end, so the state that is left tells: a workgroup whose columns are not finite then takes them again, step by step, where
+// a cut is no product.  A column has 32 lanes.  (1.2 to 4 us a step, for calls that hold such numbers only.)
+__device__ inline float column_sum(float x)              // over 32 lanes
+{
+    for (int d = 16; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+// a column of the state, every 32nd row a lane
+template <int DK>
+struct Column {
+    static constexpr int R = DK / 32;
+    float s[R];
+    int64_t place;                                       // of its first row, in p.state and p.last
+    int j;
+    bool in;
+
+    int lane;                                            // of 32
+    __device__ int row(int i) const { return lane + 32 * i; }
+    __device__ Column(const DeltaArgs &p, int64_t bh, int slice) : j(slice * 16 + (int)(threadIdx.x >> 5)), lane(threadIdx.x & 31)
+    {
+        in = j < p.value_dim;
+        place = bh * p.key_dim * p.value_dim + j;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        const int row = wave * 16 + lane4() + m;
-        if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[m];
+        for (int i = 0; i < R; ++i) s[i] = p.state && in && row(i) < p.key_dim ? p.state[place + (int64_t)row(i) * p.value_dim] : 0.0f;
     }
+    __device__ void put_last(const DeltaArgs &p) const
+    {
+        if (!p.last || !in) return;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (row(i) < p.key_dim) p.last[place + (int64_t)row(i) * p.value_dim] = s[i];
+    }
+    __device__ void keep(float *to, int columns) const   // with zeros where the state has no rows and columns
+    {
+#pragma unroll
+        for (int i = 0; i < R; ++i) to[row(i) * columns + j] = in ? s[i] : 0.0f;
+    }
+};
+template <typename T, int DK, bool KEEP>
+__device__ void chain_by_steps(const DeltaArgs &p, int64_t bh, int slice)
+{
+    const int64_t b = bh / p.heads, head = bh % p.heads, key = head / p.group;
+    Column<DK> c(p, bh, slice);
+#pragma unroll 1
+    for (int n = 0; n < p.chunks; ++n) {
+        const int64_t unit = bh * p.chunks + n, t0 = (p.chunk0 + n) * kChunk;
+        if (KEEP) c.keep(p.s + unit * DK * p.columns, p.columns);
+#pragma unroll 1
+        for (int l = 0; l < kChunk; ++l) {
+            const int64_t t = t0 + l, gate = (b * p.steps + t) * p.heads + head;
+            float y = 0.0f;
+            if (t < p.steps) {
+                const T *const k = at<T>(p.k, b, t, key), *const q = at<T>(p.q, b, t, key);
+                const bool cut = p.g[gate] < kNoCarry || (p.reset && p.reset[b * p.steps + t] != 0);
+                const float carry = cut ? 0.0f : expf(p.g[gate]);
+                float sk = 0.0f, sq = 0.0f;
+#pragma unroll
+                for (int i = 0; i < c.R; ++i) {
+                    c.s[i] = cut ? 0.0f : c.s[i] * carry;
+                    if (c.row(i) < p.key_dim) sk = fmaf(c.s[i], (float)k[c.row(i)], sk);
+                }
+                y = c.in ? (float)at<T>(p.v, b, t, head)[c.j] - column_sum(sk) : 0.0f;
+                const float u = p.beta[gate] * y;
+#pragma unroll
+                for (int i = 0; i < c.R; ++i)
+                    if (c.row(i) < p.key_dim) {
+                        c.s[i] = fmaf((float)k[c.row(i)], u, c.s[i]);
+                        sq = fmaf(c.s[i], (float)q[c.row(i)], sq);
+                    }
+                if (!KEEP) {
+                    const float o = p.scale * column_sum(sq);
+                    if (c.in && c.lane == 0) out_at<T>(p.o, b, t, head)[c.j] = (T)o;
+                }
+            }
+            if (KEEP && c.lane == 0) p.y[(unit * kChunk + l) * p.columns + c.j] = y;
+        }
+    }
+    c.put_last(p);
 }
 
 template <typename T, int DK, bool KEEP>
 __global__ void __launch_bounds__(512, kPlanes<T> == 1 ? 4 : 2) delta_chain_kernel(DeltaArgs p)
 {
     __shared__ ChainShared<DK> sh;
+    __shared__ int32_t bad;
+    if (threadIdx.x == 0) bad = 0;
     // workgroups go round the 8 dies in turn; those of a head read the same matrices and share a die's cache
     const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / p.slices * 8 + die;
     if (bh >= p.batch * p.heads) return;
-    if (threadIdx.x < 256) run_chain<T, DK, KEEP, false>(p, sh, bh, (int)(place % p.slices));
-    else run_chain<T, DK, KEEP, true>(p, sh, bh, (int)(place % p.slices));
+    const int slice = (int)(place % p.slices);
+    const f4 state = threadIdx.x < 256 ? run_chain<T, DK, KEEP, false>(p, sh, bh, slice) : run_chain<T, DK, KEEP, true>(p, sh, bh, slice);
+    const int wave = threadIdx.x >> 6;
+    if (wave < DK / 16 && not_finite(state)) bad = 1;
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(bad)) chain_by_steps<T, DK, KEEP>(arguments_again(), bh, slice);
+    else if (wave < DK / 16) put_state(p, bh, wave * 16, slice * 16 + lane16(), state);
 }
 
 // ---- backward: the chain from the last chunk to the first ----------------------------------------------------------------
@@ -619,16 +736,19 @@ struct alignas(16) BackShared {
     // (q is read to a chunk's end, so the next chunk's has a place of its own)
     __bf16 s[3 * 16 * DK], o[kPlanes<T> * 16 * kChunk], q[2][3 * 16 * kChunk], z[3 * 16 * kChunk], u[3 * 16 * kChunk];
     f4 e[4][64];
+    int32_t bad;                                         // the state at the end is not finite
 };
 
+// Returns whether the state at the end is finite; if not, it is not written
 template <typename T, int DK, bool FEEDS>
-__device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh, int64_t bh, int slice)
+__device__ inline bool run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh, int64_t bh, int slice)
 {
     constexpr int NI = kPlanes<T>, Square = kChunk * kChunk, Inputs = NI * kChunk * DK;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tile = wave & 3;
     const bool mine = wave < DK / 16;
     const int64_t b = bh / p.heads, head = bh % p.heads, key = head / p.group, kbh = b * (p.heads / p.group) + key, end = p.chunks - 1;
     const int column = slice * 16, j = column + lane16();
+    if (threadIdx.x == 0) sh.bad = 0;
     f4 state{};
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
@@ -766,12 +886,47 @@ __device__ inline void run_back_chain(const DeltaArgs &p, BackShared<T, DK> &sh,
         state = mmp(kt[0], u[0], state) + mmp(kt[1], u[1], f4{});
         load_turned_of();
     }
-    if (!p.last || !mine || j >= p.value_dim) return;
+    if (mine && not_finite(state)) sh.bad = 1;
+    all_waves();
+    if (__builtin_amdgcn_readfirstlane(sh.bad)) return false;
+    if (mine) put_state(p, bh, wave * 16, j, state);
+    return true;
+}
+
+template <typename T, int DK>
+__device__ void back_chain_by_steps(const DeltaArgs &p, int64_t bh, int slice)
+{
+    const int64_t b = bh / p.heads, head = bh % p.heads, key = head / p.group;
+    Column<DK> c(p, bh, slice);
+#pragma unroll 1
+    for (int n = p.chunks - 1; n >= 0; --n) {
+        const int64_t unit = bh * p.chunks + n, t0 = (p.chunk0 + n) * kChunk;
+        c.keep(p.ds + unit * DK * p.columns, p.columns);
+#pragma unroll 1
+        for (int l = kChunk - 1; l >= 0; --l) {
+            const int64_t t = t0 + l, gate = (b * p.steps + t) * p.heads + head;
+            float dy = 0.0f;
+            if (t < p.steps) {
+                const T *const k = at<T>(p.k, b, t, key), *const q = at<T>(p.q, b, t, key);
+                const bool cut = p.g[gate] < kNoCarry || (p.reset && p.reset[b * p.steps + t] != 0);
+                const float carry = cut ? 0.0f : expf(p.g[gate]), d = c.in ? p.scale * (float)at<T>(p.dout, b, t, head)[c.j] : 0.0f;
+                float sk = 0.0f;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        const int row = wave * 16 + lane4() + m;
-        if (row < p.key_dim) p.last[(bh * p.key_dim + row) * p.value_dim + j] = state[m];
+                for (int i = 0; i < c.R; ++i)
+                    if (c.row(i) < p.key_dim) {
+                        c.s[i] = fmaf((float)q[c.row(i)], d, c.s[i]);
+                        sk = fmaf(c.s[i], (float)k[c.row(i)], sk);
+                    }
+                sk = column_sum(sk);
+                dy = c.in ? p.beta[gate] * sk : 0.0f;
+#pragma unroll
+                for (int i = 0; i < c.R; ++i)
+                    if (c.row(i) < p.key_dim) c.s[i] = cut ? 0.0f : carry * fmaf((float)k[c.row(i)], -dy, c.s[i]);
+            }
+            if (c.lane == 0) p.dy[(unit * kChunk + l) * p.columns + c.j] = dy;
+        }
     }
+    c.put_last(p);
 }
 
 template <typename T, int DK>
@@ -780,8 +935,9 @@ __global__ void __launch_bounds__(512, kPlanes<T> == 1 ? 4 : 2) delta_back_chain
     __shared__ BackShared<T, DK> sh;
     const int64_t die = blockIdx.x & 7, place = blockIdx.x >> 3, bh = place / p.slices * 8 + die;
     if (bh >= p.batch * p.heads) return;
-    if (threadIdx.x < 256) run_back_chain<T, DK, false>(p, sh, bh, (int)(place % p.slices));
-    else run_back_chain<T, DK, true>(p, sh, bh, (int)(place % p.slices));
+    const int slice = (int)(place % p.slices);
+    const bool finite = threadIdx.x < 256 ? run_back_chain<T, DK, false>(p, sh, bh, slice) : run_back_chain<T, DK, true>(p, sh, bh, slice);
+    if (!finite) back_chain_by_steps<T, DK>(arguments_again(), bh, slice);
 }
 
 // ---- backward: all gradients at once -------------------------------------------------------------------------------------------
@@ -804,6 +960,22 @@ union BackOutputShared {
     } by;
 };
 
+// by the first wave, a lane a step: the gradients by the gates, from what their products with everything they decay add up to
+__device__ inline void put_gate_gradients(const DeltaArgs &p, const Gates &gates, int64_t b, int64_t head, int64_t t0, double sum, float dbeta)
+{
+    const int i = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    // the steps from here to the next cut (all behind a cut add up to 0, which their roundings would not)
+    for (int step = 1; step < kChunk; step <<= 1) {
+        const double later = __shfl_down(sum, step);
+        if (i + step < kChunk && gates.part[i + step] == gates.part[i]) sum += later;
+    }
+    if (t0 + i < p.steps) {
+        const int64_t to = (b * p.steps + t0 + i) * p.heads + head;
+        p.dg[to] = gates.cut[i] ? 0.0f : (float)sum;
+        p.dbeta[to] = dbeta;
+    }
+}
+
 // a tile on or below the diagonal as the left operand that sums over its columns, and (turned) over its rows
 __device__ inline void put_tile(__bf16 *p, __bf16 *turned, int ti, int tj, f4 v)
 {
@@ -818,6 +990,120 @@ __device__ inline void put_tile(__bf16 *p, __bf16 *turned, int ti, int tj, f4 v)
     }
 }
 
+// The same again without a product across a cut, for the chunks whose gradients are not all finite: w1 is the gradient by Q K^T, w2 the one by K K^T, w3 the one
+// by the decays, all chunk x chunk.  A wave takes a step at a time, a lane its key dimensions.
+template <typename T, int DK>
+__device__ void gradients_within_cuts(const DeltaArgs &p, Gates &gates, float *w1, float *slope, float *kept, int wave)
+{
+    const int64_t unit = blockIdx.x;
+    float *const w2 = w1 + kChunk * kChunk, *const w3 = w2 + kChunk * kChunk;
+    const int64_t bh = unit / p.chunks, chunk = unit % p.chunks, b = bh / p.heads, head = bh % p.heads, key = head / p.group, t0 = (p.chunk0 + chunk) * kChunk;
+    const int steps = (int)min<int64_t>(kChunk, p.steps - t0), lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    const int first = gates.part[0] == 0 ? 0 : -1, last = gates.part[kChunk - 1];            // what S0 reaches, and what reaches dS1
+    const float *const s = p.s + unit * DK * p.columns, *const ds = p.ds + unit * DK * p.columns;
+    const float *const ys = p.y + unit * kChunk * p.columns, *const dys = p.dy + unit * kChunk * p.columns;
+    if (wave == 0) gates.sum_within_cuts(p, (b * p.steps + t0 + lane) * p.heads + head, lane, lane < steps);
+    __syncthreads();                                     // (and what has been written is written over)
+#pragma unroll 1
+    for (int u = wave * 64 + lane; u < kChunk * kChunk; u += DK * 4) {
+        const int i = u / kChunk, j = u % kChunk;
+        float by_qk = 0.0f, by_kk = 0.0f, by_decay = 0.0f;
+        if (j <= i && i < steps && gates.part[i] == gates.part[j]) {
+            const T *const dout = at<T>(p.dout, b, t0 + i, head), *const q = at<T>(p.q, b, t0 + i, key), *const ki = at<T>(p.k, b, t0 + i, key),
+                    *const kj = at<T>(p.k, b, t0 + j, key);
+            float from_o = 0.0f, from_y = 0.0f, qk = 0.0f, kk = 0.0f;
+#pragma unroll 1
+            for (int c = 0; c < p.value_dim; ++c) {
+                const float y = ys[j * p.columns + c];
+                from_o = fmaf((float)dout[c], y, from_o);
+                if (j < i) from_y = fmaf(dys[i * p.columns + c], y, from_y);
+            }
+#pragma unroll 1
+            for (int d = 0; d < p.key_dim; ++d) {
+                qk = fmaf((float)q[d], (float)kj[d], qk);
+                if (j < i) kk = fmaf((float)ki[d], (float)kj[d], kk);
+            }
+            const float decay = gates.decay(i, j), o = p.scale * from_o * decay, f = from_y * decay;
+            by_qk = o * gates.beta[j];
+            by_kk = -f * gates.beta[j];
+            by_decay = o * qk - f * kk;
+        }
+        w1[u] = by_qk;
+        w2[u] = by_kk;
+        w3[u] = by_decay;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = wave; i < steps; i += DK / 16) {
+        const int part = gates.part[i];
+        const T *const dout = at<T>(p.dout, b, t0 + i, head), *const qi = at<T>(p.q, b, t0 + i, key), *const ki = at<T>(p.k, b, t0 + i, key);
+        float slope_sum = 0.0f, kept_sum = 0.0f;
+#pragma unroll 1
+        for (int d = lane; d < p.key_dim; d += 64) {
+            float o_state = 0.0f, y_state = 0.0f, carried = 0.0f;
+#pragma unroll 1
+            for (int c = 0; c < p.value_dim; ++c) {
+                if (part == first) {
+                    o_state = fmaf((float)dout[c], s[d * p.columns + c], o_state);
+                    y_state = fmaf(dys[i * p.columns + c], s[d * p.columns + c], y_state);
+                }
+                if (part == last) carried = fmaf(ys[i * p.columns + c], ds[d * p.columns + c], carried);
+            }
+            o_state = part == first ? o_state * gates.a[i] * p.scale : 0.0f;
+            y_state = part == first ? y_state * gates.a[i] : 0.0f;
+            carried = part == last ? carried * gates.c[i] : 0.0f;
+            slope_sum += (float)qi[d] * o_state - (float)ki[d] * y_state;
+            kept_sum = fmaf((float)ki[d], carried, kept_sum);
+            float dq = o_state, dk = (part == last ? carried * gates.beta[i] : 0.0f) - y_state;
+#pragma unroll 1
+            for (int j = 0; j < steps; ++j) {
+                if (gates.part[j] != part) continue;
+                const float k = (float)at<T>(p.k, b, t0 + j, key)[d];
+                if (j <= i) dq = fmaf(w1[i * kChunk + j], k, dq);
+                if (j < i) dk = fmaf(w2[i * kChunk + j], k, dk);
+                if (j > i) dk = fmaf(w2[j * kChunk + i], k, dk);
+                if (j >= i) dk = fmaf(w1[j * kChunk + i], (float)at<T>(p.q, b, t0 + j, key)[d], dk);
+            }
+            if (p.group > 1) {
+                p.gq[(unit * kChunk + i) * DK + d] = dq;
+                p.gk[(unit * kChunk + i) * DK + d] = dk;
+            } else {
+                out_at<T>(p.dq, b, t0 + i, head)[d] = (T)dq;
+                out_at<T>(p.dk, b, t0 + i, head)[d] = (T)dk;
+            }
+        }
+        const auto plus = [](float x, float y) { return x + y; };
+        slope_sum = wave_reduce(slope_sum, 0.0f, plus);
+        kept_sum = wave_reduce(kept_sum, 0.0f, plus);
+        if (lane == 0) slope[i] = slope_sum, kept[i] = kept_sum;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    const int i = lane, part = gates.part[i];
+    float dot = 0.0f;                                    // S0 . dS1, where nothing lies between
+    if (first == last)
+        for (int d = 0; d < p.key_dim; ++d)
+            for (int c = lane; c < p.value_dim; c += 64) dot = fmaf(s[d * p.columns + c], ds[d * p.columns + c], dot);
+    dot = wave_reduce(dot, 0.0f, [](float x, float y) { return x + y; });
+    float dbeta = 0.0f, on = 0.0f;
+    double sum = 0.0;
+    if (i < steps) {
+        float column = 0.0f, row = 0.0f;
+        for (int j = 0; j < steps; ++j) {
+            if (gates.part[j] != part) continue;
+            if (j > i) column += w3[j * kChunk + i];
+            if (j < i) row = fmaf(w3[i * kChunk + j], gates.beta[j], row);
+        }
+        const float beta = gates.beta[i], held = kept[i];
+        dbeta = held + column + w3[i * kChunk + i];
+        on = part == last ? beta * held : 0.0f;
+        sum = (double)(slope[i] + row) - (double)(beta * column) - (double)on;
+    }
+    double carried_on = on;
+    for (int step = 32; step > 0; step >>= 1) carried_on += __shfl_xor(carried_on, step);
+    if (i == kChunk - 1) sum += carried_on + (first == last ? (double)gates.a[i] * dot : 0.0);
+    put_gate_gradients(p, gates, b, head, t0, sum, dbeta);
+}
 template <typename T, int DK>
 __global__ void __launch_bounds__(DK * 4, DK == 128 ? (kPlanes<T> == 3 ? 2 : 4) : DK == 64 ? 2 : 1) delta_back_output_kernel(DeltaArgs p)
 {
@@ -826,6 +1112,7 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? (kPlanes<T> == 3 ? 2 : 4) 
     __shared__ __attribute__((aligned(16))) BackOutputShared<NI> sh;
     __shared__ float by_row[4][kChunk], by_column[4][kChunk], by_itself[kChunk]; // of the chunk x chunk matrix, by tile; its diagonal, which no decay is in
     __shared__ float by_state[W][kChunk], kept[W][kChunk], dots[W];              // by wave
+    __shared__ int32_t again;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t unit = blockIdx.x, bh = unit / p.chunks, chunk = unit % p.chunks, b = bh / p.heads, head = bh % p.heads, key = head / p.group;
     const int64_t t0 = (p.chunk0 + chunk) * kChunk, inputs = ((b * (p.heads / p.group) + key) * p.chunks + chunk) * NI * kChunk * DK;
@@ -1047,18 +1334,15 @@ __global__ void __launch_bounds__(DK * 4, DK == 128 ? (kPlanes<T> == 3 ? 2 : 4) 
         double sum = (double)slope - (double)(beta * column) - (double)on, carried_on = on;
         for (int step = 32; step > 0; step >>= 1) carried_on += __shfl_xor(carried_on, step);
         if (i == kChunk - 1) sum += carried_on + (double)gates.a[kChunk - 1] * all;
-        // the steps from here to the next cut (all behind a cut add up to 0, which their roundings would not)
-        for (int step = 1; step < kChunk; step <<= 1) {
-            const double later = __shfl_down(sum, step);
-            if (i + step < kChunk && gates.part[i + step] == gates.part[i]) sum += later;
-        }
-        if (t0 + i < p.steps) {
-            const int64_t to = (b * p.steps + t0 + i) * p.heads + head;
-            p.dg[to] = gates.cut[i] ? 0.0f : (float)sum;
-            p.dbeta[to] = dbeta;
-        }
+        // whatever is not finite among the other gradients, or what they are made of, is so in these sums of products with it
+        const uint64_t bad = __ballot(!(fabsf((float)sum + dbeta) < INFINITY));
+        if (i == 0) again = bad != 0;
+        put_gate_gradients(p, gates, b, head, t0, sum, dbeta);
     }
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(again)) gradients_within_cuts<T, DK>(arguments_again(), gates, reinterpret_cast<float *>(&sh), by_state[0], kept[0], wave);
 }
+
 
 // the gradients by queries and keys that heads share: the sum over the heads, in their order
 template <typename T>
