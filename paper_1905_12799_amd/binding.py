@@ -618,13 +618,22 @@ def _gradient_of(logits: torch.Tensor, out: Optional[torch.Tensor]) -> Tuple[tor
     return out, at, ld
 
 
+def _differentiated(logits: torch.Tensor, temperature: Optional[torch.Tensor]) -> bool:
+    """Whether autograd takes part in a call; by a temperature nothing is differentiated, and a call that asks for it is turned down."""
+    if not torch.is_grad_enabled():
+        return False
+    if temperature is not None and temperature.requires_grad:
+        raise ValueError("nothing is differentiated by the temperature: pass temperature.detach()")
+    return logits.requires_grad
+
+
 def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor], temperature: Optional[torch.Tensor] = None, top: int = 0,
                    workspace: Optional[torch.Tensor] = None) -> LogProbs:
     """Log-probability of tokens [rows] (int32; outside the row: 0, a padded position) under logits [rows, n_choices] (fp32, bf16 or fp16, rows
     contiguous), the entropy of every row, and its `top` best entries with their log-probabilities (at most MAX_TOP; -1 where there are fewer).
 
-    temperature (fp32) has an entry per row.  tokens may be None.  logprob and entropy are differentiable by the logits."""
-    if torch.is_grad_enabled() and logits.requires_grad:
+    temperature (fp32, a constant) has an entry per row.  tokens may be None.  logprob and entropy are differentiable by the logits."""
+    if _differentiated(logits, temperature):
         return LogProbs(*_LogProbs.apply(logits, tokens, temperature, top, workspace))
     at, kind, rows, n, ld = _logits(logits)
     device = logits.device
@@ -700,8 +709,9 @@ def distill_loss(logits: torch.Tensor, teacher_tokens: torch.Tensor, teacher_log
     [rows], norm fp32 [rows, 2] as token_logprobs returns it).
 
     teacher_tokens int32 and teacher_logits (fp32, bf16 or fp16; logits or log-probabilities, such as token_logprobs' alternatives) are [rows, k],
-    k at most MAX_TOP; a token outside the row is no entry.  temperature (fp32) has an entry per row.  The loss is differentiable by the logits."""
-    if torch.is_grad_enabled() and logits.requires_grad:
+    k at most MAX_TOP; a token outside the row is no entry.  temperature (fp32) has an entry per row.  The loss is differentiable by the logits; the
+    teacher and the temperature are constants."""
+    if _differentiated(logits, temperature):
         return _Distill.apply(logits, teacher_tokens, teacher_logits, temperature, workspace)
     at, kind, rows, n, ld = _logits(logits)
     token_at, teacher_at, teacher_kind, k = _teacher(teacher_tokens, teacher_logits, rows)
