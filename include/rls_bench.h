@@ -62,6 +62,8 @@ int32_t rls_scan_overlap(const rls_scan_shape *shape, const rls_sequence *x, int
 /* Workspace that the chunks of one launch of a gated delta rule may take together before its sequences are cut into segments, a few launches
  * each, for the calls of the host thread that sets it; 0: a chunk of every head at a time; a negative value restores the default.  For tests. */
 int32_t rls_delta_segment_bytes(int64_t bytes);
+/* Chunks of 64 steps in a segment of such a call (the last segment may have fewer); 0 where the steps are taken one by one. */
+int64_t rls_delta_segment_chunks(const rls_delta_shape *shape, int32_t backward);
 
 #ifdef __cplusplus
 }

@@ -1705,6 +1705,12 @@ int32_t rls_delta_segment_bytes(int64_t bytes)
     return RLS_OK;
 }
 
+int64_t rls_delta_segment_chunks(const rls_delta_shape *shape, int32_t backward)
+{
+    const int32_t rc = check_delta(shape);
+    return rc != RLS_OK ? rc : plan_delta(*shape, backward != 0).segment;
+}
+
 int64_t rls_gated_delta_workspace_bytes(const rls_delta_shape *shape, int32_t backward)
 {
     const int32_t rc = check_delta(shape);
