@@ -450,6 +450,7 @@ typedef struct {
  * as they are.  What is not finite, an input or a state, makes not finite what follows from it step by step in its head, from there on up to the next
  * reset or gate that keeps nothing, and nothing else.  Steps are taken in chunks; a head whose state is not finite at the end of one of a call's
  * launches has that launch's steps taken one by one instead (some 1 to 4 us each), also where it was a product over a chunk that passed the largest number.
+ * The workspace is bounded along the steps; it holds a chunk of every sequence and head at least (up to 0.2 MB with 128 x 128, 0.5 MB for the backward pass).
  * 1 <= key_dim <= RLS_MAX_KEY_DIM, 1 <= value_dim <= RLS_MAX_VALUE_DIM, batch * heads <= 2^17, batch * steps <= 2^30.
  */
 #define RLS_MAX_KEY_DIM 128

@@ -15,9 +15,9 @@
 // fp32 number as the sum of three bf16 numbers (24 bits, what is left out is 2^-27 of it), an fp16 input as two and a bf16 input as it is, and of the products
 // of two such sums those that count in fp32: three for a bf16 input with an fp32 operand, six for two of fp32, at 1/16 of an fp32 instruction's time each.
 // Small and awkward products (the inverse) are left to the fp32 instructions.
-// What it takes, heads of 128 x 128 in bf16: a token of 64 x 32 heads 59 us (4.6 TB/s of state); 8191 steps of 32 heads 361, of that 114 to prepare the chunks and
-// 270 in the chain, 2.1 a chunk (all of it with fp32 instructions and outputs apart: 1349); gradients of 4 x 2048 steps of 16 heads 591: 72, 149, 187 in the
-// chain back, 189 for all gradients (1288).  (Launches by themselves, as a profiler has them, add up to more than a pass among others.)
+// What it takes, heads of 128 x 128 in bf16: a token of 64 x 32 heads 59 us (4.6 TB/s of state); 8191 steps of 32 heads 361 a pass, in a profiler's trace 2 x 57 to
+// prepare the chunks and 2 x 136 in the chain, 2.1 a chunk (all of it with fp32 instructions and outputs apart: 1349); gradients of 4 x 2048 steps of 16
+// heads 610 a pass, in a trace 77, 151, 190 in the chain back, 202 for all gradients (1288).  fp16 and fp32: 8191 steps 547 and 716, gradients 864 and 1040.
 #include <algorithm>
 #include <type_traits>
 
@@ -943,7 +943,8 @@ __global__ void __launch_bounds__(512, kPlanes<T> == 1 ? 4 : 2) delta_back_chain
 // ---- backward: all gradients at once -------------------------------------------------------------------------------------------
 // Over the value dimensions, 64 at a time: dO S^T, dY S^T, Y dS^T (16 key dimensions by a wave) and dO Y^T, dY Y^T; then with the gradient by Q K^T, and after
 // it with the one by K K^T, the products over the chunk's steps.  LDS and registers for two workgroups on a compute unit: it waits for memory and barriers
-// two thirds of the time (one workgroup: 320 us for 4 x 2048 steps x 16 heads of 128 x 128).
+// two thirds of the time (one workgroup: 320 us for 4 x 2048 steps x 16 heads of 128 x 128).  fp16 spills 35 registers so, and is no slower for it: the
+// whole pass 864 us, with one workgroup and no spills 874.
 
 __device__ inline float row_sum(float x)
 {
@@ -1458,11 +1459,14 @@ __global__ void __launch_bounds__(256) delta_step_kernel(DeltaArgs p)
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
 
-// Up to so many steps are taken one by one.  (A step adds 1.5 to 2 us, 2.6 us with 256 heads of 128 x 128 and 18 us with 2048, which the chunks take in 17 us for
-// 32 heads, 51 for 256 and 400 for 2048.)
+// Up to so many steps are taken one by one.  (One by one and in chunks, us: 32 heads of 128 x 128 in bf16 6 steps 19.0 and 18.1, 8 23.9 and 18.0; 16 of 64 x 64 6
+// 13.4 and 15.1, 8 17.0 and 15.1; one of 16 x 16 8 12.3 and 13.3, 10 14.9 and 13.2.  256 of 128 x 128 12 37.7 and 40.1, 16 48.3 and 39.5; 2048 12 254 and 280, 16 326
+// and 279; 4096 of 32 x 32 16 138 and 146, 24 207 and 155.)
 int64_t few_steps(int64_t batch, int64_t heads) { return batch * heads >= 256 ? 16 : 6; }
-// Workspace of the chunks that a launch takes.  Forward: what the last-level cache holds, nearly (8191 steps x 32 heads in 128, 256, 512, 1024 MB: 460, 372, 366,
-// 409 us).  Backward: more, as the states before every segment but the first cost a forward pass without outputs.
+// Workspace of the chunks that a launch takes, counted as for fp32 and keys that are not shared: bf16 touches half of it, with two heads a key three eighths.
+// Forward: 8191 steps x 32 heads in 96, 192, 384, 768 MB, us: bf16 418, 391, 386, 399 (two heads a key 399, 361, 348, 374); fp16 619, 589, 666, 656; fp32 702, 737, 805, 781.
+// Backward: more, as the states before every segment but the first cost a forward pass without outputs (4 x 2048 steps x 16 heads in 256 MB, 512 MB, 1 GB, 2 GB: bf16
+// 742, 717, 615, 617; fp32 1214, 1255, 1040, 1041).  A chunk of every head is held at least, however many heads there are.
 constexpr int64_t kSegmentBytes = 384ll << 20, kBackSegmentBytes = 2ll << 30;
 thread_local int64_t g_segment_bytes = -1;
 

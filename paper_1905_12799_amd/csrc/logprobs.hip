@@ -11,8 +11,8 @@
 // at or above it lies with those few threads, which read their part again and list it.
 //
 // Reading the logits bounds the forward pass, reading and writing them the backward one: 4096 x 50021 in bf16 forward 89 us (4.6 TB/s), 8192 x 32001 in bf16
-// backward 211 (5.0 TB/s, what a large copy reaches), 2048 x 128003 with 64 entries of a teacher 216 (4.9).  Where there is little to read it is dependent steps:
-// 524288 x 3 in fp32 5 us forward and 6 backward, 524288 x 20 33 and 45, 64 x 128003 in bf16 with 20 alternatives 18 and 8 (7 and 4 without).
+// backward 211 (5.0 TB/s; a copy of 2 GiB 4.9), 2048 x 128003 with 64 entries of a teacher 216 (4.9).  Where there is little to read it is dependent steps: 524288 x 3
+// in fp32 5 us forward and 5 backward, 524288 x 20 33 and 41 (bf16 46 and 65: fewer lanes have entries), 64 x 128003 in bf16 with 20 alternatives 18 and 8 (7 and 4 without).
 #include <algorithm>
 
 #include "element_types.h"
