@@ -937,7 +937,10 @@ __global__ void __launch_bounds__(512, kPlanes<T> == 1 ? 4 : 2) delta_back_chain
     if (bh >= p.batch * p.heads) return;
     const int slice = (int)(place % p.slices);
     const bool finite = threadIdx.x < 256 ? run_back_chain<T, DK, false>(p, sh, bh, slice) : run_back_chain<T, DK, true>(p, sh, bh, slice);
-    if (!finite) back_chain_by_steps<T, DK>(arguments_again(), bh, slice);
+    if (!finite) {
+        __syncthreads();                                 // (for what the chain has written, which is written over)
+        back_chain_by_steps<T, DK>(arguments_again(), bh, slice);
+    }
 }
 
 // ---- backward: all gradients at once -------------------------------------------------------------------------------------------
