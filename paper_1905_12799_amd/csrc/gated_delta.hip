@@ -606,7 +606,10 @@ __device__ inline f4 run_chain(const DeltaArgs &p, ChainShared<DK> &sh, int64_t 
             put_v();
             load_v_of(min(n + 2, p.chunks - 1));
             if (kQueries) {
-                by_query = rows_by(rows, sh.s) * a;
+                // (a state may be finite and its product with a query not: behind a cut neither counts, and nothing of it is left in the state to tell)
+                by_query = rows_by(rows, sh.s);
+#pragma unroll
+                for (int m = 0; m < 4; ++m) by_query[m] = a[m] == 0.0f ? 0.0f : by_query[m] * a[m];
                 load_rows_of();
             }
         }

@@ -185,3 +185,21 @@ def test_gradients_of_numbers_that_are_not_finite(rls, cut_segments, T, cuts, at
                         (reached[1, 1:2] if n == "state" else reached[1, :, 0:1] if n in "qk" else reached[1, :, 1:2])[:] = True
                     terms = (d["beta"][:, a:e].nan_to_num(1.0, 1.0) * want[p]["beta"]).abs().max()
                     close(torch.where(reached, 0.0, x.double()).to(x.dtype), torch.where(reached, 0.0, w), T, K, 2, (name, what, p, n, segment), terms if n == "g" else 0.0)
+
+
+@pytest.mark.parametrize("T", [6, 40])
+def test_answers_beyond_the_largest_number_before_a_cut(rls, T):                 # noqa: F811
+    """A finite state whose product with a query is not: what lies behind the cut is answered without it."""
+    d = inputs(2, T, 2, 1, 32, 16, "f32", T)
+    with_cuts(d, (4,), False)
+    d["state"] = torch.full_like(d["state"], 3e38)
+    d["q"] = torch.full_like(d["q"], 32 ** -0.5)                                   # q . S is 5.7 times a row's entry
+    d["k"].zero_()
+    d["k"][..., 3] = 1.0
+    d["g"][:, :4] = 0.0
+    d["beta"][:, :4] = 0.0
+    o, last = rls.gated_delta(**d, scale=1.0)
+    want, end = by_steps(d, 1.0)
+    assert not bool(o[:, :4].isfinite().any())
+    close(o[:, 4:], want[:, 4:], T, 32, 1, "o")
+    close(last, end, T, 32, 1, "last")
